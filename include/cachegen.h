@@ -382,6 +382,152 @@ int cg_decode_tokens(const cg_params* p, const uint32_t* words, const uint64_t* 
                      uint16_t* kv_out_f16, void* workspace, uint64_t workspace_bytes,
                      hipStream_t stream);
 
+/* ---- 8-bit serving cache -------------------------------------------------------------------
+ * Where a decoded context is answered from. The paper's system hands the decoded cache to the
+ * model (Sec. 6, generate_with_kv); a server that holds many contexts keeps them in 8 bits, the
+ * form the paper measures against (Sec. 7.1), and drops the tokens that attention passes by
+ * before it encodes again (Sec. 7.2, CacheGen on top of token dropping).
+ *
+ * A cache is a pool of pages. A page holds CG_KV8_PAGE = 64 consecutive tokens of one sequence,
+ * for every KV head, and K and V of a (page, head) are int8 codes under one fp32 scale each:
+ * value = code * scale. Attention's two products contract over K's channels and V's tokens, so K
+ * lies token by token and V channel by channel. A sequence is a row of page numbers (the table)
+ * and a length; token t of it is token t % 64 of page table[t / 64].
+ *
+ * The struct arguments are HOST memory read during the call; the pointers in them are DEVICE
+ * memory of the caller. Page numbers and lengths are read on the device and never trusted: a page
+ * number outside [0, n_pages) is a page without tokens, a length is cut to the table's row and to
+ * the caller's bound. Every call is asynchronous on the given stream and none allocates. Rows of
+ * K, V, queries and outputs are fp16 or bf16 with any strides (the last dimension contiguous);
+ * 16-byte aligned rows are read and written 16 bytes at a time. */
+#define CG_KV8_PAGE 64
+
+enum { CG_KV8_F16 = 0, CG_KV8_BF16 = 1 };
+
+typedef struct cg_kv8_cache {
+  int32_t n_pages;        /* P */
+  int32_t n_heads;        /* H, KV heads */
+  int32_t head_dim;       /* D: 64, 128 or 256 */
+  int8_t* k_codes;        /* [P][H][64][D], 16-byte aligned */
+  int8_t* v_codes;        /* [P][H][D][64], 16-byte aligned */
+  float* k_scale;         /* [P][H] */
+  float* v_scale;         /* [P][H] */
+  int8_t* k_bounds;       /* [P][H][2][D], 16-byte aligned: lowest and highest K code of each
+                             channel over the page's tokens; NULL: not kept (cg_kv8_select
+                             needs them) */
+} cg_kv8_cache;
+
+typedef struct cg_kv8_seqs {
+  int32_t n_seq;
+  int32_t max_pages;      /* columns of the table */
+  const int32_t* table;   /* [n_seq][max_pages] page numbers */
+} cg_kv8_seqs;
+
+typedef struct cg_kv8_rows {
+  void* data;             /* row (seq, token, head) starts at seq * seq_stride + token *
+                             token_stride + head * head_stride elements and has head_dim */
+  int64_t seq_stride, token_stride, head_stride;
+} cg_kv8_rows;
+
+/* Put rows into the pages: row i of sequence b becomes its token starts[b] + i, for i < counts[b].
+ *   starts   [n_seq] tokens that each sequence holds already. The tokens before it in its page
+ *            keep their values; what the page held from starts[b] on is gone.
+ *   counts   [n_seq], at most n_tokens each; NULL: n_tokens for every sequence. Sequences with
+ *            none are left alone.
+ *   k, v     [n_seq][n_tokens][H] rows of `dtype`.
+ *   status   NULL, or a device uint32_t that receives 0, or non-zero where a row held NaN or
+ *            +-Inf (cg_get_status). Those set no scale: an Inf becomes code +-127, a NaN code 0.
+ * Per page, head and K/V, with m the largest |x| of the page's new rows: scale s = m / 127, or the
+ * page's own if that is larger and earlier tokens stay in it; code = rint(clamp(x / s, +-127))
+ * (s = 0: code 0). Where s grows, the earlier tokens are coded again from code * old scale. All
+ * quotients and products are IEEE fp32, as in the codec. Pages are shared with no other sequence
+ * of the call, or the result is undefined. Asynchronous. */
+int cg_kv8_store(const cg_kv8_cache* c, const cg_kv8_seqs* s, const int32_t* starts,
+                 const int32_t* counts, int32_t n_tokens, int32_t dtype, const cg_kv8_rows* k,
+                 const cg_kv8_rows* v, uint32_t* status, hipStream_t stream);
+
+/* Read rows back: row i of sequence b is its token starts[b] + i for i < counts[b] (NULL:
+ * n_tokens), code * scale rounded to `dtype`; rows counts[b] .. n_tokens - 1 are zeros, and so
+ * are rows of pages that do not exist. Asynchronous. */
+int cg_kv8_load(const cg_kv8_cache* c, const cg_kv8_seqs* s, const int32_t* starts,
+                const int32_t* counts, int32_t n_tokens, int32_t dtype, const cg_kv8_rows* k,
+                const cg_kv8_rows* v, hipStream_t stream);
+
+/* Attention of n_q query tokens per sequence over its pages.
+ * Token j of a sequence of length n is visible to its query token i of q_lens[b] where
+ * j <= n - q_lens[b] + i: the queries are the last tokens, already stored. Query head hq reads KV
+ * head hq / (n_q_heads / H). With S = scale * q . k over the visible tokens:
+ *   out = softmax(S) v,   lse = log sum exp(S);
+ * a query that sees no token, and one with i >= q_lens[b], gets out = 0 and lse = -inf. */
+typedef struct cg_kv8_attn {
+  int32_t n_q;              /* query tokens per sequence */
+  int32_t n_q_heads;        /* a multiple of H */
+  int32_t dtype;            /* of q and out */
+  float scale;
+  const int32_t* lengths;   /* [n_seq] tokens of each sequence, the queries' own among them */
+  int32_t max_len;          /* no length is above it (longer ones are cut to it) */
+  const int32_t* q_lens;    /* [n_seq] query tokens of each sequence, or NULL: n_q */
+  cg_kv8_rows q, out;       /* [n_seq][n_q][n_q_heads] */
+  float* lse;               /* NULL, or out [n_seq][n_q][n_q_heads] */
+  /* Attention over chosen pages only: picks [n_seq][n_q][H][n_picks], as cg_kv8_select writes
+   * them: for each query token and KV head the table columns it reads, each at most once; entries
+   * outside the sequence are skipped. NULL: all pages. */
+  const int32_t* picks;
+  int32_t n_picks;
+  /* The weight each token got: mass_out [P][H][64] receives, for every token of the sequences,
+   * decay * mass_in + the sum over the query tokens and the heads of its group of their softmax
+   * weight on it. mass_in NULL: the sum alone; it may be mass_out. mass_out NULL: no weights. Not
+   * together with picks. */
+  const float* mass_in;
+  float* mass_out;
+  float decay;
+} cg_kv8_attn;
+
+/* Device scratch that cg_kv8_attend needs (bytes); 0 if an argument is invalid or none is needed. */
+uint64_t cg_kv8_attend_workspace_bytes(const cg_kv8_cache* c, const cg_kv8_seqs* s,
+                                       const cg_kv8_attn* a);
+
+/* The attention above. Products take fp16 operands (the codes and fp16 queries exactly, bf16
+ * queries under a power of two per row, softmax weights rounded to fp16) and sum in 32 bits;
+ * maxima, sums, lse and mass are 32-bit. Results do not depend on the order in which parts of the
+ * work end.
+ *   workspace   device scratch of workspace_bytes >= cg_kv8_attend_workspace_bytes, 256-byte
+ *               aligned (may be NULL where that is 0); its contents on entry do not matter.
+ * Asynchronous. */
+int cg_kv8_attend(const cg_kv8_cache* c, const cg_kv8_seqs* s, const cg_kv8_attn* a,
+                  void* workspace, uint64_t workspace_bytes, hipStream_t stream);
+
+/* Device scratch that cg_kv8_select needs (bytes); 0 if an argument is invalid. */
+uint64_t cg_kv8_select_workspace_bytes(const cg_kv8_cache* c, const cg_kv8_seqs* s,
+                                       const cg_kv8_attn* a);
+
+/* The pages each query token should read: picks_out [n_seq][n_q][H][a->n_picks], table columns in
+ * ascending order, -1 behind the last. Of a query token that sees n tokens, the last `recent` of
+ * its ceil(n / 64) pages are taken, and of the others the best by
+ *   score(page) = fp32(sum over the group's heads and the channels of max(q8 lo, q8 hi)) * k_scale
+ * with q8 = rint(clamp(q * 2^(6 - e), +-127)), 2^e the power of two at or below the largest |q| of
+ * the group, and lo, hi the page's bounds: an upper bound of the page's summed q . k, in whole
+ * numbers. Equal scores go to the lower column. Uses q, lengths, max_len, q_lens, n_picks and
+ * dtype of `a`. Asynchronous. */
+int cg_kv8_select(const cg_kv8_cache* c, const cg_kv8_seqs* s, const cg_kv8_attn* a,
+                  int32_t recent, int32_t* picks_out, void* workspace, uint64_t workspace_bytes,
+                  hipStream_t stream);
+
+/* Cut every sequence longer than `keep` to `keep` tokens, in new pages. Per sequence and KV head
+ * the last min(recent, keep) tokens stay, and of the others the heaviest by mass [P][H][64]
+ * (equal weights: the earlier token; a NaN weighs least). The tokens that stay are coded again
+ * page by page (scale: their largest |code * scale| over 127) into the pages of `to`, in their
+ * order, bounds and weights moving along; shorter sequences move whole.
+ *   lengths      [n_seq], none above max_len.
+ *   to           the same n_seq, at least ceil(min(keep, max_len) / 64) columns; its pages must
+ *                be no page of `s`, nor shared within the call.
+ *   kept         out [n_seq][H][keep]: the tokens that stay, ascending, -1 behind the last.
+ *   new_lengths  out [n_seq] = min(length, keep).
+ * Asynchronous. */
+int cg_kv8_evict(const cg_kv8_cache* c, const cg_kv8_seqs* s, const int32_t* lengths,
+                 int32_t max_len, float* mass, int32_t keep, int32_t recent,
+                 const cg_kv8_seqs* to, int32_t* kept, int32_t* new_lengths, hipStream_t stream);
+
 /* Static description of a return code; never NULL. */
 const char* cg_strerror(int code);
 

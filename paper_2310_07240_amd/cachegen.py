@@ -28,7 +28,9 @@ EXPORTS = ("cg_num_chunks", "cg_num_streams", "cg_encode_bound_words",
            "cg_num_token_streams", "cg_encode_tokens_bound_words",
            "cg_encode_tokens_workspace_bytes", "cg_decode_tokens_workspace_bytes",
            "cg_encode_tokens", "cg_decode_tokens", "cg_get_status", "cg_encode_noalloc",
-           "cg_fit_cdf_levels", "cg_encode_with_scales", "cg_strerror")
+           "cg_fit_cdf_levels", "cg_encode_with_scales", "cg_strerror",
+           "cg_kv8_store", "cg_kv8_load", "cg_kv8_attend_workspace_bytes", "cg_kv8_attend",
+           "cg_kv8_select_workspace_bytes", "cg_kv8_select", "cg_kv8_evict")   # bound in kv8
 CG_FIT_GLOBAL_WORKSPACE_BYTES = 8192
 CG_NOALLOC_SCRATCH_BYTES = 64 << 20
 

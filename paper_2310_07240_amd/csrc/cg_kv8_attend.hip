@@ -1,0 +1,440 @@
+// cg_kv8_attend.hip — attention over the pages of the 8-bit cache (cg_kv8_attend).
+//
+// For each (sequence, KV head) the queries of its group are the rows of two matrix products,
+// S = q K^T and O = P V, with the softmax carried along: running maximum m, running sum l, and O
+// under the reference m, all in 32 bits. The codes go into the matrix units as fp16 (exact), the
+// scales of the page are applied to S and to the page's share of O in 32 bits, and P is rounded
+// to fp16 for the second product (relative 2^-11 a weight, the rounding that the fp16 result gets
+// anyway; l sums the unrounded weights).
+//
+// Operand layout (v_mfma_f32_16x16x32_f16; lane = 16 g + m): both products are taken transposed,
+// S^T = K q^T and O^T = V^T P^T, so a lane's results belong to one query row (m) throughout and
+// the softmax needs only the four lanes of equal m. The order of the contracted index is free as
+// long as both operands agree: row m of K tile t is token 16 (m >> 2) + 4 t + (m & 3), which makes
+// the 16 tokens whose S a lane gets the consecutive 16 g .. 16 g + 15, exactly the k slots that it
+// supplies for the second product, and the V operand 16 consecutive bytes of a channel.
+#include "cg_kv8.h"
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kNegInf = -__builtin_inff();
+
+__device__ __forceinline__ float quad_max(float x) {   // over the lanes of equal m
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+// One 16-row tile's queries as B operands, and what a row needs of them.
+template <int D>
+struct QTile {
+  half8 q[D / 32];
+  float unit;        // times the page's K scale: S in units of log2
+  int visible;       // tokens that the lane's row sees
+};
+
+// Where the rows of a (virtual) sequence come from. With picks every query token is a sequence
+// of its own, whose rows are the heads of the group.
+struct RowsOf {
+  int seq, i0, nq;   // sequence, first query token, query tokens
+  int len, q_len;
+};
+
+__device__ __forceinline__ RowsOf rows_of(const KvSeqs& S, const KvAttn& A, int vseq) {
+  RowsOf r;
+  const bool sparse = A.picks != nullptr;
+  r.seq = sparse ? vseq / A.nq : vseq;
+  r.i0 = sparse ? vseq % A.nq : 0;
+  r.nq = sparse ? 1 : A.nq;
+  int len = A.lengths[r.seq];
+  const int64_t room = (int64_t)S.width * kPage;
+  if (len > A.max_len) len = A.max_len;
+  if (len > room) len = (int)room;
+  r.len = len > 0 ? len : 0;
+  const int ql = A.q_lens ? A.q_lens[r.seq] : A.nq;
+  r.q_len = ql < A.nq ? ql : A.nq;
+  return r;
+}
+
+// Tokens that query token i sees: those up to its own place, the last q_len tokens being the
+// queries' own.
+__device__ __forceinline__ int visible_of(const RowsOf& r, int i) {
+  if (i >= r.q_len) return 0;
+  const int64_t n = (int64_t)r.len - r.q_len + i + 1;
+  return n > 0 ? (int)n : 0;
+}
+
+// Rows 16 tile .. 16 tile + 15 of the group's queries; rows past the last one see nothing.
+// bf16 rows are scaled by a power of two to [1, 2) at their largest, so that fp16 holds them to
+// 2^-25 of it; fp16 rows go as they are.
+template <int D, bool BF16>
+__device__ __forceinline__ void load_q(const KvAttn& A, const RowsOf& R, int h, int tile,
+                                       QTile<D>& Q) {
+  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+  const int row = tile * 16 + m;
+  const int i = R.i0 + row / A.group, head = h * A.group + row % A.group;
+  const bool live = row < R.nq * A.group;
+  Q.visible = live ? visible_of(R, i) : 0;
+  const uint16_t* src = static_cast<const uint16_t*>(A.q.p) + R.seq * A.q.seq +
+                        (int64_t)i * A.q.tok + (int64_t)head * A.q.head;
+  uint16_t u[D / 32][8];
+#pragma unroll
+  for (int s = 0; s < D / 32; ++s) {
+    const int d = (s >> 1) * 64 + g * 16 + (s & 1) * 8;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) u[s][c] = live ? src[d + c] : 0;
+  }
+  int e = 0;
+  if (BF16) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s)
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const uint32_t a = u[s][c] & 0x7fffu;
+        top = a > top && a < 0x7f80u ? a : top;
+      }
+    uint32_t o = __shfl_xor(top, 16);
+    top = o > top ? o : top;
+    o = __shfl_xor(top, 32);
+    top = o > top ? o : top;
+    e = (int)(top >> 7) - 127;
+    if (e < -126) e = -126;
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s)
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        Q.q[s][c] = (_Float16)__builtin_ldexpf(kv_widen<true>(u[s][c]), -e);
+  } else {
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s)
+#pragma unroll
+      for (int c = 0; c < 8; ++c) Q.q[s][c] = __builtin_bit_cast(_Float16, u[s][c]);
+  }
+  Q.unit = __builtin_ldexpf(A.scale * kLog2e, e);
+}
+
+// S^T of one page: x[4 t + i] is token 16 g + 4 t + i against the lane's row, unscaled.
+template <int D>
+__device__ __forceinline__ void page_scores(const int8_t* k, const QTile<D>& Q, float x[16]) {
+  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const int8_t* row = k + (16 * (m >> 2) + 4 * t + (m & 3)) * D + 16 * g;
+    float4v acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int s = 0; s < D / 64; ++s) {
+      const uint4v c = *reinterpret_cast<const uint4v*>(row + 64 * s);
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv_widen8(c[0], c[1]), Q.q[2 * s], acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv_widen8(c[2], c[3]), Q.q[2 * s + 1], acc, 0, 0,
+                                                   0);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[4 * t + i] = acc[i];
+  }
+}
+
+// A wave's state for one 16-row tile: O^T (row m of the lane, channels 16 dt + 4 g + i), m and l.
+template <int D>
+struct Acc {
+  float4v o[D / 16];
+  float m, l;
+};
+
+// One page into the state.
+template <int D>
+__device__ __forceinline__ void page_step(const int8_t* k, const int8_t* v, float ks, float vs,
+                                          int pos0, const QTile<D>& Q, Acc<D>& S) {
+  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+  float x[16];
+  page_scores<D>(k, Q, x);
+  const float f = Q.unit * ks;
+  float top = kNegInf;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    x[j] = pos0 + 16 * g + j < Q.visible ? x[j] * f : kNegInf;
+    top = fmaxf(top, x[j]);
+  }
+  // P is taken relative to the page's own maximum, so that fp16 loses no light page beside a heavy
+  // one; w brings the page to the running reference.
+  top = quad_max(top);
+  const float mine = top == kNegInf ? 0.0f : top;      // nothing of the page is visible
+  const float both = fmaxf(S.m, top);
+  const float ref = both == kNegInf ? 0.0f : both;
+  const float keep = __builtin_amdgcn_exp2f(S.m - ref), w = __builtin_amdgcn_exp2f(top - ref);
+  float sum = 0.0f;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    x[j] = __builtin_amdgcn_exp2f(x[j] - mine);
+    sum += x[j];
+  }
+  S.l = __builtin_fmaf(S.l, keep, sum * w);
+  S.m = both;
+  const float vw = vs * w;
+  half8 p[2];
+#pragma unroll
+  for (int j = 0; j < 16; ++j) p[j >> 3][j & 7] = (_Float16)x[j];
+#pragma unroll
+  for (int dt = 0; dt < D / 16; ++dt) {
+    const uint4v c = *reinterpret_cast<const uint4v*>(v + (16 * dt + m) * kPage + 16 * g);
+    float4v acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv_widen8(c[0], c[1]), p[0], acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv_widen8(c[2], c[3]), p[1], acc, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      S.o[dt][i] = __builtin_fmaf(acc[i], vw, S.o[dt][i] * keep);
+  }
+}
+
+template <int D, bool BF16>
+__device__ __forceinline__ void put_out(const KvAttn& A, const RowsOf& R, int h, int row, int d,
+                                        const float* o, int n) {
+  const int i = R.i0 + row / A.group, head = h * A.group + row % A.group;
+  uint16_t* p = static_cast<uint16_t*>(A.out.p) + R.seq * A.out.seq + (int64_t)i * A.out.tok +
+                (int64_t)head * A.out.head + d;
+  for (int c = 0; c < n; ++c) p[c] = kv_narrow<BF16>(o[c]);
+}
+
+__device__ __forceinline__ int64_t lse_at(const KvAttn& A, const RowsOf& R, int H, int h,
+                                          int row) {
+  const int i = R.i0 + row / A.group, head = h * A.group + row % A.group;
+  return ((int64_t)R.seq * A.nq + i) * ((int64_t)H * A.group) + head;
+}
+
+// Workgroup = (virtual sequence, KV head, 16-row tile, split of the pages); its four waves take
+// the split's pages in turn and meet in LDS. splits == 1 writes the result, else a partial state:
+// O [16][D], m [16], l [16] in 32 bits.
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void attend_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles,
+                                                     int splits, int64_t items, float* part,
+                                                     float* lse) {
+  __shared__ float os[4][16][D + 4];
+  __shared__ float ms[4][16], ls[4][16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
+  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const int split = (int)(it % splits);
+    int64_t r = it / splits;
+    const int tile = (int)(r % tiles);
+    r /= tiles;
+    const int h = (int)(r % pool.H);
+    const int vseq = (int)(r / pool.H);
+    const RowsOf R = rows_of(S, A, vseq);
+    QTile<D> Q;
+    load_q<D, BF16>(A, R, h, tile, Q);
+    // the pages that any row of the tile sees
+    int most = Q.visible;
+    for (int o = 1; o < 16; o <<= 1) {
+      const int v = __shfl_xor(most, o);
+      most = v > most ? v : most;
+    }
+    most = __builtin_amdgcn_readfirstlane(most);
+    const int n = A.picks ? A.n_picks : (most + kPage - 1) / kPage;
+    const int per = (n + splits - 1) / splits;
+    const int j0 = split * per, j1 = j0 + per < n ? j0 + per : n;
+    const int32_t* picks = A.picks ? A.picks + ((int64_t)vseq * pool.H + h) * A.n_picks : nullptr;
+    Acc<D> acc;
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) acc.o[dt] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+    acc.m = kNegInf;
+    acc.l = 0.0f;
+    for (int j = j0 + wave; j < j1; j += 4) {
+      const int at = picks ? picks[j] : j;
+      if (at < 0 || (int64_t)at * kPage >= most) continue;
+      const int page = kv_page(S, pool.P, R.seq, at);
+      if (page < 0) continue;
+      const int64_t b = (int64_t)page * pool.H + h;
+      page_step<D>(pool.k + b * (kPage * D), pool.v + b * (kPage * D), pool.ks[b], pool.vs[b],
+                   at * kPage, Q, acc);
+    }
+    acc.l = quad_sum(acc.l);
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) os[wave][m][16 * dt + 4 * g + i] = acc.o[dt][i];
+    if (g == 0) {
+      ms[wave][m] = acc.m;
+      ls[wave][m] = acc.l;
+    }
+    __syncthreads();
+    // 16 threads a row, D / 16 channels each
+    const int row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * (D / 16);
+    float top = kNegInf;
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, ms[w][row]);
+    const float ref = top == kNegInf ? 0.0f : top;
+    float l = 0.0f, o[D / 16];
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) o[c] = 0.0f;
+    for (int w = 0; w < 4; ++w) {
+      const float f = __builtin_amdgcn_exp2f(ms[w][row] - ref);
+      l = __builtin_fmaf(ls[w][row], f, l);
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) o[c] = __builtin_fmaf(os[w][row][d0 + c], f, o[c]);
+    }
+    if (splits > 1) {
+      float* p = part + it * (16 * (D + 2));
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) p[row * D + d0 + c] = o[c];
+      if (d0 == 0) {
+        p[16 * D + row] = top;
+        p[16 * D + 16 + row] = l;
+      }
+    } else if (tile * 16 + row < R.nq * A.group) {
+      const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) o[c] *= inv;
+      put_out<D, BF16>(A, R, h, tile * 16 + row, d0, o, D / 16);
+      if (lse && d0 == 0)
+        lse[lse_at(A, R, pool.H, h, tile * 16 + row)] =
+            (top + __builtin_amdgcn_logf(l)) * kLn2;
+    }
+    __syncthreads();
+  }
+}
+
+// The splits of one 16-row tile joined: 16 threads a row.
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void join_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles,
+                                                   int splits, int64_t items, const float* part,
+                                                   float* lse) {
+  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const int tile = (int)(it % tiles);
+    const int64_t r = it / tiles;
+    const int h = (int)(r % pool.H);
+    const RowsOf R = rows_of(S, A, (int)(r / pool.H));
+    const int row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * (D / 16);
+    if (tile * 16 + row >= R.nq * A.group) continue;
+    const float* p = part + it * splits * (16 * (D + 2));
+    float top = kNegInf;
+    for (int s = 0; s < splits; ++s) top = fmaxf(top, p[s * (16 * (D + 2)) + 16 * D + row]);
+    const float ref = top == kNegInf ? 0.0f : top;
+    float l = 0.0f, o[D / 16];
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) o[c] = 0.0f;
+    for (int s = 0; s < splits; ++s) {
+      const float* q = p + s * (16 * (D + 2));
+      const float f = __builtin_amdgcn_exp2f(q[16 * D + row] - ref);
+      l = __builtin_fmaf(q[16 * D + 16 + row], f, l);
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) o[c] = __builtin_fmaf(q[row * D + d0 + c], f, o[c]);
+    }
+    const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) o[c] *= inv;
+    put_out<D, BF16>(A, R, h, tile * 16 + row, d0, o, D / 16);
+    if (lse && d0 == 0)
+      lse[lse_at(A, R, pool.H, h, tile * 16 + row)] = (top + __builtin_amdgcn_logf(l)) * kLn2;
+  }
+}
+
+// What every cached token got: decay * mass_in + the sum over the rows of exp(S - lse). One wave
+// per (sequence, KV head, page) walks the row tiles; the sum over the 16 rows of a tile is taken
+// once at the end, so no result depends on any order of arrival.
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void mass_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles,
+                                                   int np, int64_t items, const float* lse) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
+  for (int64_t it = (int64_t)blockIdx.x * 4 + wave; it < items; it += (int64_t)gridDim.x * 4) {
+    const int j = (int)(it % np);
+    const int64_t r = it / np;
+    const int h = (int)(r % pool.H), seq = (int)(r / pool.H);
+    const RowsOf R = rows_of(S, A, seq);
+    if (j * (int64_t)kPage >= R.len) continue;
+    const int page = kv_page(S, pool.P, seq, j);
+    if (page < 0) continue;
+    const int64_t b = (int64_t)page * pool.H + h;
+    const float ks = pool.ks[b];
+    float sum[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sum[e] = 0.0f;
+    for (int tile = 0; tile < tiles; ++tile) {
+      QTile<D> Q;
+      load_q<D, BF16>(A, R, h, tile, Q);
+      if (!__any(Q.visible > j * kPage)) continue;
+      const int row = tile * 16 + m;
+      const float z = row < R.nq * A.group ? lse[lse_at(A, R, pool.H, h, row)] * kLog2e : 0.0f;
+      float x[16];
+      page_scores<D>(pool.k + b * (kPage * D), Q, x);
+      const float f = Q.unit * ks;
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (j * kPage + 16 * g + e < Q.visible)
+          sum[e] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], f, -z));
+    }
+    float mine = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      float t = sum[e];
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) t += __shfl_xor(t, o);
+      mine = m == e ? t : mine;
+    }
+    const int t = 16 * g + m;
+    if (j * kPage + t < R.len) {
+      const int64_t at = b * kPage + t;
+      A.mass_out[at] = A.mass_in ? __builtin_fmaf(A.decay, A.mass_in[at], mine) : mine;
+    }
+  }
+}
+
+unsigned grid_of(int64_t items) { return (unsigned)(items < (1 << 22) ? items : (1 << 22)); }
+
+template <int D, bool BF16>
+hipError_t attend_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, void* ws,
+                    hipStream_t st) {
+  const KvAttnPlan P = cg_kv8_plan(pool, S, A, D);
+  char* base = static_cast<char*>(ws);
+  float* part = reinterpret_cast<float*>(base + P.part_off);
+  float* lse = A.lse ? A.lse : A.mass_out ? reinterpret_cast<float*>(base + P.lse_off) : nullptr;
+  const int vseqs = A.picks ? S.n * A.nq : S.n;
+  const int64_t units = (int64_t)vseqs * pool.H * P.tiles;
+  hipLaunchKernelGGL((attend_kernel<D, BF16>), dim3(grid_of(units * P.splits)), dim3(256), 0, st,
+                     pool, S, A, P.tiles, P.splits, units * P.splits, part, lse);
+  if (P.splits > 1)
+    hipLaunchKernelGGL((join_kernel<D, BF16>), dim3(grid_of(units)), dim3(256), 0, st, pool, S, A,
+                       P.tiles, P.splits, units, part, lse);
+  if (A.mass_out) {
+    const int np = (int)(((int64_t)A.max_len + kPage - 1) / kPage);
+    const int64_t items = (int64_t)S.n * pool.H * np;
+    hipLaunchKernelGGL((mass_kernel<D, BF16>), dim3(grid_of((items + 3) / 4)), dim3(256), 0, st,
+                       pool, S, A, P.tiles, np, items, lse);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& S, const KvAttn& A, int D) {
+  KvAttnPlan P;
+  const int64_t rows = (int64_t)(A.picks ? 1 : A.nq) * A.group;
+  P.tiles = (int)((rows + 15) / 16);
+  const int64_t vseqs = A.picks ? (int64_t)S.n * A.nq : S.n;
+  const int64_t units = vseqs * pool.H * P.tiles;
+  const int64_t pages = A.picks ? A.n_picks : ((int64_t)A.max_len + kPage - 1) / kPage;
+  // enough workgroups to fill the card, each wave with a page of its own at least
+  int64_t s = (1024 + units - 1) / units;
+  const int64_t most = (pages + 3) / 4;
+  if (s > most) s = most;
+  if (s < 1) s = 1;
+  P.splits = (int)s;
+  uint64_t at = 0;
+  P.part_off = at;
+  if (s > 1) at += (uint64_t)units * (uint64_t)s * (16ull * (D + 2)) * 4ull;
+  at = (at + 255) & ~255ull;
+  P.lse_off = at;
+  if (A.mass_out && !A.lse) at += (uint64_t)S.n * A.nq * pool.H * A.group * 4ull;
+  P.total = (at + 255) & ~255ull;
+  return P;
+}
+
+hipError_t cg_launch_kv8_attend(const KvPool& pool, const KvSeqs& S, int D, bool bf16,
+                                const KvAttn& A, void* ws, hipStream_t st) {
+  switch (D) {
+    case 64: return (bf16 ? attend_d<64, true> : attend_d<64, false>)(pool, S, A, ws, st);
+    case 128: return (bf16 ? attend_d<128, true> : attend_d<128, false>)(pool, S, A, ws, st);
+    default: return (bf16 ? attend_d<256, true> : attend_d<256, false>)(pool, S, A, ws, st);
+  }
+}

@@ -1,0 +1,219 @@
+// cg_kv8_store.hip — rows of K and V into the pages of the 8-bit cache, and back (cg_kv8_store,
+// cg_kv8_load).
+//
+// One workgroup per (sequence, page it touches, KV head): 2 D threads, thread (rg, cg) holding
+// rows 4 rg .. 4 rg + 3 of channels 8 cg .. 8 cg + 7, so a wave's load of one row index is whole
+// 2 D-byte rows and four tokens of a channel meet in one lane, as the transposed V codes want
+// them. The scale is the page's absolute maximum over 127, and the page is held in registers from
+// its maximum to its codes: one read of the rows, one write of the codes. Bound by those bytes.
+#include "cg_kv8.h"
+
+namespace {
+
+// Row elements at p: 8 of them, 16-byte loads where VEC.
+template <bool BF16, bool VEC>
+__device__ __forceinline__ void get8(const uint16_t* p, float* x) {
+  uint16_t u[8];
+  if (VEC) {
+    *reinterpret_cast<uint4v*>(u) = *reinterpret_cast<const uint4v*>(p);
+  } else {
+#pragma unroll
+    for (int c = 0; c < 8; ++c) u[c] = p[c];
+  }
+#pragma unroll
+  for (int c = 0; c < 8; ++c) x[c] = kv_widen<BF16>(u[c]);
+}
+
+template <int D, bool BF16, bool VEC>
+__global__ __launch_bounds__(2 * D) void store_kernel(KvPool pool, KvSeqs S,
+                                                      const int32_t* __restrict__ starts,
+                                                      const int32_t* __restrict__ counts,
+                                                      int n_tokens, int np, int64_t items,
+                                                      KvRows k, KvRows v, uint32_t* status) {
+  __shared__ StoreLds<D> L;
+  const int tid = threadIdx.x, cg = tid % (D / 8), rg = tid / (D / 8);
+  uint32_t bad = 0;
+  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const int h = (int)(it % pool.H);
+    const int64_t r0 = it / pool.H;
+    const int seq = (int)(r0 / np);
+    const int start = starts[seq];
+    int count = counts ? counts[seq] : n_tokens;
+    count = count < n_tokens ? count : n_tokens;
+    if (start < 0 || count <= 0) continue;
+    const int64_t j = start / kPage + r0 % np;        // the sequence's page
+    const int64_t end = (int64_t)start + count;
+    if (j * kPage >= end) continue;
+    const int page = j < S.width ? kv_page(S, pool.P, seq, (int)j) : -1;
+    if (page < 0) continue;                           // no such page: nothing is written
+    const int held = start > j * kPage ? (int)(start - j * kPage) : 0;
+    const int last = end - j * kPage < kPage ? (int)(end - j * kPage) : kPage;
+    const int64_t row0 = j * kPage - start;           // row of the page's first token
+    float x[4][8], y[4][8];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int t = 4 * rg + r;
+      if (t >= held && t < last) {
+        const int64_t row = row0 + t;
+        get8<BF16, VEC>(static_cast<const uint16_t*>(k.p) + seq * k.seq + row * k.tok +
+                            h * k.head + 8 * cg, x[r]);
+        get8<BF16, VEC>(static_cast<const uint16_t*>(v.p) + seq * v.seq + row * v.tok +
+                            h * v.head + 8 * cg, y[r]);
+      } else {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) x[r][c] = y[r][c] = 0.0f;
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const float a = __builtin_fabsf(x[r][c]), b = __builtin_fabsf(y[r][c]);
+        if (!(a <= 3.4028234e38f) || !(b <= 3.4028234e38f)) bad |= 1;
+      }
+    put_page<D, false>(pool, page, h, x, held, last, L);
+    put_page<D, true>(pool, page, h, y, held, last, L);
+  }
+  if (status && __any(bad) && (tid & 63) == 0) atomicOr(status, 1u);
+}
+
+__global__ void kv_zero_word(uint32_t* p) { *p = 0u; }
+
+template <int D, bool BF16, bool VEC>
+__global__ __launch_bounds__(2 * D) void load_kernel(KvPool pool, KvSeqs S,
+                                                     const int32_t* __restrict__ starts,
+                                                     const int32_t* __restrict__ counts,
+                                                     int n_tokens, int np, int64_t items,
+                                                     KvRows k, KvRows v) {
+  __shared__ uint32_t vt[D * 17];
+  constexpr int NT = 2 * D;
+  const int tid = threadIdx.x, cg = tid % (D / 8), rg = tid / (D / 8);
+  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const int h = (int)(it % pool.H);
+    const int64_t r0 = it / pool.H;
+    const int seq = (int)(r0 / np);
+    int start = starts[seq];
+    int count = counts ? counts[seq] : n_tokens;
+    count = count < n_tokens ? count : n_tokens;
+    if (start < 0) start = count = 0;
+    const int64_t j = start / kPage + r0 % np;
+    const int64_t row0 = j * kPage - start;           // row of the page's first token
+    const int page = j * kPage < (int64_t)start + count && j < S.width
+                         ? kv_page(S, pool.P, seq, (int)j) : -1;
+    const int64_t at = (int64_t)page * pool.H + h;
+    float ks = 0.0f, vs = 0.0f;
+    if (page >= 0) {
+      ks = pool.ks[at];
+      vs = pool.vs[at];
+      const int8_t* src = pool.v + at * (kPage * D);
+#pragma unroll
+      for (int i = tid; i < D * 4; i += NT) {
+        const int d = i >> 2, q = i & 3;
+        const uint4v o = *reinterpret_cast<const uint4v*>(src + d * kPage + 16 * q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) vt[d * 17 + 4 * q + e] = o[e];
+      }
+    }
+    __syncthreads();
+    uint32_t w[8];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) w[c] = vt[(8 * cg + c) * 17 + rg];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int64_t row = row0 + 4 * rg + r;
+      if (row < 0 || row >= n_tokens) continue;
+      const bool live = page >= 0 && row < count;
+      uint16_t a[8], b[8];
+      uint2v kc = {0, 0};
+      if (live)
+        kc = *reinterpret_cast<const uint2v*>(pool.k + at * (kPage * D) + (4 * rg + r) * D +
+                                              8 * cg);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const int qk = (int8_t)(kc[c >> 2] >> (8 * (c & 3)));
+        const int qv = (int8_t)(w[c] >> (8 * r));
+        a[c] = live ? kv_narrow<BF16>((float)qk * ks) : 0;
+        b[c] = live ? kv_narrow<BF16>((float)qv * vs) : 0;
+      }
+      uint16_t* ka = static_cast<uint16_t*>(k.p) + seq * k.seq + row * k.tok + h * k.head + 8 * cg;
+      uint16_t* va = static_cast<uint16_t*>(v.p) + seq * v.seq + row * v.tok + h * v.head + 8 * cg;
+      if (VEC) {
+        *reinterpret_cast<uint4v*>(ka) = *reinterpret_cast<uint4v*>(a);
+        *reinterpret_cast<uint4v*>(va) = *reinterpret_cast<uint4v*>(b);
+      } else {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          ka[c] = a[c];
+          va[c] = b[c];
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
+bool wide(const KvRows& r) {
+  return ((uintptr_t)r.p & 15) == 0 && ((r.seq | r.tok | r.head) & 7) == 0;
+}
+
+// Pages that n tokens can touch, wherever in a page they start.
+int touched(int n) { return (int)(((int64_t)n + 2 * kPage - 2) / kPage); }
+
+// Workgroups for `items`: all at once, below 2^32 threads and well inside the grid's limit; the
+// kernels walk on where there are more.
+unsigned grid_of(int64_t items) { return (unsigned)(items < (1 << 22) ? items : (1 << 22)); }
+
+template <int D, bool BF16>
+hipError_t store_d(const KvPool& pool, const KvSeqs& S, const int32_t* starts,
+                   const int32_t* counts, int n, const KvRows& k, const KvRows& v,
+                   uint32_t* status, hipStream_t st) {
+  const int np = touched(n);
+  const int64_t items = (int64_t)S.n * np * pool.H;
+  if (wide(k) && wide(v))
+    hipLaunchKernelGGL((store_kernel<D, BF16, true>), dim3(grid_of(items)), dim3(2 * D), 0, st,
+                       pool, S, starts, counts, n, np, items, k, v, status);
+  else
+    hipLaunchKernelGGL((store_kernel<D, BF16, false>), dim3(grid_of(items)), dim3(2 * D), 0, st,
+                       pool, S, starts, counts, n, np, items, k, v, status);
+  return hipGetLastError();
+}
+
+template <int D, bool BF16>
+hipError_t load_d(const KvPool& pool, const KvSeqs& S, const int32_t* starts,
+                  const int32_t* counts, int n, const KvRows& k, const KvRows& v,
+                  hipStream_t st) {
+  const int np = touched(n);
+  const int64_t items = (int64_t)S.n * np * pool.H;
+  if (wide(k) && wide(v))
+    hipLaunchKernelGGL((load_kernel<D, BF16, true>), dim3(grid_of(items)), dim3(2 * D), 0, st,
+                       pool, S, starts, counts, n, np, items, k, v);
+  else
+    hipLaunchKernelGGL((load_kernel<D, BF16, false>), dim3(grid_of(items)), dim3(2 * D), 0, st,
+                       pool, S, starts, counts, n, np, items, k, v);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t cg_launch_kv8_store(const KvPool& pool, const KvSeqs& S, int D, bool bf16,
+                               const int32_t* starts, const int32_t* counts, int n,
+                               const KvRows& k, const KvRows& v, uint32_t* status,
+                               hipStream_t st) {
+  if (status) hipLaunchKernelGGL(kv_zero_word, dim3(1), dim3(1), 0, st, status);
+  if (n <= 0) return hipGetLastError();
+  switch (D) {
+    case 64: return (bf16 ? store_d<64, true> : store_d<64, false>)(pool, S, starts, counts, n, k, v, status, st);
+    case 128: return (bf16 ? store_d<128, true> : store_d<128, false>)(pool, S, starts, counts, n, k, v, status, st);
+    default: return (bf16 ? store_d<256, true> : store_d<256, false>)(pool, S, starts, counts, n, k, v, status, st);
+  }
+}
+
+hipError_t cg_launch_kv8_load(const KvPool& pool, const KvSeqs& S, int D, bool bf16,
+                              const int32_t* starts, const int32_t* counts, int n,
+                              const KvRows& k, const KvRows& v, hipStream_t st) {
+  switch (D) {
+    case 64: return (bf16 ? load_d<64, true> : load_d<64, false>)(pool, S, starts, counts, n, k, v, st);
+    case 128: return (bf16 ? load_d<128, true> : load_d<128, false>)(pool, S, starts, counts, n, k, v, st);
+    default: return (bf16 ? load_d<256, true> : load_d<256, false>)(pool, S, starts, counts, n, k, v, st);
+  }
+}

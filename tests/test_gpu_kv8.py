@@ -1,0 +1,469 @@
+"""GPU: the 8-bit serving cache (store, load, attend, select, evict) against the definition in
+numpy (tests/kv8_reference.py).
+
+Codes, scales, bounds, picks, kept tokens and moved weights are compared bit for bit. Attention is
+compared in 64 bits under bounds that follow from its arithmetic: products are exact, sums of D
+products in fp32 are off by at most D 2^-24 of the sum of magnitudes (`spread`, in units of the
+logits), a weight by that much relatively (twice, for the logit and for the sum of weights) plus
+the exponential's and the references' roundings (2^-18 in all at these sizes), and rounding P to
+fp16 by 2^-11; the output adds half a unit of its type."""
+import numpy as np
+import pytest
+
+import kv8_reference as R
+from gpu_helpers import assert_same, say, torch_cuda
+
+pytestmark = pytest.mark.gpu
+
+PAGE = 64
+UNIT = {"float16": 2.0 ** -11, "bfloat16": 2.0 ** -8}
+
+
+def make(torch, n_pages, H, D, bounds=True):
+    from paper_2310_07240_amd.kv8 import Kv8Cache
+    dev = "cuda"
+    buf = {"k_codes": torch.randint(-127, 128, (n_pages, H, PAGE, D), device=dev).to(torch.int8),
+           "v_codes": torch.randint(-127, 128, (n_pages, H, D, PAGE), device=dev).to(torch.int8),
+           "k_scale": torch.rand((n_pages, H), device=dev) * 0.02 + 0.001,
+           "v_scale": torch.rand((n_pages, H), device=dev) * 0.02 + 0.001,
+           "k_bounds": None}
+    if bounds:
+        buf["k_bounds"] = torch.stack([buf["k_codes"].amin(2), buf["k_codes"].amax(2)],
+                                      2).contiguous()
+    return Kv8Cache(n_pages, H, D, buffers=buf)
+
+
+def tables(torch, rng, B, width, extra=2):
+    """A table of distinct pages in no order, and how many pages the pool has."""
+    n = B * width + extra
+    t = rng.permutation(n)[:B * width].reshape(B, width).astype(np.int32)
+    return t, torch.from_numpy(t).cuda(), n
+
+
+def ints(torch, x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def same_cache(cache, ref, pages=None):
+    at = slice(None) if pages is None else pages
+    assert_same("k codes", cache.k_codes.cpu().numpy()[at], ref.k[at])
+    assert_same("v codes", cache.v_codes.cpu().numpy().transpose(0, 1, 3, 2)[at], ref.v[at])
+    assert_same("k scale", cache.k_scale.cpu().numpy()[at], ref.ks[at])
+    assert_same("v scale", cache.v_scale.cpu().numpy()[at], ref.vs[at])
+    if ref.bounds is not None:
+        assert_same("bounds", cache.k_bounds.cpu().numpy()[at], ref.bounds[at])
+
+
+# ---- store and load ---------------------------------------------------------------------------
+@pytest.mark.parametrize("D,H,dtype,T,starts,counts", [
+    (128, 2, "float16", 200, [0, 5, 64], [200, 130, 64]),
+    (64, 3, "bfloat16", 1, [0, 63, 64, 127], [1, 1, 1, 1]),
+    (256, 1, "float16", 65, [1, 62, 100], [65, 3, 0]),
+    (128, 5, "bfloat16", 129, [127, 0], None),
+])
+def test_store_and_load(D, H, dtype, T, starts, counts):
+    torch = torch_cuda()
+    rng = np.random.default_rng(D + T)
+    B = len(starts)
+    t, table, n = tables(torch, rng, B, (max(starts) + T) // PAGE + 1)
+    cache = make(torch, n, H, D)
+    ref = R.Ref(cache)
+    dt = getattr(torch, dtype)
+    k = (torch.randn(B, T, H, D) * torch.exp(torch.randn(H, D))).to(dt).cuda()
+    v = torch.randn(B, T, H, D).to(dt).cuda()
+    k[0, 0, 0] = 0                             # a row of zeros, and one far above the rest
+    v[-1, 0, 0, 3] = 77.0
+    cnt = [T] * B if counts is None else counts
+    say(f"store {D} {H} {dtype} {T}")
+    cache.store(k, v, table, ints(torch, starts), None if counts is None else ints(torch, counts))
+    torch.cuda.synchronize()
+    ref.store(k.float().cpu().numpy(), v.float().cpu().numpy(), t, starts, cnt)
+    same_cache(cache, ref)
+    # once more: what is stored already stays as it is
+    cache.store(k, v, table, ints(torch, starts), ints(torch, cnt))
+    ref.store(k.float().cpu().numpy(), v.float().cpu().numpy(), t, starts, cnt)
+    same_cache(cache, ref)
+    for out_type in ("float16", "bfloat16"):
+        ot = getattr(torch, out_type)
+        back = cache.load(table, ints(torch, starts), T, ints(torch, cnt), dtype=ot)
+        torch.cuda.synchronize()
+        for codes, scale, got in ((ref.k, ref.ks, back[0]), (ref.v, ref.vs, back[1])):
+            want = np.zeros((B, T, H, D), np.float32)
+            for b in range(B):
+                for i in range(cnt[b]):
+                    p = t[b, (starts[b] + i) // PAGE]
+                    want[b, i] = codes[p, :, (starts[b] + i) % PAGE].astype(np.float32) \
+                        * scale[p][:, None]
+            assert_same(out_type, got.view(torch.int16).cpu().numpy(),
+                        torch.from_numpy(want).to(ot).view(torch.int16).numpy())
+
+
+@pytest.mark.parametrize("off", [0, 1])
+def test_store_strides(off):
+    """Rows inside a [ctx][layer][K/V][token][channel] cache; off = 1: not 16-byte aligned."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(3)
+    B, L, T, H, D = 2, 3, 70, 2, 64
+    flat = torch.randn(B * L * 2 * T * H * D + 8).half().cuda()
+    kv = flat[off:off + B * L * 2 * T * H * D].view(B * L, 2, T, H, D)
+    t, table, n = tables(torch, rng, B * L, 2)
+    cache = make(torch, n, H, D, bounds=False)
+    ref = R.Ref(cache)
+    zero = [0] * (B * L)
+    cache.store(kv[:, 0], kv[:, 1], table, ints(torch, zero))
+    x = kv.float().cpu().numpy()
+    ref.store(x[:, 0], x[:, 1], t, zero, [T] * (B * L))
+    same_cache(cache, ref)
+    out = torch.zeros_like(flat)[off:off + kv.numel()].view(kv.shape)
+    cache.load(table, ints(torch, zero), T, k=out[:, 0], v=out[:, 1])
+    again = cache.load(table, ints(torch, zero), T)
+    assert torch.equal(out[:, 0], again[0]) and torch.equal(out[:, 1], again[1])
+
+
+def test_store_pages_and_values_out_of_place():
+    """Page numbers off the pool are skipped, NaN and Inf set no scale and are reported."""
+    torch = torch_cuda()
+    from paper_2310_07240_amd.cachegen import cg_get_status
+    t = np.array([[1, -1, 3], [99, 0, 5]], np.int32)
+    table = torch.from_numpy(t).cuda()
+    cache = make(torch, 6, 1, 64)
+    ref = R.Ref(cache)
+    k, v = torch.randn(2, 150, 1, 64).half(), torch.randn(2, 150, 1, 64).half()
+    status = ints(torch, [7])
+    args = (table, ints(torch, [0, 10]))
+    cache.store(k.cuda(), v.cuda(), *args, status=status)
+    assert cg_get_status(status) == 0
+    ref.store(k.float().numpy(), v.float().numpy(), t, [0, 10], [150, 150])
+    same_cache(cache, ref)
+    k[0, 3, 0, 5], k[1, 140, 0, 1], v[0, 0, 0, 0] = float("nan"), float("-inf"), float("inf")
+    v[1, 100:, 0] = float("nan")
+    cache.store(k.cuda(), v.cuda(), *args, status=status)
+    assert cg_get_status(status) == -4
+    ref.store(k.float().numpy(), v.float().numpy(), t, [0, 10], [150, 150])
+    same_cache(cache, ref)
+    kb, vb = cache.load(table, ints(torch, [0, 10]), 150)
+    assert (kb[0, 64:128] == 0).all() and (vb[1, :54] == 0).all()
+
+
+@pytest.mark.parametrize("size", [1e-38, 1e-41, 3e38])
+def test_store_extreme_sizes(size):
+    """bf16 rows whose scale is subnormal, or near the largest."""
+    torch = torch_cuda()
+    cache = make(torch, 3, 1, 64)
+    ref = R.Ref(cache)
+    t = np.array([[2]], np.int32)
+    k = (torch.rand(1, 64, 1, 64) * size).bfloat16()
+    v = -k
+    cache.store(k.cuda(), v.cuda(), torch.from_numpy(t).cuda(), ints(torch, [0]))
+    ref.store(k.float().numpy(), v.float().numpy(), t, [0], [64])
+    same_cache(cache, ref)
+
+
+# ---- attention --------------------------------------------------------------------------------
+def check_attend(torch, cache, q, table, t, lengths, q_lens=None, picks=None, mass=False,
+                 scale=None, max_len=None, decay=0.5):
+    B, Q, HQ, D = q.shape
+    scale = D ** -0.5 if scale is None else scale
+    name = str(q.dtype).split(".")[1]
+    lse = torch.full((B, Q, HQ), 7.0, device="cuda")
+    out = torch.full_like(q, 7.0)
+    more = {}
+    if mass:
+        old = torch.rand((cache.n_pages, cache.n_heads, PAGE), device="cuda")
+        got_mass = torch.full_like(old, -1.0)
+        more = {"mass": old, "mass_out": got_mass, "decay": decay}
+    dev_picks = None if picks is None else torch.from_numpy(picks).cuda()
+    say(f"attend {tuple(q.shape)} {name} lengths {list(lengths)[:4]} picks {picks is not None}")
+    for _ in range(2):                        # the same bits each time
+        first = out.clone()
+        cache.attend(q, table, ints(torch, lengths), scale=scale, max_len=max_len, out=out,
+                     q_lens=None if q_lens is None else ints(torch, q_lens), lse=lse,
+                     picks=dev_picks, **more)
+    torch.cuda.synchronize()
+    assert torch.equal(first, out) or torch.isnan(out).any()
+    ql = [Q] * B if q_lens is None else q_lens
+    cut = [min(x, table.shape[1] * PAGE if max_len is None else max_len) for x in lengths]
+    want, wl, wm, size, spread = R.attend(R.Ref(cache), q.float().cpu().numpy(), t, cut, ql, scale,
+                                          picks)
+    off = 4 * D * 2.0 ** -24 * spread + 2.0 ** -18
+    bound = UNIT[name] * np.abs(want) + (2.0 ** -11 + off)[..., None] * size * 1.01 + 1e-7
+    err = np.abs(out.float().cpu().numpy().astype(np.float64) - want)
+    assert (err <= bound).all(), (err / bound).max()
+    g = lse.cpu().numpy().astype(np.float64)
+    assert (np.isinf(g) == np.isinf(wl)).all()
+    fin = np.isfinite(wl)
+    lerr = np.abs(np.where(fin, g - np.where(fin, wl, 0), 0))
+    lim = off + 2.0 ** -20 * np.abs(np.where(fin, wl, 0))
+    assert (lerr <= lim).all(), (lerr / lim).max()
+    if mass:
+        seen = np.zeros(wm.shape, bool)
+        for b in range(B):
+            for j in range(min(cut[b], table.shape[1] * PAGE)):
+                p = t[b, j // PAGE]
+                if 0 <= p < cache.n_pages:
+                    seen[p, :, j % PAGE] = True
+        gm = got_mass.cpu().numpy().astype(np.float64)
+        wm = wm + decay * old.cpu().numpy().astype(np.float64)
+        assert (gm[~seen] == -1.0).all()
+        lim = (off.max(initial=0) * 2 + 2.0 ** -22 * Q * HQ + 2.0 ** -20) * wm + 1e-12
+        assert (np.abs(gm - wm)[seen] <= lim[seen]).all()
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("D,HQ,H,lengths", [
+    (128, 4, 1, [1, 2, 63, 64, 65, 0, 700]),
+    (64, 8, 2, [300, 17]),
+    (256, 3, 3, [129, 128]),
+    (128, 17, 1, [200]),                      # a group past one 16-row tile
+    (64, 40, 1, [333]),
+])
+def test_attend_one_token(dtype, D, HQ, H, lengths):
+    torch = torch_cuda()
+    rng = np.random.default_rng(D + HQ)
+    t, table, n = tables(torch, rng, len(lengths), max(lengths) // PAGE + 2)
+    cache = make(torch, n, H, D)
+    q = (torch.randn(len(lengths), 1, HQ, D) * 2).to(getattr(torch, dtype)).cuda()
+    check_attend(torch, cache, q, table, t, lengths, mass=True)
+    check_attend(torch, cache, q, table, t, lengths, max_len=max(lengths))
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("D,HQ,H,Q,lengths,q_lens", [
+    (128, 4, 2, 5, [5, 70, 3, 64], [5, 3, 3, 0]),
+    (64, 2, 1, 33, [33, 200], None),
+    (128, 8, 1, 40, [100, 40, 0], [40, 39, 0]),
+    (256, 2, 2, 17, [130], None),
+    (128, 3, 1, 90, [250, 90], None),
+    (64, 6, 2, 130, [450], None),
+    (128, 8, 2, 70, [513, 64, 300], [70, 1, 64]),
+])
+def test_attend_many_tokens(dtype, D, HQ, H, Q, lengths, q_lens):
+    torch = torch_cuda()
+    rng = np.random.default_rng(Q)
+    t, table, n = tables(torch, rng, len(lengths), max(lengths) // PAGE + 1)
+    cache = make(torch, n, H, D)
+    q = (torch.randn(len(lengths), Q, HQ, D) * 2).to(getattr(torch, dtype)).cuda()
+    check_attend(torch, cache, q, table, t, lengths, q_lens=q_lens, mass=True)
+
+
+def test_attend_more_queries_than_tokens():
+    """A call whose first queries stand before the sequence's first token: empty rows."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(9)
+    t, table, n = tables(torch, rng, 2, 2)
+    cache = make(torch, n, 2, 64)
+    q = torch.randn(2, 30, 4, 64).half().cuda()
+    check_attend(torch, cache, q, table, t, [7, 29], mass=True)
+
+
+def test_attend_strides_and_garbage_outside():
+    """Strided queries and outputs, page numbers off the pool, lengths past the table, NaN scales
+    in pages that no sequence reads, codes of all kinds behind the length."""
+    torch = torch_cuda()
+    t = np.array([[0, 3, 77, 2], [4, -5, 1, 6]], np.int32)
+    table = torch.from_numpy(t).cuda()
+    cache = make(torch, 9, 2, 128)
+    cache.k_scale[5] = float("nan")
+    cache.v_scale[7] = float("inf")
+    big = torch.randn(2, 4, 3, 3, 128).half().cuda()
+    q = big[:, :, 1, :2]
+    check_attend(torch, cache, q, table, t, [1000, 200], mass=True)
+    o = torch.full((2, 2, 4, 130), 5.0, dtype=torch.float16, device="cuda")
+    view = o.permute(0, 2, 1, 3)[..., 1:129]
+    a = cache.attend(q, table, ints(torch, [200, 90]))
+    cache.attend(q, table, ints(torch, [200, 90]), out=view)
+    assert torch.equal(a, view)
+    assert (o[..., 0] == 5).all() and (o[..., 129] == 5).all()
+
+
+def test_attend_nan_query_stays_in_its_row():
+    torch = torch_cuda()
+    for dtype in (torch.float16, torch.bfloat16):
+        rng = np.random.default_rng(2)
+        t, table, n = tables(torch, rng, 1, 3)
+        cache = make(torch, n, 1, 128)
+        q = torch.randn(1, 3, 4, 128).to(dtype).cuda()
+        good = cache.attend(q, table, ints(torch, [150]))
+        q[0, 1, 2, 7] = float("nan")
+        q[0, 2, 3, 9] = float("inf")
+        got = cache.attend(q, table, ints(torch, [150]))
+        bad = torch.zeros((1, 3, 4), dtype=torch.bool, device="cuda")
+        bad[0, 1, 2] = bad[0, 2, 3] = True
+        assert torch.equal(got[~bad], good[~bad])
+        assert torch.isnan(got[0, 1, 2]).all()
+
+
+@pytest.mark.parametrize("scale", [-0.3, 0.0, 3.0])
+def test_attend_scales_and_extremes(scale):
+    """Logits far apart (a few hundred), equal, and in reverse; one heavy token before a long
+    light tail whose sum still counts."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(4)
+    t, table, n = tables(torch, rng, 1, 20)
+    cache = make(torch, n, 1, 64)
+    q = torch.randn(1, 2, 5, 64).half().cuda()
+    check_attend(torch, cache, q, table, t, [1234], scale=scale, mass=True)
+    cache.k_codes.zero_()
+    cache.k_codes[int(t[0, 0]), 0, 5, :] = 100
+    cache.k_scale.fill_(0.01)
+    cache.v_scale[int(t[0, 3])] = 1e-4
+    cache.v_scale[int(t[0, 4])] = 0.0
+    q.fill_(0.25)
+    check_attend(torch, cache, q, table, t, [1234], scale=1.0)
+
+
+def test_attend_long_and_split():
+    """Long enough for many splits; lengths far below the bound, so that splits stay empty."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(5)
+    t, table, n = tables(torch, rng, 2, 160)
+    cache = make(torch, n, 1, 64)
+    q = torch.randn(2, 1, 2, 64).half().cuda()
+    check_attend(torch, cache, q, table, t, [10171, 65], mass=True)
+
+
+def test_attend_on_another_stream():
+    torch = torch_cuda()
+    rng = np.random.default_rng(6)
+    t, table, n = tables(torch, rng, 2, 40)
+    cache = make(torch, n, 2, 128)
+    q = torch.randn(2, 1, 8, 128).half().cuda()
+    L = ints(torch, [2500, 900])
+    want = cache.attend(q, table, L)
+    torch.cuda.synchronize()
+    other = torch.cuda.Stream()
+    got = cache.attend(q, table, L, stream=other)
+    other.synchronize()
+    assert torch.equal(want, got)
+
+
+def test_attend_graph_replay():
+    """Captured once, replayed between eager work with new contents: the same as eager."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(7)
+    t, table, n = tables(torch, rng, 3, 30)
+    cache = make(torch, n, 2, 128)
+    q = torch.randn(3, 1, 8, 128).half().cuda()
+    k, v = torch.randn(3, 1, 2, 128).half().cuda(), torch.randn(3, 1, 2, 128).half().cuda()
+    starts, L = ints(torch, [100, 700, 1500]), ints(torch, [101, 701, 1501])
+    out = torch.empty_like(q)
+    mass = torch.zeros((n, 2, PAGE), device="cuda")
+    got_mass = torch.zeros_like(mass)
+    picks = torch.zeros((3, 1, 2, 4), dtype=torch.int32, device="cuda")
+    sparse = torch.empty_like(q)
+
+    def step():
+        cache.store(k, v, table, starts)
+        cache.attend(q, table, L, out=out, mass=mass, mass_out=got_mass)
+        cache.select(q, table, L, 4, out=picks)
+        cache.attend(q, table, L, out=sparse, picks=picks)
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(4):
+        q.copy_(torch.randn(q.shape))
+        k.copy_(torch.randn(k.shape))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in (out, got_mass, picks, sparse)]
+        step()
+        torch.cuda.synchronize()
+        for a, b in zip(got, (out, got_mass, picks, sparse)):
+            assert torch.equal(a, b), i
+
+
+# ---- select and sparse attention --------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("D,HQ,H,Q,lengths,n_picks,recent", [
+    (128, 8, 2, 1, [1, 64, 65, 1000, 0], 3, 1),
+    (64, 3, 1, 2, [640, 641], 5, 2),
+    (256, 2, 1, 1, [2000], 4, 0),
+    (128, 16, 1, 3, [900], 2, 5),
+    (64, 2, 2, 1, [20000], 70, 1),
+])
+def test_select_and_sparse(dtype, D, HQ, H, Q, lengths, n_picks, recent):
+    torch = torch_cuda()
+    rng = np.random.default_rng(D + n_picks)
+    B = len(lengths)
+    t, table, n = tables(torch, rng, B, max(lengths) // PAGE + 1)
+    cache = make(torch, n, H, D)
+    # ranges that differ, some alike: scores that differ, and ties
+    part = torch.randint(1, 9, (n, H, 1, 1), device="cuda") / 8.0
+    cache.k_codes.copy_((cache.k_codes.float() * part).round())
+    cache.k_codes[: n // 2] = cache.k_codes[0]
+    cache.k_scale[: n // 2] = 0.01
+    cache.k_bounds.copy_(torch.stack([cache.k_codes.amin(2), cache.k_codes.amax(2)], 2))
+    q = torch.randn(B, Q, HQ, D).to(getattr(torch, dtype)).cuda()
+    q[0, 0, 0, 0] = 0.0
+    say(f"select {D} {HQ} {H} {lengths}")
+    q_lens = [min(Q, x) for x in lengths]
+    picks = cache.select(q, table, ints(torch, lengths), n_picks, recent=recent,
+                         q_lens=ints(torch, q_lens))
+    want = R.select(R.Ref(cache), q.float().cpu().numpy(), t, lengths, q_lens, n_picks, recent)
+    assert_same("picks", picks.cpu().numpy(), want)
+    check_attend(torch, cache, q, table, t, lengths, q_lens=q_lens, picks=want)
+
+
+def test_sparse_with_odd_picks():
+    """Entries outside the sequence are skipped; no entry at all gives an empty row."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(8)
+    t, table, n = tables(torch, rng, 2, 6)
+    cache = make(torch, n, 1, 128)
+    q = torch.randn(2, 1, 4, 128).half().cuda()
+    picks = np.array([[[[5, -1, 0, 99, -7]]], [[[-1, 4, 77, -1, -1]]]], np.int32)
+    check_attend(torch, cache, q, table, t, [330, 200], picks=picks)
+
+
+def test_select_zero_queries_and_lost_pages():
+    torch = torch_cuda()
+    t = np.array([[0, 1, 50, 3, 4, -2, 6]], np.int32)
+    table = torch.from_numpy(t).cuda()
+    cache = make(torch, 8, 1, 64)
+    q = torch.zeros(1, 1, 2, 64).half().cuda()
+    for lengths in ([400], [7 * 64]):
+        picks = cache.select(q, table, ints(torch, lengths), 3)
+        want = R.select(R.Ref(cache), np.zeros((1, 1, 2, 64), np.float32), t, lengths, [1], 3, 1)
+        assert_same("picks", picks.cpu().numpy(), want)
+
+
+# ---- eviction ---------------------------------------------------------------------------------
+@pytest.mark.parametrize("D,H,lengths,keep,recent", [
+    (128, 2, [500, 64, 130, 0, 129], 130, 30),
+    (64, 3, [300], 1, 0),
+    (64, 1, [300, 299], 65, 65),
+    (256, 1, [200], 100, 150),
+    (128, 1, [5000, 4000], 1000, 100),
+])
+def test_evict(D, H, lengths, keep, recent):
+    torch = torch_cuda()
+    rng = np.random.default_rng(D + keep)
+    B = len(lengths)
+    width, new_width = max(lengths) // PAGE + 1, (keep + PAGE - 1) // PAGE
+    n = B * (width + new_width) + 2
+    order = rng.permutation(n).astype(np.int32)
+    t = order[:B * width].reshape(B, width).copy()
+    to = order[B * width:B * (width + new_width)].reshape(B, new_width).copy()
+    cache = make(torch, n, H, D)
+    mass = torch.rand((n, H, PAGE), device="cuda")
+    mass[torch.rand(mass.shape, device="cuda") < 0.3] = 0.25          # ties
+    mass[torch.rand(mass.shape, device="cuda") < 0.1] = 0.0
+    mass[torch.rand(mass.shape, device="cuda") < 0.05] = -0.0
+    mass[torch.rand(mass.shape, device="cuda") < 0.02] = float("nan")
+    mass[torch.rand(mass.shape, device="cuda") < 0.02] = float("inf")
+    ref, rm = R.Ref(cache), mass.cpu().numpy().copy()
+    say(f"evict {D} {H} {lengths} {keep} {recent}")
+    kept, new = cache.evict(torch.from_numpy(t).cuda(), ints(torch, lengths), mass, keep, recent,
+                            torch.from_numpy(to).cuda())
+    torch.cuda.synchronize()
+    wk, wn = R.evict(ref, t, lengths, rm, keep, recent, to)
+    assert_same("kept", kept.cpu().numpy(), wk)
+    assert_same("lengths", new.cpu().numpy(), wn)
+    same_cache(cache, ref)
+    assert_same("mass", mass.cpu().numpy().view(np.int32), rm.view(np.int32))

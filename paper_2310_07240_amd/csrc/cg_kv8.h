@@ -231,7 +231,8 @@ struct KvAttn {
 };
 
 struct KvAttnPlan {
-  int32_t tiles, splits;        // row tiles and splits of the pages for each (sequence, KV head)
+  int32_t tiles, splits;        // 16-row tiles and splits of the pages for each (sequence, KV head)
+  int32_t big, blocks;          // prompt_kernel: tiles of 128 blocks rows; big = 0: attend_kernel
   uint64_t part_off, lse_off, total;   // workspace, in bytes
 };
 

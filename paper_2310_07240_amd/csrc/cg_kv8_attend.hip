@@ -380,6 +380,341 @@ __global__ __launch_bounds__(256) void mass_kernel(KvPool pool, KvSeqs S, KvAttn
   }
 }
 
+// ---- many rows ------------------------------------------------------------------------------
+// Where a KV head has many rows, the matrix units bound: v_mfma_f32_32x32x16_f16, transposed as
+// above (lane = 32 half + m, results of row m), a wave with NB blocks of 32 rows. The workgroup's
+// four waves share each page through LDS: it is loaded as codes one page ahead, widened to fp16
+// once, and read as operands by every wave. Row m of a 32-token K tile is the token whose place
+// makes a lane's 16 results the consecutive tokens 16 half .. 16 half + 15 (`tile_row`), the k
+// slots it supplies for P V.
+//
+// The weights of a page enter the second product times the page's V scale, relative to a running
+// reference of that product (`ref`, log2), so O needs no further factor; l has a reference of its
+// own (`ref_l`). `ref` moves only where a row passes it by more than 2^kSlack, so the accumulators
+// are rescaled on few pages: what fp16 holds is at most 2^(kLift + kSlack), and normal down to
+// 2^-(14 + kLift) of the reference (2^-(24 + kLift) in steps of that), far below what a sum
+// around 1 shows.
+constexpr int kLift = 4, kSlack = 8;
+
+__device__ __forceinline__ int tile_row(int t) {       // of token t of 32: its row in the K tile
+  return 8 * ((t & 15) >> 2) + 4 * (t >> 4) + (t & 3);
+}
+
+// A value and that of the lane with the other half. The copy is made opaque: given one value as
+// both operands of the swap, the compiler takes its two results to be equal.
+__device__ __forceinline__ void both_halves(uint32_t u, uint32_t& lo, uint32_t& hi) {
+  uint32_t w = u;
+  asm("" : "+v"(w));
+  const auto r = __builtin_amdgcn_permlane32_swap(u, w, false, false);
+  lo = r[0];
+  hi = r[1];
+}
+// The largest of three, without the canonicalization that fmaxf of unknown values costs.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+__device__ __forceinline__ float half_max(float x) {   // over the lanes of equal m
+  uint32_t lo, hi;
+  both_halves(__builtin_bit_cast(uint32_t, x), lo, hi);
+  return fmaxf(__builtin_bit_cast(float, lo), __builtin_bit_cast(float, hi));
+}
+__device__ __forceinline__ float half_sum(float x) {
+  uint32_t lo, hi;
+  both_halves(__builtin_bit_cast(uint32_t, x), lo, hi);
+  return __builtin_bit_cast(float, lo) + __builtin_bit_cast(float, hi);
+}
+
+// One row's queries as B operands of the 32-row products: q[s] holds channels 16 s + 8 half ..
+// + 7. Returns what S is multiplied by (bf16 rows scaled as in load_q, the scale's sign taken
+// into the queries so that a row's largest product is its largest S).
+template <int D, bool BF16>
+__device__ __forceinline__ float load_row32(const KvAttn& A, const uint16_t* src, bool live,
+                                            half8* q) {
+  const int half = (threadIdx.x & 63) >> 5;
+  uint16_t u[D / 16][8];
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+    for (int c = 0; c < 8; ++c) u[s][c] = live ? src[16 * s + 8 * half + c] : 0;
+  int e = 0;
+  const uint16_t flip = A.scale < 0.0f ? 0x8000u : 0;
+  if (BF16) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const uint32_t a = u[s][c] & 0x7fffu;
+        top = a > top && a < 0x7f80u ? a : top;
+      }
+    uint32_t lo, hi;
+    both_halves(top, lo, hi);
+    top = lo > hi ? lo : hi;
+    e = (int)(top >> 7) - 127;
+    if (e < -126) e = -126;
+  }
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const uint16_t w = u[s][c] ^ flip;
+      q[s][c] = BF16 ? (_Float16)__builtin_ldexpf(kv_widen<true>(w), -e)
+                     : __builtin_bit_cast(_Float16, w);
+    }
+  return __builtin_ldexpf(__builtin_fabsf(A.scale) * kLog2e, e);
+}
+
+template <int D>
+struct PromptLds {
+  _Float16 k[2][kPage][D + 8];       // rows in the order of tile_row; 16 bytes of padding a row
+  _Float16 v[2][D][kPage + 8];       // keep the lanes' 16-byte reads off one another's banks
+};
+
+// Codes of one page on their way to LDS: 16 bytes a thread and step.
+template <int D>
+struct PageRegs {
+  uint4v k[D / 64], v[D / 64];
+};
+
+template <int D>
+__device__ __forceinline__ void page_fetch(const KvPool& pool, int64_t at, PageRegs<D>& r) {
+  const uint4v* k = reinterpret_cast<const uint4v*>(pool.k + at * (kPage * D));
+  const uint4v* v = reinterpret_cast<const uint4v*>(pool.v + at * (kPage * D));
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) {
+    r.k[i] = k[i * 256 + threadIdx.x];
+    r.v[i] = v[i * 256 + threadIdx.x];
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void page_widen(const PageRegs<D>& r, PromptLds<D>& L, int buf) {
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) {
+    const int n = i * 256 + threadIdx.x;
+    const int t = n / (D / 16), d = n % (D / 16) * 16;
+    _Float16* k = &L.k[buf][(t & 32) + tile_row(t & 31)][d];
+    *reinterpret_cast<half8*>(k) = kv_widen8(r.k[i][0], r.k[i][1]);
+    *reinterpret_cast<half8*>(k + 8) = kv_widen8(r.k[i][2], r.k[i][3]);
+    _Float16* v = &L.v[buf][n >> 2][(n & 3) * 16];
+    *reinterpret_cast<half8*>(v) = kv_widen8(r.v[i][0], r.v[i][1]);
+    *reinterpret_cast<half8*>(v + 8) = kv_widen8(r.v[i][2], r.v[i][3]);
+  }
+}
+
+// Workgroup = (sequence, KV head, tile of 128 NB rows, split of the pages).
+template <int D, bool BF16, int NB>
+__global__ __launch_bounds__(256, 1) void prompt_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles,
+                                                        int splits, int64_t items, float* part,
+                                                        float* lse) {
+  __shared__ PromptLds<D> L;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 31, half = lane >> 5;
+  const int64_t it = blockIdx.x;
+  if (it >= items) return;
+  const int h = (int)(it % pool.H);
+  int64_t r = it / pool.H;
+  const int split = (int)(r % splits);
+  r /= splits;
+  const int tile = tiles - 1 - (int)(r % tiles);       // the tiles that see most go first
+  const int seq = (int)(r / tiles);
+  const RowsOf R = rows_of(S, A, seq);
+  const int rows = R.nq * A.group, base = (tile * 4 + wave) * (32 * NB);
+
+  half8 q[NB][D / 16];
+  float unit[NB];
+  int visible[NB], low = 0x7fffffff, high = 0;
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    const int row = base + 32 * b + m;
+    const int i = row / A.group, head = h * A.group + row % A.group;
+    const int see = row < rows ? visible_of(R, i) : 0;
+    const uint16_t* src = static_cast<const uint16_t*>(A.q.p) + R.seq * A.q.seq +
+                          (int64_t)i * A.q.tok + (int64_t)head * A.q.head;
+    unit[b] = load_row32<D, BF16>(A, src, see > 0, q[b]);
+    high = see > high ? see : high;
+    // a row that sees nothing is not masked page by page: it is written as empty at the end
+    visible[b] = see > 0 ? see : 0x7fffffff;
+    low = visible[b] < low ? visible[b] : low;
+  }
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    int v = __shfl_xor(high, o);
+    high = v > high ? v : high;
+    v = __shfl_xor(low, o);
+    low = v < low ? v : low;
+  }
+  high = __builtin_amdgcn_readfirstlane(high);
+  low = __builtin_amdgcn_readfirstlane(low);
+  // the workgroup's pages: up to what its last live row sees
+  int last = (tile + 1) * (128 * NB) - 1;
+  last = last < rows ? last : rows - 1;
+  int top_token = last / A.group;
+  if (top_token >= R.q_len) top_token = R.q_len - 1;
+  const int most = top_token >= 0 ? visible_of(R, top_token) : 0;
+  const int n = (most + kPage - 1) / kPage;
+  const int per = (n + splits - 1) / splits;
+  const int j0 = split * per, j1 = j0 + per < n ? j0 + per : n;
+
+  float16v o[NB][D / 32];
+  float ref[NB], ref_l[NB], l[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    ref[b] = ref_l[b] = -1e30f;
+    l[b] = 0.0f;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[b][dt][e] = 0.0f;
+  }
+  float v_top = 0.0f;
+
+  PageRegs<D> regs;
+  float ks = 0.0f, vs = 0.0f;
+  int page = j0 < j1 ? kv_page(S, pool.P, seq, j0) : -1;
+  if (page >= 0) {
+    const int64_t at = (int64_t)page * pool.H + h;
+    page_fetch<D>(pool, at, regs);
+    ks = pool.ks[at];
+    vs = pool.vs[at];
+    page_widen<D>(regs, L, j0 & 1);
+  }
+  for (int j = j0; j < j1; ++j) {
+    const int next = j + 1 < j1 ? kv_page(S, pool.P, seq, j + 1) : -1;
+    float ks_n = 0.0f, vs_n = 0.0f;
+    if (next >= 0) {
+      const int64_t at = (int64_t)next * pool.H + h;
+      page_fetch<D>(pool, at, regs);
+      ks_n = pool.ks[at];
+      vs_n = pool.vs[at];
+    }
+    __syncthreads();                 // page j is in LDS, and nobody reads page j - 1 any more
+    const int buf = j & 1, pos0 = j * kPage;
+    if (page >= 0 && pos0 < high) {
+      float16v x[NB][2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[b][u][e] = 0.0f;
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) {
+          const half8 a =
+              *reinterpret_cast<const half8*>(&L.k[buf][32 * u + m][16 * s + 8 * half]);
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+            x[b][u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, q[b][s], x[b][u], 0, 0, 0);
+        }
+      }
+      if (pos0 + kPage > low) {      // the page ends beyond what some row sees
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (pos0 + 32 * u + 16 * half + e >= visible[b]) x[b][u][e] = kNegInf;
+      }
+      // a V scale 2^60 below an earlier one (or 0) adds nothing to O, only its weights to l
+      v_top = fmaxf(v_top, vs);
+      const bool with_v = vs > v_top * 0x1p-60f;
+      const float lv = with_v ? __builtin_amdgcn_logf(vs) : 0.0f;
+      half8 p[NB][4];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        // never 0, so that what is masked stays -inf (products of codes and queries are < 2^31)
+        const float f = fmaxf(unit[b] * ks, 0x1p-120f);
+        float t = kNegInf;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) t = max3(t, x[b][0][e], x[b][1][e]);
+        t = half_max(t) * f;
+        if (with_v && __any(t + lv > ref[b] + (float)kSlack)) {
+          const float now = t + lv > ref[b] ? t + lv : ref[b];
+          const float a = __builtin_amdgcn_exp2f(ref[b] - now);
+          ref[b] = now;
+#pragma unroll
+          for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[b][dt][e] *= a;
+        }
+        const float top_l = t > ref_l[b] ? t : ref_l[b];
+        const float c = with_v ? lv + (float)kLift - ref[b] : -top_l;
+        float sum = 0.0f;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][u][e], f, c));
+            sum += w;
+            p[b][2 * u + (e >> 3)][e & 7] = (_Float16)w;
+          }
+        if (with_v) sum *= __builtin_amdgcn_exp2f(-top_l - c);
+        l[b] = __builtin_fmaf(l[b], __builtin_amdgcn_exp2f(ref_l[b] - top_l), sum);
+        ref_l[b] = top_l;
+      }
+      if (with_v) {
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const half8 a = *reinterpret_cast<const half8*>(
+                &L.v[buf][32 * dt + m][32 * (e >> 1) + 16 * half + 8 * (e & 1)]);
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+              o[b][dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, p[b][e], o[b][dt], 0, 0, 0);
+          }
+      }
+    }
+    if (next >= 0) page_widen<D>(regs, L, (j + 1) & 1);
+    page = next;
+    ks = ks_n;
+    vs = vs_n;
+  }
+
+  // lane (m, half) has row m, channels 32 dt + 8 a + 4 half + 0 .. 3
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    const int row = base + 32 * b + m;
+    const float sum = half_sum(l[b]);
+    if (row >= rows) continue;
+    const bool empty = visible[b] == 0x7fffffff || !(sum > 0.0f || sum != sum);
+    const float unit_o = __builtin_amdgcn_exp2f(ref[b] - (float)kLift - ref_l[b]);
+    if (splits > 1) {
+      const int64_t u16 = ((int64_t)seq * pool.H + h) * ((rows + 15) / 16) + row / 16;
+      float* dst = part + (u16 * splits + split) * (16 * (D + 2));
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          float4v w;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = empty ? 0.0f : o[b][dt][4 * a + e] * unit_o;
+          *reinterpret_cast<float4v*>(dst + (row & 15) * D + 32 * dt + 8 * a + 4 * half) = w;
+        }
+      if (half == 0) {
+        dst[16 * D + (row & 15)] = empty ? kNegInf : ref_l[b];
+        dst[16 * D + 16 + (row & 15)] = empty ? 0.0f : sum;
+      }
+    } else {
+      const float f = empty ? 0.0f : unit_o / sum;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          float w[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = empty ? 0.0f : o[b][dt][4 * a + e] * f;
+          put_out<D, BF16>(A, R, h, row, 32 * dt + 8 * a + 4 * half, w, 4);
+        }
+      if (lse && half == 0)
+        lse[lse_at(A, R, pool.H, h, row)] =
+            empty ? kNegInf : (ref_l[b] + __builtin_amdgcn_logf(sum)) * kLn2;
+    }
+  }
+}
+
 unsigned grid_of(int64_t items) { return (unsigned)(items < (1 << 22) ? items : (1 << 22)); }
 
 template <int D, bool BF16>
@@ -391,8 +726,19 @@ hipError_t attend_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, void* 
   float* lse = A.lse ? A.lse : A.mass_out ? reinterpret_cast<float*>(base + P.lse_off) : nullptr;
   const int vseqs = A.picks ? S.n * A.nq : S.n;
   const int64_t units = (int64_t)vseqs * pool.H * P.tiles;
-  hipLaunchKernelGGL((attend_kernel<D, BF16>), dim3(grid_of(units * P.splits)), dim3(256), 0, st,
-                     pool, S, A, P.tiles, P.splits, units * P.splits, part, lse);
+  if (P.big) {
+    const int64_t items = (int64_t)vseqs * pool.H * P.big * P.splits;
+    constexpr int NB = D == 256 ? 1 : 2;
+    if (P.blocks == NB)
+      hipLaunchKernelGGL((prompt_kernel<D, BF16, NB>), dim3((unsigned)items), dim3(256), 0, st,
+                         pool, S, A, P.big, P.splits, items, part, lse);
+    else
+      hipLaunchKernelGGL((prompt_kernel<D, BF16, 1>), dim3((unsigned)items), dim3(256), 0, st,
+                         pool, S, A, P.big, P.splits, items, part, lse);
+  } else {
+    hipLaunchKernelGGL((attend_kernel<D, BF16>), dim3(grid_of(units * P.splits)), dim3(256), 0,
+                       st, pool, S, A, P.tiles, P.splits, units * P.splits, part, lse);
+  }
   if (P.splits > 1)
     hipLaunchKernelGGL((join_kernel<D, BF16>), dim3(grid_of(units)), dim3(256), 0, st, pool, S, A,
                        P.tiles, P.splits, units, part, lse);
@@ -414,9 +760,20 @@ KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& S, const KvAttn& A, int
   const int64_t vseqs = A.picks ? (int64_t)S.n * A.nq : S.n;
   const int64_t units = vseqs * pool.H * P.tiles;
   const int64_t pages = A.picks ? A.n_picks : ((int64_t)A.max_len + kPage - 1) / kPage;
-  // enough workgroups to fill the card, each wave with a page of its own at least
-  int64_t s = (1024 + units - 1) / units;
-  const int64_t most = (pages + 3) / 4;
+  // From three 16-row tiles on, the rows share the pages through LDS (prompt_kernel).
+  P.big = P.blocks = 0;
+  int64_t s, most;
+  if (P.tiles > 2) {
+    P.blocks = D == 256 || rows <= 128 ? 1 : 2;
+    P.big = (int)((rows + 128 * P.blocks - 1) / (128 * P.blocks));
+    const int64_t groups = vseqs * pool.H * P.big;
+    s = (256 + groups - 1) / groups;
+    most = pages / 4;
+  } else {
+    // enough workgroups to fill the card, each wave with a page of its own at least
+    s = (1024 + units - 1) / units;
+    most = (pages + 3) / 4;
+  }
   if (s > most) s = most;
   if (s < 1) s = 1;
   P.splits = (int)s;

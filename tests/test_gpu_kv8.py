@@ -312,6 +312,39 @@ def test_attend_scales_and_extremes(scale):
     check_attend(torch, cache, q, table, t, [1234], scale=1.0)
 
 
+@pytest.mark.parametrize("D,dtype", [(128, "float16"), (64, "bfloat16"), (256, "float16")])
+@pytest.mark.parametrize("scale", [-0.2, 0.0, 2.0])
+def test_attend_many_tokens_scales_and_extremes(D, dtype, scale):
+    """The same for a prompt: pages of zeros, of V scales far apart and of none, lost pages, one
+    heavy token before a light tail."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(11)
+    t, table, n = tables(torch, rng, 2, 12)
+    cache = make(torch, n, 1, D)
+    for j, f in enumerate((1.0, 30.0, 1e-3, 0.0, 1.0, 1e-25, 3.0, 1.0)):
+        cache.v_scale[int(t[0, j])] *= f
+    cache.k_scale[int(t[0, 2])] = 0.0
+    cache.k_codes[int(t[1, 1])] = 0
+    t[1, 3] = -1
+    table[1, 3] = -1
+    q = torch.randn(2, 70, 3, D).to(getattr(torch, dtype)).cuda()
+    check_attend(torch, cache, q, table, t, [700, 333], scale=scale, mass=True)
+    cache.k_codes.zero_()
+    cache.k_codes[int(t[0, 0]), 0, 5, :] = 100
+    cache.k_scale.fill_(0.01)
+    q.fill_(0.25)
+    check_attend(torch, cache, q, table, t, [700, 70], scale=scale * 8)
+
+
+def test_attend_long_prompt_split():
+    torch = torch_cuda()
+    rng = np.random.default_rng(12)
+    t, table, n = tables(torch, rng, 1, 60)
+    cache = make(torch, n, 1, 64)
+    q = torch.randn(1, 100, 1, 64).half().cuda()
+    check_attend(torch, cache, q, table, t, [3800], mass=True)
+
+
 def test_attend_long_and_split():
     """Long enough for many splits; lengths far below the bound, so that splits stay empty."""
     torch = torch_cuda()

@@ -228,6 +228,7 @@ struct KvAttn {
   KvRows q, out;
   int32_t max_len, nq, group, n_picks;
   float scale, decay;
+  bool wide_q, wide_out;        // rows on 16-byte boundaries
 };
 
 struct KvAttnPlan {

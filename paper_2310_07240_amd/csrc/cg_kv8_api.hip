@@ -37,6 +37,10 @@ KvRows rows(const cg_kv8_rows& r) {
   return KvRows{r.data, r.seq_stride, r.token_stride, r.head_stride};
 }
 
+bool wide(const cg_kv8_rows& r) {
+  return aligned(r.data, 16) && ((r.seq_stride | r.token_stride | r.head_stride) & 7) == 0;
+}
+
 bool bad_dtype(int32_t d) { return d != CG_KV8_F16 && d != CG_KV8_BF16; }
 
 // What attend and select share: shapes, queries and lengths.
@@ -54,6 +58,7 @@ int check_queries(const cg_kv8_attn* a, const KvPool& pool, const KvSeqs& S, KvA
   out->lengths = a->lengths;
   out->q_lens = a->q_lens;
   out->q = rows(a->q);
+  out->wide_q = wide(a->q);
   out->max_len = a->max_len;
   out->nq = a->n_q;
   out->group = a->n_q_heads / pool.H;
@@ -74,6 +79,7 @@ int check_attend(const cg_kv8_cache* c, const cg_kv8_seqs* s, const cg_kv8_attn*
     return CG_ERR_ARG;
   if ((a->mass_in && !a->mass_out) || (a->mass_out && a->picks)) return CG_ERR_ARG;
   A->out = rows(a->out);
+  A->wide_out = wide(a->out);
   A->lse = a->lse;
   A->picks = a->picks;
   A->mass_in = a->mass_in;

@@ -29,6 +29,15 @@ __device__ __forceinline__ float quad_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
+// Eight row elements; `wide`: rows lie on 16-byte boundaries.
+__device__ __forceinline__ uint4v load8(const uint16_t* p, bool wide) {
+  if (wide) return *reinterpret_cast<const uint4v*>(p);
+  uint16_t u[8];
+#pragma unroll
+  for (int c = 0; c < 8; ++c) u[c] = p[c];
+  return *reinterpret_cast<uint4v*>(u);
+}
+
 // One 16-row tile's queries as B operands, and what a row needs of them.
 template <int D>
 struct QTile {
@@ -83,11 +92,9 @@ __device__ __forceinline__ void load_q(const KvAttn& A, const RowsOf& R, int h, 
                         (int64_t)i * A.q.tok + (int64_t)head * A.q.head;
   uint16_t u[D / 32][8];
 #pragma unroll
-  for (int s = 0; s < D / 32; ++s) {
-    const int d = (s >> 1) * 64 + g * 16 + (s & 1) * 8;
-#pragma unroll
-    for (int c = 0; c < 8; ++c) u[s][c] = live ? src[d + c] : 0;
-  }
+  for (int s = 0; s < D / 32; ++s)
+    *reinterpret_cast<uint4v*>(u[s]) =
+        live ? load8(src + (s >> 1) * 64 + g * 16 + (s & 1) * 8, A.wide_q) : uint4v{0, 0, 0, 0};
   int e = 0;
   if (BF16) {
     uint32_t top = 0;
@@ -436,8 +443,8 @@ __device__ __forceinline__ float load_row32(const KvAttn& A, const uint16_t* src
   uint16_t u[D / 16][8];
 #pragma unroll
   for (int s = 0; s < D / 16; ++s)
-#pragma unroll
-    for (int c = 0; c < 8; ++c) u[s][c] = live ? src[16 * s + 8 * half + c] : 0;
+    *reinterpret_cast<uint4v*>(u[s]) =
+        live ? load8(src + 16 * s + 8 * half, A.wide_q) : uint4v{0, 0, 0, 0};
   int e = 0;
   const uint16_t flip = A.scale < 0.0f ? 0x8000u : 0;
   if (BF16) {
@@ -504,15 +511,15 @@ __device__ __forceinline__ void page_widen(const PageRegs<D>& r, PromptLds<D>& L
   }
 }
 
-// Workgroup = (sequence, KV head, tile of 128 NB rows, split of the pages).
+// Workgroup = (sequence, KV head, tile of 128 NB rows, split of the pages). `it0`: where this
+// launch starts (see in_launches).
 template <int D, bool BF16, int NB>
 __global__ __launch_bounds__(256, 1) void prompt_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles,
-                                                        int splits, int64_t items, float* part,
+                                                        int splits, int64_t it0, float* part,
                                                         float* lse) {
   __shared__ PromptLds<D> L;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 31, half = lane >> 5;
-  const int64_t it = blockIdx.x;
-  if (it >= items) return;
+  const int64_t it = it0 + blockIdx.x;
   const int h = (int)(it % pool.H);
   int64_t r = it / pool.H;
   const int split = (int)(r % splits);
@@ -715,7 +722,211 @@ __global__ __launch_bounds__(256, 1) void prompt_kernel(KvPool pool, KvSeqs S, K
   }
 }
 
+// ---- weights of many rows -------------------------------------------------------------------
+// The same sum as mass_kernel where there are many rows: a wave keeps one page's K as operands in
+// registers and adds up its 64 tokens' weights row tile by row tile; the queries come through LDS,
+// shared by the PW pages of the workgroup. The eight waves are PW pages x 8 / PW shares of the row
+// tiles (every 8 / PW-th), whose sums meet in LDS at the end in a fixed order.
+template <int D, int RG>
+struct MassLds {
+  _Float16 q[2][RG * 32][D + 8];
+  float unit[2][RG * 32], z[2][RG * 32];       // factor of S, log2 of the row's sum
+  int visible[2][RG * 32];                     // 0: no such row, or an empty one
+  float sum[8][kPage];
+};
+
+template <int D, bool BF16, int PW>
+__global__ __launch_bounds__(512, 1) void mass_rows_kernel(KvPool pool, KvSeqs S, KvAttn A, int np,
+                                                           int64_t it0, const float* lse) {
+  constexpr int RG = 8 / PW, LR = D / 8;       // lanes that load one row
+  constexpr int CH = RG * 32 * LR / 512;       // 16-byte pieces a thread loads a step
+  __shared__ MassLds<D, RG> L;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 31, half = lane >> 5;
+  const int share = wave / PW;
+  const int64_t it = it0 + blockIdx.x;
+  const int h = (int)(it % pool.H);
+  const int64_t r0 = it / pool.H;
+  const int groups = (np + PW - 1) / PW;
+  const int j0 = (int)(r0 % groups) * PW, seq = (int)(r0 / groups);
+  const int j = j0 + wave % PW, pos0 = j * kPage;
+  const RowsOf R = rows_of(S, A, seq);
+  if (j0 * (int64_t)kPage >= R.len) return;
+  const int page = j < np && pos0 < R.len ? kv_page(S, pool.P, seq, j) : -1;
+  const int64_t at = (int64_t)page * pool.H + h;
+  half8 k[2][D / 16];
+  float ks = 0.0f;
+  if (page >= 0) {
+    ks = pool.ks[at];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int8_t* row = pool.k + at * (kPage * D) + (32 * u + m) * D + 16 * half;
+#pragma unroll
+      for (int s = 0; s < D / 32; ++s) {
+        const uint4v c = *reinterpret_cast<const uint4v*>(row + 32 * s);
+        k[u][2 * s] = kv_widen8(c[0], c[1]);
+        k[u][2 * s + 1] = kv_widen8(c[2], c[3]);
+      }
+    }
+  }
+  float sum[2][16];
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sum[u][e] = 0.0f;
+
+  // the first row that sees the workgroup's first page
+  const int rows = (R.q_len > 0 ? R.q_len : 0) * A.group;
+  const int64_t first = (int64_t)j0 * kPage - R.len + R.q_len;   // first query token that does
+  const int step = RG * 32;
+  int base = first > 0 ? (int)(first * A.group) / step * step : 0;
+
+  uint4v u[CH];
+  float z_n = 0.0f;
+  const auto fetch = [&](int b0) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int row = b0 + (c * 512 + tid) / LR, d = tid % LR * 8;
+      u[c] = uint4v{0, 0, 0, 0};
+      if (row < rows) {
+        const uint16_t* src = static_cast<const uint16_t*>(A.q.p) + R.seq * A.q.seq +
+                              (int64_t)(row / A.group) * A.q.tok +
+                              (int64_t)(h * A.group + row % A.group) * A.q.head + d;
+        u[c] = load8(src, A.wide_q);
+      }
+    }
+    if (tid < step) {
+      const int row = b0 + tid;
+      z_n = row < rows ? lse[lse_at(A, R, pool.H, h, row)] * kLog2e : 0.0f;
+    }
+  };
+  const auto put = [&](int b0, int buf) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int slot = (c * 512 + tid) / LR, d = tid % LR * 8;
+      half8 q;
+      int e = 0;
+      if (BF16) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint32_t w = (u[c][i >> 1] >> (16 * (i & 1))) & 0x7fffu;
+          top = w > top && w < 0x7f80u ? w : top;
+        }
+#pragma unroll
+        for (int o = 1; o < LR; o <<= 1) {
+          const uint32_t v = __shfl_xor(top, o);
+          top = v > top ? v : top;
+        }
+        e = (int)(top >> 7) - 127;
+        if (e < -126) e = -126;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          q[i] = (_Float16)__builtin_ldexpf(
+              kv_widen<true>((uint16_t)(u[c][i >> 1] >> (16 * (i & 1)))), -e);
+      } else {
+        q = __builtin_bit_cast(half8, u[c]);
+      }
+      *reinterpret_cast<half8*>(&L.q[buf][slot][d]) = q;
+      if (tid % LR == 0) L.unit[buf][slot] = __builtin_ldexpf(A.scale * kLog2e, e);
+    }
+    if (tid < step) {
+      const int row = b0 + tid;
+      L.visible[buf][tid] = row < rows ? visible_of(R, row / A.group) : 0;
+      L.z[buf][tid] = z_n;
+    }
+  };
+  if (base < rows) {
+    fetch(base);
+    put(base, 0);
+  }
+  for (int buf = 0; base < rows; base += step, buf ^= 1) {
+    const bool more = base + step < rows;
+    if (more) fetch(base + step);
+    __syncthreads();
+    const int slot = share * 32 + m;
+    const int see = L.visible[buf][slot];
+    if (page >= 0 && __any(see > pos0)) {
+      const float f = L.unit[buf][slot] * ks;
+      // an empty row has weight 0 everywhere
+      const float z = see > 0 ? -L.z[buf][slot] : kNegInf;
+      float16v x[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[t][e] = 0.0f;
+      }
+#pragma unroll
+      for (int s = 0; s < D / 16; ++s) {
+        const half8 q = *reinterpret_cast<const half8*>(
+            &L.q[buf][slot][32 * (s >> 1) + 16 * half + 8 * (s & 1)]);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          x[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[t][s], q, x[t], 0, 0, 0);
+      }
+      if (__any(see > 0 && see < pos0 + kPage)) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (pos0 + 32 * t + 8 * (e >> 2) + 4 * half + (e & 3) < see)
+              sum[t][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][e], f, z));
+      } else {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            sum[t][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][e], f, z));
+      }
+    }
+    if (more) put(base + step, buf ^ 1);
+  }
+  // over the 32 rows of a tile, then over the shares
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      float s = sum[t][e];
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) s += __shfl_xor(s, o);
+      if (m == 0) L.sum[wave][32 * t + 8 * (e >> 2) + 4 * half + (e & 3)] = s;
+    }
+  __syncthreads();
+  if (share == 0 && page >= 0 && pos0 + lane < R.len) {
+    float s = 0.0f;
+#pragma unroll
+    for (int w = 0; w < RG; ++w) s += L.sum[w * PW + wave][lane];
+    const int64_t to = at * kPage + lane;
+    A.mass_out[to] = A.mass_in ? __builtin_fmaf(A.decay, A.mass_in[to], s) : s;
+  }
+}
+
 unsigned grid_of(int64_t items) { return (unsigned)(items < (1 << 22) ? items : (1 << 22)); }
+
+// Kernels of one workgroup per item: as many launches as keep each below 2^32 threads.
+template <class Launch>
+void in_launches(int64_t items, Launch launch) {
+  constexpr int64_t kMost = 1 << 22;
+  for (int64_t it0 = 0; it0 < items; it0 += kMost)
+    launch(it0, (unsigned)(items - it0 < kMost ? items - it0 : kMost));
+}
+
+template <int D, bool BF16, int NB>
+void prompt_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, const KvAttnPlan& P,
+              float* part, float* lse, hipStream_t st) {
+  in_launches((int64_t)S.n * pool.H * P.big * P.splits, [&](int64_t it0, unsigned n) {
+    hipLaunchKernelGGL((prompt_kernel<D, BF16, NB>), dim3(n), dim3(256), 0, st, pool, S, A, P.big,
+                       P.splits, it0, part, lse);
+  });
+}
+
+template <int D, bool BF16, int PW>
+void mass_rows_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, int np, const float* lse,
+                 hipStream_t st) {
+  in_launches((int64_t)S.n * pool.H * ((np + PW - 1) / PW), [&](int64_t it0, unsigned n) {
+    hipLaunchKernelGGL((mass_rows_kernel<D, BF16, PW>), dim3(n), dim3(512), 0, st, pool, S, A, np,
+                       it0, lse);
+  });
+}
 
 template <int D, bool BF16>
 hipError_t attend_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, void* ws,
@@ -726,27 +937,27 @@ hipError_t attend_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, void* 
   float* lse = A.lse ? A.lse : A.mass_out ? reinterpret_cast<float*>(base + P.lse_off) : nullptr;
   const int vseqs = A.picks ? S.n * A.nq : S.n;
   const int64_t units = (int64_t)vseqs * pool.H * P.tiles;
-  if (P.big) {
-    const int64_t items = (int64_t)vseqs * pool.H * P.big * P.splits;
-    constexpr int NB = D == 256 ? 1 : 2;
-    if (P.blocks == NB)
-      hipLaunchKernelGGL((prompt_kernel<D, BF16, NB>), dim3((unsigned)items), dim3(256), 0, st,
-                         pool, S, A, P.big, P.splits, items, part, lse);
-    else
-      hipLaunchKernelGGL((prompt_kernel<D, BF16, 1>), dim3((unsigned)items), dim3(256), 0, st,
-                         pool, S, A, P.big, P.splits, items, part, lse);
-  } else {
+  if (P.blocks == 1)
+    prompt_d<D, BF16, 1>(pool, S, A, P, part, lse, st);
+  else if (P.blocks == 2)
+    prompt_d<D, BF16, D == 256 ? 1 : 2>(pool, S, A, P, part, lse, st);
+  else
     hipLaunchKernelGGL((attend_kernel<D, BF16>), dim3(grid_of(units * P.splits)), dim3(256), 0,
                        st, pool, S, A, P.tiles, P.splits, units * P.splits, part, lse);
-  }
   if (P.splits > 1)
     hipLaunchKernelGGL((join_kernel<D, BF16>), dim3(grid_of(units)), dim3(256), 0, st, pool, S, A,
                        P.tiles, P.splits, units, part, lse);
-  if (A.mass_out) {
-    const int np = (int)(((int64_t)A.max_len + kPage - 1) / kPage);
+  const int np = (int)(((int64_t)A.max_len + kPage - 1) / kPage);
+  if (A.mass_out && np) {
     const int64_t items = (int64_t)S.n * pool.H * np;
-    hipLaunchKernelGGL((mass_kernel<D, BF16>), dim3(grid_of((items + 3) / 4)), dim3(256), 0, st,
-                       pool, S, A, P.tiles, np, items, lse);
+    // four pages a workgroup share each query tile; two where that gives too few workgroups
+    if (P.big && items >= 2048)
+      mass_rows_d<D, BF16, 4>(pool, S, A, np, lse, st);
+    else if (P.big)
+      mass_rows_d<D, BF16, 2>(pool, S, A, np, lse, st);
+    else
+      hipLaunchKernelGGL((mass_kernel<D, BF16>), dim3(grid_of((items + 3) / 4)), dim3(256), 0, st,
+                         pool, S, A, P.tiles, np, items, lse);
   }
   return hipGetLastError();
 }

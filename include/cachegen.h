@@ -402,6 +402,11 @@ int cg_decode_tokens(const cg_params* p, const uint32_t* words, const uint64_t* 
  * 16-byte aligned rows are read and written 16 bytes at a time. */
 #define CG_KV8_PAGE 64
 
+/* The workspaces of cg_kv8_attend and cg_kv8_select start with this many bytes of counters, which
+ * the caller clears once, before a workspace's first use; every call leaves them zero. The rest of
+ * a workspace may hold anything. Calls that may overlap need workspaces of their own. */
+#define CG_KV8_WORKSPACE_ZEROED 4096
+
 enum { CG_KV8_F16 = 0, CG_KV8_BF16 = 1 };
 
 typedef struct cg_kv8_cache {
@@ -492,7 +497,8 @@ uint64_t cg_kv8_attend_workspace_bytes(const cg_kv8_cache* c, const cg_kv8_seqs*
  * maxima, sums, lse and mass are 32-bit. Results do not depend on the order in which parts of the
  * work end.
  *   workspace   device scratch of workspace_bytes >= cg_kv8_attend_workspace_bytes, 256-byte
- *               aligned (may be NULL where that is 0); its contents on entry do not matter.
+ *               aligned (may be NULL where that is 0), its first CG_KV8_WORKSPACE_ZEROED bytes
+ *               zero.
  * Asynchronous. */
 int cg_kv8_attend(const cg_kv8_cache* c, const cg_kv8_seqs* s, const cg_kv8_attn* a,
                   void* workspace, uint64_t workspace_bytes, hipStream_t stream);
@@ -508,7 +514,7 @@ uint64_t cg_kv8_select_workspace_bytes(const cg_kv8_cache* c, const cg_kv8_seqs*
  * with q8 = rint(clamp(q * 2^(6 - e), +-127)), 2^e the power of two at or below the largest |q| of
  * the group, and lo, hi the page's bounds: an upper bound of the page's summed q . k, in whole
  * numbers. Equal scores go to the lower column. Uses q, lengths, max_len, q_lens, n_picks and
- * dtype of `a`. Asynchronous. */
+ * dtype of `a`; the workspace as for cg_kv8_attend. Asynchronous. */
 int cg_kv8_select(const cg_kv8_cache* c, const cg_kv8_seqs* s, const cg_kv8_attn* a,
                   int32_t recent, int32_t* picks_out, void* workspace, uint64_t workspace_bytes,
                   hipStream_t stream);

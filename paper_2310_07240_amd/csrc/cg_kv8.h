@@ -231,10 +231,17 @@ struct KvAttn {
   bool wide_q, wide_out;        // rows on 16-byte boundaries
 };
 
+// The workspaces' first bytes: a counter for each tile whose pages are split, zero between calls
+// (a tile is split only where there are fewer than kKv8Counters of them).
+constexpr int kKv8Counters = 1024;
+constexpr uint64_t kKv8Front = CG_KV8_WORKSPACE_ZEROED;
+static_assert(kKv8Front == kKv8Counters * 4, "one 32-bit counter a tile");
+
 struct KvAttnPlan {
   int32_t tiles, splits;        // 16-row tiles and splits of the pages for each (sequence, KV head)
   int32_t big, blocks;          // prompt_kernel: tiles of 128 blocks rows; big = 0: attend_kernel
-  uint64_t part_off, lse_off, total;   // workspace, in bytes
+  bool keep_scores;             // for the weights (see cg_kv8_plan)
+  uint64_t part_off, lse_off, score_off, total;   // workspace, in bytes
 };
 
 KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& seqs, const KvAttn& a, int D);

@@ -125,17 +125,44 @@ __device__ __forceinline__ void load_q(const KvAttn& A, const RowsOf& R, int h, 
   Q.unit = __builtin_ldexpf(A.scale * kLog2e, e);
 }
 
-// S^T of one page: x[4 t + i] is token 16 g + 4 t + i against the lane's row, unscaled.
+// The page's K codes as the lane's operands: piece s of row 16 (m >> 2) + 4 t + (m & 3).
 template <int D>
-__device__ __forceinline__ void page_scores(const int8_t* k, const QTile<D>& Q, float x[16]) {
+struct KRegs {
+  uint4v c[4][D / 64];
+};
+template <int D>
+struct VRegs {
+  uint4v c[D / 16];
+};
+
+template <int D>
+__device__ __forceinline__ void load_k(const int8_t* k, KRegs<D>& K) {
+  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+  const int8_t* row = k + (16 * (m >> 2) + (m & 3)) * D + 16 * g;
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int s = 0; s < D / 64; ++s)
+      K.c[t][s] = *reinterpret_cast<const uint4v*>(row + 4 * t * D + 64 * s);
+}
+
+template <int D>
+__device__ __forceinline__ void load_v(const int8_t* v, VRegs<D>& V) {
   const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
 #pragma unroll
+  for (int dt = 0; dt < D / 16; ++dt)
+    V.c[dt] = *reinterpret_cast<const uint4v*>(v + (16 * dt + m) * kPage + 16 * g);
+}
+
+// S^T of one page: x[4 t + i] is token 16 g + 4 t + i against the lane's row, unscaled.
+template <int D>
+__device__ __forceinline__ void page_scores(const KRegs<D>& K, const QTile<D>& Q, float x[16]) {
+#pragma unroll
   for (int t = 0; t < 4; ++t) {
-    const int8_t* row = k + (16 * (m >> 2) + 4 * t + (m & 3)) * D + 16 * g;
     float4v acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int s = 0; s < D / 64; ++s) {
-      const uint4v c = *reinterpret_cast<const uint4v*>(row + 64 * s);
+      const uint4v c = K.c[t][s];
       acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv_widen8(c[0], c[1]), Q.q[2 * s], acc, 0, 0, 0);
       acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv_widen8(c[2], c[3]), Q.q[2 * s + 1], acc, 0, 0,
                                                    0);
@@ -152,13 +179,13 @@ struct Acc {
   float m, l;
 };
 
-// One page into the state.
+// The softmax of one page's scores (left at `kept`, if given, as the lane's row has them): P as
+// operands in p, m and l moved on; `keep` brings O to the
+// new reference, the return value (times the V scale) the page's share.
 template <int D>
-__device__ __forceinline__ void page_step(const int8_t* k, const int8_t* v, float ks, float vs,
-                                          int pos0, const QTile<D>& Q, Acc<D>& S) {
-  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
-  float x[16];
-  page_scores<D>(k, Q, x);
+__device__ __forceinline__ float page_softmax(float x[16], float ks, int pos0, const QTile<D>& Q,
+                                              Acc<D>& S, half8 p[2], float& keep, float* kept) {
+  const int g = (threadIdx.x & 63) >> 4;
   const float f = Q.unit * ks;
   float top = kNegInf;
 #pragma unroll
@@ -166,28 +193,37 @@ __device__ __forceinline__ void page_step(const int8_t* k, const int8_t* v, floa
     x[j] = pos0 + 16 * g + j < Q.visible ? x[j] * f : kNegInf;
     top = fmaxf(top, x[j]);
   }
+  if (kept) {
+#pragma unroll
+    for (int j = 0; j < 16; j += 4)
+      *reinterpret_cast<float4v*>(kept + 16 * g + j) = float4v{x[j], x[j + 1], x[j + 2], x[j + 3]};
+  }
   // P is taken relative to the page's own maximum, so that fp16 loses no light page beside a heavy
   // one; w brings the page to the running reference.
   top = quad_max(top);
   const float mine = top == kNegInf ? 0.0f : top;      // nothing of the page is visible
   const float both = fmaxf(S.m, top);
   const float ref = both == kNegInf ? 0.0f : both;
-  const float keep = __builtin_amdgcn_exp2f(S.m - ref), w = __builtin_amdgcn_exp2f(top - ref);
+  keep = __builtin_amdgcn_exp2f(S.m - ref);
+  const float w = __builtin_amdgcn_exp2f(top - ref);
   float sum = 0.0f;
 #pragma unroll
   for (int j = 0; j < 16; ++j) {
     x[j] = __builtin_amdgcn_exp2f(x[j] - mine);
     sum += x[j];
+    p[j >> 3][j & 7] = (_Float16)x[j];
   }
   S.l = __builtin_fmaf(S.l, keep, sum * w);
   S.m = both;
-  const float vw = vs * w;
-  half8 p[2];
-#pragma unroll
-  for (int j = 0; j < 16; ++j) p[j >> 3][j & 7] = (_Float16)x[j];
+  return w;
+}
+
+template <int D>
+__device__ __forceinline__ void page_values(const VRegs<D>& V, const half8 p[2], float keep,
+                                            float vw, Acc<D>& S) {
 #pragma unroll
   for (int dt = 0; dt < D / 16; ++dt) {
-    const uint4v c = *reinterpret_cast<const uint4v*>(v + (16 * dt + m) * kPage + 16 * g);
+    const uint4v c = V.c[dt];
     float4v acc = {0.0f, 0.0f, 0.0f, 0.0f};
     acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv_widen8(c[0], c[1]), p[0], acc, 0, 0, 0);
     acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv_widen8(c[2], c[3]), p[1], acc, 0, 0, 0);
@@ -212,128 +248,257 @@ __device__ __forceinline__ int64_t lse_at(const KvAttn& A, const RowsOf& R, int 
   return ((int64_t)R.seq * A.nq + i) * ((int64_t)H * A.group) + head;
 }
 
+// Partial states of one 16-row tile in 32 bits: O [16][D], then (m, l) [16].
+template <int D>
+constexpr int kPart = 16 * (D + 2);
+constexpr int kMostSplits = 128;
+
+// Pairs of floats past this XCD's caches.
+__device__ __forceinline__ void put_pair(float* p, float a, float b) {
+  const uint64_t w = (uint64_t)__builtin_bit_cast(uint32_t, b) << 32 |
+                     __builtin_bit_cast(uint32_t, a);
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), w, __ATOMIC_RELAXED,
+                     __HIP_MEMORY_SCOPE_AGENT);
+}
+template <bool FAR>
+__device__ __forceinline__ void get_pair(const float* p, float& a, float& b) {
+  const uint64_t* q = reinterpret_cast<const uint64_t*>(p);
+  const uint64_t w = FAR ? __hip_atomic_load(const_cast<uint64_t*>(q), __ATOMIC_RELAXED,
+                                             __HIP_MEMORY_SCOPE_AGENT)
+                         : *q;
+  a = __builtin_bit_cast(float, (uint32_t)w);
+  b = __builtin_bit_cast(float, (uint32_t)(w >> 32));
+}
+
+// The rows of one 16-row tile from n partial states kPart apart, in the order of the states, and
+// out: the 256 threads first fetch every state's (m, l) at once, then each takes pairs of channels
+// through all states. FAR: written by other workgroups of this launch. w [n][16]: LDS. rows0: rows
+// of the tile that exist.
+template <int D, bool BF16, bool FAR>
+__device__ __forceinline__ void join_tile(const KvAttn& A, const RowsOf& R, int H, int h, int tile,
+                                          int rows0, const float* p, int n, float* w, float* lse) {
+  const int tid = threadIdx.x;
+  const int row = tid >> 4, sub = tid & 15;            // 16 threads a row
+  // the first states' channels are on their way while the factors are found
+  constexpr int kAhead = 8;
+  float2 ahead[kAhead];
+  const int e0 = tid < rows0 * (D / 2) ? tid : 0;
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i)
+    get_pair<FAR>(p + (i < n ? i : 0) * kPart<D> + e0 / (D / 2) * D + e0 % (D / 2) * 2, ahead[i].x,
+                  ahead[i].y);
+  float top = kNegInf, l = 0.0f;
+  if (row < rows0) {
+    for (int i = sub; i < n; i += 16) {
+      float m, x;
+      get_pair<FAR>(p + i * kPart<D> + 16 * D + 2 * row, m, x);
+      w[i * 16 + row] = m;
+      const float both = fmaxf(top, m), ref = both == kNegInf ? 0.0f : both;
+      l = l * __builtin_amdgcn_exp2f(top - ref) + x * __builtin_amdgcn_exp2f(m - ref);
+      top = both;
+    }
+  }
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) {
+    const float m = __shfl_xor(top, o), x = __shfl_xor(l, o);
+    const float both = fmaxf(top, m), ref = both == kNegInf ? 0.0f : both;
+    l = l * __builtin_amdgcn_exp2f(top - ref) + x * __builtin_amdgcn_exp2f(m - ref);
+    top = both;
+  }
+  const float ref = top == kNegInf ? 0.0f : top;
+  if (row < rows0) {
+    const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+    for (int i = sub; i < n; i += 16)
+      w[i * 16 + row] = __builtin_amdgcn_exp2f(w[i * 16 + row] - ref) * inv;
+    if (lse && sub == 0)
+      lse[lse_at(A, R, H, h, tile * 16 + row)] = (top + __builtin_amdgcn_logf(l)) * kLn2;
+  }
+  __syncthreads();
+  for (int e = tid; e < rows0 * (D / 2); e += 256) {
+    const int r = e / (D / 2), d = e % (D / 2) * 2;
+    float o[2] = {0.0f, 0.0f};
+    const float* q = p + r * D + d;
+    int i = 0;
+    if (e == tid) {
+#pragma unroll
+      for (; i < kAhead; ++i) {
+        const float f = i < n ? w[i * 16 + r] : 0.0f;
+        o[0] = i < n ? __builtin_fmaf(ahead[i].x, f, o[0]) : o[0];
+        o[1] = i < n ? __builtin_fmaf(ahead[i].y, f, o[1]) : o[1];
+      }
+    }
+#pragma unroll 8
+    for (; i < n; ++i) {
+      float a, b;
+      get_pair<FAR>(q + i * kPart<D>, a, b);
+      const float f = w[i * 16 + r];
+      o[0] = __builtin_fmaf(a, f, o[0]);
+      o[1] = __builtin_fmaf(b, f, o[1]);
+    }
+    put_out<D, BF16>(A, R, h, tile * 16 + r, d, o, 2);
+  }
+}
+
+// One joined row's channels to `out`, and its log-sum-exp.
+template <int D, bool BF16, int N>
+__device__ __forceinline__ void finish_row(const KvAttn& A, const RowsOf& R, int H, int h, int row,
+                                           int d0, float* o, float top, float l, float* lse) {
+  const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+#pragma unroll
+  for (int c = 0; c < N; ++c) o[c] *= inv;
+  put_out<D, BF16>(A, R, h, row, d0, o, N);
+  if (lse && d0 == 0)
+    lse[lse_at(A, R, H, h, row)] = (top + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
 // Workgroup = (virtual sequence, KV head, 16-row tile, split of the pages); its four waves take
-// the split's pages in turn and meet in LDS. splits == 1 writes the result, else a partial state:
-// O [16][D], m [16], l [16] in 32 bits.
+// the split's pages in turn and meet in LDS. A page's K is requested as soon as the scores have
+// used the last one's, its V as soon as the second product has: each wave has a page in flight all
+// the time, which is what carries the memory's rate at 8 waves a CU. With splits, the workgroup
+// leaves its partial state in memory and counts itself in; the last of a tile joins them all, in
+// the order of the splits, and clears the counter for the next call. The states are written and
+// read past the XCDs' own caches (agent scope), and counted when they have arrived: a release
+// fence instead writes back the whole L2 for every workgroup (25 -> 197 us for 32 sequences of 2K).
 template <int D, bool BF16>
-__global__ __launch_bounds__(256) void attend_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles,
-                                                     int splits, int64_t items, float* part,
-                                                     float* lse) {
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles,
+                                                        int splits, int64_t items, float* part,
+                                                        uint32_t* arrived, float* lse,
+                                                        float* scores, int np) {
   __shared__ float os[4][16][D + 4];
-  __shared__ float ms[4][16], ls[4][16];
+  __shared__ float ml[4][32];
+  __shared__ uint32_t others;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const int split = (int)(it % splits);
-    int64_t r = it / splits;
-    const int tile = (int)(r % tiles);
-    r /= tiles;
-    const int h = (int)(r % pool.H);
-    const int vseq = (int)(r / pool.H);
+    const int64_t unit = it / splits;
+    const int tile = (int)(unit % tiles);
+    const int h = (int)(unit / tiles % pool.H);
+    const int vseq = (int)(unit / tiles / pool.H);
     const RowsOf R = rows_of(S, A, vseq);
-    QTile<D> Q;
-    load_q<D, BF16>(A, R, h, tile, Q);
     // the pages that any row of the tile sees
-    int most = Q.visible;
-    for (int o = 1; o < 16; o <<= 1) {
-      const int v = __shfl_xor(most, o);
-      most = v > most ? v : most;
-    }
-    most = __builtin_amdgcn_readfirstlane(most);
+    const int rows = R.nq * A.group;
+    int last = tile * 16 + 15 < rows ? tile * 16 + 15 : rows - 1;
+    last = R.i0 + last / A.group;
+    const int most = R.q_len > 0 ? visible_of(R, last < R.q_len ? last : R.q_len - 1) : 0;
     const int n = A.picks ? A.n_picks : (most + kPage - 1) / kPage;
     const int per = (n + splits - 1) / splits;
     const int j0 = split * per, j1 = j0 + per < n ? j0 + per : n;
     const int32_t* picks = A.picks ? A.picks + ((int64_t)vseq * pool.H + h) * A.n_picks : nullptr;
+    // the next page of this wave from column j on, or -1; j moves behind it
+    int at = 0;
+    const auto next_page = [&](int& j) -> int64_t {
+      while (j < j1) {
+        at = picks ? picks[j] : j;
+        j += 4;
+        if (at < 0 || (int64_t)at * kPage >= most) continue;
+        const int page = kv_page(S, pool.P, R.seq, at);
+        if (page >= 0) return (int64_t)page * pool.H + h;
+      }
+      return -1;
+    };
+    int j = j0 + __builtin_amdgcn_readfirstlane(wave);
+    int64_t b = next_page(j);
+    KRegs<D> K;
+    VRegs<D> V;
+    if (b >= 0) {
+      load_k<D>(pool.k + b * (kPage * D), K);
+      load_v<D>(pool.v + b * (kPage * D), V);
+    }
+    QTile<D> Q;
+    load_q<D, BF16>(A, R, h, tile, Q);
     Acc<D> acc;
 #pragma unroll
     for (int dt = 0; dt < D / 16; ++dt) acc.o[dt] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
     acc.m = kNegInf;
     acc.l = 0.0f;
-    for (int j = j0 + wave; j < j1; j += 4) {
-      const int at = picks ? picks[j] : j;
-      if (at < 0 || (int64_t)at * kPage >= most) continue;
-      const int page = kv_page(S, pool.P, R.seq, at);
-      if (page < 0) continue;
-      const int64_t b = (int64_t)page * pool.H + h;
-      page_step<D>(pool.k + b * (kPage * D), pool.v + b * (kPage * D), pool.ks[b], pool.vs[b],
-                   at * kPage, Q, acc);
+    float* const kept = scores && tile * 16 + m < rows
+        ? scores + (((int64_t)R.seq * pool.H + h) * rows + tile * 16 + m) * np * kPage : nullptr;
+    while (b >= 0) {
+      const float ks = pool.ks[b], vs = pool.vs[b];
+      const int pos0 = at * kPage;
+      float x[16], keep;
+      half8 p[2];
+      const int64_t bn = next_page(j);
+      page_scores<D>(K, Q, x);
+      if (bn >= 0) load_k<D>(pool.k + bn * (kPage * D), K);
+      const float w = page_softmax<D>(x, ks, pos0, Q, acc, p, keep, kept ? kept + pos0 : nullptr);
+      page_values<D>(V, p, keep, w * vs, acc);
+      if (bn >= 0) load_v<D>(pool.v + bn * (kPage * D), V);
+      b = bn;
     }
     acc.l = quad_sum(acc.l);
 #pragma unroll
     for (int dt = 0; dt < D / 16; ++dt)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) os[wave][m][16 * dt + 4 * g + i] = acc.o[dt][i];
+      *reinterpret_cast<float4v*>(&os[wave][m][16 * dt + 4 * g]) = acc.o[dt];
     if (g == 0) {
-      ms[wave][m] = acc.m;
-      ls[wave][m] = acc.l;
+      ml[wave][m] = acc.m;
+      ml[wave][16 + m] = acc.l;
     }
     __syncthreads();
     // 16 threads a row, D / 16 channels each
-    const int row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * (D / 16);
-    float top = kNegInf;
-    for (int w = 0; w < 4; ++w) top = fmaxf(top, ms[w][row]);
-    const float ref = top == kNegInf ? 0.0f : top;
-    float l = 0.0f, o[D / 16];
+    constexpr int N = D / 16;
+    const int row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * N;
+    const bool live = tile * 16 + row < rows;
+    float o[N], top, l;
+    if (live) {
+      // the waves' states are 16 (D + 4) apart in os and 32 in ml: joined in wave order
+      top = kNegInf;
 #pragma unroll
-    for (int c = 0; c < D / 16; ++c) o[c] = 0.0f;
-    for (int w = 0; w < 4; ++w) {
-      const float f = __builtin_amdgcn_exp2f(ms[w][row] - ref);
-      l = __builtin_fmaf(ls[w][row], f, l);
+      for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w][row]);
+      const float ref = top == kNegInf ? 0.0f : top;
+      l = 0.0f;
 #pragma unroll
-      for (int c = 0; c < D / 16; ++c) o[c] = __builtin_fmaf(os[w][row][d0 + c], f, o[c]);
-    }
-    if (splits > 1) {
-      float* p = part + it * (16 * (D + 2));
+      for (int c = 0; c < N; ++c) o[c] = 0.0f;
 #pragma unroll
-      for (int c = 0; c < D / 16; ++c) p[row * D + d0 + c] = o[c];
-      if (d0 == 0) {
-        p[16 * D + row] = top;
-        p[16 * D + 16 + row] = l;
+      for (int w = 0; w < 4; ++w) {
+        const float f = __builtin_amdgcn_exp2f(ml[w][row] - ref);
+        l = __builtin_fmaf(ml[w][16 + row], f, l);
+#pragma unroll
+        for (int c = 0; c < N; ++c) o[c] = __builtin_fmaf(os[w][row][d0 + c], f, o[c]);
       }
-    } else if (tile * 16 + row < R.nq * A.group) {
-      const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+    }
+    if (splits == 1) {
+      if (live) finish_row<D, BF16, N>(A, R, pool.H, h, tile * 16 + row, d0, o, top, l, lse);
+    } else {
+      float* mine = part + it * kPart<D>;
+      if (live) {
 #pragma unroll
-      for (int c = 0; c < D / 16; ++c) o[c] *= inv;
-      put_out<D, BF16>(A, R, h, tile * 16 + row, d0, o, D / 16);
-      if (lse && d0 == 0)
-        lse[lse_at(A, R, pool.H, h, tile * 16 + row)] =
-            (top + __builtin_amdgcn_logf(l)) * kLn2;
+        for (int c = 0; c < N; c += 2) put_pair(mine + row * D + d0 + c, o[c], o[c + 1]);
+        if (d0 == 0) put_pair(mine + 16 * D + 2 * row, top, l);
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's part has arrived
+      __syncthreads();
+      if (threadIdx.x == 0)
+        others = __hip_atomic_fetch_add(&arrived[unit], 1u, __ATOMIC_RELAXED,
+                                        __HIP_MEMORY_SCOPE_AGENT);
+      __syncthreads();
+      if (others == (uint32_t)splits - 1) {
+        if (threadIdx.x == 0)
+          __hip_atomic_store(&arrived[unit], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        // (os has room for the factors of 128 states; its readers have passed two barriers)
+        join_tile<D, BF16, true>(A, R, pool.H, h, tile, rows - tile * 16 < 16 ? rows - tile * 16 : 16,
+                                 part + unit * splits * kPart<D>, splits, &os[0][0][0], lse);
+      }
     }
     __syncthreads();
   }
 }
 
-// The splits of one 16-row tile joined: 16 threads a row.
+// The splits of prompt_kernel joined: a workgroup a 16-row tile.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void join_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles,
                                                    int splits, int64_t items, const float* part,
                                                    float* lse) {
+  __shared__ float w[kMostSplits * 16];
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const int tile = (int)(it % tiles);
     const int64_t r = it / tiles;
     const int h = (int)(r % pool.H);
     const RowsOf R = rows_of(S, A, (int)(r / pool.H));
-    const int row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * (D / 16);
-    if (tile * 16 + row >= R.nq * A.group) continue;
-    const float* p = part + it * splits * (16 * (D + 2));
-    float top = kNegInf;
-    for (int s = 0; s < splits; ++s) top = fmaxf(top, p[s * (16 * (D + 2)) + 16 * D + row]);
-    const float ref = top == kNegInf ? 0.0f : top;
-    float l = 0.0f, o[D / 16];
-#pragma unroll
-    for (int c = 0; c < D / 16; ++c) o[c] = 0.0f;
-    for (int s = 0; s < splits; ++s) {
-      const float* q = p + s * (16 * (D + 2));
-      const float f = __builtin_amdgcn_exp2f(q[16 * D + row] - ref);
-      l = __builtin_fmaf(q[16 * D + 16 + row], f, l);
-#pragma unroll
-      for (int c = 0; c < D / 16; ++c) o[c] = __builtin_fmaf(q[row * D + d0 + c], f, o[c]);
-    }
-    const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-#pragma unroll
-    for (int c = 0; c < D / 16; ++c) o[c] *= inv;
-    put_out<D, BF16>(A, R, h, tile * 16 + row, d0, o, D / 16);
-    if (lse && d0 == 0)
-      lse[lse_at(A, R, pool.H, h, tile * 16 + row)] = (top + __builtin_amdgcn_logf(l)) * kLn2;
+    const int rows = R.nq * A.group - tile * 16;
+    join_tile<D, BF16, false>(A, R, pool.H, h, tile, rows < 16 ? rows : 16,
+                              part + it * splits * kPart<D>, splits, w, lse);
+    __syncthreads();
   }
 }
 
@@ -354,6 +519,8 @@ __global__ __launch_bounds__(256) void mass_kernel(KvPool pool, KvSeqs S, KvAttn
     if (page < 0) continue;
     const int64_t b = (int64_t)page * pool.H + h;
     const float ks = pool.ks[b];
+    KRegs<D> K;
+    load_k<D>(pool.k + b * (kPage * D), K);
     float sum[16];
 #pragma unroll
     for (int e = 0; e < 16; ++e) sum[e] = 0.0f;
@@ -364,7 +531,7 @@ __global__ __launch_bounds__(256) void mass_kernel(KvPool pool, KvSeqs S, KvAttn
       const int row = tile * 16 + m;
       const float z = row < R.nq * A.group ? lse[lse_at(A, R, pool.H, h, row)] * kLog2e : 0.0f;
       float x[16];
-      page_scores<D>(pool.k + b * (kPage * D), Q, x);
+      page_scores<D>(K, Q, x);
       const float f = Q.unit * ks;
 #pragma unroll
       for (int e = 0; e < 16; ++e)
@@ -383,6 +550,37 @@ __global__ __launch_bounds__(256) void mass_kernel(KvPool pool, KvSeqs S, KvAttn
     if (j * kPage + t < R.len) {
       const int64_t at = b * kPage + t;
       A.mass_out[at] = A.mass_in ? __builtin_fmaf(A.decay, A.mass_in[at], mine) : mine;
+    }
+  }
+}
+
+// The same from scores that attend_kernel has kept: a lane a token, one wave a page. Bound by the
+// scores' bytes.
+__global__ __launch_bounds__(256) void mass_scores_kernel(KvPool pool, KvSeqs S, KvAttn A, int np,
+                                                          int64_t items, const float* scores,
+                                                          const float* lse) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int64_t it = (int64_t)blockIdx.x * 4 + wave; it < items; it += (int64_t)gridDim.x * 4) {
+    const int j = (int)(it % np);
+    const int64_t r = it / np;
+    const int h = (int)(r % pool.H), seq = (int)(r / pool.H);
+    const RowsOf R = rows_of(S, A, seq);
+    const int t = j * kPage + lane;
+    if (t - lane >= R.len) continue;
+    const int page = kv_page(S, pool.P, seq, j);
+    if (page < 0) continue;
+    const int rows = R.nq * A.group;
+    const float* x = scores + r * rows * np * kPage + t;
+    float sum = 0.0f;
+#pragma unroll 4
+    for (int row = 0; row < rows; ++row) {
+      const int see = visible_of(R, row / A.group);
+      const float z = lse[lse_at(A, R, pool.H, h, row)] * kLog2e;
+      if (t < see) sum += __builtin_amdgcn_exp2f(x[(int64_t)row * np * kPage] - z);
+    }
+    if (t < R.len) {
+      const int64_t at = ((int64_t)page * pool.H + h) * kPage + lane;
+      A.mass_out[at] = A.mass_in ? __builtin_fmaf(A.decay, A.mass_in[at], sum) : sum;
     }
   }
 }
@@ -690,7 +888,7 @@ __global__ __launch_bounds__(256, 1) void prompt_kernel(KvPool pool, KvSeqs S, K
     const float unit_o = __builtin_amdgcn_exp2f(ref[b] - (float)kLift - ref_l[b]);
     if (splits > 1) {
       const int64_t u16 = ((int64_t)seq * pool.H + h) * ((rows + 15) / 16) + row / 16;
-      float* dst = part + (u16 * splits + split) * (16 * (D + 2));
+      float* dst = part + (u16 * splits + split) * kPart<D>;
 #pragma unroll
       for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -701,8 +899,8 @@ __global__ __launch_bounds__(256, 1) void prompt_kernel(KvPool pool, KvSeqs S, K
           *reinterpret_cast<float4v*>(dst + (row & 15) * D + 32 * dt + 8 * a + 4 * half) = w;
         }
       if (half == 0) {
-        dst[16 * D + (row & 15)] = empty ? kNegInf : ref_l[b];
-        dst[16 * D + 16 + (row & 15)] = empty ? 0.0f : sum;
+        dst[16 * D + 2 * (row & 15)] = empty ? kNegInf : ref_l[b];
+        dst[16 * D + 2 * (row & 15) + 1] = empty ? 0.0f : sum;
       }
     } else {
       const float f = empty ? 0.0f : unit_o / sum;
@@ -935,6 +1133,8 @@ hipError_t attend_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, void* 
   char* base = static_cast<char*>(ws);
   float* part = reinterpret_cast<float*>(base + P.part_off);
   float* lse = A.lse ? A.lse : A.mass_out ? reinterpret_cast<float*>(base + P.lse_off) : nullptr;
+  float* scores = P.keep_scores ? reinterpret_cast<float*>(base + P.score_off) : nullptr;
+  const int np = (int)(((int64_t)A.max_len + kPage - 1) / kPage);
   const int vseqs = A.picks ? S.n * A.nq : S.n;
   const int64_t units = (int64_t)vseqs * pool.H * P.tiles;
   if (P.blocks == 1)
@@ -943,11 +1143,11 @@ hipError_t attend_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, void* 
     prompt_d<D, BF16, D == 256 ? 1 : 2>(pool, S, A, P, part, lse, st);
   else
     hipLaunchKernelGGL((attend_kernel<D, BF16>), dim3(grid_of(units * P.splits)), dim3(256), 0,
-                       st, pool, S, A, P.tiles, P.splits, units * P.splits, part, lse);
-  if (P.splits > 1)
+                       st, pool, S, A, P.tiles, P.splits, units * P.splits, part,
+                       reinterpret_cast<uint32_t*>(base), lse, scores, np);
+  if (P.splits > 1 && P.big)
     hipLaunchKernelGGL((join_kernel<D, BF16>), dim3(grid_of(units)), dim3(256), 0, st, pool, S, A,
                        P.tiles, P.splits, units, part, lse);
-  const int np = (int)(((int64_t)A.max_len + kPage - 1) / kPage);
   if (A.mass_out && np) {
     const int64_t items = (int64_t)S.n * pool.H * np;
     // four pages a workgroup share each query tile; two where that gives too few workgroups
@@ -955,6 +1155,9 @@ hipError_t attend_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, void* 
       mass_rows_d<D, BF16, 4>(pool, S, A, np, lse, st);
     else if (P.big)
       mass_rows_d<D, BF16, 2>(pool, S, A, np, lse, st);
+    else if (P.keep_scores)
+      hipLaunchKernelGGL(mass_scores_kernel, dim3(grid_of((items + 3) / 4)), dim3(256), 0, st, pool,
+                         S, A, np, items, scores, lse);
     else
       hipLaunchKernelGGL((mass_kernel<D, BF16>), dim3(grid_of((items + 3) / 4)), dim3(256), 0, st,
                          pool, S, A, P.tiles, np, items, lse);
@@ -971,29 +1174,41 @@ KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& S, const KvAttn& A, int
   const int64_t vseqs = A.picks ? (int64_t)S.n * A.nq : S.n;
   const int64_t units = vseqs * pool.H * P.tiles;
   const int64_t pages = A.picks ? A.n_picks : ((int64_t)A.max_len + kPage - 1) / kPage;
-  // From three 16-row tiles on, the rows share the pages through LDS (prompt_kernel).
+  // From three 16-row tiles on, the rows share the pages through LDS (prompt_kernel); every query
+  // token with pages of its own is a tile or more to itself.
   P.big = P.blocks = 0;
   int64_t s, most;
-  if (P.tiles > 2) {
+  if (P.tiles > 2 && !A.picks) {
     P.blocks = D == 256 || rows <= 128 ? 1 : 2;
     P.big = (int)((rows + 128 * P.blocks - 1) / (128 * P.blocks));
     const int64_t groups = vseqs * pool.H * P.big;
     s = (256 + groups - 1) / groups;
     most = pages / 4;
   } else {
-    // enough workgroups to fill the card, each wave with a page of its own at least
-    s = (1024 + units - 1) / units;
+    // As many workgroups as the registers let the card hold at once (3, 2 or 1 a CU), each wave
+    // with a page of its own at least: a second round of half-filled CUs costs more than longer
+    // splits do (4 sequences of 8K, 32 heads: 50 us with 512 workgroups, 64 with 768, 58 with
+    // 1024; 32 of 2K, 8 heads: 26, 34 and 33). No more splits than one workgroup joins quickly.
+    s = (D == 64 ? 768 : D == 128 ? 512 : 256) / units;
     most = (pages + 3) / 4;
   }
+  if (most > kMostSplits) most = kMostSplits;
   if (s > most) s = most;
   if (s < 1) s = 1;
   P.splits = (int)s;
-  uint64_t at = 0;
+  // Weights of few rows: their scores are kept for the second launch (8 bytes a row and token to
+  // write and read again) where that is at most half of reading K again (D bytes a token).
+  P.keep_scores = A.mass_out && !P.big && rows * 16 <= D;
+  const bool parts = s > 1, weights = A.mass_out && !A.lse;
+  uint64_t at = parts || weights || P.keep_scores ? kKv8Front : 0;
   P.part_off = at;
-  if (s > 1) at += (uint64_t)units * (uint64_t)s * (16ull * (D + 2)) * 4ull;
+  if (parts) at += (uint64_t)units * (uint64_t)s * (16ull * (D + 2)) * 4ull;
   at = (at + 255) & ~255ull;
   P.lse_off = at;
-  if (A.mass_out && !A.lse) at += (uint64_t)S.n * A.nq * pool.H * A.group * 4ull;
+  if (weights) at += (uint64_t)S.n * A.nq * pool.H * A.group * 4ull;
+  at = (at + 255) & ~255ull;
+  P.score_off = at;
+  if (P.keep_scores) at += (uint64_t)S.n * pool.H * rows * pages * kPage * 4ull;
   P.total = (at + 255) & ~255ull;
   return P;
 }

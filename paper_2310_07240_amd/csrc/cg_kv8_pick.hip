@@ -13,83 +13,112 @@ __device__ __forceinline__ uint32_t order_key(float f) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+constexpr int kBins = 2048;          // of a pass: 11 bits of the keys
+constexpr int kHeld = 64;            // keys a lane keeps in registers
+
 template <int NT>
 struct PickLds {
-  uint32_t hist[256];
+  uint32_t hist[kBins];
   uint32_t above[NT / 64], equal[NT / 64];
   uint32_t digit, rest;
 };
 
 // The best `need` (1 <= need < n) of key(0 .. n - 1): emit(position, index) for each, positions
-// ascending with the index. Four passes over the keys' bytes, highest first, narrow them to the
-// smallest key that is taken and the number of its equals that are; a fifth pass emits. Counts are
-// whole numbers, so no order of the LDS additions changes anything.
-template <int NT, class Key, class Emit>
-__device__ __forceinline__ void pick_best(int n, int need, PickLds<NT>& L, Key key, Emit emit) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+// ascending with the index. Every wave has a run of whole 64-key blocks (key_block(j, lane): key
+// of index 64 j + lane), the first kHeld of them in registers, so the keys are read once. Three
+// passes over the keys' bits, highest first, narrow them to the smallest key that is taken and the
+// number of its equals that are; then each wave counts and emits its run by ballots. Counts are
+// whole numbers, so no order of the LDS additions changes anything. Bound by the first pass's LDS
+// additions (weights crowd into a few octaves, so lanes meet on a bin: hence 11 bits and not 8).
+template <int NT, class KeyBlock, class Emit>
+__device__ __forceinline__ void pick_best(int n, int need, PickLds<NT>& L, KeyBlock key_block,
+                                          Emit emit) {
+  constexpr int NW = NT / 64;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int blocks = (n + 63) / 64, per = (blocks + NW - 1) / NW;
+  const int first = wave * per;
+  const int mine = first + per < blocks ? per : blocks > first ? blocks - first : 0;
+  uint32_t held[kHeld];
+#pragma unroll
+  for (int r = 0; r < kHeld; ++r)
+    if (r < mine) held[r] = key_block(first + r, lane);
+  // f(round, key) for the lane's keys; indices from n on are nobody's
+  const auto each = [&](auto f) {
+#pragma unroll
+    for (int r = 0; r < kHeld; ++r)
+      if (r < mine) f(r, held[r]);
+    for (int r = kHeld; r < mine; ++r) f(r, key_block(first + r, lane));
+  };
+  const auto live = [&](int r) { return (first + r) * 64 + lane < n; };
+
   uint32_t prefix = 0, mask = 0;
   uint32_t rest = (uint32_t)need;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = tid; i < 256; i += NT) L.hist[i] = 0;
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+    const uint32_t width = pass == 2 ? 1023u : 2047u;
+    for (int i = tid; i < kBins; i += NT) L.hist[i] = 0;
     __syncthreads();
-    for (int i = tid; i < n; i += NT) {
-      const uint32_t k = key(i);
-      if ((k & mask) == prefix) atomicAdd(&L.hist[(k >> shift) & 255u], 1u);
+    each([&](int r, uint32_t k) {
+      if (live(r) && (k & mask) == prefix) atomicAdd(&L.hist[(k >> shift) & width], 1u);
+    });
+    __syncthreads();
+    // the bins from the highest down, kBins / NT a thread
+    constexpr int BT = kBins / NT;
+    uint32_t c[BT], s = 0;
+#pragma unroll
+    for (int i = 0; i < BT; ++i) {
+      c[i] = L.hist[kBins - 1 - (tid * BT + i)];
+      s += c[i];
     }
+    uint32_t before = s;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t v = __shfl_up(before, o);
+      if (lane >= o) before += v;
+    }
+    if (lane == 63) L.above[wave] = before;
     __syncthreads();
-    if (wave == 0) {
-      // lane l holds bins 255 - 4 l .. 252 - 4 l, the highest first
-      uint32_t c[4], s = 0;
+    before -= s;
+    for (int w = 0; w < wave; ++w) before += L.above[w];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        c[i] = L.hist[255 - 4 * lane - i];
-        s += c[i];
+    for (int i = 0; i < BT; ++i) {
+      if (before < rest && rest <= before + c[i]) {     // true in one thread, for one bin
+        L.digit = (uint32_t)(kBins - 1 - (tid * BT + i));
+        L.rest = rest - before;
       }
-      uint32_t before = s;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t v = __shfl_up(before, o);
-        if (lane >= o) before += v;
-      }
-      before -= s;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (before < rest && rest <= before + c[i]) {   // true in one lane, for one bin
-          L.digit = (uint32_t)(255 - 4 * lane - i);
-          L.rest = rest - before;
-        }
-        before += c[i];
-      }
+      before += c[i];
     }
     __syncthreads();
     prefix |= L.digit << shift;
-    mask |= 255u << shift;
+    mask |= width << shift;
     rest = L.rest;
   }
-  uint32_t above = 0, equal = 0;     // taken or equal before this round
-  for (int i0 = 0; i0 < n; i0 += NT) {
-    const int i = i0 + tid;
-    const uint32_t k = i < n ? key(i) : 0u;
-    const bool a = i < n && k > prefix, e = i < n && k == prefix;
-    const uint64_t ba = __ballot(a), be = __ballot(e);
-    if (lane == 0) {
-      L.above[wave] = (uint32_t)__popcll(ba);
-      L.equal[wave] = (uint32_t)__popcll(be);
-    }
-    __syncthreads();
-    const uint64_t below = ((uint64_t)1 << lane) - 1;
-    uint32_t na = above + (uint32_t)__popcll(ba & below), ne = equal + (uint32_t)__popcll(be & below);
-    for (int w = 0; w < NT / 64; ++w) {
-      if (w < wave) {
-        na += L.above[w];
-        ne += L.equal[w];
-      }
-      above += L.above[w];
-      equal += L.equal[w];
-    }
-    if (a || (e && ne < rest)) emit((int)(na + (ne < rest ? ne : rest)), i);
-    __syncthreads();
+  uint32_t na = 0, ne = 0;           // of the wave's run: taken for sure, and equal to the last
+  each([&](int r, uint32_t k) {
+    na += (uint32_t)__popcll(__ballot(live(r) && k > prefix));
+    ne += (uint32_t)__popcll(__ballot(live(r) && k == prefix));
+  });
+  __syncthreads();
+  if (lane == 0) {
+    L.above[wave] = na;
+    L.equal[wave] = ne;
   }
+  __syncthreads();
+  na = ne = 0;
+  for (int w = 0; w < wave; ++w) {
+    na += L.above[w];
+    ne += L.equal[w];
+  }
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
+  each([&](int r, uint32_t k) {
+    const bool a = live(r) && k > prefix, e = live(r) && k == prefix;
+    const uint64_t ba = __ballot(a), be = __ballot(e);
+    const uint32_t ra = na + (uint32_t)__popcll(ba & below), re = ne + (uint32_t)__popcll(be & below);
+    if (a || (e && re < rest)) emit((int)(ra + (re < rest ? re : rest)), (first + r) * 64 + lane);
+    na += (uint32_t)__popcll(ba);
+    ne += (uint32_t)__popcll(be);
+  });
 }
 
 __device__ __forceinline__ int held_tokens(const KvSeqs& S, const int32_t* lengths, int max_len,
@@ -125,10 +154,10 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(KvPool pool, KvSeqs 
   if (need == 0) return;
   pick_best<kKeepThreads>(
       old, need, L,
-      [&](int i) {
-        const int page = kv_page(S, pool.P, seq, i / kPage);
+      [&](int j, int lane) {
+        const int page = kv_page(S, pool.P, seq, j);
         if (page < 0) return 0u;
-        return order_key(mass[((int64_t)page * pool.H + h) * kPage + i % kPage]);
+        return order_key(mass[((int64_t)page * pool.H + h) * kPage + lane]);
       },
       [&](int at, int i) { out[at] = i; });
 }
@@ -207,33 +236,46 @@ __global__ __launch_bounds__(2 * D) void move_kernel(KvPool pool, KvSeqs S, KvSe
 }
 
 constexpr int kSelectThreads = 256;
+constexpr int kScoreRounds = 4;      // pages a lane group scores at once
 
-// One workgroup per (sequence, query token, KV head): scores of the pages, then the best ones.
-// The group's queries are taken at 8 bits under one power of two, so a score is a whole number
-// times the page's K scale, and the same on any machine.
+// One workgroup per (sequence, query token, KV head) and split of its pages: scores of the pages,
+// then the best ones. The group's queries are taken at 8 bits under one power of two, so a score is
+// a whole number times the page's K scale, and the same on any machine. max(q8 lo, q8 hi) is q8 hi
+// where q8 > 0 and q8 lo where it is not, so the sum over the group's heads goes into the weights
+// first: one weight per channel and bound, at most 127 group in size, taken as 128 w1 + w0 for the
+// 8-bit dot products. Bound by the bounds' bytes for long sequences and by latency for short ones.
+// With splits, the last workgroup of a row to leave its keys picks (as attend_kernel joins).
 template <int D, bool BF16>
 __global__ __launch_bounds__(kSelectThreads) void select_kernel(KvPool pool, KvSeqs S, KvAttn A,
-                                                                int recent, int32_t* out,
-                                                                uint32_t* keys, int np) {
+                                                                int recent, int splits,
+                                                                int32_t* out, uint32_t* keys,
+                                                                int np, uint32_t* arrived,
+                                                                int64_t row0) {
   __shared__ PickLds<kSelectThreads> L;
   __shared__ float red[kSelectThreads / 64];
-  __shared__ int up[D], down[D];
+  __shared__ uint32_t w0[2 * D / 4], w1[2 * D / 4];    // of the lowest codes, then the highest
+  __shared__ uint32_t others;
   const int tid = threadIdx.x;
-  const int h = blockIdx.x % pool.H, vseq = blockIdx.x / pool.H;
+  const int split = blockIdx.x % splits;
+  const int64_t row = row0 + blockIdx.x / splits;
+  const int h = (int)(row % pool.H), vseq = (int)(row / pool.H);
   const int seq = vseq / A.nq, i = vseq % A.nq;
-  int32_t* picks = out + (int64_t)blockIdx.x * A.n_picks;
+  int32_t* picks = out + row * A.n_picks;
   const int len = held_tokens(S, A.lengths, A.max_len, seq);
   int ql = A.q_lens ? A.q_lens[seq] : A.nq;
   if (ql > A.nq) ql = A.nq;
-  const int seen = i < ql && len - ql + i + 1 > 0 ? len - ql + i + 1 : 0;
+  const int64_t sees = i < ql ? (int64_t)len - ql + i + 1 : 0;
+  const int seen = sees > 0 ? (int)sees : 0;
   const int pages = (seen + kPage - 1) / kPage;
-  if (pages <= A.n_picks) {
-    for (int e = tid; e < A.n_picks; e += kSelectThreads) picks[e] = e < pages ? e : -1;
-    return;
-  }
   const int last = recent < A.n_picks ? recent : A.n_picks;
   const int need = A.n_picks - last, old = pages - last;
-  for (int e = tid; e < last; e += kSelectThreads) picks[need + e] = old + e;
+  if (pages <= A.n_picks) {
+    if (split == 0)
+      for (int e = tid; e < A.n_picks; e += kSelectThreads) picks[e] = e < pages ? e : -1;
+    return;
+  }
+  if (split == 0)
+    for (int e = tid; e < last; e += kSelectThreads) picks[need + e] = old + e;
   if (need == 0) return;
 
   const uint16_t* q = static_cast<const uint16_t*>(A.q.p) + seq * A.q.seq +
@@ -245,41 +287,95 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(KvPool pool, KvS
   }
   top = wg_max<kSelectThreads>(top, red);
   const int shift = 6 - (top > 0.0f ? __builtin_amdgcn_frexp_expf(top) - 1 : 0);
-  for (int d = tid; d < D; d += kSelectThreads) {
-    int u = 0, w = 0;
-    for (int g = 0; g < A.group; ++g) {
-      const float f = __builtin_ldexpf(kv_widen<BF16>(q[(int64_t)g * A.q.head + d]), shift);
-      const int c = f != f ? 0
-                           : (int)__builtin_rintf(fminf(fmaxf(f, -127.0f), 127.0f));
-      u += c > 0 ? c : 0;
-      w += c < 0 ? c : 0;
-    }
-    up[d] = u;
-    down[d] = w;
-  }
-  __syncthreads();
-  // D / 8 lanes a page, 16 bytes of its bounds each: the lowest codes, then the highest
-  constexpr int LP = D / 8;
-  uint32_t* mine = keys + (int64_t)blockIdx.x * np;
+  // D / 8 lanes a page, 16 bytes of its bounds each: the lowest codes, then the highest. Groups
+  // past 128 heads are taken 128 heads at a time, whose weights fit two 8-bit digits.
+  constexpr int LP = D / 8, PG = kSelectThreads / LP;
+  const int per = (old + splits - 1) / splits;
+  const int a0 = split * per, a1 = a0 + per < old ? a0 + per : old;
+  uint32_t* mine = keys + row * np;
   const int sub = tid % LP;
-  for (int j = tid / LP; j < old; j += kSelectThreads / LP) {
-    const int page = kv_page(S, pool.P, seq, j);
-    int sum = 0;
-    if (page >= 0) {
-      const uint4v c = *reinterpret_cast<const uint4v*>(
-          pool.bounds + ((int64_t)page * pool.H + h) * (2 * D) + 16 * sub);
-      const int* w = sub < LP / 2 ? down + 16 * sub : up + 16 * sub - D;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) sum += w[e] * (int)(int8_t)(c[e >> 2] >> (8 * (e & 3)));
+  for (int g0 = 0; g0 < A.group; g0 += 128) {
+    const int g1 = g0 + 128 < A.group ? g0 + 128 : A.group;
+    __syncthreads();
+    for (int d = tid; d < D; d += kSelectThreads) {
+      int up = 0, down = 0;
+      for (int g = g0; g < g1; ++g) {
+        const float f = __builtin_ldexpf(kv_widen<BF16>(q[(int64_t)g * A.q.head + d]), shift);
+        const int c = f != f ? 0 : (int)__builtin_rintf(fminf(fmaxf(f, -127.0f), 127.0f));
+        up += c > 0 ? c : 0;
+        down -= c < 0 ? c : 0;
+      }
+      reinterpret_cast<uint8_t*>(w0)[d] = (uint8_t)(down & 127);
+      reinterpret_cast<uint8_t*>(w1)[d] = (uint8_t)(down >> 7);
+      reinterpret_cast<uint8_t*>(w0)[D + d] = (uint8_t)(up & 127);
+      reinterpret_cast<uint8_t*>(w1)[D + d] = (uint8_t)(up >> 7);
     }
+    __syncthreads();
+    int v0[4], v1[4];
 #pragma unroll
-    for (int o = 1; o < LP; o <<= 1) sum += __shfl_xor(sum, o);
-    if (sub == 0)
-      mine[j] = page < 0 ? 0u : order_key((float)sum * pool.ks[(int64_t)page * pool.H + h]);
+    for (int e = 0; e < 4; ++e) {
+      v0[e] = (int)w0[4 * sub + e];
+      v1[e] = (int)w1[4 * sub + e];
+    }
+    for (int j0 = a0 + tid / LP; j0 < a1; j0 += kScoreRounds * PG) {
+      uint4v c[kScoreRounds];
+      int page[kScoreRounds];
+      float ks[kScoreRounds];
+#pragma unroll
+      for (int r = 0; r < kScoreRounds; ++r) {
+        const int j = j0 + r * PG;
+        page[r] = j < a1 ? kv_page(S, pool.P, seq, j) : -1;
+      }
+#pragma unroll
+      for (int r = 0; r < kScoreRounds; ++r) {
+        const int64_t at = (int64_t)(page[r] < 0 ? 0 : page[r]) * pool.H + h;
+        c[r] = *reinterpret_cast<const uint4v*>(pool.bounds + at * (2 * D) + 16 * sub);
+        ks[r] = pool.ks[at];
+      }
+#pragma unroll
+      for (int r = 0; r < kScoreRounds; ++r) {
+        int lo = 0, hi = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          lo = __builtin_amdgcn_sdot4((int)c[r][e], v0[e], lo, false);
+          hi = __builtin_amdgcn_sdot4((int)c[r][e], v1[e], hi, false);
+        }
+        int sum = hi * 128 + lo;
+        sum = sub < LP / 2 ? -sum : sum;               // the lowest codes' weights are negative
+#pragma unroll
+        for (int o = 1; o < LP; o <<= 1) sum += __shfl_xor(sum, o);
+        const int j = j0 + r * PG;
+        if (sub == 0 && j < a1) {
+          // whole numbers until the last head is in
+          if (g0 > 0)
+            sum += (int)__hip_atomic_load(&mine[j], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          const uint32_t k = g1 < A.group ? (uint32_t)sum
+                             : page[r] < 0 ? 0u : order_key((float)sum * ks[r]);
+          __hip_atomic_store(&mine[j], k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+      }
+    }
   }
+  if (splits > 1) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // this wave's keys have arrived
+    __syncthreads();
+    if (tid == 0)
+      others = __hip_atomic_fetch_add(&arrived[row], 1u, __ATOMIC_RELAXED,
+                                      __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (others != (uint32_t)splits - 1) return;
+    if (tid == 0)
+      __hip_atomic_store(&arrived[row], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   pick_best<kSelectThreads>(
-      old, need, L, [&](int j) { return mine[j]; }, [&](int at, int j) { picks[at] = j; });
+      old, need, L,
+      [&](int j, int lane) {
+        const int e = j * 64 + lane < old ? j * 64 + lane : 0;
+        return __hip_atomic_load(&mine[e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      },
+      [&](int at, int j) { picks[at] = j; });
 }
 
 unsigned grid_of(int64_t items) { return (unsigned)(items < (1 << 22) ? items : (1 << 22)); }
@@ -294,22 +390,36 @@ void move_d(const KvPool& pool, const KvSeqs& S, const KvSeqs& to, const int32_t
 
 template <int D, bool BF16>
 void select_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, int recent, int32_t* picks,
-              uint32_t* keys, hipStream_t st) {
+              char* ws, hipStream_t st) {
   const int np = (int)(((int64_t)A.max_len + kPage - 1) / kPage);
-  hipLaunchKernelGGL((select_kernel<D, BF16>), dim3((unsigned)(S.n * A.nq * pool.H)),
-                     dim3(kSelectThreads), 0, st, pool, S, A, recent, picks, keys, np);
+  const int64_t rows = (int64_t)S.n * A.nq * pool.H;
+  // a page needs D / 8 lanes: kScoreRounds rounds of the workgroup's lanes a split, and no more
+  // splits than fill the card
+  const int round = kScoreRounds * kSelectThreads / (D / 8);
+  int64_t splits = rows < kKv8Counters ? (1024 + rows - 1) / rows : 1;
+  if (splits > (np + round - 1) / round) splits = (np + round - 1) / round;
+  if (splits < 1) splits = 1;
+  uint32_t* keys = reinterpret_cast<uint32_t*>(ws + kKv8Front);
+  constexpr int64_t kMost = 1 << 23;                   // workgroups a launch, below 2^32 threads
+  for (int64_t row0 = 0; row0 < rows; row0 += kMost) {
+    const int64_t n = rows - row0 < kMost ? rows - row0 : kMost;
+    hipLaunchKernelGGL((select_kernel<D, BF16>), dim3((unsigned)(n * splits)),
+                       dim3(kSelectThreads), 0, st, pool, S, A, recent, (int)splits, picks, keys,
+                       np, reinterpret_cast<uint32_t*>(ws), row0);
+  }
 }
 
 }  // namespace
 
 uint64_t cg_kv8_select_ws(const KvSeqs& S, int H, int nq, int max_len) {
-  return ((uint64_t)S.n * nq * H * (((uint64_t)max_len + kPage - 1) / kPage) * 4ull + 255) & ~255ull;
+  return ((uint64_t)S.n * nq * H * (((uint64_t)max_len + kPage - 1) / kPage) * 4ull + kKv8Front + 255) &
+         ~255ull;
 }
 
 hipError_t cg_launch_kv8_select(const KvPool& pool, const KvSeqs& S, int D, bool bf16,
                                 const KvAttn& A, int recent, int32_t* picks, void* ws,
                                 hipStream_t st) {
-  uint32_t* keys = static_cast<uint32_t*>(ws);
+  char* keys = static_cast<char*>(ws);
   switch (D) {
     case 64: (bf16 ? select_d<64, true> : select_d<64, false>)(pool, S, A, recent, picks, keys, st); break;
     case 128: (bf16 ? select_d<128, true> : select_d<128, false>)(pool, S, A, recent, picks, keys, st); break;

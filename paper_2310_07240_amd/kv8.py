@@ -86,6 +86,7 @@ class Kv8Cache:
     def __init__(self, n_pages, n_heads, head_dim, device="cuda", buffers=None):
         import torch
         self.torch = torch
+        self._i32, self._f32 = torch.int32, torch.float32
         P, H, D = int(n_pages), int(n_heads), int(head_dim)
         self.n_pages, self.n_heads, self.head_dim = P, H, D
         if P <= 0 or H <= 0 or D not in (64, 128, 256):
@@ -96,6 +97,7 @@ class Kv8Cache:
         if buffers is None:
             buffers = {n: torch.zeros(s, dtype=t, device=device) for n, (s, t) in want.items()}
         self.device = buffers["k_codes"].device
+        self._index = self.device.index or 0
         for n, (s, t) in want.items():
             b = buffers.get(n)
             _need(b is not None or n == "k_bounds", f"{n} is missing")
@@ -105,44 +107,74 @@ class Kv8Cache:
         self._c = _Cache(P, H, D, *(None if (b := getattr(self, n)) is None else b.data_ptr()
                                     for n in want))
         self._cp = ctypes.byref(self._c)
-        self._ws = {}
+        self._ws, self._captured = {}, []
         self._types = {torch.float16: 0, torch.bfloat16: 1}
 
     # ---- marshalling ---------------------------------------------------------------------
+    # (a call of one token takes a few microseconds on the GPU: no message is put together and no
+    # stream object made unless it is needed)
     def _tensor(self, t, name, dtype, shape=None):
-        _need(t.dtype == dtype and t.device == self.device and t.is_contiguous()
-              and (shape is None or t.shape == shape),
-              f"{name}: a contiguous {dtype} tensor{'' if shape is None else ' of ' + str(tuple(shape))}"
-              f" on {self.device} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
-        return t.data_ptr()
+        if (t.dtype is dtype and t.device == self.device and t.is_contiguous()
+                and (shape is None or t.shape == shape)):
+            return t.data_ptr()
+        raise ValueError(f"{name}: a contiguous {dtype} tensor"
+                         f"{'' if shape is None else ' of ' + str(tuple(shape))} on {self.device} "
+                         f"is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
 
     def _seqs(self, table):
-        p = self._tensor(table, "table", self.torch.int32)
-        _need(table.dim() == 2, "table: [n_seq, columns] is wanted")
-        return _Seqs(table.shape[0], table.shape[1], p)
+        p = self._tensor(table, "table", self._i32)
+        if table.dim() != 2:
+            raise ValueError("table: [n_seq, columns] is wanted")
+        n, width = table.shape
+        return _Seqs(n, width, p)
 
     def _per_seq(self, t, name, n):
-        return None if t is None else self._tensor(t, name, self.torch.int32, (n,))
+        return None if t is None else self._tensor(t, name, self._i32, (n,))
 
     def _rows(self, t, name, shape, dtype):
-        _need(t.dtype == dtype and t.shape == shape and t.device == self.device
-              and t.stride(3) == 1,
-              f"{name}: {dtype} rows {tuple(shape)} with a contiguous last dimension on "
-              f"{self.device} are wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
-        s = t.stride()
-        return _Rows(t.data_ptr(), s[0], s[1], s[2])
+        if t.dtype is dtype and t.shape == shape and t.device == self.device:
+            a, b, c, d = t.stride()
+            if d == 1:
+                return _Rows(t.data_ptr(), a, b, c)
+        raise ValueError(f"{name}: {dtype} rows {tuple(shape)} with a contiguous last dimension "
+                         f"on {self.device} are wanted, got {t.dtype} {tuple(t.shape)} on "
+                         f"{t.device}")
 
-    def _scratch(self, stream, need):
-        """The stream's scratch, allocated on that stream so that its reuse is ordered there."""
-        ws = self._ws.get(stream.cuda_stream)
-        if ws is None or ws.numel() < need:
-            with self.torch.cuda.stream(stream):
-                ws = self.torch.empty((need,), dtype=self.torch.uint8, device=self.device)
-            self._ws[stream.cuda_stream] = ws
-        return ws.data_ptr(), ws.numel()
+    def _handle(self, stream):
+        """The HIP stream's handle: the caller's, or torch's current one."""
+        if stream is not None:
+            return stream.cuda_stream
+        return self.torch._C._cuda_getCurrentRawStream(self._index)
 
-    def _stream(self, stream):
-        return self.torch.cuda.current_stream(self.device) if stream is None else stream
+    def _new(self, make, shape, dtype, stream):
+        """A tensor whose memory's reuse is ordered on the stream."""
+        if stream is None:
+            return make(shape, dtype=dtype, device=self.device)
+        with self.torch.cuda.stream(stream):
+            return make(shape, dtype=dtype, device=self.device)
+
+    def _empty(self, shape, dtype, stream):
+        return self._new(self.torch.empty, shape, dtype, stream)
+
+    def _scratch(self, stream, handle, need):
+        """The stream's own scratch (address, bytes), cleared once. Scratch made while the stream
+        is being captured is cleared by the graph alone, so only that call has it; it is kept for
+        the graph's sake."""
+        ws = self._ws.get(handle)
+        if ws is None or ws[1] < need:
+            t = self._new(self.torch.zeros, (need,), self.torch.uint8, stream)
+            ws = (t.data_ptr(), need, t)
+            if self._capturing(stream):
+                self._captured.append(t)
+            else:
+                self._ws[handle] = ws
+        return ws
+
+    def _capturing(self, stream):
+        if stream is None:
+            return self.torch.cuda.is_current_stream_capturing()
+        with self.torch.cuda.stream(stream):
+            return self.torch.cuda.is_current_stream_capturing()
 
     # ---- rows in and out -----------------------------------------------------------------
     def store(self, k, v, table, starts, counts=None, status=None, stream=None):
@@ -150,48 +182,50 @@ class Kv8Cache:
         ``starts`` on (``counts``: how many of each; default all). ``status``: an int32 tensor of
         one element that receives 0, or non-zero for NaN / Inf."""
         s = self._seqs(table)
-        _need(k.dtype in self._types, "k: float16 or bfloat16 is wanted")
-        shape = (s.n_seq, k.shape[1], self.n_heads, self.head_dim)
-        kr, vr = self._rows(k, "k", shape, k.dtype), self._rows(v, "v", shape, k.dtype)
+        kind = self._types.get(k.dtype)
+        _need(kind is not None and k.dim() == 4, "k: float16 or bfloat16 [n_seq, n_tokens, "
+              "n_heads, head_dim] is wanted")
         _need(starts is not None, "starts is missing")
-        st = None if status is None else self._tensor(status, "status", self.torch.int32, (1,))
-        _check(_lib().cg_kv8_store(self._cp, s, self._per_seq(starts, "starts", s.n_seq),
-                                   self._per_seq(counts, "counts", s.n_seq), shape[1],
-                                   self._types[k.dtype], kr, vr, st,
-                                   self._stream(stream).cuda_stream), "cg_kv8_store")
+        n = s.n_seq
+        shape = (n, k.shape[1], self.n_heads, self.head_dim)
+        _check(_lib().cg_kv8_store(
+            self._cp, s, self._per_seq(starts, "starts", n), self._per_seq(counts, "counts", n),
+            shape[1], kind, self._rows(k, "k", shape, k.dtype), self._rows(v, "v", shape, k.dtype),
+            None if status is None else self._tensor(status, "status", self._i32, (1,)),
+            self._handle(stream)), "cg_kv8_store")
 
     def load(self, table, starts, n_tokens, counts=None, dtype=None, k=None, v=None, stream=None):
         """(k, v) [n_seq, n_tokens, n_heads, head_dim]: the sequences' tokens from ``starts`` on,
         zeros behind ``counts``. ``k``, ``v``: tensors to write into."""
         s = self._seqs(table)
-        shape = (s.n_seq, int(n_tokens), self.n_heads, self.head_dim)
-        stream = self._stream(stream)
+        n = s.n_seq
+        shape = (n, int(n_tokens), self.n_heads, self.head_dim)
         if k is None or v is None:
-            dtype = dtype or self.torch.float16
-            with self.torch.cuda.stream(stream):
-                k = self.torch.empty(shape, dtype=dtype, device=self.device) if k is None else k
-                v = self.torch.empty(shape, dtype=dtype, device=self.device) if v is None else v
-        _need(k.dtype in self._types, "k: float16 or bfloat16 is wanted")
+            dtype = dtype or (self.torch.float16 if k is None and v is None else
+                              (v if k is None else k).dtype)
+            k = self._empty(shape, dtype, stream) if k is None else k
+            v = self._empty(shape, dtype, stream) if v is None else v
+        kind = self._types.get(k.dtype)
+        _need(kind is not None, "k: float16 or bfloat16 is wanted")
         _need(starts is not None, "starts is missing")
-        _check(_lib().cg_kv8_load(self._cp, s, self._per_seq(starts, "starts", s.n_seq),
-                                  self._per_seq(counts, "counts", s.n_seq), shape[1],
-                                  self._types[k.dtype], self._rows(k, "k", shape, k.dtype),
-                                  self._rows(v, "v", shape, k.dtype), stream.cuda_stream),
-               "cg_kv8_load")
+        _check(_lib().cg_kv8_load(
+            self._cp, s, self._per_seq(starts, "starts", n), self._per_seq(counts, "counts", n),
+            shape[1], kind, self._rows(k, "k", shape, k.dtype), self._rows(v, "v", shape, k.dtype),
+            self._handle(stream)), "cg_kv8_load")
         return k, v
 
     # ---- attention -----------------------------------------------------------------------
     def _attn(self, q, s, lengths, q_lens, max_len):
-        _need(q.dim() == 4 and q.dtype in self._types, "q: float16 or bfloat16 "
+        kind = self._types.get(q.dtype)
+        _need(q.dim() == 4 and kind is not None, "q: float16 or bfloat16 "
               "[n_seq, n_q, n_q_heads, head_dim] is wanted")
         _need(lengths is not None, "lengths is missing")
-        a = _Attn()
-        a.n_q, a.n_q_heads, a.dtype = q.shape[1], q.shape[2], self._types[q.dtype]
-        a.lengths = self._per_seq(lengths, "lengths", s.n_seq)
-        a.max_len = s.max_pages * PAGE if max_len is None else max_len
-        a.q_lens = self._per_seq(q_lens, "q_lens", s.n_seq)
-        a.q = self._rows(q, "q", (s.n_seq, a.n_q, a.n_q_heads, self.head_dim), q.dtype)
-        return a
+        n = s.n_seq
+        _, nq, heads, _ = q.shape
+        return _Attn(nq, heads, kind, 0.0, self._per_seq(lengths, "lengths", n),
+                     s.max_pages * PAGE if max_len is None else max_len,
+                     self._per_seq(q_lens, "q_lens", n),
+                     self._rows(q, "q", (n, nq, heads, self.head_dim), q.dtype))
 
     def attend(self, q, table, lengths, scale=None, q_lens=None, max_len=None, out=None, lse=None,
                picks=None, mass=None, mass_out=None, decay=1.0, stream=None):
@@ -208,30 +242,28 @@ class Kv8Cache:
                   in place)."""
         s = self._seqs(table)
         a = self._attn(q, s, lengths, q_lens, max_len)
-        stream = self._stream(stream)
-        f32 = self.torch.float32
         a.scale = 1.0 / math.sqrt(self.head_dim) if scale is None else scale
         if out is None:
-            with self.torch.cuda.stream(stream):
-                out = self.torch.empty(q.shape, dtype=q.dtype, device=self.device)
+            out = self._empty(q.shape, q.dtype, stream)
         a.out = self._rows(out, "out", q.shape, q.dtype)
         if lse is not None:
-            a.lse = self._tensor(lse, "lse", f32, q.shape[:3])
+            a.lse = self._tensor(lse, "lse", self._f32, q.shape[:3])
         if picks is not None:
             _need(picks.dim() == 4, "picks: [n_seq, n_q, n_heads, n] is wanted")
             a.n_picks = picks.shape[3]
-            a.picks = self._tensor(picks, "picks", self.torch.int32,
+            a.picks = self._tensor(picks, "picks", self._i32,
                                    (s.n_seq, a.n_q, self.n_heads, a.n_picks))
         if mass is not None or mass_out is not None:
             shape = (self.n_pages, self.n_heads, PAGE)
             mass_out = mass if mass_out is None else mass_out
-            a.mass_in = None if mass is None else self._tensor(mass, "mass", f32, shape)
-            a.mass_out = self._tensor(mass_out, "mass_out", f32, shape)
+            a.mass_in = None if mass is None else self._tensor(mass, "mass", self._f32, shape)
+            a.mass_out = self._tensor(mass_out, "mass_out", self._f32, shape)
             a.decay = decay
         L = _lib()
+        handle = self._handle(stream)
         need = L.cg_kv8_attend_workspace_bytes(self._cp, s, a)
-        ws, size = self._scratch(stream, need) if need else (None, 0)
-        _check(L.cg_kv8_attend(self._cp, s, a, ws, size, stream.cuda_stream), "cg_kv8_attend")
+        ws = self._scratch(stream, handle, need) if need else (None, 0)
+        _check(L.cg_kv8_attend(self._cp, s, a, ws[0], ws[1], handle), "cg_kv8_attend")
         return out
 
     def select(self, q, table, lengths, n_picks, recent=1, q_lens=None, max_len=None, out=None,
@@ -241,18 +273,16 @@ class Kv8Cache:
         of the others by the bound of their q . k."""
         s = self._seqs(table)
         a = self._attn(q, s, lengths, q_lens, max_len)
-        stream = self._stream(stream)
-        a.n_picks = int(n_picks)
+        a.n_picks = n_picks
         shape = (s.n_seq, a.n_q, self.n_heads, max(0, a.n_picks))
         if out is None:
-            with self.torch.cuda.stream(stream):
-                out = self.torch.empty(shape, dtype=self.torch.int32, device=self.device)
+            out = self._empty(shape, self._i32, stream)
         L = _lib()
+        handle = self._handle(stream)
         need = L.cg_kv8_select_workspace_bytes(self._cp, s, a)
-        ws, size = self._scratch(stream, need) if need else (None, 0)
-        _check(L.cg_kv8_select(self._cp, s, a, int(recent),
-                               self._tensor(out, "out", self.torch.int32, shape), ws, size,
-                               stream.cuda_stream), "cg_kv8_select")
+        ws = self._scratch(stream, handle, need) if need else (None, 0)
+        _check(L.cg_kv8_select(self._cp, s, a, recent, self._tensor(out, "out", self._i32, shape),
+                               ws[0], ws[1], handle), "cg_kv8_select")
         return out
 
     # ---- eviction ------------------------------------------------------------------------
@@ -262,17 +292,14 @@ class Kv8Cache:
         [n_pages, n_heads, 64], which moves along. Returns (kept [n_seq, n_heads, keep],
         new_lengths [n_seq])."""
         s, to = self._seqs(table), self._seqs(new_table)
-        stream = self._stream(stream)
-        t = self.torch
-        with t.cuda.stream(stream):
-            kept = t.empty((s.n_seq, self.n_heads, max(0, int(keep))), dtype=t.int32,
-                           device=self.device)
-            new_lengths = t.empty((s.n_seq,), dtype=t.int32, device=self.device)
         _need(lengths is not None and mass is not None, "lengths and mass are wanted")
+        n = s.n_seq
+        kept = self._empty((n, self.n_heads, max(0, keep)), self._i32, stream)
+        new_lengths = self._empty((n,), self._i32, stream)
         _check(_lib().cg_kv8_evict(
-            self._cp, s, self._per_seq(lengths, "lengths", s.n_seq),
-            s.max_pages * PAGE if max_len is None else int(max_len),
-            self._tensor(mass, "mass", t.float32, (self.n_pages, self.n_heads, PAGE)), int(keep),
-            int(recent), to, kept.data_ptr(), new_lengths.data_ptr(), stream.cuda_stream),
+            self._cp, s, self._per_seq(lengths, "lengths", n),
+            s.max_pages * PAGE if max_len is None else max_len,
+            self._tensor(mass, "mass", self._f32, (self.n_pages, self.n_heads, PAGE)), keep,
+            recent, to, kept.data_ptr(), new_lengths.data_ptr(), self._handle(stream)),
             "cg_kv8_evict")
         return kept, new_lengths

@@ -419,6 +419,7 @@ def test_attend_graph_replay():
     (256, 2, 1, 1, [2000], 4, 0),
     (128, 16, 1, 3, [900], 2, 5),
     (64, 2, 2, 1, [20000], 70, 1),
+    (64, 200, 1, 1, [700], 4, 1),
 ])
 def test_select_and_sparse(dtype, D, HQ, H, Q, lengths, n_picks, recent):
     torch = torch_cuda()
@@ -473,6 +474,7 @@ def test_select_zero_queries_and_lost_pages():
     (64, 1, [300, 299], 65, 65),
     (256, 1, [200], 100, 150),
     (128, 1, [5000, 4000], 1000, 100),
+    (64, 1, [70000], 3000, 100),              # more keys than the lanes keep in registers
 ])
 def test_evict(D, H, lengths, keep, recent):
     torch = torch_cuda()

@@ -113,6 +113,33 @@ struct StoreLds {
   uint32_t lo[16 * D / 4], hi[16 * D / 4];   // per row group: bounds of each channel
 };
 
+// V codes [D][64] from L.vt, a quarter of a channel's tokens (16 bytes) a thread and step.
+template <int D>
+__device__ __forceinline__ void write_v(int8_t* codes, const StoreLds<D>& L) {
+#pragma unroll
+  for (int i = threadIdx.x; i < D * 4; i += 2 * D) {
+    const int d = i >> 2, j = i & 3;
+    const uint4v o = {L.vt[d * 17 + 4 * j], L.vt[d * 17 + 4 * j + 1], L.vt[d * 17 + 4 * j + 2],
+                      L.vt[d * 17 + 4 * j + 3]};
+    *reinterpret_cast<uint4v*>(codes + d * kPage + 16 * j) = o;
+  }
+}
+
+// Bounds [2][D] from the 16 row groups': thread d the lowest of channel d, thread D + d the
+// highest.
+template <int D>
+__device__ __forceinline__ void write_bounds(int8_t* bounds, const StoreLds<D>& L) {
+  const int tid = threadIdx.x;
+  const int8_t* src = reinterpret_cast<const int8_t*>(tid < D ? L.lo : L.hi) + tid % D;
+  int b = src[0];
+#pragma unroll
+  for (int g = 1; g < 16; ++g) {
+    const int o = src[g * D];
+    b = tid < D ? (o < b ? o : b) : (o > b ? o : b);
+  }
+  bounds[tid] = (int8_t)b;
+}
+
 // Writes one page of a head from the 2 D threads' rows x[4][8]: thread (rg, cg) = (tid / (D / 8),
 // tid % (D / 8)) has rows 4 rg .. 4 rg + 3 of channels 8 cg .. 8 cg + 7. Rows held .. end - 1 are
 // new, the `held` before them keep their codes (re-coded where the scale grows), rows from `end`
@@ -171,13 +198,7 @@ __device__ __forceinline__ void put_page(const KvPool& pool, int page, int h, co
     for (int c = 0; c < 8; ++c)
       L.vt[(8 * cg + c) * 17 + rg] = pack4(q[0][c], q[1][c], q[2][c], q[3][c]);
     __syncthreads();
-#pragma unroll
-    for (int i = tid; i < D * 4; i += NT) {          // 16 bytes: a quarter of a channel's tokens
-      const int d = i >> 2, j = i & 3;
-      const uint4v o = {L.vt[d * 17 + 4 * j], L.vt[d * 17 + 4 * j + 1], L.vt[d * 17 + 4 * j + 2],
-                        L.vt[d * 17 + 4 * j + 3]};
-      *reinterpret_cast<uint4v*>(codes + d * kPage + 16 * j) = o;
-    }
+    write_v<D>(codes, L);
   } else {
 #pragma unroll
     for (int r = 0; r < 4; ++r)
@@ -203,15 +224,7 @@ __device__ __forceinline__ void put_page(const KvPool& pool, int page, int h, co
       L.hi[w] = pack4(hi[0], hi[1], hi[2], hi[3]);
       L.hi[w + 1] = pack4(hi[4], hi[5], hi[6], hi[7]);
       __syncthreads();
-      // thread d: the lowest of channel d; thread D + d: the highest
-      const int d = tid % D;
-      const int8_t* src = reinterpret_cast<const int8_t*>(tid < D ? L.lo : L.hi) + d;
-      int b = src[0];
-      for (int g = 1; g < 16; ++g) {
-        const int o = src[g * D];
-        b = tid < D ? (o < b ? o : b) : (o > b ? o : b);
-      }
-      pool.bounds[at * (2 * D) + tid] = (int8_t)b;
+      write_bounds<D>(pool.bounds + at * (2 * D), L);
     }
   }
   __syncthreads();                   // the LDS may be used again

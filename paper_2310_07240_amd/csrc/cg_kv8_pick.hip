@@ -41,8 +41,11 @@ __device__ __forceinline__ void pick_best(int n, int need, PickLds<NT>& L, KeyBl
   const int mine = first + per < blocks ? per : blocks > first ? blocks - first : 0;
   uint32_t held[kHeld];
 #pragma unroll
-  for (int r = 0; r < kHeld; ++r)
-    if (r < mine) held[r] = key_block(first + r, lane);
+  for (int r = 0; r < kHeld; r += 8)
+    if (r < mine) {                  // eight blocks on their way at once
+#pragma unroll
+      for (int i = r; i < r + 8; ++i) held[i] = key_block(first + (i < mine ? i : mine - 1), lane);
+    }
   // f(round, key) for the lane's keys; indices from n on are nobody's
   const auto each = [&](auto f) {
 #pragma unroll
@@ -215,11 +218,17 @@ __global__ __launch_bounds__(2 * D) void move_kernel(KvPool pool, KvSeqs S, KvSe
       for (int i = 0; i < 8; ++i) x[e][i] = (float)(int8_t)(c[i >> 2] >> (8 * (i & 3))) * s;
     }
     // V: a lane is a token, so a wave reads one channel of neighbouring slots
-    for (int d = tid / kPage; d < D; d += NT / kPage) {
-      const int t = tid % kPage;
+    {
+      const int t = tid % kPage, d0 = tid / kPage;
       const int64_t f = from[t];
-      vt[d * (kPage + 4) + t] =
-          f >= 0 ? (uint8_t)pool.v[f * (kPage * D) + (int64_t)d * kPage + slot[t]] : 0;
+      const int8_t* src = pool.v + (f < 0 ? 0 : f) * (kPage * D) + slot[t];
+      constexpr int kSteps = D / (NT / kPage);
+      int8_t c[kSteps];
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) c[i] = src[(d0 + i * (NT / kPage)) * kPage];
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i)
+        vt[(d0 + i * (NT / kPage)) * (kPage + 4) + t] = f >= 0 ? (uint8_t)c[i] : 0;
     }
     put_page<D, false>(pool, page, h, x, 0, end, L);   // its barriers cover vt
 #pragma unroll

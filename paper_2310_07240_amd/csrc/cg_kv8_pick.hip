@@ -6,11 +6,17 @@
 namespace {
 
 // Keys in the order of the values: a larger value has a larger key, -0 and +0 the same, a NaN the
-// lowest of all.
+// lowest of all. 0 is no value's key.
 __device__ __forceinline__ uint32_t order_key(float f) {
-  if (f != f) return 0u;
+  if (f != f) return 1u;
   const uint32_t u = __builtin_bit_cast(uint32_t, f + 0.0f);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// How many lanes below this one are in the mask.
+__device__ __forceinline__ uint32_t lanes_below(uint64_t mask) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32),
+                                   __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
 
 constexpr int kBins = 2048;          // of a pass: 11 bits of the keys
@@ -23,15 +29,18 @@ struct PickLds {
   uint32_t digit, rest;
 };
 
-// The best `need` (1 <= need < n) of key(0 .. n - 1): emit(position, index) for each, positions
-// ascending with the index. Every wave has a run of whole 64-key blocks (key_block(j, lane): key
-// of index 64 j + lane), the first kHeld of them in registers, so the keys are read once. Three
-// passes over the keys' bits, highest first, narrow them to the smallest key that is taken and the
-// number of its equals that are; then each wave counts and emits its run by ballots. Counts are
-// whole numbers, so no order of the LDS additions changes anything. Bound by the first pass's LDS
-// additions (weights crowd into a few octaves, so lanes meet on a bin: hence 11 bits and not 8).
-template <int NT, class KeyBlock, class Emit>
-__device__ __forceinline__ void pick_best(int n, int need, PickLds<NT>& L, KeyBlock key_block,
+// The best `need` (1 <= need < n) of n keys: emit(position, index) for each, positions ascending
+// with the index. Of a block j of 64 keys, place(j) says where it lies, raw() loads and key() makes
+// the key of index 64 j + lane, 0 from n on (no key is 0, so such places are never among the best);
+// they are called apart so that no load waits for another. Every wave has a run of whole blocks, the first kHeld of
+// them in registers, so the keys are read once. Three passes over the keys' bits, highest first,
+// narrow them to the smallest key that is taken and the number of its equals that are; then each
+// wave counts and emits its run by ballots. Counts are whole numbers, so no order of the LDS
+// additions changes anything. Bound by the vector instructions of the one CU (about 45 a block in
+// all) and the first pass's LDS additions: weights crowd into a few octaves, so lanes meet on a bin,
+// hence 11 bits and not 8.
+template <int NT, class Keys, class Emit>
+__device__ __forceinline__ void pick_best(int n, int need, PickLds<NT>& L, const Keys& keys,
                                           Emit emit) {
   constexpr int NW = NT / 64;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -40,30 +49,44 @@ __device__ __forceinline__ void pick_best(int n, int need, PickLds<NT>& L, KeyBl
   const int first = wave * per;
   const int mine = first + per < blocks ? per : blocks > first ? blocks - first : 0;
   uint32_t held[kHeld];
+  // a lane finds a block's place, then eight blocks are on their way at once
+  const int place = keys.place(first + (lane < mine ? lane : 0));
 #pragma unroll
   for (int r = 0; r < kHeld; r += 8)
-    if (r < mine) {                  // eight blocks on their way at once
+    if (r < mine) {
+      uint32_t raw[8];
+      int at[8];
 #pragma unroll
-      for (int i = r; i < r + 8; ++i) held[i] = key_block(first + (i < mine ? i : mine - 1), lane);
+      for (int i = 0; i < 8; ++i) {
+        at[i] = __builtin_amdgcn_readlane(place, r + i);
+        raw[i] = keys.raw(at[i], first + (r + i < mine ? r + i : 0), lane);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        held[r + i] = r + i < mine ? keys.key(raw[i], at[i], first + r + i, lane) : 0u;
     }
-  // f(round, key) for the lane's keys; indices from n on are nobody's
+  // f(block, key) for the wave's keys, eight blocks of registers a branch
   const auto each = [&](auto f) {
 #pragma unroll
-    for (int r = 0; r < kHeld; ++r)
-      if (r < mine) f(r, held[r]);
-    for (int r = kHeld; r < mine; ++r) f(r, key_block(first + r, lane));
+    for (int r = 0; r < kHeld; r += 8)
+      if (r < mine) {
+#pragma unroll
+        for (int i = r; i < r + 8; ++i) f(first + i, held[i]);
+      }
+    for (int r = kHeld; r < mine; ++r) {
+      const int at = keys.place(first + r);
+      f(first + r, keys.key(keys.raw(at, first + r, lane), at, first + r, lane));
+    }
   };
-  const auto live = [&](int r) { return (first + r) * 64 + lane < n; };
 
-  uint32_t prefix = 0, mask = 0;
+  uint32_t prefix = 0;
   uint32_t rest = (uint32_t)need;
-  for (int pass = 0; pass < 3; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-    const uint32_t width = pass == 2 ? 1023u : 2047u;
+  // the keys' bits `shift` .. of those that agree with `prefix` above `free` bits
+  const auto narrow = [&](int shift, uint32_t width, auto agrees) {
     for (int i = tid; i < kBins; i += NT) L.hist[i] = 0;
     __syncthreads();
-    each([&](int r, uint32_t k) {
-      if (live(r) && (k & mask) == prefix) atomicAdd(&L.hist[(k >> shift) & width], 1u);
+    each([&](int, uint32_t k) {
+      if (agrees(k)) atomicAdd(&L.hist[(k >> shift) & width], 1u);
     });
     __syncthreads();
     // the bins from the highest down, kBins / NT a thread
@@ -94,13 +117,16 @@ __device__ __forceinline__ void pick_best(int n, int need, PickLds<NT>& L, KeyBl
     }
     __syncthreads();
     prefix |= L.digit << shift;
-    mask |= width << shift;
     rest = L.rest;
-  }
+  };
+  narrow(21, 2047u, [](uint32_t) { return true; });
+  narrow(10, 2047u, [&](uint32_t k) { return (k ^ prefix) < (1u << 21); });
+  narrow(0, 1023u, [&](uint32_t k) { return (k ^ prefix) < (1u << 10); });
+
   uint32_t na = 0, ne = 0;           // of the wave's run: taken for sure, and equal to the last
-  each([&](int r, uint32_t k) {
-    na += (uint32_t)__popcll(__ballot(live(r) && k > prefix));
-    ne += (uint32_t)__popcll(__ballot(live(r) && k == prefix));
+  each([&](int, uint32_t k) {
+    na += (uint32_t)__popcll(__ballot(k > prefix));
+    ne += (uint32_t)__popcll(__ballot(k == prefix));
   });
   __syncthreads();
   if (lane == 0) {
@@ -113,14 +139,17 @@ __device__ __forceinline__ void pick_best(int n, int need, PickLds<NT>& L, KeyBl
     na += L.above[w];
     ne += L.equal[w];
   }
-  const uint64_t below = ((uint64_t)1 << lane) - 1;
-  each([&](int r, uint32_t k) {
-    const bool a = live(r) && k > prefix, e = live(r) && k == prefix;
-    const uint64_t ba = __ballot(a), be = __ballot(e);
-    const uint32_t ra = na + (uint32_t)__popcll(ba & below), re = ne + (uint32_t)__popcll(be & below);
-    if (a || (e && re < rest)) emit((int)(ra + (re < rest ? re : rest)), (first + r) * 64 + lane);
-    na += (uint32_t)__popcll(ba);
-    ne += (uint32_t)__popcll(be);
+  na = __builtin_amdgcn_readfirstlane(na);
+  ne = __builtin_amdgcn_readfirstlane(ne);
+  each([&](int j, uint32_t k) {
+    const uint64_t ba = __ballot(k > prefix), be = __ballot(k == prefix);
+    if (ba | be) {
+      const uint32_t re = ne + lanes_below(be);
+      const uint32_t at = na + lanes_below(ba) + (re < rest ? re : rest);
+      if (k > prefix || (k == prefix && re < rest)) emit((int)at, j * 64 + lane);
+      na += (uint32_t)__popcll(ba);
+      ne += (uint32_t)__popcll(be);
+    }
   });
 }
 
@@ -134,6 +163,23 @@ __device__ __forceinline__ int held_tokens(const KvSeqs& S, const int32_t* lengt
 }
 
 constexpr int kKeepThreads = 1024;
+
+// The weights of one sequence and head as keys: a block is a page.
+struct MassKeys {
+  const KvPool& pool;
+  const KvSeqs& S;
+  const float* mass;
+  int seq, h, n;
+  __device__ __forceinline__ int place(int j) const { return kv_page(S, pool.P, seq, j); }
+  __device__ __forceinline__ uint32_t raw(int page, int, int lane) const {
+    return __builtin_bit_cast(
+        uint32_t, mass[((int64_t)(page < 0 ? 0 : page) * pool.H + h) * kPage + lane]);
+  }
+  __device__ __forceinline__ uint32_t key(uint32_t raw, int page, int j, int lane) const {
+    const uint32_t k = page < 0 ? 1u : order_key(__builtin_bit_cast(float, raw));
+    return j * kPage + lane < n ? k : 0u;
+  }
+};
 
 // One workgroup per (sequence, KV head): the tokens that stay.
 __global__ __launch_bounds__(kKeepThreads) void keep_kernel(KvPool pool, KvSeqs S,
@@ -156,12 +202,7 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(KvPool pool, KvSeqs 
   for (int i = tid; i < last; i += kKeepThreads) out[need + i] = old + i;
   if (need == 0) return;
   pick_best<kKeepThreads>(
-      old, need, L,
-      [&](int j, int lane) {
-        const int page = kv_page(S, pool.P, seq, j);
-        if (page < 0) return 0u;
-        return order_key(mass[((int64_t)page * pool.H + h) * kPage + lane]);
-      },
+      old, need, L, MassKeys{pool, S, mass, seq, h, old},
       [&](int at, int i) { out[at] = i; });
 }
 
@@ -243,6 +284,20 @@ __global__ __launch_bounds__(2 * D) void move_kernel(KvPool pool, KvSeqs S, KvSe
     put_page<D, true>(pool, page, h, x, 0, end, L);
   }
 }
+
+// Keys that other workgroups of the launch have left in memory.
+struct LeftKeys {
+  uint32_t* keys;
+  int n;
+  __device__ __forceinline__ int place(int) const { return 0; }
+  __device__ __forceinline__ uint32_t raw(int, int j, int lane) const {
+    const int e = j * 64 + lane;
+    return __hip_atomic_load(keys + (e < n ? e : 0), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __device__ __forceinline__ uint32_t key(uint32_t raw, int, int j, int lane) const {
+    return j * 64 + lane < n ? raw : 0u;
+  }
+};
 
 constexpr int kSelectThreads = 256;
 constexpr int kScoreRounds = 4;      // pages a lane group scores at once
@@ -359,7 +414,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(KvPool pool, KvS
           if (g0 > 0)
             sum += (int)__hip_atomic_load(&mine[j], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
           const uint32_t k = g1 < A.group ? (uint32_t)sum
-                             : page[r] < 0 ? 0u : order_key((float)sum * ks[r]);
+                             : page[r] < 0 ? 1u : order_key((float)sum * ks[r]);
           __hip_atomic_store(&mine[j], k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
       }
@@ -379,11 +434,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(KvPool pool, KvS
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   pick_best<kSelectThreads>(
-      old, need, L,
-      [&](int j, int lane) {
-        const int e = j * 64 + lane < old ? j * 64 + lane : 0;
-        return __hip_atomic_load(&mine[e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      },
+      old, need, L, LeftKeys{mine, old},
       [&](int at, int j) { picks[at] = j; });
 }
 

@@ -230,6 +230,106 @@ __device__ __forceinline__ void put_page(const KvPool& pool, int page, int h, co
   __syncthreads();                   // the LDS may be used again
 }
 
+// Codes of a thread's rows at scale s, as floats whose low byte is the code: v / s rounded to a
+// whole number by adding 1.5 2^23. The quotient is taken as v * inv, which below 127.0001 is
+// within 2.3e-5 of the correctly rounded v / s; only where it comes within 2^-15 of a half-integer
+// could the two round apart, and there (one row of 64 x 8 values in 30) the wave divides. No clamp:
+// |v| <= 127 s (1 + 2^-23).
+template <class Rows>
+__device__ __forceinline__ void fast_codes(const Rows& rows, float s, float inv, float q[4][8]) {
+  constexpr float kMagic = 12582912.0f;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    float x[8], far = 0.0f;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      x[c] = rows.value(r, c);
+      const float v = __builtin_fmaf(x[c], inv, 0.0f);
+      q[r][c] = v + kMagic;
+      far = fmaxf(far, __builtin_fabsf(v - (q[r][c] - kMagic)));
+    }
+    if (__builtin_expect(__any(far >= 0.5f - 0x1p-15f), 0)) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) q[r][c] = (s > 0.0f ? x[c] / s : 0.0f) + kMagic;
+    }
+  }
+}
+
+__device__ __forceinline__ uint32_t low_bytes(float a, float b, float c, float d) {
+  const uint32_t ab = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, b),
+                                            __builtin_bit_cast(uint32_t, a), 0x0c0c0400u);
+  const uint32_t cd = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, d),
+                                            __builtin_bit_cast(uint32_t, c), 0x04000c0cu);
+  return ab | cd;
+}
+
+// A page whose rows are all new, finite and of scales far from the subnormals: put_page's result
+// for K and V together, under the scales ks, vs of their maxima, with one barrier.
+template <int D, class KRows, class VRows>
+__device__ __forceinline__ void put_fresh(const KvPool& pool, int64_t at, const KRows& k,
+                                          const VRows& v, int end, float ks, float vs,
+                                          StoreLds<D>& L) {
+  const int tid = threadIdx.x, cg = tid % (D / 8), rg = tid / (D / 8);
+  float q[4][8];
+  fast_codes(v, vs, vs > 0.0f ? 1.0f / vs : 0.0f, q);
+#pragma unroll
+  for (int c = 0; c < 8; ++c)
+    L.vt[(8 * cg + c) * 17 + rg] = low_bytes(q[0][c], q[1][c], q[2][c], q[3][c]);
+  fast_codes(k, ks, ks > 0.0f ? 1.0f / ks : 0.0f, q);
+  int8_t* kc = pool.k + at * (kPage * D);
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    *reinterpret_cast<uint2v*>(kc + (4 * rg + r) * D + 8 * cg) =
+        uint2v{low_bytes(q[r][0], q[r][1], q[r][2], q[r][3]),
+               low_bytes(q[r][4], q[r][5], q[r][6], q[r][7])};
+  if (pool.bounds) {
+    float lo[8], hi[8];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      lo[c] = 12582912.0f + 127.0f;
+      hi[c] = 12582912.0f - 127.0f;
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (4 * rg + r < end) {
+          lo[c] = fminf(lo[c], q[r][c]);
+          hi[c] = fmaxf(hi[c], q[r][c]);
+        }
+    }
+    const int w = rg * (D / 4) + 2 * cg;
+    L.lo[w] = low_bytes(lo[0], lo[1], lo[2], lo[3]);
+    L.lo[w + 1] = low_bytes(lo[4], lo[5], lo[6], lo[7]);
+    L.hi[w] = low_bytes(hi[0], hi[1], hi[2], hi[3]);
+    L.hi[w + 1] = low_bytes(hi[4], hi[5], hi[6], hi[7]);
+  }
+  if (tid == 0) {
+    pool.ks[at] = ks;
+    pool.vs[at] = vs;
+  }
+  __syncthreads();
+  write_v<D>(pool.v + at * (kPage * D), L);
+  if (pool.bounds) write_bounds<D>(pool.bounds + at * (2 * D), L);
+}
+
+// put_page for K and V of any page.
+template <int D, class KRows, class VRows>
+__device__ __forceinline__ void put_any(const KvPool& pool, int page, int h, const KRows& k,
+                                        const VRows& v, int held, int end, StoreLds<D>& L) {
+  float x[4][8];
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int c = 0; c < 8; ++c) x[r][c] = k.value(r, c);
+  put_page<D, false>(pool, page, h, x, held, end, L);
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int c = 0; c < 8; ++c) x[r][c] = v.value(r, c);
+  put_page<D, true>(pool, page, h, x, held, end, L);
+}
+
+// Whether put_fresh may code under this scale.
+__device__ __forceinline__ bool plain_scale(float s) { return s == 0.0f || s >= 0x1p-100f; }
+
 // Launchers; arguments are checked by the C ABI.
 struct KvAttn {
   const int32_t* lengths;

@@ -206,19 +206,43 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(KvPool pool, KvSeqs 
       [&](int at, int i) { out[at] = i; });
 }
 
+// A thread's rows of moved tokens: codes times their own pages' scales.
+struct MovedK {
+  const uint2v* c;                             // row r, channels 0 .. 7
+  const float* s;
+  __device__ __forceinline__ float value(int r, int i) const {
+    return (float)(int8_t)(c[r][i >> 2] >> (8 * (i & 3))) * s[r];
+  }
+};
+struct MovedV {
+  const uint32_t* w;                           // channel i, rows 0 .. 3
+  const float* s;
+  __device__ __forceinline__ float value(int r, int i) const {
+    return (float)(int8_t)(w[i] >> (8 * r)) * s[r];
+  }
+};
+
+__device__ __forceinline__ int code_size(int c) { return c < 0 ? -c : c; }
+
 // One workgroup of 2 D threads per (sequence, new page, KV head): gathers the page's tokens,
-// codes them under the scale of their own largest value, and moves their weights along.
+// codes them under the scale of their own largest value, and moves their weights along. K is read
+// row by row; V (whose tokens lie a byte apart) with a token a lane, so that a wave's load is one
+// channel of neighbouring slots, and turned in LDS. The largest value of a token is its largest
+// code times its scale. Bound by latency: lengths, kept, table and codes are read one after the
+// other, then 4 workgroups a CU.
 template <int D>
 __global__ __launch_bounds__(2 * D) void move_kernel(KvPool pool, KvSeqs S, KvSeqs to,
                                                      const int32_t* __restrict__ lengths,
                                                      int max_len, float* mass, int keep,
                                                      const int32_t* __restrict__ kept,
                                                      int64_t items) {
+  constexpr int NT = 2 * D, NW = NT / 64;
   __shared__ StoreLds<D> L;
   __shared__ int64_t from[kPage];              // (page, head) of a slot's token, or -1
   __shared__ int32_t slot[kPage];
-  __shared__ uint8_t vt[D * (kPage + 4)];
-  constexpr int NT = 2 * D;
+  __shared__ float k_scale[kPage], v_scale[kPage];
+  __shared__ uint32_t vt[D * 17];              // V codes [D][64 + 4]
+  __shared__ uint32_t tops[NW][2];
   const int tid = threadIdx.x, cg = tid % (D / 8), rg = tid / (D / 8);
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const int h = (int)(it % pool.H);
@@ -229,6 +253,7 @@ __global__ __launch_bounds__(2 * D) void move_kernel(KvPool pool, KvSeqs S, KvSe
     if (j * (int64_t)kPage >= total) continue;
     const int page = kv_page(to, pool.P, seq, j);
     if (page < 0) continue;
+    const int64_t at = (int64_t)page * pool.H + h;
     const int end = total - j * kPage < kPage ? total - j * kPage : kPage;
     if (tid < kPage) {
       int64_t f = -1;
@@ -240,48 +265,78 @@ __global__ __launch_bounds__(2 * D) void move_kernel(KvPool pool, KvSeqs S, KvSe
       }
       from[tid] = f;
       slot[tid] = t % kPage;
-      mass[((int64_t)page * pool.H + h) * kPage + tid] =
-          f >= 0 ? mass[f * kPage + t % kPage] : 0.0f;
+      k_scale[tid] = f >= 0 ? pool.ks[f] : 0.0f;
+      v_scale[tid] = f >= 0 ? pool.vs[f] : 0.0f;
+      mass[at * kPage + tid] = f >= 0 ? mass[f * kPage + t % kPage] : 0.0f;
     }
     __syncthreads();
-    float x[4][8];
+    uint2v kc[4];
+    float ks[4], vs[4];
+    uint32_t k_top = 0, v_top = 0;             // magnitude bits: ordered as the magnitudes are
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int t = 4 * rg + e;
       const int64_t f = from[t];
-      uint2v c = {0, 0};
-      float s = 0.0f;
-      if (f >= 0) {
-        c = *reinterpret_cast<const uint2v*>(pool.k + f * (kPage * D) + slot[t] * D + 8 * cg);
-        s = pool.ks[f];
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[e][i] = (float)(int8_t)(c[i >> 2] >> (8 * (i & 3))) * s;
+      kc[e] = *reinterpret_cast<const uint2v*>(pool.k + (f < 0 ? 0 : f) * (kPage * D) +
+                                               slot[t] * D + 8 * cg);
+      ks[e] = k_scale[t];
+      vs[e] = v_scale[t];
     }
-    // V: a lane is a token, so a wave reads one channel of neighbouring slots
     {
+      constexpr int kSteps = D / NW;
       const int t = tid % kPage, d0 = tid / kPage;
       const int64_t f = from[t];
       const int8_t* src = pool.v + (f < 0 ? 0 : f) * (kPage * D) + slot[t];
-      constexpr int kSteps = D / (NT / kPage);
       int8_t c[kSteps];
 #pragma unroll
-      for (int i = 0; i < kSteps; ++i) c[i] = src[(d0 + i * (NT / kPage)) * kPage];
+      for (int i = 0; i < kSteps; ++i) c[i] = src[(d0 + i * NW) * kPage];
+      int top = 0;
 #pragma unroll
-      for (int i = 0; i < kSteps; ++i)
-        vt[(d0 + i * (NT / kPage)) * (kPage + 4) + t] = f >= 0 ? (uint8_t)c[i] : 0;
+      for (int i = 0; i < kSteps; ++i) {
+        const int v = f >= 0 ? c[i] : 0;
+        top = code_size(v) > top ? code_size(v) : top;
+        reinterpret_cast<uint8_t*>(vt)[(d0 + i * NW) * 68 + t] = (uint8_t)v;
+      }
+      v_top = __builtin_bit_cast(uint32_t, (float)top * v_scale[t]) & 0x7fffffffu;
     }
-    put_page<D, false>(pool, page, h, x, 0, end, L);   // its barriers cover vt
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int t = 4 * rg + e;
-      const int64_t f = from[t];
-      const float s = f >= 0 ? pool.vs[f] : 0.0f;
+      int top = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        x[e][i] = (float)(int8_t)vt[(8 * cg + i) * (kPage + 4) + t] * s;
+      for (int i = 0; i < 8; ++i) {
+        const int c = code_size((int8_t)(kc[e][i >> 2] >> (8 * (i & 3))));
+        top = c > top ? c : top;
+      }
+      const uint32_t b = __builtin_bit_cast(uint32_t, (float)top * ks[e]) & 0x7fffffffu;
+      k_top = b > k_top ? b : k_top;           // (rows of no token have scale 0)
     }
-    put_page<D, true>(pool, page, h, x, 0, end, L);
+#pragma unroll
+    for (int o = 32; o; o >>= 1) {
+      const uint32_t a = __shfl_xor(k_top, o), b = __shfl_xor(v_top, o);
+      k_top = a > k_top ? a : k_top;
+      v_top = b > v_top ? b : v_top;
+    }
+    if ((tid & 63) == 0) {
+      tops[tid >> 6][0] = k_top;
+      tops[tid >> 6][1] = v_top;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      k_top = tops[w][0] > k_top ? tops[w][0] : k_top;
+      v_top = tops[w][1] > v_top ? tops[w][1] : v_top;
+    }
+    uint32_t vw[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) vw[i] = vt[(8 * cg + i) * 17 + rg];
+    const float k_new = __builtin_bit_cast(float, k_top) / 127.0f;
+    const float v_new = __builtin_bit_cast(float, v_top) / 127.0f;
+    const bool finite = k_top < 0x7f800000u && v_top < 0x7f800000u;
+    if (finite && plain_scale(k_new) && plain_scale(v_new))
+      put_fresh<D>(pool, at, MovedK{kc, ks}, MovedV{vw, vs}, end, k_new, v_new, L);
+    else
+      put_any<D>(pool, page, h, MovedK{kc, ks}, MovedV{vw, vs}, 0, end, L);
+    __syncthreads();
   }
 }
 

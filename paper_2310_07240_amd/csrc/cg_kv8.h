@@ -17,6 +17,7 @@ constexpr int kPage = CG_KV8_PAGE;
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef float float2v __attribute__((ext_vector_type(2)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
@@ -352,7 +353,7 @@ static_assert(kKv8Front == kKv8Counters * 4, "one 32-bit counter a tile");
 
 struct KvAttnPlan {
   int32_t tiles, splits;        // 16-row tiles and splits of the pages for each (sequence, KV head)
-  int32_t big, blocks;          // prompt_kernel: tiles of 128 blocks rows; big = 0: attend_kernel
+  int32_t big;                  // prompt_kernel's row tiles; 0: attend_kernel
   bool keep_scores;             // for the weights (see cg_kv8_plan)
   uint64_t part_off, lse_off, score_off, total;   // workspace, in bytes
 };

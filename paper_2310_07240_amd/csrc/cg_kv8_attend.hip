@@ -46,6 +46,9 @@ struct QTile {
   int visible;       // tokens that the lane's row sees
 };
 
+// A value that is the same in every lane, in a scalar register.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 // Where the rows of a (virtual) sequence come from. With picks every query token is a sequence
 // of its own, whose rows are the heads of the group.
 struct RowsOf {
@@ -587,19 +590,21 @@ __global__ __launch_bounds__(256) void mass_scores_kernel(KvPool pool, KvSeqs S,
 
 // ---- many rows ------------------------------------------------------------------------------
 // Where a KV head has many rows, the matrix units bound: v_mfma_f32_32x32x16_f16, transposed as
-// above (lane = 32 half + m, results of row m), a wave with NB blocks of 32 rows. The workgroup's
-// four waves share each page through LDS: it is loaded as codes one page ahead, widened to fp16
-// once, and read as operands by every wave. Row m of a 32-token K tile is the token whose place
-// makes a lane's 16 results the consecutive tokens 16 half .. 16 half + 15 (`tile_row`), the k
-// slots it supplies for P V.
+// above (lane = 32 half + m, results of row m), 32 rows a wave. The workgroup's waves share each
+// page through LDS: it is loaded as codes ahead of its turn, widened to fp16 once, and read as
+// operands by every wave. Row m of a 32-token K tile is the token whose place makes a lane's 16
+// results the consecutive tokens 16 half .. 16 half + 15 (`tile_row`), the k slots it supplies for
+// P V.
 //
 // The weights of a page enter the second product times the page's V scale, relative to a running
-// reference of that product (`ref`, log2), so O needs no further factor; l has a reference of its
-// own (`ref_l`). `ref` moves only where a row passes it by more than 2^kSlack, so the accumulators
-// are rescaled on few pages: what fp16 holds is at most 2^(kLift + kSlack), and normal down to
-// 2^-(14 + kLift) of the reference (2^-(24 + kLift) in steps of that), far below what a sum
-// around 1 shows.
-constexpr int kLift = 4, kSlack = 8;
+// reference of that product (`ref`, log2), so O needs no further factor, and l sums them without
+// the scale. No maximum is taken: the weights go by the reference that is there, and only where
+// they sum to more than kMost (less than fp16 holds) a tile's maximum is found, the accumulators
+// move to it, and the weights are taken again; a row's first tile does that. What fp16 holds is
+// normal down to 2^-(14 + kLift) of the reference (and steps of 2^-(24 + kLift) below), far
+// under what a sum around 1 shows.
+constexpr int kLift = 4;
+constexpr float kMost = 32768.0f;
 
 __device__ __forceinline__ int tile_row(int t) {       // of token t of 32: its row in the K tile
   return 8 * ((t & 15) >> 2) + 4 * (t >> 4) + (t & 3);
@@ -614,11 +619,10 @@ __device__ __forceinline__ void both_halves(uint32_t u, uint32_t& lo, uint32_t& 
   lo = r[0];
   hi = r[1];
 }
-// The largest of three, without the canonicalization that fmaxf of unknown values costs.
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
+// The larger of two in one instruction: fmaxf of a product's result costs a second one that quiets
+// NaNs. (Not through inline assembly, whose reads of a matrix result the compiler does not pad.)
+__device__ __forceinline__ float max2(float a, float b) {
+  return __builtin_amdgcn_fmed3f(a, b, __builtin_inff());
 }
 __device__ __forceinline__ float half_max(float x) {   // over the lanes of equal m
   uint32_t lo, hi;
@@ -671,89 +675,118 @@ __device__ __forceinline__ float load_row32(const KvAttn& A, const uint16_t* src
   return __builtin_ldexpf(__builtin_fabsf(A.scale) * kLog2e, e);
 }
 
+// K pages in LDS: with three a page takes one barrier, with two (all that 256 channels leave room
+// for) it takes two.
+template <int D>
+constexpr int kPagesK = D == 256 ? 2 : 3;
+
 template <int D>
 struct PromptLds {
-  _Float16 k[2][kPage][D + 8];       // rows in the order of tile_row; 16 bytes of padding a row
-  _Float16 v[2][D][kPage + 8];       // keep the lanes' 16-byte reads off one another's banks
-};
+  _Float16 k[kPagesK<D>][kPage][D + 8];   // rows in the order of tile_row; 16 bytes of padding a
+  _Float16 v[2][D][kPage + 8];            // row keep the lanes' 16-byte reads off one another's
+};                                        // banks
 
-// Codes of one page on their way to LDS: 16 bytes a thread and step.
-template <int D>
+// Codes of one page's K or V on their way to LDS: 16 bytes a thread and step.
+template <int D, int NT>
+constexpr int kPieces = (4 * D + NT - 1) / NT;         // of the page's 4 D, a thread
+template <int D, int NT>
+constexpr bool kWhole = 4 * D % NT == 0;
+template <int D, int NT>
 struct PageRegs {
-  uint4v k[D / 64], v[D / 64];
+  uint4v c[kPieces<D, NT>];
 };
 
-template <int D>
-__device__ __forceinline__ void page_fetch(const KvPool& pool, int64_t at, PageRegs<D>& r) {
-  const uint4v* k = reinterpret_cast<const uint4v*>(pool.k + at * (kPage * D));
-  const uint4v* v = reinterpret_cast<const uint4v*>(pool.v + at * (kPage * D));
+template <int D, int NT>
+__device__ __forceinline__ void page_fetch(const int8_t* codes, PageRegs<D, NT>& r) {
+  const uint4v* p = reinterpret_cast<const uint4v*>(codes);
 #pragma unroll
-  for (int i = 0; i < D / 64; ++i) {
-    r.k[i] = k[i * 256 + threadIdx.x];
-    r.v[i] = v[i * 256 + threadIdx.x];
-  }
+  for (int i = 0; i < kPieces<D, NT>; ++i)
+    if (kWhole<D, NT> || threadIdx.x < 4 * D) r.c[i] = p[i * NT + threadIdx.x];
 }
 
-template <int D>
-__device__ __forceinline__ void page_widen(const PageRegs<D>& r, PromptLds<D>& L, int buf) {
+template <int D, int NT>
+__device__ __forceinline__ void widen_k(const PageRegs<D, NT>& r, _Float16 (*k)[D + 8]) {
 #pragma unroll
-  for (int i = 0; i < D / 64; ++i) {
-    const int n = i * 256 + threadIdx.x;
+  for (int i = 0; i < kPieces<D, NT>; ++i) {
+    const int n = i * NT + threadIdx.x;
+    if (!kWhole<D, NT> && n >= 4 * D) break;
     const int t = n / (D / 16), d = n % (D / 16) * 16;
-    _Float16* k = &L.k[buf][(t & 32) + tile_row(t & 31)][d];
-    *reinterpret_cast<half8*>(k) = kv_widen8(r.k[i][0], r.k[i][1]);
-    *reinterpret_cast<half8*>(k + 8) = kv_widen8(r.k[i][2], r.k[i][3]);
-    _Float16* v = &L.v[buf][n >> 2][(n & 3) * 16];
-    *reinterpret_cast<half8*>(v) = kv_widen8(r.v[i][0], r.v[i][1]);
-    *reinterpret_cast<half8*>(v + 8) = kv_widen8(r.v[i][2], r.v[i][3]);
+    _Float16* to = &k[(t & 32) + tile_row(t & 31)][d];
+    *reinterpret_cast<half8*>(to) = kv_widen8(r.c[i][0], r.c[i][1]);
+    *reinterpret_cast<half8*>(to + 8) = kv_widen8(r.c[i][2], r.c[i][3]);
   }
 }
 
-// Workgroup = (sequence, KV head, tile of 128 NB rows, split of the pages). `it0`: where this
+template <int D, int NT>
+__device__ __forceinline__ void widen_v(const PageRegs<D, NT>& r, _Float16 (*v)[kPage + 8]) {
+#pragma unroll
+  for (int i = 0; i < kPieces<D, NT>; ++i) {
+    const int n = i * NT + threadIdx.x;
+    if (!kWhole<D, NT> && n >= 4 * D) break;
+    _Float16* to = &v[n >> 2][(n & 3) * 16];
+    *reinterpret_cast<half8*>(to) = kv_widen8(r.c[i][0], r.c[i][1]);
+    *reinterpret_cast<half8*>(to + 8) = kv_widen8(r.c[i][2], r.c[i][3]);
+  }
+}
+
+// S^T of 32 tokens (rows k of the K tile) against the wave's rows.
+template <int D>
+__device__ __forceinline__ float16v tile_scores(const _Float16 (*k)[D + 8],
+                                                const half8 (&q)[D / 16]) {
+  const int m = threadIdx.x & 31, half = (threadIdx.x & 63) >> 5;
+  float16v x;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) x[e] = 0.0f;
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) {
+    const half8 a = *reinterpret_cast<const half8*>(&k[m][16 * s + 8 * half]);
+    x = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, q[s], x, 0, 0, 0);
+  }
+  return x;
+}
+
+// Waves of a workgroup: with 256 channels a wave's registers leave room for one on a SIMD.
+template <int D>
+constexpr int kPromptWaves = D == 256 ? 4 : 8;
+
+// Workgroup = (sequence, KV head, tile of 32 rows a wave, split of the pages). `it0`: where this
 // launch starts (see in_launches).
-template <int D, bool BF16, int NB>
-__global__ __launch_bounds__(256, 1) void prompt_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles,
-                                                        int splits, int64_t it0, float* part,
-                                                        float* lse) {
+template <int D, bool BF16>
+__global__ __launch_bounds__(64 * kPromptWaves<D>, kPromptWaves<D> / 4)
+void prompt_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles, int splits, int64_t it0,
+                   float* part, float* lse) {
+  constexpr int NT = 64 * kPromptWaves<D>;
   __shared__ PromptLds<D> L;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 31, half = lane >> 5;
   const int64_t it = it0 + blockIdx.x;
-  const int h = (int)(it % pool.H);
+  const int h = uniform((int)(it % pool.H));
   int64_t r = it / pool.H;
-  const int split = (int)(r % splits);
+  const int split = uniform((int)(r % splits));
   r /= splits;
-  const int tile = tiles - 1 - (int)(r % tiles);       // the tiles that see most go first
-  const int seq = (int)(r / tiles);
-  const RowsOf R = rows_of(S, A, seq);
-  const int rows = R.nq * A.group, base = (tile * 4 + wave) * (32 * NB);
+  const int tile = uniform(tiles - 1 - (int)(r % tiles));   // the tiles that see most go first
+  const int seq = uniform((int)(r / tiles));
+  RowsOf R = rows_of(S, A, seq);
+  R.len = uniform(R.len);
+  R.q_len = uniform(R.q_len);
+  const int rows = R.nq * A.group, row = (tile * kPromptWaves<D> + wave) * 32 + m;
 
-  half8 q[NB][D / 16];
-  float unit[NB];
-  int visible[NB], low = 0x7fffffff, high = 0;
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    const int row = base + 32 * b + m;
-    const int i = row / A.group, head = h * A.group + row % A.group;
-    const int see = row < rows ? visible_of(R, i) : 0;
-    const uint16_t* src = static_cast<const uint16_t*>(A.q.p) + R.seq * A.q.seq +
-                          (int64_t)i * A.q.tok + (int64_t)head * A.q.head;
-    unit[b] = load_row32<D, BF16>(A, src, see > 0, q[b]);
-    high = see > high ? see : high;
-    // a row that sees nothing is not masked page by page: it is written as empty at the end
-    visible[b] = see > 0 ? see : 0x7fffffff;
-    low = visible[b] < low ? visible[b] : low;
-  }
+  half8 q[D / 16];
+  // a row that sees nothing is not masked tile by tile: it is written as empty at the end
+  const int i_row = row / A.group, head = h * A.group + row % A.group;
+  const int see = row < rows ? visible_of(R, i_row) : 0;
+  const int visible = see > 0 ? see : 0x7fffffff;
+  const float unit = load_row32<D, BF16>(
+      A, static_cast<const uint16_t*>(A.q.p) + R.seq * A.q.seq + (int64_t)i_row * A.q.tok +
+             (int64_t)head * A.q.head, see > 0, q);
+  int low = visible;                                   // what every row of the wave sees
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    int v = __shfl_xor(high, o);
-    high = v > high ? v : high;
-    v = __shfl_xor(low, o);
+    const int v = __shfl_xor(low, o);
     low = v < low ? v : low;
   }
-  high = __builtin_amdgcn_readfirstlane(high);
   low = __builtin_amdgcn_readfirstlane(low);
   // the workgroup's pages: up to what its last live row sees
-  int last = (tile + 1) * (128 * NB) - 1;
+  int last = (tile + 1) * (32 * kPromptWaves<D>) - 1;
   last = last < rows ? last : rows - 1;
   int top_token = last / A.group;
   if (top_token >= R.q_len) top_token = R.q_len - 1;
@@ -762,161 +795,213 @@ __global__ __launch_bounds__(256, 1) void prompt_kernel(KvPool pool, KvSeqs S, K
   const int per = (n + splits - 1) / splits;
   const int j0 = split * per, j1 = j0 + per < n ? j0 + per : n;
 
-  float16v o[NB][D / 32];
-  float ref[NB], ref_l[NB], l[NB];
+  float16v o[D / 32];
 #pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    ref[b] = ref_l[b] = -1e30f;
-    l[b] = 0.0f;
+  for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) o[b][dt][e] = 0.0f;
-  }
+    for (int e = 0; e < 16; ++e) o[dt][e] = 0.0f;
+  float ref = -1e30f, l = 0.0f;      // O and l in units of 2^(ref - kLift)
+  float ref0 = -1e30f, l0 = 0.0f;    // l of the pages without V, in units of 2^ref0
   float v_top = 0.0f;
 
-  PageRegs<D> regs;
-  float ks = 0.0f, vs = 0.0f;
-  int page = j0 < j1 ? kv_page(S, pool.P, seq, j0) : -1;
-  if (page >= 0) {
-    const int64_t at = (int64_t)page * pool.H + h;
-    page_fetch<D>(pool, at, regs);
-    ks = pool.ks[at];
-    vs = pool.vs[at];
-    page_widen<D>(regs, L, j0 & 1);
-  }
-  for (int j = j0; j < j1; ++j) {
-    const int next = j + 1 < j1 ? kv_page(S, pool.P, seq, j + 1) : -1;
-    float ks_n = 0.0f, vs_n = 0.0f;
-    if (next >= 0) {
-      const int64_t at = (int64_t)next * pool.H + h;
-      page_fetch<D>(pool, at, regs);
-      ks_n = pool.ks[at];
-      vs_n = pool.vs[at];
+  // The pages in turn, those that do not exist left out.
+  int jn = j0;
+  const auto next_page = [&](int& j) -> int64_t {
+    while (jn < j1) {
+      j = jn++;
+      const int page = uniform(kv_page(S, pool.P, seq, j));
+      if (page >= 0) return (int64_t)page * pool.H + h;
     }
-    __syncthreads();                 // page j is in LDS, and nobody reads page j - 1 any more
-    const int buf = j & 1, pos0 = j * kPage;
-    if (page >= 0 && pos0 < high) {
-      float16v x[NB][2];
+    return -1;
+  };
+  // One tile of 32 tokens: its scores x become weights and go into O, while the scores of the
+  // tile after it (the return value) are computed from `next` and `put` widens codes for later
+  // ones. k, v: the tile's own operands.
+  const auto tile_step = [&](float16v x, const _Float16 (*k)[D + 8], const _Float16 (*next)[D + 8],
+                             const _Float16 (*v)[kPage + 8], int pos0, float ks, float vs,
+                             auto put) -> float16v {
+    const auto mask = [&](float16v& z) {               // where the tile ends beyond some row
+      if (pos0 + 32 > low) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) x[b][u][e] = 0.0f;
-#pragma unroll
-        for (int s = 0; s < D / 16; ++s) {
-          const half8 a =
-              *reinterpret_cast<const half8*>(&L.k[buf][32 * u + m][16 * s + 8 * half]);
-#pragma unroll
-          for (int b = 0; b < NB; ++b)
-            x[b][u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, q[b][s], x[b][u], 0, 0, 0);
-        }
+        for (int e = 0; e < 16; ++e)
+          if (pos0 + 16 * half + e >= visible) z[e] = kNegInf;
       }
-      if (pos0 + kPage > low) {      // the page ends beyond what some row sees
+    };
+    mask(x);
+    // never 0, so that what is masked stays -inf (products of codes and queries are < 2^31)
+    const float f = fmaxf(unit * ks, 0x1p-120f);
+    // a V scale 2^60 below an earlier one (or 0) adds nothing to O, only its weights to a sum of
+    // their own: they must not move the reference that the others are rounded by
+    const bool with_v = vs > v_top * 0x1p-60f;
+    const float lv = with_v ? __builtin_amdgcn_logf(vs) + (float)kLift : 0.0f;
+    const float c = with_v ? lv - ref : kNegInf;
+    const float16v y = tile_scores<D>(next, q);
+    float sum = 0.0f;
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+    for (int e = 0; e < 16; ++e) {
+      x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], f, c));
+      sum += x[e];
+    }
+    // requested before the weights are looked at, so that the products need not wait (and again
+    // behind the rare case, which has no registers for them)
+    half8 a[D / 32][2];
+    const auto values = [&] {
 #pragma unroll
-          for (int u = 0; u < 2; ++u)
+      for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
-              if (pos0 + 32 * u + 16 * half + e >= visible[b]) x[b][u][e] = kNegInf;
-      }
-      // a V scale 2^60 below an earlier one (or 0) adds nothing to O, only its weights to l
-      v_top = fmaxf(v_top, vs);
-      const bool with_v = vs > v_top * 0x1p-60f;
-      const float lv = with_v ? __builtin_amdgcn_logf(vs) : 0.0f;
-      half8 p[NB][4];
+        for (int e = 0; e < 2; ++e)
+          a[dt][e] = *reinterpret_cast<const half8*>(&v[32 * dt + m][16 * half + 8 * e]);
+    };
+    if (__builtin_expect(__any(!(sum <= kMost)) || !with_v, 0)) {
+      float16v z = tile_scores<D>(k, q);
+      mask(z);
+      float t = z[0];
 #pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        // never 0, so that what is masked stays -inf (products of codes and queries are < 2^31)
-        const float f = fmaxf(unit[b] * ks, 0x1p-120f);
-        float t = kNegInf;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) t = max3(t, x[b][0][e], x[b][1][e]);
-        t = half_max(t) * f;
-        if (with_v && __any(t + lv > ref[b] + (float)kSlack)) {
-          const float now = t + lv > ref[b] ? t + lv : ref[b];
-          const float a = __builtin_amdgcn_exp2f(ref[b] - now);
-          ref[b] = now;
-#pragma unroll
-          for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) o[b][dt][e] *= a;
-        }
-        const float top_l = t > ref_l[b] ? t : ref_l[b];
-        const float c = with_v ? lv + (float)kLift - ref[b] : -top_l;
-        float sum = 0.0f;
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][u][e], f, c));
-            sum += w;
-            p[b][2 * u + (e >> 3)][e & 7] = (_Float16)w;
-          }
-        if (with_v) sum *= __builtin_amdgcn_exp2f(-top_l - c);
-        l[b] = __builtin_fmaf(l[b], __builtin_amdgcn_exp2f(ref_l[b] - top_l), sum);
-        ref_l[b] = top_l;
-      }
+      for (int e = 1; e < 16; ++e) t = max2(t, z[e]);
+      t = half_max(t) * f;
       if (with_v) {
+        const float now = fmaxf(ref, t + lv - (float)kLift);
+        const float g = __builtin_amdgcn_exp2f(ref - now);
+        ref = now;
+        l *= g;
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const half8 a = *reinterpret_cast<const half8*>(
-                &L.v[buf][32 * dt + m][32 * (e >> 1) + 16 * half + 8 * (e & 1)]);
+          for (int e = 0; e < 16; ++e) o[dt][e] *= g;
+        sum = 0.0f;
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
-              o[b][dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, p[b][e], o[b][dt], 0, 0, 0);
-          }
+        for (int e = 0; e < 16; ++e) {
+          x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[e], f, lv - ref));
+          sum += x[e];
+        }
+      } else {
+        const float now = fmaxf(ref0, t);
+        l0 *= __builtin_amdgcn_exp2f(ref0 - now);
+        ref0 = now;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          l0 += __builtin_amdgcn_exp2f(__builtin_fmaf(z[e], f, -now));
       }
     }
-    if (next >= 0) page_widen<D>(regs, L, (j + 1) & 1);
-    page = next;
+    values();
+    l = __builtin_fmaf(sum, with_v ? 1.0f / vs : 0.0f, l);
+    half8 p[2];
+#pragma unroll
+    for (int e = 0; e < 16; e += 2) {
+      const half2v h2 = __builtin_convertvector((float2v{x[e], x[e + 1]}), half2v);
+      p[e >> 3][e & 7] = h2[0];
+      p[e >> 3][(e & 7) + 1] = h2[1];
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[dt][e], p[e], o[dt], 0, 0, 0);
+    put();
+    return y;
+  };
+
+  // What page i's turn does besides its own two tiles: K of page i + kAhead is widened into LDS
+  // beside the first and V of page i + 1 beside the second, and the registers they leave take the
+  // codes of the page after. With kAhead = 2 the first scores of page i + 1, which come with the
+  // second tile, find K there since the last barrier; with 1 they need one of their own. (Behind
+  // the last page registers, buffers and scores are stale, and nobody uses them.)
+  constexpr int kAhead = kPagesK<D> - 1;
+  PageRegs<D, NT> kr, vr;
+  float16v x;
+  int pos[4];
+  int64_t at[4];                     // this page and the next three
+  float ks = 0.0f, vs = 0.0f, ks_n = 0.0f, vs_n = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    pos[i] = 0;
+    at[i] = i && at[i ? i - 1 : 0] < 0 ? -1 : next_page(pos[i]);
+  }
+  const auto fetch_k = [&](int64_t a) {
+    if (a >= 0) page_fetch<D, NT>(pool.k + a * (kPage * D), kr);
+  };
+  const auto fetch_v = [&](int64_t a) {
+    if (a < 0) return;
+    page_fetch<D, NT>(pool.v + a * (kPage * D), vr);
+    ks_n = pool.ks[a];
+    vs_n = pool.vs[a];
+  };
+  if (at[0] >= 0) {
+    fetch_k(at[0]);
+    fetch_v(at[0]);
     ks = ks_n;
     vs = vs_n;
+    widen_k<D, NT>(kr, L.k[0]);
+    widen_v<D, NT>(vr, L.v[0]);
+    fetch_k(at[1]);
+    fetch_v(at[1]);
+    if (kAhead == 2 && at[1] >= 0) {
+      widen_k<D, NT>(kr, L.k[1]);
+      fetch_k(at[2]);
+    }
+    __syncthreads();
+    x = tile_scores<D>(L.k[0], q);
+  }
+  int k0 = 0, k1 = 1;                // K buffers of this page and the next
+  for (int buf = 0; at[0] >= 0; buf ^= 1) {
+    v_top = fmaxf(v_top, vs);
+    const int k2 = kAhead == 2 ? 3 - k0 - k1 : k0;
+    const int pos0 = pos[0] * kPage;
+    x = tile_step(x, L.k[k0], L.k[k0] + 32, L.v[buf], pos0, ks, vs,
+                  [&] { widen_k<D, NT>(kr, L.k[kAhead == 2 ? k2 : k1]); });
+    fetch_k(at[kAhead + 1]);
+    if (kAhead == 1) __syncthreads();
+    x = tile_step(x, L.k[k0] + 32, L.k[k1],
+                  reinterpret_cast<const _Float16 (*)[kPage + 8]>(&L.v[buf][0][32]), pos0 + 32, ks,
+                  vs, [&] { widen_v<D, NT>(vr, L.v[buf ^ 1]); });
+    ks = ks_n;
+    vs = vs_n;
+    fetch_v(at[2]);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      at[i] = at[i + 1];
+      pos[i] = pos[i + 1];
+    }
+    at[3] = at[2] < 0 ? -1 : next_page(pos[3]);
+    k0 = k1;
+    k1 = k2;
+    __syncthreads();
   }
 
   // lane (m, half) has row m, channels 32 dt + 8 a + 4 half + 0 .. 3
+  l = half_sum(l);
+  l0 = half_sum(l0);
+  if (row >= rows) return;
+  // both sums to one reference, and O with them
+  ref -= (float)kLift;
+  const bool some = l > 0.0f || l != l, some0 = l0 > 0.0f || l0 != l0;
+  const bool empty = see <= 0 || !(some || some0);
+  const float top = fmaxf(some ? ref : -1e30f, some0 ? ref0 : -1e30f);
+  const float to_top = some ? __builtin_amdgcn_exp2f(ref - top) : 0.0f;
+  const float sum = l * to_top + (some0 ? l0 * __builtin_amdgcn_exp2f(ref0 - top) : 0.0f);
+  const float g = empty ? 0.0f : splits > 1 ? to_top : to_top / sum;
+  const int64_t u16 = ((int64_t)seq * pool.H + h) * ((rows + 15) / 16) + row / 16;
+  float* dst = splits > 1 ? part + (u16 * splits + split) * kPart<D> : nullptr;
 #pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    const int row = base + 32 * b + m;
-    const float sum = half_sum(l[b]);
-    if (row >= rows) continue;
-    const bool empty = visible[b] == 0x7fffffff || !(sum > 0.0f || sum != sum);
-    const float unit_o = __builtin_amdgcn_exp2f(ref[b] - (float)kLift - ref_l[b]);
-    if (splits > 1) {
-      const int64_t u16 = ((int64_t)seq * pool.H + h) * ((rows + 15) / 16) + row / 16;
-      float* dst = part + (u16 * splits + split) * kPart<D>;
+  for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt)
+    for (int a = 0; a < 4; ++a) {
+      float4v w;
 #pragma unroll
-        for (int a = 0; a < 4; ++a) {
-          float4v w;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) w[e] = empty ? 0.0f : o[b][dt][4 * a + e] * unit_o;
-          *reinterpret_cast<float4v*>(dst + (row & 15) * D + 32 * dt + 8 * a + 4 * half) = w;
-        }
-      if (half == 0) {
-        dst[16 * D + 2 * (row & 15)] = empty ? kNegInf : ref_l[b];
-        dst[16 * D + 2 * (row & 15) + 1] = empty ? 0.0f : sum;
-      }
-    } else {
-      const float f = empty ? 0.0f : unit_o / sum;
-#pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-        for (int a = 0; a < 4; ++a) {
-          float w[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) w[e] = empty ? 0.0f : o[b][dt][4 * a + e] * f;
-          put_out<D, BF16>(A, R, h, row, 32 * dt + 8 * a + 4 * half, w, 4);
-        }
-      if (lse && half == 0)
-        lse[lse_at(A, R, pool.H, h, row)] =
-            empty ? kNegInf : (ref_l[b] + __builtin_amdgcn_logf(sum)) * kLn2;
+      for (int e = 0; e < 4; ++e) w[e] = empty ? 0.0f : o[dt][4 * a + e] * g;
+      const int d = 32 * dt + 8 * a + 4 * half;
+      if (dst)
+        *reinterpret_cast<float4v*>(dst + (row & 15) * D + d) = w;
+      else
+        put_out<D, BF16>(A, R, h, row, d, reinterpret_cast<const float*>(&w), 4);
     }
+  if (half != 0) return;
+  if (dst) {
+    dst[16 * D + 2 * (row & 15)] = empty ? kNegInf : top;
+    dst[16 * D + 2 * (row & 15) + 1] = empty ? 0.0f : sum;
+  } else if (lse) {
+    lse[lse_at(A, R, pool.H, h, row)] =
+        empty ? kNegInf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
   }
 }
 
@@ -1108,12 +1193,12 @@ void in_launches(int64_t items, Launch launch) {
     launch(it0, (unsigned)(items - it0 < kMost ? items - it0 : kMost));
 }
 
-template <int D, bool BF16, int NB>
+template <int D, bool BF16>
 void prompt_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, const KvAttnPlan& P,
               float* part, float* lse, hipStream_t st) {
   in_launches((int64_t)S.n * pool.H * P.big * P.splits, [&](int64_t it0, unsigned n) {
-    hipLaunchKernelGGL((prompt_kernel<D, BF16, NB>), dim3(n), dim3(256), 0, st, pool, S, A, P.big,
-                       P.splits, it0, part, lse);
+    hipLaunchKernelGGL((prompt_kernel<D, BF16>), dim3(n), dim3(64 * kPromptWaves<D>), 0, st, pool,
+                       S, A, P.big, P.splits, it0, part, lse);
   });
 }
 
@@ -1137,10 +1222,8 @@ hipError_t attend_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, void* 
   const int np = (int)(((int64_t)A.max_len + kPage - 1) / kPage);
   const int vseqs = A.picks ? S.n * A.nq : S.n;
   const int64_t units = (int64_t)vseqs * pool.H * P.tiles;
-  if (P.blocks == 1)
-    prompt_d<D, BF16, 1>(pool, S, A, P, part, lse, st);
-  else if (P.blocks == 2)
-    prompt_d<D, BF16, D == 256 ? 1 : 2>(pool, S, A, P, part, lse, st);
+  if (P.big)
+    prompt_d<D, BF16>(pool, S, A, P, part, lse, st);
   else
     hipLaunchKernelGGL((attend_kernel<D, BF16>), dim3(grid_of(units * P.splits)), dim3(256), 0,
                        st, pool, S, A, P.tiles, P.splits, units * P.splits, part,
@@ -1176,11 +1259,11 @@ KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& S, const KvAttn& A, int
   const int64_t pages = A.picks ? A.n_picks : ((int64_t)A.max_len + kPage - 1) / kPage;
   // From three 16-row tiles on, the rows share the pages through LDS (prompt_kernel); every query
   // token with pages of its own is a tile or more to itself.
-  P.big = P.blocks = 0;
+  P.big = 0;
   int64_t s, most;
   if (P.tiles > 2 && !A.picks) {
-    P.blocks = D == 256 || rows <= 128 ? 1 : 2;
-    P.big = (int)((rows + 128 * P.blocks - 1) / (128 * P.blocks));
+    const int per = D == 256 ? 32 * kPromptWaves<256> : 32 * kPromptWaves<128>;
+    P.big = (int)((rows + per - 1) / per);
     const int64_t groups = vseqs * pool.H * P.big;
     s = (256 + groups - 1) / groups;
     most = pages / 4;

@@ -29,6 +29,22 @@ __device__ __forceinline__ float quad_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
+// N sums over N neighbouring lanes at once: afterwards lane i of the N holds the sum of v[i].
+template <int N, int LEN>
+__device__ __forceinline__ float sum_across(float (&v)[LEN]) {
+  if constexpr (N > 1) {
+    const bool upper = threadIdx.x & (N / 2);
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      const float mine = upper ? v[i + N / 2] : v[i], other = upper ? v[i] : v[i + N / 2];
+      v[i] = mine + __shfl_xor(other, N / 2);
+    }
+    return sum_across<N / 2>(v);
+  } else {
+    return v[0];
+  }
+}
+
 // Eight row elements; `wide`: rows lie on 16-byte boundaries.
 __device__ __forceinline__ uint4v load8(const uint16_t* p, bool wide) {
   if (wide) return *reinterpret_cast<const uint4v*>(p);
@@ -95,9 +111,17 @@ __device__ __forceinline__ void load_q(const KvAttn& A, const RowsOf& R, int h, 
                         (int64_t)i * A.q.tok + (int64_t)head * A.q.head;
   uint16_t u[D / 32][8];
 #pragma unroll
-  for (int s = 0; s < D / 32; ++s)
-    *reinterpret_cast<uint4v*>(u[s]) =
-        live ? load8(src + (s >> 1) * 64 + g * 16 + (s & 1) * 8, A.wide_q) : uint4v{0, 0, 0, 0};
+  for (int s = 0; s < D / 32; ++s) *reinterpret_cast<uint4v*>(u[s]) = uint4v{0, 0, 0, 0};
+  if (live && A.wide_q) {
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s)
+      *reinterpret_cast<uint4v*>(u[s]) =
+          *reinterpret_cast<const uint4v*>(src + (s >> 1) * 64 + g * 16 + (s & 1) * 8);
+  } else if (live) {
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s)
+      *reinterpret_cast<uint4v*>(u[s]) = load8(src + (s >> 1) * 64 + g * 16 + (s & 1) * 8, false);
+  }
   int e = 0;
   if (BF16) {
     uint32_t top = 0;
@@ -541,14 +565,7 @@ __global__ __launch_bounds__(256) void mass_kernel(KvPool pool, KvSeqs S, KvAttn
         if (j * kPage + 16 * g + e < Q.visible)
           sum[e] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], f, -z));
     }
-    float mine = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      float t = sum[e];
-#pragma unroll
-      for (int o = 1; o < 16; o <<= 1) t += __shfl_xor(t, o);
-      mine = m == e ? t : mine;
-    }
+    const float mine = sum_across<16>(sum);
     const int t = 16 * g + m;
     if (j * kPage + t < R.len) {
       const int64_t at = b * kPage + t;
@@ -644,9 +661,17 @@ __device__ __forceinline__ float load_row32(const KvAttn& A, const uint16_t* src
   const int half = (threadIdx.x & 63) >> 5;
   uint16_t u[D / 16][8];
 #pragma unroll
-  for (int s = 0; s < D / 16; ++s)
-    *reinterpret_cast<uint4v*>(u[s]) =
-        live ? load8(src + 16 * s + 8 * half, A.wide_q) : uint4v{0, 0, 0, 0};
+  for (int s = 0; s < D / 16; ++s) *reinterpret_cast<uint4v*>(u[s]) = uint4v{0, 0, 0, 0};
+  if (live && A.wide_q) {
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+      *reinterpret_cast<uint4v*>(u[s]) =
+          *reinterpret_cast<const uint4v*>(src + 16 * s + 8 * half);
+  } else if (live) {
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+      *reinterpret_cast<uint4v*>(u[s]) = load8(src + 16 * s + 8 * half, false);
+  }
   int e = 0;
   const uint16_t flip = A.scale < 0.0f ? 0x8000u : 0;
   if (BF16) {
@@ -1007,177 +1032,168 @@ void prompt_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles, int splits, int64
 
 // ---- weights of many rows -------------------------------------------------------------------
 // The same sum as mass_kernel where there are many rows: a wave keeps one page's K as operands in
-// registers and adds up its 64 tokens' weights row tile by row tile; the queries come through LDS,
-// shared by the PW pages of the workgroup. The eight waves are PW pages x 8 / PW shares of the row
-// tiles (every 8 / PW-th), whose sums meet in LDS at the end in a fixed order.
-template <int D, int RG>
-struct MassLds {
-  _Float16 q[2][RG * 32][D + 8];
-  float unit[2][RG * 32], z[2][RG * 32];       // factor of S, log2 of the row's sum
-  int visible[2][RG * 32];                     // 0: no such row, or an empty one
-  float sum[8][kPage];
-};
+// registers (in the queries' own type: the codes are exact in either) and adds up its 64 tokens'
+// weights row tile by row tile. A tile's queries are read as whole rows, since a load whose lanes
+// lie in different rows takes a cache access for each of them, and turned through LDS of the
+// wave's own, without barriers: the two waves of a SIMD drift apart, and one's products run beside
+// the other's exponentials. The waves of a workgroup are pages x `shares` shares of the row tiles
+// (every shares-th), whose sums meet in LDS at the end in a fixed order.
+typedef __bf16 bhalf8 __attribute__((ext_vector_type(8)));
 
-template <int D, bool BF16, int PW>
-__global__ __launch_bounds__(512, 1) void mass_rows_kernel(KvPool pool, KvSeqs S, KvAttn A, int np,
-                                                           int64_t it0, const float* lse) {
-  constexpr int RG = 8 / PW, LR = D / 8;       // lanes that load one row
-  constexpr int CH = RG * 32 * LR / 512;       // 16-byte pieces a thread loads a step
-  __shared__ MassLds<D, RG> L;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 31, half = lane >> 5;
-  const int share = wave / PW;
+// Eight codes in the queries' type.
+template <bool BF16>
+__device__ __forceinline__ uint4v widen_as(uint32_t a, uint32_t b) {
+  if (!BF16) return __builtin_bit_cast(uint4v, kv_widen8(a, b));
+  uint4v w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t c = i < 2 ? a : b;
+    const uint32_t lo = __builtin_bit_cast(uint32_t, (float)(int8_t)(c >> (16 * (i & 1))));
+    const uint32_t hi = __builtin_bit_cast(uint32_t, (float)(int8_t)(c >> (16 * (i & 1) + 8)));
+    w[i] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);   // the upper halves: exact for 8 bits
+  }
+  return w;
+}
+
+template <bool BF16>
+__device__ __forceinline__ float16v mfma32(uint4v a, uint4v b, float16v c) {
+  if (BF16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bhalf8, a),
+                                                   __builtin_bit_cast(bhalf8, b), c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a),
+                                                __builtin_bit_cast(half8, b), c, 0, 0, 0);
+}
+
+template <int D, bool BF16>
+__global__ __launch_bounds__(64 * kPromptWaves<D>, kPromptWaves<D> / 4)
+void mass_rows_kernel(KvPool pool, KvSeqs S, KvAttn A, int np, int shares, int64_t it0,
+                      const float* lse) {
+  constexpr int LR = D / 8, RC = 64 / LR;      // lanes a row, rows a load
+  __shared__ __align__(16) uint16_t rows_of_wave[kPromptWaves<D>][32][D + 8];
+  __shared__ float sums[kPromptWaves<D>][kPage];
+  const int lane = threadIdx.x & 63, m = lane & 31, half = lane >> 5;
+  const int wave = uniform(threadIdx.x >> 6), pages = kPromptWaves<D> / shares;
+  const int share = wave / pages;
   const int64_t it = it0 + blockIdx.x;
-  const int h = (int)(it % pool.H);
+  const int h = uniform((int)(it % pool.H));
   const int64_t r0 = it / pool.H;
-  const int groups = (np + PW - 1) / PW;
-  const int j0 = (int)(r0 % groups) * PW, seq = (int)(r0 / groups);
-  const int j = j0 + wave % PW, pos0 = j * kPage;
+  const int groups = (np + pages - 1) / pages;
+  const int j = uniform((int)(r0 % groups) * pages + wave % pages), seq = uniform((int)(r0 / groups));
+  const int pos0 = j * kPage;
   const RowsOf R = rows_of(S, A, seq);
-  if (j0 * (int64_t)kPage >= R.len) return;
-  const int page = j < np && pos0 < R.len ? kv_page(S, pool.P, seq, j) : -1;
+  const int page = j < np && pos0 < R.len ? uniform(kv_page(S, pool.P, seq, j)) : -1;
   const int64_t at = (int64_t)page * pool.H + h;
-  half8 k[2][D / 16];
-  float ks = 0.0f;
+  float sum[32];                     // 16 results of each 32-token tile
+#pragma unroll
+  for (int e = 0; e < 32; ++e) sum[e] = 0.0f;
   if (page >= 0) {
-    ks = pool.ks[at];
+    const float f = A.scale * kLog2e * pool.ks[at];
+    uint4v k[2][D / 16];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int8_t* row = pool.k + at * (kPage * D) + (32 * u + m) * D + 16 * half;
 #pragma unroll
       for (int s = 0; s < D / 32; ++s) {
         const uint4v c = *reinterpret_cast<const uint4v*>(row + 32 * s);
-        k[u][2 * s] = kv_widen8(c[0], c[1]);
-        k[u][2 * s + 1] = kv_widen8(c[2], c[3]);
+        k[u][2 * s] = widen_as<BF16>(c[0], c[1]);
+        k[u][2 * s + 1] = widen_as<BF16>(c[2], c[3]);
       }
     }
-  }
-  float sum[2][16];
-#pragma unroll
-  for (int u = 0; u < 2; ++u)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) sum[u][e] = 0.0f;
-
-  // the first row that sees the workgroup's first page
-  const int rows = (R.q_len > 0 ? R.q_len : 0) * A.group;
-  const int64_t first = (int64_t)j0 * kPage - R.len + R.q_len;   // first query token that does
-  const int step = RG * 32;
-  int base = first > 0 ? (int)(first * A.group) / step * step : 0;
-
-  uint4v u[CH];
-  float z_n = 0.0f;
-  const auto fetch = [&](int b0) {
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      const int row = b0 + (c * 512 + tid) / LR, d = tid % LR * 8;
-      u[c] = uint4v{0, 0, 0, 0};
-      if (row < rows) {
-        const uint16_t* src = static_cast<const uint16_t*>(A.q.p) + R.seq * A.q.seq +
-                              (int64_t)(row / A.group) * A.q.tok +
-                              (int64_t)(h * A.group + row % A.group) * A.q.head + d;
-        u[c] = load8(src, A.wide_q);
+    const int rows = (R.q_len > 0 ? R.q_len : 0) * A.group;
+    // the tile of the first query token that sees the page
+    const int64_t first = (int64_t)pos0 - R.len + R.q_len;
+    int tile = first > 0 ? uniform((int)(first * A.group / 32)) : 0;
+    tile += (share - tile % shares + shares) % shares;
+    // Rows as (query token, place in the group), moved on without divisions: the lane's first row
+    // to load (i, g), RC further ones apart, and the row m whose results it gets (im, gm).
+    struct Place {
+      int i, g;
+      __device__ __forceinline__ void move(int di, int dg, int group) {
+        i += di;
+        g += dg;
+        if (g >= group) {
+          g -= group;
+          ++i;
+        }
       }
-    }
-    if (tid < step) {
-      const int row = b0 + tid;
-      z_n = row < rows ? lse[lse_at(A, R, pool.H, h, row)] * kLog2e : 0.0f;
-    }
-  };
-  const auto put = [&](int b0, int buf) {
+    };
+    const auto place = [&](int row) { return Place{row / A.group, row % A.group}; };
+    const int step = 32 * shares, step_i = uniform(step / A.group), step_g = step - step_i * A.group;
+    const int near_i = uniform(RC / A.group), near_g = RC - near_i * A.group;
+    Place from = place(32 * tile + lane / LR), own = place(32 * tile + m);
+    const uint16_t* const q0 = static_cast<const uint16_t*>(A.q.p) + R.seq * A.q.seq +
+                               (int64_t)h * A.group * A.q.head + lane % LR * 8;
+    const float* const lse0 = lse + (int64_t)R.seq * A.nq * pool.H * A.group + h * A.group;
+    constexpr int CH = 32 / RC;
+    uint4v u[CH];
+    float z;
+    int see;
+    const auto fetch = [&] {
+      const uint16_t* src[CH];
+      Place p = from;
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      const int slot = (c * 512 + tid) / LR, d = tid % LR * 8;
-      half8 q;
-      int e = 0;
-      if (BF16) {
-        uint32_t top = 0;
+      for (int c = 0; c < CH; ++c) {
+        // (behind the last row some row, whose results are not used)
+        src[c] = q0 + (int64_t)(p.i < R.q_len ? p.i : 0) * A.q.tok + (int64_t)p.g * A.q.head;
+        p.move(near_i, near_g, A.group);
+      }
+      if (A.wide_q) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const uint32_t w = (u[c][i >> 1] >> (16 * (i & 1))) & 0x7fffu;
-          top = w > top && w < 0x7f80u ? w : top;
-        }
-#pragma unroll
-        for (int o = 1; o < LR; o <<= 1) {
-          const uint32_t v = __shfl_xor(top, o);
-          top = v > top ? v : top;
-        }
-        e = (int)(top >> 7) - 127;
-        if (e < -126) e = -126;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          q[i] = (_Float16)__builtin_ldexpf(
-              kv_widen<true>((uint16_t)(u[c][i >> 1] >> (16 * (i & 1)))), -e);
+        for (int c = 0; c < CH; ++c) u[c] = load8(src[c], true);
       } else {
-        q = __builtin_bit_cast(half8, u[c]);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) u[c] = load8(src[c], false);
       }
-      *reinterpret_cast<half8*>(&L.q[buf][slot][d]) = q;
-      if (tid % LR == 0) L.unit[buf][slot] = __builtin_ldexpf(A.scale * kLog2e, e);
-    }
-    if (tid < step) {
-      const int row = b0 + tid;
-      L.visible[buf][tid] = row < rows ? visible_of(R, row / A.group) : 0;
-      L.z[buf][tid] = z_n;
-    }
-  };
-  if (base < rows) {
-    fetch(base);
-    put(base, 0);
-  }
-  for (int buf = 0; base < rows; base += step, buf ^= 1) {
-    const bool more = base + step < rows;
-    if (more) fetch(base + step);
-    __syncthreads();
-    const int slot = share * 32 + m;
-    const int see = L.visible[buf][slot];
-    if (page >= 0 && __any(see > pos0)) {
-      const float f = L.unit[buf][slot] * ks;
-      // an empty row has weight 0 everywhere
-      const float z = see > 0 ? -L.z[buf][slot] : kNegInf;
+      see = own.i < R.q_len ? visible_of(R, own.i) : 0;
+      z = lse0[(int64_t)(own.i < R.q_len ? own.i : 0) * pool.H * A.group + own.g];
+      from.move(step_i, step_g, A.group);
+      own.move(step_i, step_g, A.group);
+    };
+    uint16_t(*const mine)[D + 8] = rows_of_wave[wave];
+    if (32 * tile < rows) fetch();
+    for (; 32 * tile < rows; tile += shares) {
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+        *reinterpret_cast<uint4v*>(&mine[c * RC + lane / LR][lane % LR * 8]) = u[c];
+      const float c0 = -z * kLog2e;
+      const int seen = see;
+      if (32 * (tile + shares) < rows) fetch();
       float16v x[2];
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e) x[t][e] = 0.0f;
-      }
 #pragma unroll
       for (int s = 0; s < D / 16; ++s) {
-        const half8 q = *reinterpret_cast<const half8*>(
-            &L.q[buf][slot][32 * (s >> 1) + 16 * half + 8 * (s & 1)]);
+        const uint4v q = *reinterpret_cast<const uint4v*>(
+            &mine[m][32 * (s >> 1) + 16 * half + 8 * (s & 1)]);
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-          x[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[t][s], q, x[t], 0, 0, 0);
+        for (int t = 0; t < 2; ++t) x[t] = mfma32<BF16>(k[t][s], q, x[t]);
       }
-      if (__any(see > 0 && see < pos0 + kPage)) {
+      if (__any(seen < pos0 + kPage)) {          // some row sees the page in part or not at all
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (pos0 + 32 * t + 8 * (e >> 2) + 4 * half + (e & 3) < see)
-              sum[t][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][e], f, z));
+          for (int e = 0; e < 16; ++e) {
+            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][e], f, c0));
+            sum[16 * t + e] += pos0 + 32 * t + 8 * (e >> 2) + 4 * half + (e & 3) < seen ? w : 0.0f;
+          }
       } else {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            sum[t][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][e], f, z));
+            sum[16 * t + e] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][e], f, c0));
       }
     }
-    if (more) put(base + step, buf ^ 1);
   }
-  // over the 32 rows of a tile, then over the shares
-#pragma unroll
-  for (int t = 0; t < 2; ++t)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      float s = sum[t][e];
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) s += __shfl_xor(s, o);
-      if (m == 0) L.sum[wave][32 * t + 8 * (e >> 2) + 4 * half + (e & 3)] = s;
-    }
+  // over the 32 rows of a tile (lane m has result 16 t + e = m), then over the shares
+  const float total = sum_across<32>(sum);
+  sums[wave][32 * (m >> 4) + 8 * (m >> 2 & 3) + 4 * half + (m & 3)] = total;
   __syncthreads();
   if (share == 0 && page >= 0 && pos0 + lane < R.len) {
     float s = 0.0f;
-#pragma unroll
-    for (int w = 0; w < RG; ++w) s += L.sum[w * PW + wave][lane];
+    for (int w = 0; w < shares; ++w) s += sums[w * pages + wave][lane];
     const int64_t to = at * kPage + lane;
     A.mass_out[to] = A.mass_in ? __builtin_fmaf(A.decay, A.mass_in[to], s) : s;
   }
@@ -1202,12 +1218,17 @@ void prompt_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, const KvAttn
   });
 }
 
-template <int D, bool BF16, int PW>
+template <int D, bool BF16>
 void mass_rows_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, int np, const float* lse,
                  hipStream_t st) {
-  in_launches((int64_t)S.n * pool.H * ((np + PW - 1) / PW), [&](int64_t it0, unsigned n) {
-    hipLaunchKernelGGL((mass_rows_kernel<D, BF16, PW>), dim3(n), dim3(512), 0, st, pool, S, A, np,
-                       it0, lse);
+  // a wave a page where that makes two for every SIMD, else several share a page's rows
+  const int64_t items = (int64_t)S.n * pool.H * np;
+  int shares = items >= 2048 ? 1 : items >= 1024 ? 2 : items >= 512 ? 4 : 8;
+  if (shares > kPromptWaves<D>) shares = kPromptWaves<D>;
+  const int pages = kPromptWaves<D> / shares;
+  in_launches((int64_t)S.n * pool.H * ((np + pages - 1) / pages), [&](int64_t it0, unsigned n) {
+    hipLaunchKernelGGL((mass_rows_kernel<D, BF16>), dim3(n), dim3(64 * kPromptWaves<D>), 0, st, pool, S, A, np,
+                       shares, it0, lse);
   });
 }
 
@@ -1233,11 +1254,8 @@ hipError_t attend_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, void* 
                        P.tiles, P.splits, units, part, lse);
   if (A.mass_out && np) {
     const int64_t items = (int64_t)S.n * pool.H * np;
-    // four pages a workgroup share each query tile; two where that gives too few workgroups
-    if (P.big && items >= 2048)
-      mass_rows_d<D, BF16, 4>(pool, S, A, np, lse, st);
-    else if (P.big)
-      mass_rows_d<D, BF16, 2>(pool, S, A, np, lse, st);
+    if (P.big)
+      mass_rows_d<D, BF16>(pool, S, A, np, lse, st);
     else if (P.keep_scores)
       hipLaunchKernelGGL(mass_scores_kernel, dim3(grid_of((items + 3) / 4)), dim3(256), 0, st, pool,
                          S, A, np, items, scores, lse);

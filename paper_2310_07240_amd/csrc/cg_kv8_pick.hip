@@ -8,9 +8,9 @@ namespace {
 // Keys in the order of the values: a larger value has a larger key, -0 and +0 the same, a NaN the
 // lowest of all. 0 is no value's key.
 __device__ __forceinline__ uint32_t order_key(float f) {
-  if (f != f) return 1u;
   const uint32_t u = __builtin_bit_cast(uint32_t, f + 0.0f);
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  const uint32_t k = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+  return f != f ? 1u : k;
 }
 
 // How many lanes below this one are in the mask.
@@ -30,9 +30,9 @@ struct PickLds {
 };
 
 // The best `need` (1 <= need < n) of n keys: emit(position, index) for each, positions ascending
-// with the index. Of a block j of 64 keys, place(j) says where it lies, raw() loads and key() makes
-// the key of index 64 j + lane, 0 from n on (no key is 0, so such places are never among the best);
-// they are called apart so that no load waits for another. Every wave has a run of whole blocks, the first kHeld of
+// with the index. Of a block j of 64 keys, place(j) says where it lies (below 0: nowhere, its keys
+// are the lowest), raw() loads and key() makes the key of index 64 j + lane; they are called apart
+// so that no load waits for another. Places from n on get 0, which is no key. Every wave has a run of whole blocks, the first kHeld of
 // them in registers, so the keys are read once. Three passes over the keys' bits, highest first,
 // narrow them to the smallest key that is taken and the number of its equals that are; then each
 // wave counts and emits its run by ballots. Counts are whole numbers, so no order of the LDS
@@ -55,15 +55,25 @@ __device__ __forceinline__ void pick_best(int n, int need, PickLds<NT>& L, const
   for (int r = 0; r < kHeld; r += 8)
     if (r < mine) {
       uint32_t raw[8];
-      int at[8];
+      int at[8], lost = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         at[i] = __builtin_amdgcn_readlane(place, r + i);
+        lost |= at[i];
         raw[i] = keys.raw(at[i], first + (r + i < mine ? r + i : 0), lane);
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        held[r + i] = r + i < mine ? keys.key(raw[i], at[i], first + r + i, lane) : 0u;
+      for (int i = 0; i < 8; ++i) held[r + i] = keys.key(raw[i]);
+      // blocks that lie nowhere, and the end of the run or of the keys
+      if (lost < 0) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) held[r + i] = at[i] < 0 ? 1u : held[r + i];
+      }
+      if (r + 8 >= mine) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          held[r + i] = r + i < mine && (first + r + i) * 64 + lane < n ? held[r + i] : 0u;
+      }
     }
   // f(block, key) for the wave's keys, eight blocks of registers a branch
   const auto each = [&](auto f) {
@@ -75,7 +85,8 @@ __device__ __forceinline__ void pick_best(int n, int need, PickLds<NT>& L, const
       }
     for (int r = kHeld; r < mine; ++r) {
       const int at = keys.place(first + r);
-      f(first + r, keys.key(keys.raw(at, first + r, lane), at, first + r, lane));
+      const uint32_t k = at < 0 ? 1u : keys.key(keys.raw(at, first + r, lane));
+      f(first + r, (first + r) * 64 + lane < n ? k : 0u);
     }
   };
 
@@ -143,13 +154,16 @@ __device__ __forceinline__ void pick_best(int n, int need, PickLds<NT>& L, const
   ne = __builtin_amdgcn_readfirstlane(ne);
   each([&](int j, uint32_t k) {
     const uint64_t ba = __ballot(k > prefix), be = __ballot(k == prefix);
-    if (ba | be) {
+    const uint32_t before = na + (ne < rest ? ne : rest);
+    if (be) {
       const uint32_t re = ne + lanes_below(be);
       const uint32_t at = na + lanes_below(ba) + (re < rest ? re : rest);
       if (k > prefix || (k == prefix && re < rest)) emit((int)at, j * 64 + lane);
-      na += (uint32_t)__popcll(ba);
       ne += (uint32_t)__popcll(be);
+    } else if (k > prefix) {
+      emit((int)(before + lanes_below(ba)), j * 64 + lane);
     }
+    na += (uint32_t)__popcll(ba);
   });
 }
 
@@ -169,15 +183,14 @@ struct MassKeys {
   const KvPool& pool;
   const KvSeqs& S;
   const float* mass;
-  int seq, h, n;
+  int seq, h;
   __device__ __forceinline__ int place(int j) const { return kv_page(S, pool.P, seq, j); }
   __device__ __forceinline__ uint32_t raw(int page, int, int lane) const {
     return __builtin_bit_cast(
         uint32_t, mass[((int64_t)(page < 0 ? 0 : page) * pool.H + h) * kPage + lane]);
   }
-  __device__ __forceinline__ uint32_t key(uint32_t raw, int page, int j, int lane) const {
-    const uint32_t k = page < 0 ? 1u : order_key(__builtin_bit_cast(float, raw));
-    return j * kPage + lane < n ? k : 0u;
+  __device__ __forceinline__ uint32_t key(uint32_t raw) const {
+    return order_key(__builtin_bit_cast(float, raw));
   }
 };
 
@@ -202,7 +215,7 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(KvPool pool, KvSeqs 
   for (int i = tid; i < last; i += kKeepThreads) out[need + i] = old + i;
   if (need == 0) return;
   pick_best<kKeepThreads>(
-      old, need, L, MassKeys{pool, S, mass, seq, h, old},
+      old, need, L, MassKeys{pool, S, mass, seq, h},
       [&](int at, int i) { out[at] = i; });
 }
 
@@ -349,9 +362,7 @@ struct LeftKeys {
     const int e = j * 64 + lane;
     return __hip_atomic_load(keys + (e < n ? e : 0), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
-  __device__ __forceinline__ uint32_t key(uint32_t raw, int, int j, int lane) const {
-    return j * 64 + lane < n ? raw : 0u;
-  }
+  __device__ __forceinline__ uint32_t key(uint32_t raw) const { return raw; }
 };
 
 constexpr int kSelectThreads = 256;

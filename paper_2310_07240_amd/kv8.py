@@ -12,6 +12,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import struct
 
 from .cachegen import CodecError, _check, lib
 
@@ -42,6 +43,13 @@ class _Attn(ctypes.Structure):
                 ("decay", ctypes.c_float)]
 
 
+# The same structures as bytes: a call of one token takes a few microseconds on the GPU, and packing
+# a structure at once takes a fraction of setting it field by field.
+_SEQS = struct.Struct("@iiP")
+_ROWS = struct.Struct("@Pqqq")
+_ATTN = struct.Struct("@iiifPiPPqqqPqqqPPiPPf0P")
+assert (_SEQS.size, _ROWS.size, _ATTN.size) == tuple(map(ctypes.sizeof, (_Seqs, _Rows, _Attn)))
+
 _LIB = None
 
 
@@ -49,16 +57,16 @@ def _lib():
     global _LIB
     if _LIB is None:
         L = lib()
-        C, S, R, A = (ctypes.POINTER(t) for t in (_Cache, _Seqs, _Rows, _Attn))
-        L.cg_kv8_store.argtypes = [C, S, _P, _P, _I32, _I32, R, R, _P, _P]
-        L.cg_kv8_load.argtypes = [C, S, _P, _P, _I32, _I32, R, R, _P]
-        L.cg_kv8_attend_workspace_bytes.argtypes = [C, S, A]
-        L.cg_kv8_attend_workspace_bytes.restype = ctypes.c_uint64
-        L.cg_kv8_attend.argtypes = [C, S, A, _P, ctypes.c_uint64, _P]
-        L.cg_kv8_select_workspace_bytes.argtypes = [C, S, A]
-        L.cg_kv8_select_workspace_bytes.restype = ctypes.c_uint64
-        L.cg_kv8_select.argtypes = [C, S, A, _I32, _P, _P, ctypes.c_uint64, _P]
-        L.cg_kv8_evict.argtypes = [C, S, _P, _I32, _P, _I32, _I32, S, _P, _P, _P]
+        U64 = ctypes.c_uint64
+        L.cg_kv8_store.argtypes = [_P, _P, _P, _P, _I32, _I32, _P, _P, _P, _P]
+        L.cg_kv8_load.argtypes = [_P, _P, _P, _P, _I32, _I32, _P, _P, _P]
+        L.cg_kv8_attend_workspace_bytes.argtypes = [_P, _P, _P]
+        L.cg_kv8_attend_workspace_bytes.restype = U64
+        L.cg_kv8_attend.argtypes = [_P, _P, _P, _P, U64, _P]
+        L.cg_kv8_select_workspace_bytes.argtypes = [_P, _P, _P]
+        L.cg_kv8_select_workspace_bytes.restype = U64
+        L.cg_kv8_select.argtypes = [_P, _P, _P, _I32, _P, _P, U64, _P]
+        L.cg_kv8_evict.argtypes = [_P, _P, _P, _I32, _P, _I32, _I32, _P, _P, _P, _P]
         for n in ("store", "load", "attend", "select", "evict"):
             getattr(L, "cg_kv8_" + n).restype = ctypes.c_int
         _LIB = L
@@ -106,13 +114,13 @@ class Kv8Cache:
             setattr(self, n, b)
         self._c = _Cache(P, H, D, *(None if (b := getattr(self, n)) is None else b.data_ptr()
                                     for n in want))
-        self._cp = ctypes.byref(self._c)
+        self._cp = ctypes.addressof(self._c)
+        self._raw_stream = torch._C._cuda_getCurrentRawStream
         self._ws, self._captured = {}, []
         self._types = {torch.float16: 0, torch.bfloat16: 1}
+        self._scale = 1.0 / math.sqrt(D)
 
-    # ---- marshalling ---------------------------------------------------------------------
-    # (a call of one token takes a few microseconds on the GPU: no message is put together and no
-    # stream object made unless it is needed)
+    # ---- marshalling (no message is put together and no stream object made until needed) ----
     def _tensor(self, t, name, dtype, shape=None):
         if (t.dtype is dtype and t.device == self.device and t.is_contiguous()
                 and (shape is None or t.shape == shape)):
@@ -122,29 +130,34 @@ class Kv8Cache:
                          f"is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
 
     def _seqs(self, table):
+        """(cg_kv8_seqs, n_seq, columns)"""
         p = self._tensor(table, "table", self._i32)
         if table.dim() != 2:
             raise ValueError("table: [n_seq, columns] is wanted")
         n, width = table.shape
-        return _Seqs(n, width, p)
+        return _SEQS.pack(n, width, p), n, width
 
     def _per_seq(self, t, name, n):
-        return None if t is None else self._tensor(t, name, self._i32, (n,))
+        return 0 if t is None else self._tensor(t, name, self._i32, (n,))
 
-    def _rows(self, t, name, shape, dtype):
+    def _strided(self, t, name, shape, dtype):
+        """The fields of cg_kv8_rows."""
         if t.dtype is dtype and t.shape == shape and t.device == self.device:
             a, b, c, d = t.stride()
             if d == 1:
-                return _Rows(t.data_ptr(), a, b, c)
+                return t.data_ptr(), a, b, c
         raise ValueError(f"{name}: {dtype} rows {tuple(shape)} with a contiguous last dimension "
                          f"on {self.device} are wanted, got {t.dtype} {tuple(t.shape)} on "
                          f"{t.device}")
+
+    def _rows(self, t, name, shape, dtype):
+        return _ROWS.pack(*self._strided(t, name, shape, dtype))
 
     def _handle(self, stream):
         """The HIP stream's handle: the caller's, or torch's current one."""
         if stream is not None:
             return stream.cuda_stream
-        return self.torch._C._cuda_getCurrentRawStream(self._index)
+        return self._raw_stream(self._index)
 
     def _new(self, make, shape, dtype, stream):
         """A tensor whose memory's reuse is ordered on the stream."""
@@ -181,12 +194,11 @@ class Kv8Cache:
         """Rows k, v [n_seq, n_tokens, n_heads, head_dim] become the sequences' tokens from
         ``starts`` on (``counts``: how many of each; default all). ``status``: an int32 tensor of
         one element that receives 0, or non-zero for NaN / Inf."""
-        s = self._seqs(table)
+        s, n, _ = self._seqs(table)
         kind = self._types.get(k.dtype)
         _need(kind is not None and k.dim() == 4, "k: float16 or bfloat16 [n_seq, n_tokens, "
               "n_heads, head_dim] is wanted")
         _need(starts is not None, "starts is missing")
-        n = s.n_seq
         shape = (n, k.shape[1], self.n_heads, self.head_dim)
         _check(_lib().cg_kv8_store(
             self._cp, s, self._per_seq(starts, "starts", n), self._per_seq(counts, "counts", n),
@@ -197,8 +209,7 @@ class Kv8Cache:
     def load(self, table, starts, n_tokens, counts=None, dtype=None, k=None, v=None, stream=None):
         """(k, v) [n_seq, n_tokens, n_heads, head_dim]: the sequences' tokens from ``starts`` on,
         zeros behind ``counts``. ``k``, ``v``: tensors to write into."""
-        s = self._seqs(table)
-        n = s.n_seq
+        s, n, _ = self._seqs(table)
         shape = (n, int(n_tokens), self.n_heads, self.head_dim)
         if k is None or v is None:
             dtype = dtype or (self.torch.float16 if k is None and v is None else
@@ -215,17 +226,12 @@ class Kv8Cache:
         return k, v
 
     # ---- attention -----------------------------------------------------------------------
-    def _attn(self, q, s, lengths, q_lens, max_len):
+    def _queries(self, q, n):
         kind = self._types.get(q.dtype)
         _need(q.dim() == 4 and kind is not None, "q: float16 or bfloat16 "
               "[n_seq, n_q, n_q_heads, head_dim] is wanted")
-        _need(lengths is not None, "lengths is missing")
-        n = s.n_seq
         _, nq, heads, _ = q.shape
-        return _Attn(nq, heads, kind, 0.0, self._per_seq(lengths, "lengths", n),
-                     s.max_pages * PAGE if max_len is None else max_len,
-                     self._per_seq(q_lens, "q_lens", n),
-                     self._rows(q, "q", (n, nq, heads, self.head_dim), q.dtype))
+        return kind, nq, heads, (n, nq, heads, self.head_dim)
 
     def attend(self, q, table, lengths, scale=None, q_lens=None, max_len=None, out=None, lse=None,
                picks=None, mass=None, mass_out=None, decay=1.0, stream=None):
@@ -240,25 +246,28 @@ class Kv8Cache:
         mass_out  float32 [n_pages, n_heads, 64] that receives decay * mass + the weight each
                   token got (``mass`` may be None, or the same tensor; given alone it is updated
                   in place)."""
-        s = self._seqs(table)
-        a = self._attn(q, s, lengths, q_lens, max_len)
-        a.scale = 1.0 / math.sqrt(self.head_dim) if scale is None else scale
+        s, n, width = self._seqs(table)
+        kind, nq, heads, shape = self._queries(q, n)
+        _need(lengths is not None, "lengths is missing")
         if out is None:
             out = self._empty(q.shape, q.dtype, stream)
-        a.out = self._rows(out, "out", q.shape, q.dtype)
-        if lse is not None:
-            a.lse = self._tensor(lse, "lse", self._f32, q.shape[:3])
+        n_picks = picks_p = mass_p = mass_out_p = 0
         if picks is not None:
             _need(picks.dim() == 4, "picks: [n_seq, n_q, n_heads, n] is wanted")
-            a.n_picks = picks.shape[3]
-            a.picks = self._tensor(picks, "picks", self._i32,
-                                   (s.n_seq, a.n_q, self.n_heads, a.n_picks))
+            n_picks = picks.shape[3]
+            picks_p = self._tensor(picks, "picks", self._i32, (n, nq, self.n_heads, n_picks))
         if mass is not None or mass_out is not None:
-            shape = (self.n_pages, self.n_heads, PAGE)
+            pool = (self.n_pages, self.n_heads, PAGE)
             mass_out = mass if mass_out is None else mass_out
-            a.mass_in = None if mass is None else self._tensor(mass, "mass", self._f32, shape)
-            a.mass_out = self._tensor(mass_out, "mass_out", self._f32, shape)
-            a.decay = decay
+            mass_p = 0 if mass is None else self._tensor(mass, "mass", self._f32, pool)
+            mass_out_p = self._tensor(mass_out, "mass_out", self._f32, pool)
+        a = _ATTN.pack(nq, heads, kind, self._scale if scale is None else scale,
+                       self._per_seq(lengths, "lengths", n),
+                       width * PAGE if max_len is None else max_len,
+                       self._per_seq(q_lens, "q_lens", n), *self._strided(q, "q", shape, q.dtype),
+                       *self._strided(out, "out", shape, q.dtype),
+                       0 if lse is None else self._tensor(lse, "lse", self._f32, shape[:3]),
+                       picks_p, n_picks, mass_p, mass_out_p, decay)
         L = _lib()
         handle = self._handle(stream)
         need = L.cg_kv8_attend_workspace_bytes(self._cp, s, a)
@@ -271,17 +280,21 @@ class Kv8Cache:
         """Table columns [n_seq, n_q, n_heads, n_picks] (int32, ascending, -1 behind the last) of
         the pages that each query token should read: the ``recent`` last ones it sees and the best
         of the others by the bound of their q . k."""
-        s = self._seqs(table)
-        a = self._attn(q, s, lengths, q_lens, max_len)
-        a.n_picks = n_picks
-        shape = (s.n_seq, a.n_q, self.n_heads, max(0, a.n_picks))
+        s, n, width = self._seqs(table)
+        kind, nq, heads, shape = self._queries(q, n)
+        _need(lengths is not None, "lengths is missing")
+        want = (n, nq, self.n_heads, max(0, n_picks))
         if out is None:
-            out = self._empty(shape, self._i32, stream)
+            out = self._empty(want, self._i32, stream)
+        rows = self._strided(q, "q", shape, q.dtype)
+        a = _ATTN.pack(nq, heads, kind, 0.0, self._per_seq(lengths, "lengths", n),
+                       width * PAGE if max_len is None else max_len,
+                       self._per_seq(q_lens, "q_lens", n), *rows, *rows, 0, 0, n_picks, 0, 0, 0.0)
         L = _lib()
         handle = self._handle(stream)
         need = L.cg_kv8_select_workspace_bytes(self._cp, s, a)
         ws = self._scratch(stream, handle, need) if need else (None, 0)
-        _check(L.cg_kv8_select(self._cp, s, a, recent, self._tensor(out, "out", self._i32, shape),
+        _check(L.cg_kv8_select(self._cp, s, a, recent, self._tensor(out, "out", self._i32, want),
                                ws[0], ws[1], handle), "cg_kv8_select")
         return out
 
@@ -291,14 +304,14 @@ class Kv8Cache:
         sequence of the call): the last ``recent`` stay and the heaviest of the others by ``mass``
         [n_pages, n_heads, 64], which moves along. Returns (kept [n_seq, n_heads, keep],
         new_lengths [n_seq])."""
-        s, to = self._seqs(table), self._seqs(new_table)
+        s, n, width = self._seqs(table)
+        to = self._seqs(new_table)[0]
         _need(lengths is not None and mass is not None, "lengths and mass are wanted")
-        n = s.n_seq
         kept = self._empty((n, self.n_heads, max(0, keep)), self._i32, stream)
         new_lengths = self._empty((n,), self._i32, stream)
         _check(_lib().cg_kv8_evict(
             self._cp, s, self._per_seq(lengths, "lengths", n),
-            s.max_pages * PAGE if max_len is None else max_len,
+            width * PAGE if max_len is None else max_len,
             self._tensor(mass, "mass", self._f32, (self.n_pages, self.n_heads, PAGE)), keep,
             recent, to, kept.data_ptr(), new_lengths.data_ptr(), self._handle(stream)),
             "cg_kv8_evict")

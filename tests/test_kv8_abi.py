@@ -35,8 +35,20 @@ def attn(**kw):
     return a
 
 
+class Checked:
+    """The library with the structures passed by address."""
+
+    def __getattr__(self, name):
+        fn = getattr(kv8._lib(), name)
+
+        def call(*args):
+            return fn(*(ctypes.addressof(a) if isinstance(a, ctypes.Structure) else a
+                        for a in args))
+        return call
+
+
 def L():
-    return kv8._lib()
+    return Checked()
 
 
 BAD_CACHE = [(dict(n_pages=0), -2), (dict(n_heads=-1), -2), (dict(head_dim=96), -2),

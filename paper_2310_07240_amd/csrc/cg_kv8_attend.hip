@@ -13,6 +13,8 @@
 // long as both operands agree: row m of K tile t is token 16 (m >> 2) + 4 t + (m & 3), which makes
 // the 16 tokens whose S a lane gets the consecutive 16 g .. 16 g + 15, exactly the k slots that it
 // supplies for the second product, and the V operand 16 consecutive bytes of a channel.
+#include <math.h>
+
 #include "cg_kv8.h"
 
 namespace {
@@ -307,7 +309,7 @@ __device__ __forceinline__ void join_tile(const KvAttn& A, const RowsOf& R, int 
   const int tid = threadIdx.x;
   const int row = tid >> 4, sub = tid & 15;            // 16 threads a row
   // the first states' channels are on their way while the factors are found
-  constexpr int kAhead = 8;
+  constexpr int kAhead = 16;
   float2 ahead[kAhead];
   const int e0 = tid < rows0 * (D / 2) ? tid : 0;
 #pragma unroll
@@ -345,22 +347,21 @@ __device__ __forceinline__ void join_tile(const KvAttn& A, const RowsOf& R, int 
     const int r = e / (D / 2), d = e % (D / 2) * 2;
     float o[2] = {0.0f, 0.0f};
     const float* q = p + r * D + d;
-    int i = 0;
-    if (e == tid) {
+    // kAhead states at a time, all their loads on their way together
+    for (int i0 = 0; i0 < n; i0 += kAhead) {
+      if (e != tid || i0 > 0) {
 #pragma unroll
-      for (; i < kAhead; ++i) {
-        const float f = i < n ? w[i * 16 + r] : 0.0f;
-        o[0] = i < n ? __builtin_fmaf(ahead[i].x, f, o[0]) : o[0];
-        o[1] = i < n ? __builtin_fmaf(ahead[i].y, f, o[1]) : o[1];
+        for (int i = 0; i < kAhead; ++i)
+          get_pair<FAR>(q + (i0 + i < n ? i0 + i : 0) * kPart<D>, ahead[i].x, ahead[i].y);
       }
-    }
-#pragma unroll 8
-    for (; i < n; ++i) {
-      float a, b;
-      get_pair<FAR>(q + i * kPart<D>, a, b);
-      const float f = w[i * 16 + r];
-      o[0] = __builtin_fmaf(a, f, o[0]);
-      o[1] = __builtin_fmaf(b, f, o[1]);
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        if (i0 + i < n) {
+          const float f = w[(i0 + i) * 16 + r];
+          o[0] = __builtin_fmaf(ahead[i].x, f, o[0]);
+          o[1] = __builtin_fmaf(ahead[i].y, f, o[1]);
+        }
+      }
     }
     put_out<D, BF16>(A, R, h, tile * 16 + r, d, o, 2);
   }
@@ -1289,9 +1290,14 @@ KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& S, const KvAttn& A, int
     // As many workgroups as the registers let the card hold at once (3, 2 or 1 a CU), each wave
     // with a page of its own at least: a second round of half-filled CUs costs more than longer
     // splits do (4 sequences of 8K, 32 heads: 50 us with 512 workgroups, 64 with 768, 58 with
-    // 1024; 32 of 2K, 8 heads: 26, 34 and 33). No more splits than one workgroup joins quickly.
+    // 1024; 32 of 2K, 8 heads: 26, 34 and 33). A long sequence on few heads gains a page's step of
+    // a wave with every split less of it and pays for joining one more, a tenth of that: at most
+    // twice the root of the pages (8 heads, one sequence: 16K tokens 17 us with 32 splits, 21 with
+    // 64; 4K 11 us with 16, 13 with 8).
     s = (D == 64 ? 768 : D == 128 ? 512 : 256) / units;
     most = (pages + 3) / 4;
+    const int64_t root = (int64_t)sqrt(4.0 * (double)pages);
+    if (most > root) most = root;
   }
   if (most > kMostSplits) most = kMostSplits;
   if (s > most) s = most;

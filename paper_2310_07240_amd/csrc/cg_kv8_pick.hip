@@ -20,7 +20,6 @@ __device__ __forceinline__ uint32_t lanes_below(uint64_t mask) {
 }
 
 constexpr int kBins = 2048;          // of a pass: 11 bits of the keys
-constexpr int kHeld = 64;            // keys a lane keeps in registers
 
 template <int NT>
 struct PickLds {
@@ -32,14 +31,14 @@ struct PickLds {
 // The best `need` (1 <= need < n) of n keys: emit(position, index) for each, positions ascending
 // with the index. Of a block j of 64 keys, place(j) says where it lies (below 0: nowhere, its keys
 // are the lowest), raw() loads and key() makes the key of index 64 j + lane; they are called apart
-// so that no load waits for another. Places from n on get 0, which is no key. Every wave has a run of whole blocks, the first kHeld of
-// them in registers, so the keys are read once. Three passes over the keys' bits, highest first,
+// so that no load waits for another. Places from n on get 0, which is no key. Every wave has a run
+// of whole blocks, the first kHeld of them in registers, so the keys are read once. Three passes over the keys' bits, highest first,
 // narrow them to the smallest key that is taken and the number of its equals that are; then each
 // wave counts and emits its run by ballots. Counts are whole numbers, so no order of the LDS
 // additions changes anything. Bound by the vector instructions of the one CU (about 45 a block in
 // all) and the first pass's LDS additions: weights crowd into a few octaves, so lanes meet on a bin,
 // hence 11 bits and not 8.
-template <int NT, class Keys, class Emit>
+template <int NT, int kHeld, class Keys, class Emit>
 __device__ __forceinline__ void pick_best(int n, int need, PickLds<NT>& L, const Keys& keys,
                                           Emit emit) {
   constexpr int NW = NT / 64;
@@ -97,7 +96,16 @@ __device__ __forceinline__ void pick_best(int n, int need, PickLds<NT>& L, const
     for (int i = tid; i < kBins; i += NT) L.hist[i] = 0;
     __syncthreads();
     each([&](int, uint32_t k) {
-      if (agrees(k)) atomicAdd(&L.hist[(k >> shift) & width], 1u);
+      const uint64_t who = __ballot(agrees(k));
+      if (!who) return;
+      // lanes that all meet on one bin (equal weights) add once
+      const uint32_t bin = (k >> shift) & width;
+      const uint32_t one = (uint32_t)__builtin_amdgcn_readlane((int)bin, __builtin_ctzll(who));
+      if (__ballot(agrees(k) && bin == one) == who) {
+        if (lane == 0) atomicAdd(&L.hist[one], (uint32_t)__popcll(who));
+      } else if (agrees(k)) {
+        atomicAdd(&L.hist[bin], 1u);
+      }
     });
     __syncthreads();
     // the bins from the highest down, kBins / NT a thread
@@ -130,7 +138,7 @@ __device__ __forceinline__ void pick_best(int n, int need, PickLds<NT>& L, const
     prefix |= L.digit << shift;
     rest = L.rest;
   };
-  narrow(21, 2047u, [](uint32_t) { return true; });
+  narrow(21, 2047u, [](uint32_t k) { return k != 0; });   // (nobody meets on the bin of no key)
   narrow(10, 2047u, [&](uint32_t k) { return (k ^ prefix) < (1u << 21); });
   narrow(0, 1023u, [&](uint32_t k) { return (k ^ prefix) < (1u << 10); });
 
@@ -214,7 +222,7 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(KvPool pool, KvSeqs 
   const int need = keep - last, old = n - last;
   for (int i = tid; i < last; i += kKeepThreads) out[need + i] = old + i;
   if (need == 0) return;
-  pick_best<kKeepThreads>(
+  pick_best<kKeepThreads, 64>(
       old, need, L, MassKeys{pool, S, mass, seq, h},
       [&](int at, int i) { out[at] = i; });
 }
@@ -499,7 +507,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(KvPool pool, KvS
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  pick_best<kSelectThreads>(
+  pick_best<kSelectThreads, 8>(
       old, need, L, LeftKeys{mine, old},
       [&](int at, int j) { picks[at] = j; });
 }

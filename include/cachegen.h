@@ -452,7 +452,7 @@ int cg_kv8_store(const cg_kv8_cache* c, const cg_kv8_seqs* s, const int32_t* sta
                  const cg_kv8_rows* v, uint32_t* status, hipStream_t stream);
 
 /* Read rows back: row i of sequence b is its token starts[b] + i for i < counts[b] (NULL:
- * n_tokens), code * scale rounded to `dtype`; rows counts[b] .. n_tokens - 1 are zeros, and so
+ * n_tokens), the fp32 product code * scale rounded to `dtype`; rows counts[b] .. n_tokens - 1 are zeros, and so
  * are rows of pages that do not exist. Asynchronous. */
 int cg_kv8_load(const cg_kv8_cache* c, const cg_kv8_seqs* s, const int32_t* starts,
                 const int32_t* counts, int32_t n_tokens, int32_t dtype, const cg_kv8_rows* k,

@@ -98,6 +98,34 @@ def test_store_and_load(D, H, dtype, T, starts, counts):
                         torch.from_numpy(want).to(ot).view(torch.int16).numpy())
 
 
+def test_load_rounds_the_fp32_product():
+    """Scales whose products with some codes lie so near the middle of two fp16 values that
+    rounding once and rounding through fp32 differ: the definition goes through fp32."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(5)
+    q = np.arange(1, 128, dtype=np.float64)
+    s = (rng.random(400000) * 0.05 + 0.01).astype(np.float32)
+    once = (q[None] * s[:, None].astype(np.float64)).astype(np.float16)
+    twice = (q[None].astype(np.float32) * s[:, None]).astype(np.float16)
+    found = s[(once != twice).any(1)][:40]
+    assert len(found) >= 20
+    n = len(found)
+    cache = make(torch, n, 1, 128)
+    codes = torch.arange(-63, 65, device="cuda").to(torch.int8)
+    cache.k_codes.copy_(codes.view(1, 1, 1, 128).expand(n, 1, 64, 128))
+    cache.k_codes[:, :, ::2] += 63                             # 0 .. 127 in every other row
+    cache.v_codes.copy_(cache.k_codes.transpose(2, 3))
+    for x in (cache.k_scale, cache.v_scale):
+        x.copy_(torch.from_numpy(found).view(n, 1))
+    table = torch.arange(n, dtype=torch.int32, device="cuda").view(n, 1)
+    k, v = cache.load(table, ints(torch, [0] * n), 64)
+    ref = R.Ref(cache)
+    want = (ref.k[:, 0].astype(np.float32) * ref.ks[:, :, None]).astype(np.float16)
+    for got in (k, v):
+        assert_same("rows", got[:, :, 0].view(torch.int16).cpu().numpy().view(np.uint16),
+                    want.view(np.uint16))
+
+
 @pytest.mark.parametrize("off", [0, 1])
 def test_store_strides(off):
     """Rows inside a [ctx][layer][K/V][token][channel] cache; off = 1: not 16-byte aligned."""

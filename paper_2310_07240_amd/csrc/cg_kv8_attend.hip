@@ -303,13 +303,12 @@ __device__ __forceinline__ void get_pair(const float* p, float& a, float& b) {
 // out: the 256 threads first fetch every state's (m, l) at once, then each takes pairs of channels
 // through all states. FAR: written by other workgroups of this launch. w [n][16]: LDS. rows0: rows
 // of the tile that exist.
-template <int D, bool BF16, bool FAR>
+template <int D, bool BF16, bool FAR, int kAhead>
 __device__ __forceinline__ void join_tile(const KvAttn& A, const RowsOf& R, int H, int h, int tile,
                                           int rows0, const float* p, int n, float* w, float* lse) {
   const int tid = threadIdx.x;
   const int row = tid >> 4, sub = tid & 15;            // 16 threads a row
   // the first states' channels are on their way while the factors are found
-  constexpr int kAhead = 16;
   float2 ahead[kAhead];
   const int e0 = tid < rows0 * (D / 2) ? tid : 0;
 #pragma unroll
@@ -504,7 +503,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_kernel(KvPool po
         if (threadIdx.x == 0)
           __hip_atomic_store(&arrived[unit], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         // (os has room for the factors of 128 states; its readers have passed two barriers)
-        join_tile<D, BF16, true>(A, R, pool.H, h, tile, rows - tile * 16 < 16 ? rows - tile * 16 : 16,
+        join_tile<D, BF16, true, 16>(A, R, pool.H, h, tile, rows - tile * 16 < 16 ? rows - tile * 16 : 16,
                                  part + unit * splits * kPart<D>, splits, &os[0][0][0], lse);
       }
     }
@@ -524,7 +523,7 @@ __global__ __launch_bounds__(256) void join_kernel(KvPool pool, KvSeqs S, KvAttn
     const int h = (int)(r % pool.H);
     const RowsOf R = rows_of(S, A, (int)(r / pool.H));
     const int rows = R.nq * A.group - tile * 16;
-    join_tile<D, BF16, false>(A, R, pool.H, h, tile, rows < 16 ? rows : 16,
+    join_tile<D, BF16, false, 4>(A, R, pool.H, h, tile, rows < 16 ? rows : 16,
                               part + it * splits * kPart<D>, splits, w, lse);
     __syncthreads();
   }
@@ -1105,38 +1104,44 @@ void mass_rows_kernel(KvPool pool, KvSeqs S, KvAttn A, int np, int shares, int64
     const int64_t first = (int64_t)pos0 - R.len + R.q_len;
     int tile = first > 0 ? uniform((int)(first * A.group / 32)) : 0;
     tile += (share - tile % shares + shares) % shares;
-    // Rows as (query token, place in the group), moved on without divisions: the lane's first row
-    // to load (i, g), RC further ones apart, and the row m whose results it gets (im, gm).
+    // Rows are moved on without divisions and products: `off` elements into the queries and place g
+    // in the group. A lane loads its first row of the tile and those RC apart from it, and has the
+    // results of row m.
     struct Place {
-      int i, g;
-      __device__ __forceinline__ void move(int di, int dg, int group) {
-        i += di;
+      int64_t off;
+      int g;
+      __device__ __forceinline__ void move(int64_t by, int dg, int group, int64_t wrap) {
+        off += by;
         g += dg;
-        if (g >= group) {
-          g -= group;
-          ++i;
-        }
+        const bool over = g >= group;
+        off += over ? wrap : 0;
+        g -= over ? group : 0;
       }
     };
-    const auto place = [&](int row) { return Place{row / A.group, row % A.group}; };
+    const int64_t wrap = A.q.tok - A.group * A.q.head, lse_tok = (int64_t)pool.H * A.group;
     const int step = 32 * shares, step_i = uniform(step / A.group), step_g = step - step_i * A.group;
     const int near_i = uniform(RC / A.group), near_g = RC - near_i * A.group;
-    Place from = place(32 * tile + lane / LR), own = place(32 * tile + m);
+    const int64_t step_off = step_i * A.q.tok + step_g * A.q.head;
+    const int64_t near_off = near_i * A.q.tok + near_g * A.q.head;
+    const int row_l = 32 * tile + lane / LR, row_m = 32 * tile + m;
+    Place from = {(int64_t)(row_l / A.group) * A.q.tok + (int64_t)(row_l % A.group) * A.q.head,
+                  row_l % A.group};
+    int own_i = row_m / A.group, own_g = row_m % A.group;
     const uint16_t* const q0 = static_cast<const uint16_t*>(A.q.p) + R.seq * A.q.seq +
                                (int64_t)h * A.group * A.q.head + lane % LR * 8;
-    const float* const lse0 = lse + (int64_t)R.seq * A.nq * pool.H * A.group + h * A.group;
+    const float* const lse0 = lse + (int64_t)R.seq * A.nq * lse_tok + h * A.group;
     constexpr int CH = 32 / RC;
     uint4v u[CH];
     float z;
     int see;
-    const auto fetch = [&] {
+    const auto fetch = [&](int t) {
       const uint16_t* src[CH];
       Place p = from;
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
-        // (behind the last row some row, whose results are not used)
-        src[c] = q0 + (int64_t)(p.i < R.q_len ? p.i : 0) * A.q.tok + (int64_t)p.g * A.q.head;
-        p.move(near_i, near_g, A.group);
+        // (behind the last row the first one, whose results are not used)
+        src[c] = q0 + (32 * t + c * RC + lane / LR < rows ? p.off : 0);
+        p.move(near_off, near_g, A.group, wrap);
       }
       if (A.wide_q) {
 #pragma unroll
@@ -1145,20 +1150,26 @@ void mass_rows_kernel(KvPool pool, KvSeqs S, KvAttn A, int np, int shares, int64
 #pragma unroll
         for (int c = 0; c < CH; ++c) u[c] = load8(src[c], false);
       }
-      see = own.i < R.q_len ? visible_of(R, own.i) : 0;
-      z = lse0[(int64_t)(own.i < R.q_len ? own.i : 0) * pool.H * A.group + own.g];
-      from.move(step_i, step_g, A.group);
-      own.move(step_i, step_g, A.group);
+      const bool live = 32 * t + m < rows;
+      see = live ? visible_of(R, own_i) : 0;
+      z = lse0[live ? own_i * lse_tok + own_g : 0];
+      from.move(step_off, step_g, A.group, wrap);
+      own_i += step_i;
+      own_g += step_g;
+      if (own_g >= A.group) {
+        own_g -= A.group;
+        ++own_i;
+      }
     };
     uint16_t(*const mine)[D + 8] = rows_of_wave[wave];
-    if (32 * tile < rows) fetch();
+    if (32 * tile < rows) fetch(tile);
     for (; 32 * tile < rows; tile += shares) {
 #pragma unroll
       for (int c = 0; c < CH; ++c)
         *reinterpret_cast<uint4v*>(&mine[c * RC + lane / LR][lane % LR * 8]) = u[c];
       const float c0 = -z * kLog2e;
       const int seen = see;
-      if (32 * (tile + shares) < rows) fetch();
+      if (32 * (tile + shares) < rows) fetch(tile + shares);
       float16v x[2];
 #pragma unroll
       for (int t = 0; t < 2; ++t)

@@ -92,19 +92,21 @@ __device__ __forceinline__ void pick_best(int n, int need, PickLds<NT>& L, const
   uint32_t prefix = 0;
   uint32_t rest = (uint32_t)need;
   // the keys' bits `shift` .. of those that agree with `prefix` above `free` bits
-  const auto narrow = [&](int shift, uint32_t width, auto agrees) {
+  const auto narrow = [&](int shift, uint32_t width, bool all, auto agrees) {
     for (int i = tid; i < kBins; i += NT) L.hist[i] = 0;
     __syncthreads();
     each([&](int, uint32_t k) {
-      const uint64_t who = __ballot(agrees(k));
-      if (!who) return;
-      // lanes that all meet on one bin (equal weights) add once
       const uint32_t bin = (k >> shift) & width;
-      const uint32_t one = (uint32_t)__builtin_amdgcn_readlane((int)bin, __builtin_ctzll(who));
-      if (__ballot(agrees(k) && bin == one) == who) {
-        if (lane == 0) atomicAdd(&L.hist[one], (uint32_t)__popcll(who));
-      } else if (agrees(k)) {
-        atomicAdd(&L.hist[bin], 1u);
+      const uint64_t who = all ? ~0ull : __ballot(agrees(k));
+      if (!who) return;
+      // lanes that all meet on one bin (equal weights) add once. (Places without a key are in the
+      // lowest bin, whose count nobody needs.)
+      const uint32_t one = all ? (uint32_t)__builtin_amdgcn_readfirstlane((int)bin)
+                               : (uint32_t)__builtin_amdgcn_readlane((int)bin, __builtin_ctzll(who));
+      if (__ballot(bin != one) & who) {
+        if (all ? k != 0 : agrees(k)) atomicAdd(&L.hist[bin], 1u);
+      } else if (lane == 0) {
+        atomicAdd(&L.hist[one], (uint32_t)__popcll(who));
       }
     });
     __syncthreads();
@@ -138,9 +140,9 @@ __device__ __forceinline__ void pick_best(int n, int need, PickLds<NT>& L, const
     prefix |= L.digit << shift;
     rest = L.rest;
   };
-  narrow(21, 2047u, [](uint32_t k) { return k != 0; });   // (nobody meets on the bin of no key)
-  narrow(10, 2047u, [&](uint32_t k) { return (k ^ prefix) < (1u << 21); });
-  narrow(0, 1023u, [&](uint32_t k) { return (k ^ prefix) < (1u << 10); });
+  narrow(21, 2047u, true, [](uint32_t) { return true; });
+  narrow(10, 2047u, false, [&](uint32_t k) { return (k ^ prefix) < (1u << 21); });
+  narrow(0, 1023u, false, [&](uint32_t k) { return (k ^ prefix) < (1u << 10); });
 
   uint32_t na = 0, ne = 0;           // of the wave's run: taken for sure, and equal to the last
   each([&](int, uint32_t k) {
@@ -184,7 +186,6 @@ __device__ __forceinline__ int held_tokens(const KvSeqs& S, const int32_t* lengt
   return n > 0 ? n : 0;
 }
 
-constexpr int kKeepThreads = 1024;
 
 // The weights of one sequence and head as keys: a block is a page.
 struct MassKeys {
@@ -201,6 +202,8 @@ struct MassKeys {
     return order_key(__builtin_bit_cast(float, raw));
   }
 };
+
+constexpr int kKeepThreads = 1024;
 
 // One workgroup per (sequence, KV head): the tokens that stay.
 __global__ __launch_bounds__(kKeepThreads) void keep_kernel(KvPool pool, KvSeqs S,
@@ -252,7 +255,7 @@ __device__ __forceinline__ int code_size(int c) { return c < 0 ? -c : c; }
 // code times its scale. Bound by latency: lengths, kept, table and codes are read one after the
 // other, then 4 workgroups a CU.
 template <int D>
-__global__ __launch_bounds__(2 * D) void move_kernel(KvPool pool, KvSeqs S, KvSeqs to,
+__global__ __launch_bounds__(2 * D, 4) void move_kernel(KvPool pool, KvSeqs S, KvSeqs to,
                                                      const int32_t* __restrict__ lengths,
                                                      int max_len, float* mass, int keep,
                                                      const int32_t* __restrict__ kept,

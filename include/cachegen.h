@@ -482,7 +482,7 @@ typedef struct cg_kv8_attn {
   /* The weight each token got: mass_out [P][H][64] receives, for every token of the sequences,
    * decay * mass_in + the sum over the query tokens and the heads of its group of their softmax
    * weight on it. mass_in NULL: the sum alone; it may be mass_out. mass_out NULL: no weights. Not
-   * together with picks. */
+   * together with picks, nor for sequences that share pages. */
   const float* mass_in;
   float* mass_out;
   float decay;

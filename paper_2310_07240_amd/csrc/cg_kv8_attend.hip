@@ -449,7 +449,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_kernel(KvPool po
       page_scores<D>(K, Q, x);
       if (bn >= 0) load_k<D>(pool.k + bn * (kPage * D), K);
       const float w = page_softmax<D>(x, ks, pos0, Q, acc, p, keep, kept ? kept + pos0 : nullptr);
-      page_values<D>(V, p, keep, w * vs, acc);
+      // (a row that sees nothing of the page takes nothing of its scale, whatever that is)
+      page_values<D>(V, p, keep, w == 0.0f ? 0.0f : w * vs, acc);
       if (bn >= 0) load_v<D>(pool.v + bn * (kPage * D), V);
       b = bn;
     }
@@ -827,7 +828,7 @@ void prompt_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles, int splits, int64
     for (int e = 0; e < 16; ++e) o[dt][e] = 0.0f;
   float ref = -1e30f, l = 0.0f;      // O and l in units of 2^(ref - kLift)
   float ref0 = -1e30f, l0 = 0.0f;    // l of the pages without V, in units of 2^ref0
-  float v_top = 0.0f;
+  float v_top = 0x1p-40f;            // the largest V scale so far; below 2^-100 counts as none
 
   // The pages in turn, those that do not exist left out.
   int jn = j0;
@@ -845,45 +846,38 @@ void prompt_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles, int splits, int64
   const auto tile_step = [&](float16v x, const _Float16 (*k)[D + 8], const _Float16 (*next)[D + 8],
                              const _Float16 (*v)[kPage + 8], int pos0, float ks, float vs,
                              auto put) -> float16v {
-    const auto mask = [&](float16v& z) {               // where the tile ends beyond some row
-      if (pos0 + 32 > low) {
+    // What a row does not see is taken out behind the exponentials: then neither its scores nor
+    // the page's scales reach the row, whatever they are.
+    const bool cut = pos0 + 32 > low;                  // the tile ends beyond what some row sees
+    const auto mask = [&](float16v& z, float to) {
+      if (cut) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (pos0 + 16 * half + e >= visible) z[e] = kNegInf;
+        for (int e = 0; e < 16; ++e) z[e] = pos0 + 16 * half + e < visible ? z[e] : to;
       }
     };
-    mask(x);
-    // never 0, so that what is masked stays -inf (products of codes and queries are < 2^31)
-    const float f = fmaxf(unit * ks, 0x1p-120f);
-    // a V scale 2^60 below an earlier one (or 0) adds nothing to O, only its weights to a sum of
+    const float f = unit * ks;
+    // a V scale 2^60 below an earlier one (or none) adds nothing to O, only its weights to a sum of
     // their own: they must not move the reference that the others are rounded by
-    const bool with_v = vs > v_top * 0x1p-60f;
+    const bool with_v = !(vs <= v_top * 0x1p-60f);
     const float lv = with_v ? __builtin_amdgcn_logf(vs) + (float)kLift : 0.0f;
     const float c = with_v ? lv - ref : kNegInf;
     const float16v y = tile_scores<D>(next, q);
     float sum = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], f, c));
-      sum += x[e];
-    }
-    // requested before the weights are looked at, so that the products need not wait (and again
-    // behind the rare case, which has no registers for them)
+    for (int e = 0; e < 16; ++e) x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], f, c));
+    mask(x, 0.0f);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sum += x[e];
     half8 a[D / 32][2];
-    const auto values = [&] {
-#pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-          a[dt][e] = *reinterpret_cast<const half8*>(&v[32 * dt + m][16 * half + 8 * e]);
-    };
     if (__builtin_expect(__any(!(sum <= kMost)) || !with_v, 0)) {
-      float16v z = tile_scores<D>(k, q);
-      mask(z);
-      float t = z[0];
+      const float16v z = tile_scores<D>(k, q);
+      float16v seen = z;
+      mask(seen, kNegInf);
+      float t = seen[0];
 #pragma unroll
-      for (int e = 1; e < 16; ++e) t = max2(t, z[e]);
-      t = half_max(t) * f;
+      for (int e = 1; e < 16; ++e) t = max2(t, seen[e]);
+      t = half_max(t);
+      t = t == kNegInf ? t : t * f;
       if (with_v) {
         const float now = fmaxf(ref, t + lv - (float)kLift);
         const float g = __builtin_amdgcn_exp2f(ref - now);
@@ -895,21 +889,32 @@ void prompt_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles, int splits, int64
           for (int e = 0; e < 16; ++e) o[dt][e] *= g;
         sum = 0.0f;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
+        for (int e = 0; e < 16; ++e)
           x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[e], f, lv - ref));
-          sum += x[e];
-        }
+        mask(x, 0.0f);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sum += x[e];
       } else {
         const float now = fmaxf(ref0, t);
         l0 *= __builtin_amdgcn_exp2f(ref0 - now);
         ref0 = now;
+        float16v w;
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          l0 += __builtin_amdgcn_exp2f(__builtin_fmaf(z[e], f, -now));
+        for (int e = 0; e < 16; ++e) w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[e], f, -now));
+        mask(w, 0.0f);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) l0 += w[e];
+        sum = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = 0.0f;
       }
     }
-    values();
-    l = __builtin_fmaf(sum, with_v ? 1.0f / vs : 0.0f, l);
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        a[dt][e] = *reinterpret_cast<const half8*>(&v[32 * dt + m][16 * half + 8 * e]);
+    l = sum == 0.0f ? l : __builtin_fmaf(sum, __builtin_amdgcn_rcpf(vs), l);
     half8 p[2];
 #pragma unroll
     for (int e = 0; e < 16; e += 2) {
@@ -969,7 +974,7 @@ void prompt_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles, int splits, int64
   }
   int k0 = 0, k1 = 1;                // K buffers of this page and the next
   for (int buf = 0; at[0] >= 0; buf ^= 1) {
-    v_top = fmaxf(v_top, vs);
+    v_top = vs < __builtin_inff() ? fmaxf(v_top, vs) : v_top;
     const int k2 = kAhead == 2 ? 3 - k0 - k1 : k0;
     const int pos0 = pos[0] * kPage;
     x = tile_step(x, L.k[k0], L.k[k0] + 32, L.v[buf], pos0, ks, vs,

@@ -321,6 +321,30 @@ def test_attend_nan_query_stays_in_its_row():
         assert torch.isnan(got[0, 1, 2]).all()
 
 
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("which", ["k_scale", "v_scale"])
+@pytest.mark.parametrize("Q,HQ,D", [(8, 2, 128), (80, 3, 64), (70, 2, 256), (300, 1, 128)])
+def test_attend_bad_scale_stays_with_who_sees_it(bad, which, Q, HQ, D):
+    """NaN or Inf as the scale of the sequence's last page: the queries before it are as without
+    it, bit for bit. Those that see it are not finite, except under an infinite K scale, whose
+    logits of minus infinity are weights of 0."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(13)
+    t, table, n = tables(torch, rng, 1, 6)
+    cache = make(torch, n, 1, D)
+    q = torch.randn(1, Q, HQ, D).half().cuda()
+    length = 5 * 64 + 3                        # the last three queries see the last page
+    good = cache.attend(q, table, ints(torch, [length]))
+    getattr(cache, which)[int(t[0, 5])] = bad
+    mass = torch.zeros((n, 1, PAGE), device="cuda")
+    got = cache.attend(q, table, ints(torch, [length]), mass=mass)
+    assert torch.equal(got[:, :Q - 3], good[:, :Q - 3]) and not torch.isnan(good).any()
+    if which == "v_scale" or bad != bad:
+        assert not torch.isfinite(got[:, Q - 3:]).any()
+    if which == "k_scale" and bad != bad:
+        assert torch.isnan(mass[int(t[0, 5]), 0, 0])
+
+
 @pytest.mark.parametrize("scale", [-0.3, 0.0, 3.0])
 def test_attend_scales_and_extremes(scale):
     """Logits far apart (a few hundred), equal, and in reverse; one heavy token before a long

@@ -849,10 +849,11 @@ void prompt_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles, int splits, int64
     // What a row does not see is taken out behind the exponentials: then neither its scores nor
     // the page's scales reach the row, whatever they are.
     const bool cut = pos0 + 32 > low;                  // the tile ends beyond what some row sees
+    const int seen_here = visible - pos0 - 16 * half;  // of the lane's 16 tokens
     const auto mask = [&](float16v& z, float to) {
       if (cut) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) z[e] = pos0 + 16 * half + e < visible ? z[e] : to;
+        for (int e = 0; e < 16; ++e) z[e] = e < seen_here ? z[e] : to;
       }
     };
     const float f = unit * ks;

@@ -141,13 +141,22 @@ __device__ __forceinline__ void write_bounds(int8_t* bounds, const StoreLds<D>& 
   bounds[tid] = (int8_t)b;
 }
 
+// Code (r, c) of a thread's four rows and eight channels: K's words hold four channels of a row,
+// V's the four rows of a channel.
+template <bool IS_V>
+__device__ __forceinline__ int8_t kept_code(const uint32_t* w, int r, int c) {
+  return (int8_t)(IS_V ? w[c] >> (8 * r) : w[2 * r + (c >> 2)] >> (8 * (c & 3)));
+}
+
 // Writes one page of a head from the 2 D threads' rows x[4][8]: thread (rg, cg) = (tid / (D / 8),
 // tid % (D / 8)) has rows 4 rg .. 4 rg + 3 of channels 8 cg .. 8 cg + 7. Rows held .. end - 1 are
-// new, the `held` before them keep their codes (re-coded where the scale grows), rows from `end`
-// on become zero codes. Codes, scale and, for K, the channels' bounds go to memory.
-template <int D, bool IS_V>
+// new, the `held` before them (KEPT: the page's codes `was` under its scale s_old) keep their codes,
+// re-coded where the scale grows; rows from `end` on become zero codes. Codes, scale and, for K,
+// the channels' bounds go to memory.
+template <int D, bool IS_V, bool KEPT>
 __device__ __forceinline__ void put_page(const KvPool& pool, int page, int h, const float x[4][8],
-                                         int held, int end, StoreLds<D>& L) {
+                                         const uint32_t* was, float s_old, int held, int end,
+                                         StoreLds<D>& L) {
   constexpr int NT = 2 * D;
   const int tid = threadIdx.x, cg = tid % (D / 8), rg = tid / (D / 8);
   const int64_t at = (int64_t)page * pool.H + h;
@@ -163,36 +172,27 @@ __device__ __forceinline__ void put_page(const KvPool& pool, int page, int h, co
         m = a <= 3.4028234e38f ? fmaxf(m, a) : m;     // NaN and Inf set no scale
       }
   m = wg_max<NT>(m, L.red);
-  float s = m / 127.0f, s_old = 0.0f;
-  if (held > 0) {
-    s_old = *scale;
-    s = fmaxf(s, s_old);
-  }
+  float s = m / 127.0f;
+  if (KEPT) s = fmaxf(s, s_old);
   const float inv = s > 0.0f ? 1.0f / s : 0.0f;
   const bool tiny = s < 0x1p-100f;
   int q[4][8];
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     const int t = 4 * rg + r;
-    if (t < held) {
-      int8_t was[8];
-      if (IS_V) {
+    if (KEPT && t < held) {
 #pragma unroll
-        for (int c = 0; c < 8; ++c) was[c] = codes[(8 * cg + c) * kPage + t];
-      } else {
-        *reinterpret_cast<uint2v*>(was) =
-            *reinterpret_cast<const uint2v*>(codes + t * D + 8 * cg);
+      for (int c = 0; c < 8; ++c) {
+        const int code = kept_code<IS_V>(was, r, c);
+        q[r][c] = s == s_old ? code : kv_code((float)code * s_old, s, inv, tiny);
       }
-#pragma unroll
-      for (int c = 0; c < 8; ++c)
-        q[r][c] = s == s_old ? (int)was[c] : kv_code((float)was[c] * s_old, s, inv, tiny);
     } else {
 #pragma unroll
       for (int c = 0; c < 8; ++c)
         q[r][c] = t < end && s > 0.0f ? kv_code(x[r][c], s, inv, tiny) : 0;
     }
   }
-  __syncthreads();                   // every old code and the old scale are read
+  __syncthreads();                   // all that the page held is read
   if (tid == 0) *scale = s;
   if (IS_V) {
 #pragma unroll
@@ -264,10 +264,11 @@ __device__ __forceinline__ uint32_t low_bytes(float a, float b, float c, float d
   return ab | cd;
 }
 
-// A page whose rows are all new, finite and of scales far from the subnormals: put_page's result
-// for K and V together, under the scales ks, vs of their maxima, with one barrier.
+// A page of finite rows and scales far from the subnormals: put_page's result for K and V together,
+// under the scales ks, vs, with one barrier. Rows that stay in place are given as codes times
+// their scale, which return to their codes where the scale is the same.
 template <int D, class KRows, class VRows>
-__device__ __forceinline__ void put_fresh(const KvPool& pool, int64_t at, const KRows& k,
+__device__ __forceinline__ void put_plain(const KvPool& pool, int64_t at, const KRows& k,
                                           const VRows& v, int end, float ks, float vs,
                                           StoreLds<D>& L) {
   const int tid = threadIdx.x, cg = tid % (D / 8), rg = tid / (D / 8);
@@ -302,33 +303,35 @@ __device__ __forceinline__ void put_fresh(const KvPool& pool, int64_t at, const 
     L.hi[w] = low_bytes(hi[0], hi[1], hi[2], hi[3]);
     L.hi[w + 1] = low_bytes(hi[4], hi[5], hi[6], hi[7]);
   }
+  __syncthreads();                   // all that the page held is read, its scales too
   if (tid == 0) {
     pool.ks[at] = ks;
     pool.vs[at] = vs;
   }
-  __syncthreads();
   write_v<D>(pool.v + at * (kPage * D), L);
   if (pool.bounds) write_bounds<D>(pool.bounds + at * (2 * D), L);
 }
 
-// put_page for K and V of any page.
-template <int D, class KRows, class VRows>
+// put_page for K and V of any page; of one that keeps tokens, kc and vc are their codes.
+template <int D, bool KEPT, class KRows, class VRows>
 __device__ __forceinline__ void put_any(const KvPool& pool, int page, int h, const KRows& k,
-                                        const VRows& v, int held, int end, StoreLds<D>& L) {
+                                        const VRows& v, int held, int end, StoreLds<D>& L,
+                                        const uint32_t* kc = nullptr, float ks_old = 0.0f,
+                                        const uint32_t* vc = nullptr, float vs_old = 0.0f) {
   float x[4][8];
 #pragma unroll
   for (int r = 0; r < 4; ++r)
 #pragma unroll
     for (int c = 0; c < 8; ++c) x[r][c] = k.value(r, c);
-  put_page<D, false>(pool, page, h, x, held, end, L);
+  put_page<D, false, KEPT>(pool, page, h, x, kc, ks_old, held, end, L);
 #pragma unroll
   for (int r = 0; r < 4; ++r)
 #pragma unroll
     for (int c = 0; c < 8; ++c) x[r][c] = v.value(r, c);
-  put_page<D, true>(pool, page, h, x, held, end, L);
+  put_page<D, true, KEPT>(pool, page, h, x, vc, vs_old, held, end, L);
 }
 
-// Whether put_fresh may code under this scale.
+// Whether put_plain may code under this scale.
 __device__ __forceinline__ bool plain_scale(float s) { return s == 0.0f || s >= 0x1p-100f; }
 
 // Launchers; arguments are checked by the C ABI.

@@ -357,9 +357,9 @@ __global__ __launch_bounds__(2 * D, 4) void move_kernel(KvPool pool, KvSeqs S, K
     const float v_new = __builtin_bit_cast(float, v_top) / 127.0f;
     const bool finite = k_top < 0x7f800000u && v_top < 0x7f800000u;
     if (finite && plain_scale(k_new) && plain_scale(v_new))
-      put_fresh<D>(pool, at, MovedK{kc, ks}, MovedV{vw, vs}, end, k_new, v_new, L);
+      put_plain<D>(pool, at, MovedK{kc, ks}, MovedV{vw, vs}, end, k_new, v_new, L);
     else
-      put_any<D>(pool, page, h, MovedK{kc, ks}, MovedV{vw, vs}, 0, end, L);
+      put_any<D, false>(pool, page, h, MovedK{kc, ks}, MovedV{vw, vs}, 0, end, L);
     __syncthreads();
   }
 }

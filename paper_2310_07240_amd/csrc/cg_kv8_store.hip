@@ -6,6 +6,9 @@
 // 2 D-byte rows and four tokens of a channel meet in one lane, as the transposed V codes want
 // them. The scale is the page's absolute maximum over 127, and the page is held in registers from
 // its maximum to its codes: one read of the rows, one write of the codes. Bound by those bytes.
+// Store: 537 MB of fp16 rows in and 268 MB of codes out in 176 us, 4.6 TB/s; load, the other way
+// round, 149 us, 5.4 TB/s (a copy of 1 GiB: 5.1). A call of one token for each of 8 requests is a
+// chain of dependent reads: start, table, rows and codes; 8.4 us and 5.9.
 #include "cg_kv8.h"
 
 namespace {
@@ -33,7 +36,7 @@ __device__ __forceinline__ ushort2v top_bits(const uint4v u[4]) {
   return m;
 }
 
-// A thread's rows as values (what put_fresh takes).
+// A thread's rows as values (what put_plain takes).
 template <bool BF16>
 struct NewRows {
   const uint4v* u;
@@ -42,15 +45,112 @@ struct NewRows {
   }
 };
 
-template <int D, bool BF16, bool VEC>
-__global__ __launch_bounds__(2 * D) void store_kernel(KvPool pool, KvSeqs S,
+// The same where the first `old` rows are the page's own, as codes under its last scale: K's row
+// by row, V's (KEPT_V) channel by channel.
+template <bool BF16, bool KEPT_V>
+struct KeptRows {
+  const uint4v* u;
+  const uint32_t* codes;
+  int old;
+  float scale;
+  __device__ __forceinline__ float value(int r, int c) const {
+    return r < old ? (float)kept_code<KEPT_V>(codes, r, c) * scale
+                   : kv_widen<BF16>((uint16_t)(u[r][c >> 1] >> (16 * (c & 1))));
+  }
+};
+
+// Whether put_plain may code a page of scale `old` on under max(old, fresh): both plain and one not
+// zero, and no product of a code and `old` overflows.
+__device__ __forceinline__ bool kept_plain(float old, float fresh) {
+  return plain_scale(old) && old <= 0x1p120f && plain_scale(fresh) && fmaxf(old, fresh) > 0.0f;
+}
+
+// One page of a head: rows `held` .. last - 1 from k, v, which point at the page's first row.
+// KEPT: the page keeps `held` > 0 tokens, whose codes and scales are requested with the rows: one
+// token behind the tokens of 8 requests takes 8.4 us, and 12.0 where they are read after the rows'
+// maximum, K's and V's in turn. Returns whether all rows are finite.
+template <int D, bool BF16, bool VEC, bool KEPT>
+__device__ __forceinline__ bool store_page(const KvPool& pool, int page, int h, const uint16_t* k,
+                                           int64_t k_tok, const uint16_t* v, int64_t v_tok,
+                                           int held, int last, ushort2v* tops, StoreLds<D>& L) {
+  const int tid = threadIdx.x, cg = tid % (D / 8), rg = tid / (D / 8);
+  const int64_t at = (int64_t)page * pool.H + h;
+  uint4v x[4], y[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int t = 4 * rg + r;
+    x[r] = y[r] = uint4v{0, 0, 0, 0};
+    if (t >= held && t < last) {
+      x[r] = get8<VEC>(k + t * k_tok + 8 * cg);
+      y[r] = get8<VEC>(v + t * v_tok + 8 * cg);
+    }
+  }
+  const int old = held - 4 * rg;                      // of this thread's rows (0 or less: none)
+  uint32_t kc[8], vc[8];
+  float ks_old = 0.0f, vs_old = 0.0f;
+  if constexpr (KEPT) {
+    ks_old = pool.ks[at];
+    vs_old = pool.vs[at];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      uint2v w = {0, 0};
+      if (r < old)
+        w = *reinterpret_cast<const uint2v*>(pool.k + at * (kPage * D) + (4 * rg + r) * D + 8 * cg);
+      kc[2 * r] = w[0];
+      kc[2 * r + 1] = w[1];
+    }
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+      vc[c] = old > 0 ? *reinterpret_cast<const uint32_t*>(pool.v + at * (kPage * D) +
+                                                           (8 * cg + c) * kPage + 4 * rg)
+                      : 0u;
+  }
+  // the maxima of both, K's in the high half: magnitude bits are ordered as the magnitudes are
+  const ushort2v mx = top_bits(x), my = top_bits(y);
+  ushort2v m = {my[0] > my[1] ? my[0] : my[1], mx[0] > mx[1] ? mx[0] : mx[1]};
+#pragma unroll
+  for (int o = 32; o; o >>= 1)
+    m = __builtin_elementwise_max(
+        m, __builtin_bit_cast(ushort2v, __shfl_xor(__builtin_bit_cast(int, m), o)));
+  __syncthreads();                   // the last page's LDS is read
+  if ((tid & 63) == 0) tops[tid >> 6] = m;
+  __syncthreads();
+  m = tops[0];
+#pragma unroll
+  for (int w = 1; w < 2 * D / 64; ++w) m = __builtin_elementwise_max(m, tops[w]);
+  constexpr uint16_t kInf = BF16 ? 0x7f80 : 0x7c00;
+  const bool finite = m[0] < kInf && m[1] < kInf;
+  float ks = kv_widen<BF16>(m[1]) / 127.0f, vs = kv_widen<BF16>(m[0]) / 127.0f;
+  if (!KEPT && finite && plain_scale(ks) && plain_scale(vs)) {
+    put_plain<D>(pool, at, NewRows<BF16>{x}, NewRows<BF16>{y}, last, ks, vs, L);
+  } else if (KEPT && finite && kept_plain(ks_old, ks) && kept_plain(vs_old, vs)) {
+    ks = fmaxf(ks, ks_old);
+    vs = fmaxf(vs, vs_old);
+    put_plain<D>(pool, at, KeptRows<BF16, false>{x, kc, old, ks_old},
+                 KeptRows<BF16, true>{y, vc, old, vs_old}, last, ks, vs, L);
+  } else {
+    put_any<D, KEPT>(pool, page, h, NewRows<BF16>{x}, NewRows<BF16>{y}, held, last, L, kc, ks_old,
+                     vc, vs_old);
+  }
+  return finite;
+}
+
+// Which pages a launch is for: those that keep tokens (a sequence's first, if any), those that do
+// not, or both. Keeping takes 187 registers where coding new rows takes 128, so one kernel for both
+// leaves two waves on a SIMD: 217 us for 805 MB of rows and codes, against 176 (4.6 TB/s) and 5 for
+// the second launch with one for each. Up to kFewPages pages all run at once anyway, and one launch
+// for both is the shorter.
+enum Pages { kBoth, kNew, kKept };
+
+template <int D, bool BF16, bool VEC, Pages WHICH>
+__global__ __launch_bounds__(2 * D, WHICH == kNew ? 4 : 2) void store_kernel(KvPool pool, KvSeqs S,
                                                       const int32_t* __restrict__ starts,
                                                       const int32_t* __restrict__ counts,
                                                       int n_tokens, int np, int64_t items,
                                                       KvRows k, KvRows v, uint32_t* status) {
   __shared__ StoreLds<D> L;
   __shared__ ushort2v tops[2 * D / 64];
-  const int tid = threadIdx.x, cg = tid % (D / 8), rg = tid / (D / 8);
+  const int tid = threadIdx.x;
   uint32_t bad = 0;
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const int h = (int)(it % pool.H);
@@ -63,47 +163,22 @@ __global__ __launch_bounds__(2 * D) void store_kernel(KvPool pool, KvSeqs S,
     const int64_t j = start / kPage + r0 % np;        // the sequence's page
     const int64_t end = (int64_t)start + count;
     if (j * kPage >= end) continue;
+    const int held = start > j * kPage ? (int)(start - j * kPage) : 0;
+    if (WHICH != kBoth && (held > 0) != (WHICH == kKept)) continue;
     const int page = j < S.width ? kv_page(S, pool.P, seq, (int)j) : -1;
     if (page < 0) continue;                           // no such page: nothing is written
-    const int held = start > j * kPage ? (int)(start - j * kPage) : 0;
     const int last = end - j * kPage < kPage ? (int)(end - j * kPage) : kPage;
     const int64_t row0 = j * kPage - start;           // row of the page's first token
-    uint4v x[4], y[4];
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int t = 4 * rg + r;
-      x[r] = y[r] = uint4v{0, 0, 0, 0};
-      if (t >= held && t < last) {
-        const int64_t row = row0 + t;
-        x[r] = get8<VEC>(static_cast<const uint16_t*>(k.p) + seq * k.seq + row * k.tok +
-                         h * k.head + 8 * cg);
-        y[r] = get8<VEC>(static_cast<const uint16_t*>(v.p) + seq * v.seq + row * v.tok +
-                         h * v.head + 8 * cg);
-      }
-    }
-    // the maxima of both, K's in the high half: magnitude bits are ordered as the magnitudes are
-    const ushort2v mx = top_bits(x), my = top_bits(y);
-    ushort2v m = {my[0] > my[1] ? my[0] : my[1], mx[0] > mx[1] ? mx[0] : mx[1]};
-#pragma unroll
-    for (int o = 32; o; o >>= 1)
-      m = __builtin_elementwise_max(
-          m, __builtin_bit_cast(ushort2v, __shfl_xor(__builtin_bit_cast(int, m), o)));
-    __syncthreads();                 // the last page's LDS is read
-    if ((tid & 63) == 0) tops[tid >> 6] = m;
-    __syncthreads();
-    m = tops[0];
-#pragma unroll
-    for (int w = 1; w < 2 * D / 64; ++w) m = __builtin_elementwise_max(m, tops[w]);
-    constexpr uint16_t kInf = BF16 ? 0x7f80 : 0x7c00;
-    const bool finite = m[0] < kInf && m[1] < kInf;
+    const uint16_t* kp = static_cast<const uint16_t*>(k.p) + seq * k.seq + row0 * k.tok + h * k.head;
+    const uint16_t* vp = static_cast<const uint16_t*>(v.p) + seq * v.seq + row0 * v.tok + h * v.head;
+    bool finite;
+    if (WHICH != kNew && held > 0)
+      finite = store_page<D, BF16, VEC, true>(pool, page, h, kp, k.tok, vp, v.tok, held, last, tops,
+                                              L);
+    else if (WHICH != kKept)
+      finite = store_page<D, BF16, VEC, false>(pool, page, h, kp, k.tok, vp, v.tok, 0, last, tops,
+                                               L);
     bad |= finite ? 0u : 1u;
-    const float ks = kv_widen<BF16>(m[1]) / 127.0f, vs = kv_widen<BF16>(m[0]) / 127.0f;
-    if (finite && plain_scale(ks) && plain_scale(vs) && held == 0) {
-      put_fresh<D>(pool, (int64_t)page * pool.H + h, NewRows<BF16>{x}, NewRows<BF16>{y}, last, ks,
-                   vs, L);
-    } else {
-      put_any<D>(pool, page, h, NewRows<BF16>{x}, NewRows<BF16>{y}, held, last, L);
-    }
   }
   if (status && __any(bad) && (tid & 63) == 0) atomicOr(status, 1u);
 }
@@ -202,19 +277,32 @@ int touched(int n) { return (int)(((int64_t)n + 2 * kPage - 2) / kPage); }
 // kernels walk on where there are more.
 unsigned grid_of(int64_t items) { return (unsigned)(items < (1 << 22) ? items : (1 << 22)); }
 
-template <int D, bool BF16>
+constexpr int64_t kFewPages = 2048;
+
+template <int D, bool BF16, bool VEC>
 hipError_t store_d(const KvPool& pool, const KvSeqs& S, const int32_t* starts,
                    const int32_t* counts, int n, const KvRows& k, const KvRows& v,
                    uint32_t* status, hipStream_t st) {
   const int np = touched(n);
-  const int64_t items = (int64_t)S.n * np * pool.H;
-  if (wide(k) && wide(v))
-    hipLaunchKernelGGL((store_kernel<D, BF16, true>), dim3(grid_of(items)), dim3(2 * D), 0, st,
+  const int64_t items = (int64_t)S.n * np * pool.H, first = (int64_t)S.n * pool.H;
+  if (items <= kFewPages) {
+    hipLaunchKernelGGL((store_kernel<D, BF16, VEC, kBoth>), dim3(grid_of(items)), dim3(2 * D), 0, st,
                        pool, S, starts, counts, n, np, items, k, v, status);
-  else
-    hipLaunchKernelGGL((store_kernel<D, BF16, false>), dim3(grid_of(items)), dim3(2 * D), 0, st,
+  } else {
+    hipLaunchKernelGGL((store_kernel<D, BF16, VEC, kNew>), dim3(grid_of(items)), dim3(2 * D), 0, st,
                        pool, S, starts, counts, n, np, items, k, v, status);
+    hipLaunchKernelGGL((store_kernel<D, BF16, VEC, kKept>), dim3(grid_of(first)), dim3(2 * D), 0, st,
+                       pool, S, starts, counts, n, 1, first, k, v, status);
+  }
   return hipGetLastError();
+}
+
+template <int D, bool BF16>
+hipError_t store_w(const KvPool& pool, const KvSeqs& S, const int32_t* starts,
+                   const int32_t* counts, int n, const KvRows& k, const KvRows& v,
+                   uint32_t* status, hipStream_t st) {
+  return (wide(k) && wide(v) ? store_d<D, BF16, true> : store_d<D, BF16, false>)(
+      pool, S, starts, counts, n, k, v, status, st);
 }
 
 template <int D, bool BF16>
@@ -241,9 +329,9 @@ hipError_t cg_launch_kv8_store(const KvPool& pool, const KvSeqs& S, int D, bool 
   if (status) hipLaunchKernelGGL(kv_zero_word, dim3(1), dim3(1), 0, st, status);
   if (n <= 0) return hipGetLastError();
   switch (D) {
-    case 64: return (bf16 ? store_d<64, true> : store_d<64, false>)(pool, S, starts, counts, n, k, v, status, st);
-    case 128: return (bf16 ? store_d<128, true> : store_d<128, false>)(pool, S, starts, counts, n, k, v, status, st);
-    default: return (bf16 ? store_d<256, true> : store_d<256, false>)(pool, S, starts, counts, n, k, v, status, st);
+    case 64: return (bf16 ? store_w<64, true> : store_w<64, false>)(pool, S, starts, counts, n, k, v, status, st);
+    case 128: return (bf16 ? store_w<128, true> : store_w<128, false>)(pool, S, starts, counts, n, k, v, status, st);
+    default: return (bf16 ? store_w<256, true> : store_w<256, false>)(pool, S, starts, counts, n, k, v, status, st);
   }
 }
 

@@ -187,6 +187,50 @@ def test_store_extreme_sizes(size):
     same_cache(cache, ref)
 
 
+@pytest.mark.parametrize("D,H,dtype,T,starts", [(64, 2, "float16", 1, [0, 1, 37, 63, 64, 127]),
+                                                (128, 3, "bfloat16", 30, [0, 1, 37, 63, 64, 127]),
+                                                (256, 1, "float16", 130, [5, 64, 66]),
+                                                (64, 32, "bfloat16", 2200, [37, 64])])
+@pytest.mark.parametrize("size", [0.1, 30.0, 0.0, 1e-38, 1e38])
+def test_store_behind_tokens(D, H, dtype, T, starts, size):
+    """Rows behind tokens that a page keeps: far smaller (the scale stays), far larger (it grows and
+    the codes are made anew), zero, subnormal or near the largest of their type."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(T)
+    B = len(starts)
+    t, table, n = tables(torch, rng, B, (max(starts) + T) // PAGE + 1)
+    cache = make(torch, n, H, D)
+    ref = R.Ref(cache)
+    dt = getattr(torch, dtype)
+    rows = lambda m, f: ((torch.rand(B, m, H, D) * 2 - 1) * f).to(dt)
+    top = min(size, 6e4) if dtype == "float16" else size
+    for m, at, count, f in ((max(starts), [0] * B, starts, 1.0), (T, starts, [T] * B, top)):
+        k, v = rows(m, f), rows(m, f)
+        say(f"store {D} {H} {dtype} {m} rows of size {f}")
+        cache.store(k.cuda(), v.cuda(), table, ints(torch, at), ints(torch, count))
+        torch.cuda.synchronize()
+        ref.store(k.float().numpy(), v.float().numpy(), t, at, count)
+        same_cache(cache, ref)
+
+
+@pytest.mark.parametrize("was", [0.0, 1e-39, 2.0 ** 121, float("inf")])
+def test_store_behind_odd_scales(was):
+    """A page whose scale is zero under codes that are not, subnormal, huge or infinite."""
+    torch = torch_cuda()
+    cache = make(torch, 3, 2, 64)
+    t = np.array([[1]], np.int32)
+    table = torch.from_numpy(t).cuda()
+    k = torch.randn(1, 20, 2, 64).half()
+    cache.store(k.cuda(), -k.cuda(), table, ints(torch, [0]))
+    cache.k_scale[1], cache.v_scale[1, 1] = was, was
+    for new in (torch.zeros_like(k), k):
+        ref = R.Ref(cache)
+        cache.store(new.cuda(), new.cuda(), table, ints(torch, [20]))
+        torch.cuda.synchronize()
+        ref.store(new.float().numpy(), new.float().numpy(), t, [20], [20])
+        same_cache(cache, ref)
+
+
 # ---- attention --------------------------------------------------------------------------------
 def check_attend(torch, cache, q, table, t, lengths, q_lens=None, picks=None, mass=False,
                  scale=None, max_len=None, decay=0.5):

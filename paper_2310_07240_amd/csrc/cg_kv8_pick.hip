@@ -19,25 +19,44 @@ __device__ __forceinline__ uint32_t lanes_below(uint64_t mask) {
                                    __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
 
-constexpr int kBins = 2048;          // of a pass: 11 bits of the keys
+// f over the lanes up to this one (lane 63: over all): steps within rows of 16 lanes, then lane 15's
+// result into the second and fourth row's and lane 31's into the upper half's. `none` is f's
+// identity. (Moves between lanes in the vector unit itself; __shfl_up goes through the LDS.)
+template <class F>
+__device__ __forceinline__ uint32_t over_lanes(uint32_t v, uint32_t none, F f) {
+  v = f(v, (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, 0x111, 0xf, 0xf, false));
+  v = f(v, (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, 0x112, 0xf, 0xf, false));
+  v = f(v, (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, 0x114, 0xf, 0xf, false));
+  v = f(v, (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, 0x118, 0xf, 0xf, false));
+  v = f(v, (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, 0x142, 0xa, 0xf, false));
+  return f(v, (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, 0x143, 0xc, 0xf, false));
+}
+
+constexpr int kBins = 2048;          // of a pass: 11 bits
+
+// Each counted in copies that the lanes of a wave take in turn: weights crowd into a few octaves and
+// may be equal, and lanes that meet on one word wait for each other.
+template <int NT>
+constexpr int kCopies = NT / 256;
 
 template <int NT>
 struct PickLds {
-  uint32_t hist[kBins];
+  __align__(16) uint32_t hist[kBins * kCopies<NT>];
   uint32_t above[NT / 64], equal[NT / 64];
-  uint32_t digit, rest;
+  uint32_t digit, rest, whole;
 };
 
 // The best `need` (1 <= need < n) of n keys: emit(position, index) for each, positions ascending
 // with the index. Of a block j of 64 keys, place(j) says where it lies (below 0: nowhere, its keys
 // are the lowest), raw() loads and key() makes the key of index 64 j + lane; they are called apart
 // so that no load waits for another. Places from n on get 0, which is no key. Every wave has a run
-// of whole blocks, the first kHeld of them in registers, so the keys are read once. Three passes over the keys' bits, highest first,
-// narrow them to the smallest key that is taken and the number of its equals that are; then each
-// wave counts and emits its run by ballots. Counts are whole numbers, so no order of the LDS
-// additions changes anything. Bound by the vector instructions of the one CU (about 45 a block in
-// all) and the first pass's LDS additions: weights crowd into a few octaves, so lanes meet on a bin,
-// hence 11 bits and not 8.
+// of whole blocks, the first kHeld of them in registers, so the keys are read once. Passes over the
+// keys, 11 bits of their distance from the lowest positive one at a time, narrow them to the smallest
+// key that is taken and the number of its equals that are: over the range that the keys do take,
+// two passes are enough as a rule, since a bin taken whole ends them. Then each wave counts and emits
+// its run by ballots. Counts are whole numbers, so no order of the LDS additions changes anything.
+// 65536 keys of one workgroup: 20 us at 2.3 GHz, of which the loads take 7 (what one CU gets from
+// memory), the first pass 4.5, the second 2.7, the rest is ballots and barriers.
 template <int NT, int kHeld, class Keys, class Emit>
 __device__ __forceinline__ void pick_best(int n, int need, PickLds<NT>& L, const Keys& keys,
                                           Emit emit) {
@@ -48,30 +67,34 @@ __device__ __forceinline__ void pick_best(int n, int need, PickLds<NT>& L, const
   const int first = wave * per;
   const int mine = first + per < blocks ? per : blocks > first ? blocks - first : 0;
   uint32_t held[kHeld];
-  // a lane finds a block's place, then eight blocks are on their way at once
+  // a lane finds a block's place, then all blocks are on their way at once
   const int place = keys.place(first + (lane < mine ? lane : 0));
+  int lost = 0;
 #pragma unroll
   for (int r = 0; r < kHeld; r += 8)
     if (r < mine) {
-      uint32_t raw[8];
-      int at[8], lost = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        at[i] = __builtin_amdgcn_readlane(place, r + i);
-        lost |= at[i];
-        raw[i] = keys.raw(at[i], first + (r + i < mine ? r + i : 0), lane);
+      for (int i = r; i < r + 8; ++i) {
+        const int at = __builtin_amdgcn_readlane(place, i);
+        lost |= at;
+        held[i] = keys.raw(at, first + (i < mine ? i : 0), lane);
       }
+    }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) held[r + i] = keys.key(raw[i]);
+  for (int r = 0; r < kHeld; r += 8)
+    if (r < mine) {
+#pragma unroll
+      for (int i = r; i < r + 8; ++i) held[i] = keys.key(held[i]);
       // blocks that lie nowhere, and the end of the run or of the keys
       if (lost < 0) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) held[r + i] = at[i] < 0 ? 1u : held[r + i];
+        for (int i = r; i < r + 8; ++i)
+          held[i] = __builtin_amdgcn_readlane(place, i) < 0 ? 1u : held[i];
       }
       if (r + 8 >= mine) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          held[r + i] = r + i < mine && (first + r + i) * 64 + lane < n ? held[r + i] : 0u;
+        for (int i = r; i < r + 8; ++i)
+          held[i] = i < mine && (first + i) * 64 + lane < n ? held[i] : 0u;
       }
     }
   // f(block, key) for the wave's keys, eight blocks of registers a branch
@@ -89,25 +112,42 @@ __device__ __forceinline__ void pick_best(int n, int need, PickLds<NT>& L, const
     }
   };
 
-  uint32_t prefix = 0;
+  constexpr uint32_t kZero = 0x80000000u;              // the key of 0
+  uint32_t low = ~0u, high = 0;      // the lowest key above kZero, less kZero + 1, and the highest
+  each([&](int, uint32_t k) {
+    low = k - kZero - 1 < low ? k - kZero - 1 : low;
+    high = k > high ? k : high;
+  });
+  low = over_lanes(low, ~0u, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+  high = over_lanes(high, 0u, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+  if (lane == 63) {
+    L.above[wave] = low;
+    L.equal[wave] = high;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    low = L.above[w] < low ? L.above[w] : low;
+    high = L.equal[w] > high ? L.equal[w] : high;
+  }
+  low = __builtin_amdgcn_readfirstlane(low);
+  high = __builtin_amdgcn_readfirstlane(high);
+  // The last key taken lies in prefix .. prefix + span - 1, or, before the first pass, below that.
+  uint32_t prefix = low < kZero ? low + kZero + 1 : 1, span = high - prefix + 1;
   uint32_t rest = (uint32_t)need;
-  // the keys' bits `shift` .. of those that agree with `prefix` above `free` bits
-  const auto narrow = [&](int shift, uint32_t width, bool all, auto agrees) {
-    for (int i = tid; i < kBins; i += NT) L.hist[i] = 0;
+  bool first_pass = true;
+  do {
+    const int bits = span > 1 ? 32 - __builtin_clz(span - 1) : 0;
+    const int shift = bits > 11 ? bits - 11 : 0;
+    uint4v* bins = reinterpret_cast<uint4v*>(L.hist);
+#pragma unroll
+    for (int i = 0; i < kBins * kCopies<NT> / 4 / NT; ++i) bins[i * NT + tid] = uint4v{0, 0, 0, 0};
     __syncthreads();
+    // digits from 1 up, digit d in bin d - 1: the lowest needs no count
+    const uint32_t from = prefix + (1u << shift), to = span - (1u << shift);
     each([&](int, uint32_t k) {
-      const uint32_t bin = (k >> shift) & width;
-      const uint64_t who = all ? ~0ull : __ballot(agrees(k));
-      if (!who) return;
-      // lanes that all meet on one bin (equal weights) add once. (Places without a key are in the
-      // lowest bin, whose count nobody needs.)
-      const uint32_t one = all ? (uint32_t)__builtin_amdgcn_readfirstlane((int)bin)
-                               : (uint32_t)__builtin_amdgcn_readlane((int)bin, __builtin_ctzll(who));
-      if (__ballot(bin != one) & who) {
-        if (all ? k != 0 : agrees(k)) atomicAdd(&L.hist[bin], 1u);
-      } else if (lane == 0) {
-        atomicAdd(&L.hist[one], (uint32_t)__popcll(who));
-      }
+      const uint32_t d = k - from;
+      if (d < to) atomicAdd(&L.hist[(d >> shift) * kCopies<NT> + lane % kCopies<NT>], 1u);
     });
     __syncthreads();
     // the bins from the highest down, kBins / NT a thread
@@ -115,34 +155,48 @@ __device__ __forceinline__ void pick_best(int n, int need, PickLds<NT>& L, const
     uint32_t c[BT], s = 0;
 #pragma unroll
     for (int i = 0; i < BT; ++i) {
-      c[i] = L.hist[kBins - 1 - (tid * BT + i)];
+      c[i] = 0;
+#pragma unroll
+      for (int j = 0; j < kCopies<NT>; ++j)
+        c[i] += L.hist[(kBins - 1 - (tid * BT + i)) * kCopies<NT> + j];
       s += c[i];
     }
-    uint32_t before = s;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint32_t v = __shfl_up(before, o);
-      if (lane >= o) before += v;
-    }
+    uint32_t before = over_lanes(s, 0u, [](uint32_t a, uint32_t b) { return a + b; });
     if (lane == 63) L.above[wave] = before;
     __syncthreads();
     before -= s;
-    for (int w = 0; w < wave; ++w) before += L.above[w];
+#pragma unroll
+    for (int w = 0; w < NW; ++w) before += w < wave ? L.above[w] : 0u;
 #pragma unroll
     for (int i = 0; i < BT; ++i) {
-      if (before < rest && rest <= before + c[i]) {     // true in one thread, for one bin
-        L.digit = (uint32_t)(kBins - 1 - (tid * BT + i));
+      const int digit = kBins - (tid * BT + i);
+      if (before < rest && rest <= before + c[i]) {    // true for one digit, or for none but 0
+        L.digit = (uint32_t)digit;
         L.rest = rest - before;
+        L.whole = rest == before + c[i];
       }
       before += c[i];
     }
+    if (tid == NT - 1 && before < rest) {
+      L.digit = L.whole = 0;
+      L.rest = rest - before;
+    }
     __syncthreads();
-    prefix |= L.digit << shift;
-    rest = L.rest;
-  };
-  narrow(21, 2047u, true, [](uint32_t) { return true; });
-  narrow(10, 2047u, false, [&](uint32_t k) { return (k ^ prefix) < (1u << 21); });
-  narrow(0, 1023u, false, [&](uint32_t k) { return (k ^ prefix) < (1u << 10); });
+    rest = __builtin_amdgcn_readfirstlane(L.rest);
+    const uint32_t digit = __builtin_amdgcn_readfirstlane(L.digit);
+    if (__builtin_amdgcn_readfirstlane(L.whole)) {     // the whole bin is taken
+      prefix += (digit << shift) - 1;
+      rest = 0;
+      span = 1;
+    } else if (first_pass && digit == 0) {             // or something below the first pass's range
+      span = prefix + (1u << shift) - 1;
+      prefix = 1;
+    } else {
+      prefix += digit << shift;
+      span = 1u << shift;
+    }
+    first_pass = false;
+  } while (span > 1);
 
   uint32_t na = 0, ne = 0;           // of the wave's run: taken for sure, and equal to the last
   each([&](int, uint32_t k) {
@@ -205,7 +259,9 @@ struct MassKeys {
 
 constexpr int kKeepThreads = 1024;
 
-// One workgroup per (sequence, KV head): the tokens that stay.
+// One workgroup per (sequence, KV head): the tokens that stay. The passes over a row's weights need
+// all of them at once, so a row is one CU's: 27 us for 65536 tokens of 8 heads, 11 for 32 sequences
+// of 2048. (Several workgroups a row would need a launch for every pass.)
 __global__ __launch_bounds__(kKeepThreads) void keep_kernel(KvPool pool, KvSeqs S,
                                                             const int32_t* __restrict__ lengths,
                                                             int max_len,
@@ -253,7 +309,8 @@ __device__ __forceinline__ int code_size(int c) { return c < 0 ? -c : c; }
 // row by row; V (whose tokens lie a byte apart) with a token a lane, so that a wave's load is one
 // channel of neighbouring slots, and turned in LDS. The largest value of a token is its largest
 // code times its scale. Bound by latency: lengths, kept, table and codes are read one after the
-// other, then 4 workgroups a CU.
+// other, then 4 workgroups a CU: 29 us where 32 sequences of 8 heads keep 512 tokens each, 67 MB read
+// and written (V's kept bytes lie in lines of 64 of which most are read for one).
 template <int D>
 __global__ __launch_bounds__(2 * D, 4) void move_kernel(KvPool pool, KvSeqs S, KvSeqs to,
                                                      const int32_t* __restrict__ lengths,
@@ -384,7 +441,8 @@ constexpr int kScoreRounds = 4;      // pages a lane group scores at once
 // a whole number times the page's K scale, and the same on any machine. max(q8 lo, q8 hi) is q8 hi
 // where q8 > 0 and q8 lo where it is not, so the sum over the group's heads goes into the weights
 // first: one weight per channel and bound, at most 127 group in size, taken as 128 w1 + w0 for the
-// 8-bit dot products. Bound by the bounds' bytes for long sequences and by latency for short ones.
+// 8-bit dot products. Bound by latency, the chain of table, bounds, keys and the pick's passes: 12.7 us
+// for 2048 pages of 8 heads (4 MB), 14.0 for 16 sequences of 256 pages and two queries each.
 // With splits, the last workgroup of a row to leave its keys picks (as attend_kernel joins).
 template <int D, bool BF16>
 __global__ __launch_bounds__(kSelectThreads) void select_kernel(KvPool pool, KvSeqs S, KvAttn A,

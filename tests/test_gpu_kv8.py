@@ -598,3 +598,39 @@ def test_evict(D, H, lengths, keep, recent):
     assert_same("lengths", new.cpu().numpy(), wn)
     same_cache(cache, ref)
     assert_same("mass", mass.cpu().numpy().view(np.int32), rm.view(np.int32))
+
+
+@pytest.mark.parametrize("keep", [1, 2, 60, 128, 900, 999])
+def test_evict_distributions(keep):
+    """Which tokens stay, by heads whose weights are spread in ways that a search over them has to
+    get right: mostly or all zero, all equal, one far above, neighbours in the last bit, over all
+    magnitudes, negative, infinite, not a number."""
+    torch = torch_cuda()
+    n, D = 1000, 64
+    rng = np.random.default_rng(keep)
+    f = np.float32
+    few = np.where(rng.random(n) < 0.05, rng.random(n), 0)
+    bits = lambda a: np.asarray(a, np.uint32).view(f)
+    rows = [few, np.zeros(n), np.full(n, 0.5), np.eye(1, n, 400)[0], -rng.random(n),
+            bits(0x3f800000 + rng.integers(0, 3000, n)), bits(rng.integers(0, 0x7f800000, n)),
+            bits(rng.integers(0, 1 << 32, n, dtype=np.uint64)),
+            np.where(rng.random(n) < 0.5, np.inf, np.nan), np.full(n, np.nan),
+            np.where(rng.random(n) < 0.5, -0.0, 0.0), np.where(np.arange(n) < 500, -1.0, 1.0),
+            bits(rng.integers(0, 3, n)), np.where(rng.random(n) < 0.5, -np.inf, 3e38),
+            np.exp(2 * rng.standard_normal(n)), np.arange(n), -np.arange(n)[::-1]]
+    H, pages, new = len(rows), (n + PAGE - 1) // PAGE, (keep + PAGE - 1) // PAGE
+    cache = make(torch, pages + new, H, D)
+    w = np.zeros((H, pages * PAGE), f)
+    for h, r in enumerate(rows):
+        w[h, :n] = r
+    mass = torch.zeros((pages + new, H, PAGE), device="cuda")
+    mass[:pages] = torch.from_numpy(w.reshape(H, pages, PAGE).transpose(1, 0, 2).copy()).cuda()
+    t = torch.arange(pages + new, dtype=torch.int32, device="cuda")
+    for recent in (0, 1, keep // 2):
+        say(f"evict {keep} of {n} by {H} distributions, the last {recent} kept")
+        kept, _ = cache.evict(t[None, :pages].contiguous(), ints(torch, [n]), mass, keep, recent,
+                              t[None, pages:].contiguous())
+        torch.cuda.synchronize()
+        for h in range(H):
+            assert_same(f"distribution {h}", kept[0, h].cpu().numpy(),
+                        np.asarray(R.kept_tokens(list(w[h, :n]), n, keep, recent), np.int32))

@@ -357,7 +357,7 @@ static_assert(kKv8Front == kKv8Counters * 4, "one 32-bit counter a tile");
 struct KvAttnPlan {
   int32_t tiles, splits;        // 16-row tiles and splits of the pages for each (sequence, KV head)
   int32_t big;                  // prompt_kernel's row tiles; 0: attend_kernel
-  bool keep_scores;             // for the weights (see cg_kv8_plan)
+  bool keep_scores, many;       // for the weights (see cg_kv8_plan)
   uint64_t part_off, lse_off, score_off, total;   // workspace, in bytes
 };
 

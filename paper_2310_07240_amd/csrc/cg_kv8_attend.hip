@@ -4,8 +4,8 @@
 // S = q K^T and O = P V, with the softmax carried along: running maximum m, running sum l, and O
 // under the reference m, all in 32 bits. The codes go into the matrix units as fp16 (exact), the
 // scales of the page are applied to S and to the page's share of O in 32 bits, and P is rounded
-// to fp16 for the second product (relative 2^-11 a weight, the rounding that the fp16 result gets
-// anyway; l sums the unrounded weights).
+// to fp16 for the second product (relative 2^-11 of a weight down to 2^-29 of the page's largest,
+// the rounding that the fp16 result gets anyway; l sums the unrounded weights).
 //
 // Operand layout (v_mfma_f32_16x16x32_f16; lane = 16 g + m): both products are taken transposed,
 // S^T = K q^T and O^T = V^T P^T, so a lane's results belong to one query row (m) throughout and
@@ -209,8 +209,8 @@ struct Acc {
 };
 
 // The softmax of one page's scores (left at `kept`, if given, as the lane's row has them): P as
-// operands in p, m and l moved on; `keep` brings O to the
-// new reference, the return value (times the V scale) the page's share.
+// operands in p, m and l moved on; `keep` brings O to the new reference, the return value (times
+// the V scale) the page's share.
 template <int D>
 __device__ __forceinline__ float page_softmax(float x[16], float ks, int pos0, const QTile<D>& Q,
                                               Acc<D>& S, half8 p[2], float& keep, float* kept) {
@@ -228,13 +228,14 @@ __device__ __forceinline__ float page_softmax(float x[16], float ks, int pos0, c
       *reinterpret_cast<float4v*>(kept + 16 * g + j) = float4v{x[j], x[j + 1], x[j + 2], x[j + 3]};
   }
   // P is taken relative to the page's own maximum, so that fp16 loses no light page beside a heavy
-  // one; w brings the page to the running reference.
+  // one, and that is 2^15, so that a token of a light weight keeps its bits beside the heaviest one
+  // (which may have nothing in a channel); w brings the page to the running reference.
   top = quad_max(top);
-  const float mine = top == kNegInf ? 0.0f : top;      // nothing of the page is visible
+  const float mine = top == kNegInf ? 0.0f : top - 15.0f;    // (nothing of the page is visible)
   const float both = fmaxf(S.m, top);
   const float ref = both == kNegInf ? 0.0f : both;
   keep = __builtin_amdgcn_exp2f(S.m - ref);
-  const float w = __builtin_amdgcn_exp2f(top - ref);
+  const float w = __builtin_amdgcn_exp2f(top - ref - 15.0f);
   float sum = 0.0f;
 #pragma unroll
   for (int j = 0; j < 16; ++j) {
@@ -1272,7 +1273,7 @@ hipError_t attend_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, void* 
                        P.tiles, P.splits, units, part, lse);
   if (A.mass_out && np) {
     const int64_t items = (int64_t)S.n * pool.H * np;
-    if (P.big)
+    if (P.many)
       mass_rows_d<D, BF16>(pool, S, A, np, lse, st);
     else if (P.keep_scores)
       hipLaunchKernelGGL(mass_scores_kernel, dim3(grid_of((items + 3) / 4)), dim3(256), 0, st, pool,
@@ -1293,11 +1294,18 @@ KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& S, const KvAttn& A, int
   const int64_t vseqs = A.picks ? (int64_t)S.n * A.nq : S.n;
   const int64_t units = vseqs * pool.H * P.tiles;
   const int64_t pages = A.picks ? A.n_picks : ((int64_t)A.max_len + kPage - 1) / kPage;
-  // From three 16-row tiles on, the rows share the pages through LDS (prompt_kernel); every query
-  // token with pages of its own is a tile or more to itself.
+  // From three 16-row tiles on, the rows share the pages through LDS (prompt_kernel), but not where
+  // there is little to do: a call that attend_kernel's workgroups hold at once, of at most 8192
+  // (tile, page)s or 2048 of 256 channels, is bound by latency, and theirs is shorter. (Both, us; 8
+  // heads, group 4, 128 channels: 1K tokens, 64 queries 19.0 / 23.4; 4K, 64 30.6 / 33.8, 128 45.5 /
+  // 36.6; 32 sequences of 2K, 8 queries 46.6 / 60.7, 12 69.4 / 63.3; 16 of 256 tokens, 16 queries
+  // 11.5 / 14.0, 24 17.8 / 14.3. 4 heads, group 8, 256 channels, 2K: 32 32.7 / 34.7, 48 38.8 / 36.8.)
+  // Every query token with pages of its own is a tile or more to itself.
+  const int64_t at_once = D == 64 ? 768 : D == 128 ? 512 : 256;
+  const bool little = units <= at_once && units * pages <= (D == 256 ? 2048 : 8192);
   P.big = 0;
   int64_t s, most;
-  if (P.tiles > 2 && !A.picks) {
+  if (P.tiles > 2 && !little && !A.picks) {
     const int per = D == 256 ? 32 * kPromptWaves<256> : 32 * kPromptWaves<128>;
     P.big = (int)((rows + per - 1) / per);
     const int64_t groups = vseqs * pool.H * P.big;
@@ -1311,7 +1319,7 @@ KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& S, const KvAttn& A, int
     // a wave with every split less of it and pays for joining one more, a tenth of that: at most
     // twice the root of the pages (8 heads, one sequence: 16K tokens 17 us with 32 splits, 21 with
     // 64; 4K 11 us with 16, 13 with 8).
-    s = (D == 64 ? 768 : D == 128 ? 512 : 256) / units;
+    s = at_once / units;
     most = (pages + 3) / 4;
     const int64_t root = (int64_t)sqrt(4.0 * (double)pages);
     if (most > root) most = root;
@@ -1321,8 +1329,13 @@ KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& S, const KvAttn& A, int
   if (s < 1) s = 1;
   P.splits = (int)s;
   // Weights of few rows: their scores are kept for the second launch (8 bytes a row and token to
-  // write and read again) where that is at most half of reading K again (D bytes a token).
-  P.keep_scores = A.mass_out && !P.big && rows * 16 <= D;
+  // write and read again) where that is at most half of reading K again (D bytes a token), and of 8
+  // rows at most (both, us; 128 channels: 32 sequences of 2K, 1 row 35.2 / 48.5, 4 38.8 / 48.9, 8
+  // 42.9 / 51.0; 64: 16 of 2K, 4 rows 21.6 / 22.5, 8 24.5 / 22.5; 256: 8 of 4K, 8 rows 28.2 / 28.4,
+  // 16 39.5 / 36.7). Of three tiles or more mass_rows_kernel takes them (a question of 64 tokens over
+  // 2K: 7 us; mass_kernel, whose waves walk the tiles alone, 17; of 12 tokens 6 and 6).
+  P.keep_scores = A.mass_out && rows * 16 <= D && rows <= 8;
+  P.many = P.tiles > 2 && !A.picks;
   const bool parts = s > 1, weights = A.mass_out && !A.lse;
   uint64_t at = parts || weights || P.keep_scores ? kKv8Front : 0;
   P.part_off = at;

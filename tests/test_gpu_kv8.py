@@ -432,6 +432,125 @@ def test_attend_many_tokens_scales_and_extremes(D, dtype, scale):
     check_attend(torch, cache, q, table, t, [700, 70], scale=scale * 8)
 
 
+def much_room(torch, t):
+    """The table with columns of no page behind it: the host lays such a call out as a large one,
+    which shares the pages among the rows of a workgroup, in many splits."""
+    t = np.concatenate([t, np.full((len(t), 2800 - t.shape[1]), -1, np.int32)], 1)
+    return t, torch.from_numpy(t).cuda()
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("D,HQ,H,Q,lengths,q_lens", [
+    (64, 2, 1, 33, [33, 200], None),
+    (128, 8, 1, 40, [100, 40, 0], [40, 39, 0]),
+    (256, 2, 2, 49, [130], None),
+    (64, 6, 2, 130, [450], None),
+    (128, 8, 2, 70, [513, 64, 300], [70, 1, 64]),
+    (64, 4, 1, 30, [7, 29], None),             # queries before the first token
+])
+def test_attend_large_calls(dtype, D, HQ, H, Q, lengths, q_lens):
+    torch = torch_cuda()
+    rng = np.random.default_rng(Q)
+    t, _, n = tables(torch, rng, len(lengths), max(lengths) // PAGE + 1)
+    t, table = much_room(torch, t)
+    cache = make(torch, n, H, D)
+    q = (torch.randn(len(lengths), Q, HQ, D) * 2).to(getattr(torch, dtype)).cuda()
+    check_attend(torch, cache, q, table, t, lengths, q_lens=q_lens, mass=True)
+
+
+@pytest.mark.parametrize("D,H,Q,most", [(128, 8, 12, 150), (64, 12, 13, 100), (256, 4, 12, 200)])
+def test_attend_many_sequences(D, H, Q, most):
+    """More row tiles than the card holds workgroups: no splits."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(Q)
+    B = 22
+    lengths = [int(x) for x in rng.integers(0, most, B)]
+    t, table, n = tables(torch, rng, B, most // PAGE + 1)
+    cache = make(torch, n, H, D)
+    q = torch.randn(B, Q, 4 * H, D).half().cuda()
+    check_attend(torch, cache, q, table, t, lengths, mass=True)
+
+
+@pytest.mark.parametrize("D,dtype", [(128, "float16"), (64, "bfloat16"), (256, "float16")])
+@pytest.mark.parametrize("scale", [-0.2, 0.0, 2.0])
+def test_attend_large_calls_scales_and_extremes(D, dtype, scale):
+    torch = torch_cuda()
+    rng = np.random.default_rng(11)
+    t, _, n = tables(torch, rng, 2, 12)
+    cache = make(torch, n, 1, D)
+    for j, f in enumerate((1.0, 30.0, 1e-3, 0.0, 1.0, 1e-25, 3.0, 1.0)):
+        cache.v_scale[int(t[0, j])] *= f
+    cache.k_scale[int(t[0, 2])] = 0.0
+    cache.k_codes[int(t[1, 1])] = 0
+    t[1, 3] = -1
+    t, table = much_room(torch, t)
+    q = torch.randn(2, 70, 3, D).to(getattr(torch, dtype)).cuda()
+    check_attend(torch, cache, q, table, t, [700, 333], scale=scale, mass=True)
+    cache.k_codes.zero_()
+    cache.k_codes[int(t[0, 0]), 0, 5, :] = 100
+    cache.k_scale.fill_(0.01)
+    q.fill_(0.25)
+    check_attend(torch, cache, q, table, t, [700, 70], scale=scale * 8)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("which", ["k_scale", "v_scale"])
+@pytest.mark.parametrize("Q,HQ,D", [(80, 3, 64), (70, 2, 256), (300, 1, 128)])
+def test_attend_large_calls_bad_scale(bad, which, Q, HQ, D):
+    torch = torch_cuda()
+    rng = np.random.default_rng(13)
+    t, _, n = tables(torch, rng, 1, 6)
+    t, table = much_room(torch, t)
+    cache = make(torch, n, 1, D)
+    q = torch.randn(1, Q, HQ, D).half().cuda()
+    length = 5 * 64 + 3                        # the last three queries see the last page
+    good = cache.attend(q, table, ints(torch, [length]))
+    getattr(cache, which)[int(t[0, 5])] = bad
+    mass = torch.zeros((n, 1, PAGE), device="cuda")
+    got = cache.attend(q, table, ints(torch, [length]), mass=mass)
+    assert torch.equal(got[:, :Q - 3], good[:, :Q - 3]) and not torch.isnan(good).any()
+    if which == "v_scale" or bad != bad:
+        assert not torch.isfinite(got[:, Q - 3:]).any()
+    if which == "k_scale" and bad != bad:
+        assert torch.isnan(mass[int(t[0, 5]), 0, 0])
+
+
+def test_attend_large_call_split():
+    """Splits of several pages each, of sequences of uneven length."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(12)
+    t, table, n = tables(torch, rng, 4, 60)
+    cache = make(torch, n, 8, 64)
+    q = torch.randn(4, 60, 8, 64).half().cuda()
+    check_attend(torch, cache, q, table, t, [3800, 900, 200, 130], mass=True)
+
+
+@pytest.mark.parametrize("vs", [1e-20, 1e-30, 1e-36])
+@pytest.mark.parametrize("Q", [1, 30])
+def test_attend_light_weights(vs, Q):
+    """A heavy token with nothing in half of the channels: there the light ones are all there is,
+    down to weights of 2^-28, and V is small."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(14)
+    t, table, n = tables(torch, rng, 1, 3)
+    cache = make(torch, n, 1, 128)
+    cache.k_codes.zero_()
+    for j, steps in enumerate((19, 10, 1)):    # logits of one token a page above the others'
+        cache.k_codes[int(t[0, j]), 0, 7, :] = steps
+        cache.v_codes[int(t[0, j]), 0, ::2, 7] = 0
+    cache.k_scale.fill_(1.0)
+    cache.v_scale.fill_(vs)
+    q = torch.full((1, Q, 3, 128), 1 / 128).bfloat16().cuda()
+    lse = torch.empty((1, Q, 3), device="cuda")
+    out = cache.attend(q, table, ints(torch, [192 - 30 + Q]), scale=1.0, lse=lse).float().cpu()
+    want, wl, _, size, _ = R.attend(R.Ref(cache), q.float().cpu().numpy(), t, [192 - 30 + Q], [Q],
+                                    1.0)
+    # a weight's fp16 rounding, and the rounding to bf16, whose subnormals are 2^-133 apart
+    lim = 2.0 ** -8 * np.abs(want) + 2.0 ** -10 * size + 2.0 ** -134
+    assert (np.abs(out.numpy() - want) <= lim).all()
+    assert np.abs(lse.cpu().numpy() - wl).max() <= 1e-4
+
+
 def test_attend_long_prompt_split():
     torch = torch_cuda()
     rng = np.random.default_rng(12)

@@ -210,19 +210,24 @@ class Kv8Cache:
         """(k, v) [n_seq, n_tokens, n_heads, head_dim]: the sequences' tokens from ``starts`` on,
         zeros behind ``counts``. ``k``, ``v``: tensors to write into."""
         s, n, _ = self._seqs(table)
-        shape = (n, int(n_tokens), self.n_heads, self.head_dim)
-        if k is None or v is None:
-            dtype = dtype or (self.torch.float16 if k is None and v is None else
-                              (v if k is None else k).dtype)
+        T, H, D = int(n_tokens), self.n_heads, self.head_dim
+        shape = (n, T, H, D)
+        if k is None and v is None:
+            dtype = dtype or self.torch.float16
+            k, v = self._empty(shape, dtype, stream), self._empty(shape, dtype, stream)
+            kind = self._types.get(dtype)
+            rows = [_ROWS.pack(x.data_ptr(), T * H * D, H * D, D) for x in (k, v)]
+        else:
+            dtype = dtype or (v if k is None else k).dtype
             k = self._empty(shape, dtype, stream) if k is None else k
             v = self._empty(shape, dtype, stream) if v is None else v
-        kind = self._types.get(k.dtype)
+            kind = self._types.get(k.dtype)
+            rows = self._rows(k, "k", shape, k.dtype), self._rows(v, "v", shape, k.dtype)
         _need(kind is not None, "k: float16 or bfloat16 is wanted")
         _need(starts is not None, "starts is missing")
         _check(_lib().cg_kv8_load(
             self._cp, s, self._per_seq(starts, "starts", n), self._per_seq(counts, "counts", n),
-            shape[1], kind, self._rows(k, "k", shape, k.dtype), self._rows(v, "v", shape, k.dtype),
-            self._handle(stream)), "cg_kv8_load")
+            T, kind, *rows, self._handle(stream)), "cg_kv8_load")
         return k, v
 
     # ---- attention -----------------------------------------------------------------------

@@ -753,3 +753,22 @@ def test_evict_distributions(keep):
         for h in range(H):
             assert_same(f"distribution {h}", kept[0, h].cpu().numpy(),
                         np.asarray(R.kept_tokens(list(w[h, :n]), n, keep, recent), np.int32))
+
+
+@pytest.mark.parametrize("off", [0, 1])
+@pytest.mark.parametrize("D,HQ,H,Q,lengths", [
+    (64, 64, 1, 3, [200]),                     # a token is two tiles of 32 rows
+    (64, 40, 1, 5, [130, 64]),                 # tiles begin inside a token
+    (128, 16, 2, 37, [100, 300]),
+    (256, 5, 1, 30, [90]),
+])
+def test_attend_weights_of_wide_groups(D, HQ, H, Q, lengths, off):
+    """Weights of many rows, by groups that fill whole tiles and groups that do not; off = 1: rows
+    off 16-byte boundaries."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(HQ)
+    t, table, n = tables(torch, rng, len(lengths), max(lengths) // PAGE + 1)
+    cache = make(torch, n, H, D)
+    shape = (len(lengths), Q, HQ, D)
+    q = torch.randn(int(np.prod(shape)) + 8).half().cuda()[off:off + int(np.prod(shape))].view(shape)
+    check_attend(torch, cache, q, table, t, lengths, mass=True)

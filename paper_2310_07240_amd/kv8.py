@@ -17,6 +17,7 @@ import struct
 from .cachegen import CodecError, _check, lib
 
 PAGE = 64
+ZEROED = 4096                      # CG_KV8_WORKSPACE_ZEROED
 _P = ctypes.c_void_p
 _I64 = ctypes.c_int64
 _I32 = ctypes.c_int32
@@ -85,7 +86,8 @@ class Kv8Cache:
     tokens they hold. Lengths, starts and counts are int32 [n_seq]; everything is a contiguous
     tensor on the cache's device except rows of K, V, queries and outputs, which may have any
     strides as long as the head dimension is contiguous. Calls are asynchronous on ``stream``
-    (default: the current one). Scratch is kept per stream and grows as needed.
+    (default: the current one). Scratch is kept per stream and grows as needed; calls captured with
+    ``torch.cuda.graph`` take theirs from the graph's pool.
 
     ``buffers``: tensors ``k_codes``, ``v_codes``, ``k_scale``, ``v_scale`` and (or None)
     ``k_bounds`` to use as the pool; without it they are allocated, zeroed.
@@ -116,7 +118,7 @@ class Kv8Cache:
                                     for n in want))
         self._cp = ctypes.addressof(self._c)
         self._raw_stream = torch._C._cuda_getCurrentRawStream
-        self._ws, self._captured = {}, []
+        self._ws = {}
         self._types = {torch.float16: 0, torch.bfloat16: 1}
         self._scale = 1.0 / math.sqrt(D)
 
@@ -170,21 +172,30 @@ class Kv8Cache:
         return self._new(self.torch.empty, shape, dtype, stream)
 
     def _scratch(self, stream, handle, need):
-        """The stream's own scratch (address, bytes), cleared once. Scratch made while the stream
-        is being captured is cleared by the graph alone, so only that call has it; it is kept for
-        the graph's sake."""
+        """The stream's own scratch (address, bytes, tensor), its counters cleared once. Every call
+        of a captured stream has scratch of its own instead: what eager calls use is replaced when
+        one needs more, and may be at work when the graph is replayed. It comes from the graph's
+        memory pool, which lives as long as the graph (and may give it to a later call of the same
+        capture, which runs behind this one); the graph clears its counters."""
+        if self._capturing(stream, handle):
+            return self._cleared(need, stream)
         ws = self._ws.get(handle)
         if ws is None or ws[1] < need:
-            t = self._new(self.torch.zeros, (need,), self.torch.uint8, stream)
-            ws = (t.data_ptr(), need, t)
-            if self._capturing(stream):
-                self._captured.append(t)
-            else:
-                self._ws[handle] = ws
+            ws = self._ws[handle] = self._cleared(need, stream)
         return ws
 
-    def _capturing(self, stream):
+    def _cleared(self, need, stream):
+        """Scratch of `need` bytes, of which the counters at its front have to be zero."""
+        t = self._empty((need,), self.torch.uint8, stream)
         if stream is None:
+            t[:ZEROED].zero_()
+        else:
+            with self.torch.cuda.stream(stream):
+                t[:ZEROED].zero_()
+        return t.data_ptr(), need, t
+
+    def _capturing(self, stream, handle):
+        if stream is None or handle == self._raw_stream(self._index):
             return self.torch.cuda.is_current_stream_capturing()
         with self.torch.cuda.stream(stream):
             return self.torch.cuda.is_current_stream_capturing()

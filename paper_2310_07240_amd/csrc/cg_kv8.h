@@ -49,6 +49,21 @@ __device__ __forceinline__ int kv_page(const KvSeqs& S, int P, int seq, int j) {
   return p >= 0 && p < P ? p : -1;
 }
 
+// How pick_best's waves share the blocks of 64 keys: a wave has `mine` (0 for the last ones, maybe)
+// from `first` on, and lane l looks up where block pick_block(run, l) lies (-1: none, nothing is read).
+struct PickRun {
+  int first, mine;
+};
+
+__host__ __device__ inline PickRun pick_run(int n, int waves, int wave) {
+  const int blocks = (n + 63) / 64, per = (blocks + waves - 1) / waves, first = wave * per;
+  return PickRun{first, first + per < blocks ? per : blocks > first ? blocks - first : 0};
+}
+
+__host__ __device__ inline int pick_block(const PickRun& r, int lane) {
+  return r.mine == 0 ? -1 : r.first + (lane < r.mine ? lane : 0);
+}
+
 // Rows of either 16-bit type, widened exactly.
 template <bool BF16>
 __device__ __forceinline__ float kv_widen(uint16_t u) {

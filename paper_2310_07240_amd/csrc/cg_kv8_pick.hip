@@ -63,12 +63,11 @@ __device__ __forceinline__ void pick_best(int n, int need, PickLds<NT>& L, const
   constexpr int NW = NT / 64;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int blocks = (n + 63) / 64, per = (blocks + NW - 1) / NW;
-  const int first = wave * per;
-  const int mine = first + per < blocks ? per : blocks > first ? blocks - first : 0;
+  const PickRun run = pick_run(n, NW, wave);
+  const int first = run.first, mine = run.mine;
   uint32_t held[kHeld];
   // a lane finds a block's place, then all blocks are on their way at once
-  const int place = keys.place(first + (lane < mine ? lane : 0));
+  const int block = pick_block(run, lane), place = block < 0 ? -1 : keys.place(block);
   int lost = 0;
 #pragma unroll
   for (int r = 0; r < kHeld; r += 8)

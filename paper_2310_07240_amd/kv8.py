@@ -13,6 +13,7 @@ from __future__ import annotations
 import ctypes
 import math
 import struct
+import threading
 
 from .cachegen import CodecError, _check, lib
 
@@ -87,7 +88,7 @@ class Kv8Cache:
     tensor on the cache's device except rows of K, V, queries and outputs, which may have any
     strides as long as the head dimension is contiguous. Calls are asynchronous on ``stream``
     (default: the current one). Scratch is kept per stream and grows as needed; calls captured with
-    ``torch.cuda.graph`` take theirs from the graph's pool.
+    ``torch.cuda.graph`` take theirs from the graph's pool. Threads may share a cache and a stream.
 
     ``buffers``: tensors ``k_codes``, ``v_codes``, ``k_scale``, ``v_scale`` and (or None)
     ``k_bounds`` to use as the pool; without it they are allocated, zeroed.
@@ -118,7 +119,7 @@ class Kv8Cache:
                                     for n in want))
         self._cp = ctypes.addressof(self._c)
         self._raw_stream = torch._C._cuda_getCurrentRawStream
-        self._ws = {}
+        self._ws, self._lock = {}, threading.Lock()
         self._types = {torch.float16: 0, torch.bfloat16: 1}
         self._scale = 1.0 / math.sqrt(D)
 
@@ -183,6 +184,17 @@ class Kv8Cache:
         if ws is None or ws[1] < need:
             ws = self._ws[handle] = self._cleared(need, stream)
         return ws
+
+    def _with_scratch(self, name, fn, need, stream, *args):
+        """fn(cache, *args, scratch, its bytes, stream), its launches in one piece: another thread's
+        on the same stream would find the scratch half used, or replace it."""
+        handle = self._handle(stream)
+        if not need:
+            _check(fn(self._cp, *args, None, 0, handle), name)
+            return
+        with self._lock:
+            ws = self._scratch(stream, handle, need)
+            _check(fn(self._cp, *args, ws[0], ws[1], handle), name)
 
     def _cleared(self, need, stream):
         """Scratch of `need` bytes, of which the counters at its front have to be zero."""
@@ -285,10 +297,8 @@ class Kv8Cache:
                        0 if lse is None else self._tensor(lse, "lse", self._f32, shape[:3]),
                        picks_p, n_picks, mass_p, mass_out_p, decay)
         L = _lib()
-        handle = self._handle(stream)
-        need = L.cg_kv8_attend_workspace_bytes(self._cp, s, a)
-        ws = self._scratch(stream, handle, need) if need else (None, 0)
-        _check(L.cg_kv8_attend(self._cp, s, a, ws[0], ws[1], handle), "cg_kv8_attend")
+        self._with_scratch("cg_kv8_attend", L.cg_kv8_attend,
+                           L.cg_kv8_attend_workspace_bytes(self._cp, s, a), stream, s, a)
         return out
 
     def select(self, q, table, lengths, n_picks, recent=1, q_lens=None, max_len=None, out=None,
@@ -307,11 +317,9 @@ class Kv8Cache:
                        width * PAGE if max_len is None else max_len,
                        self._per_seq(q_lens, "q_lens", n), *rows, *rows, 0, 0, n_picks, 0, 0, 0.0)
         L = _lib()
-        handle = self._handle(stream)
-        need = L.cg_kv8_select_workspace_bytes(self._cp, s, a)
-        ws = self._scratch(stream, handle, need) if need else (None, 0)
-        _check(L.cg_kv8_select(self._cp, s, a, recent, self._tensor(out, "out", self._i32, want),
-                               ws[0], ws[1], handle), "cg_kv8_select")
+        self._with_scratch("cg_kv8_select", L.cg_kv8_select,
+                           L.cg_kv8_select_workspace_bytes(self._cp, s, a), stream, s, a, recent,
+                           self._tensor(out, "out", self._i32, want))
         return out
 
     # ---- eviction ------------------------------------------------------------------------

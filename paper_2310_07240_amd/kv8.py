@@ -119,6 +119,8 @@ class Kv8Cache:
                                     for n in want))
         self._cp = ctypes.addressof(self._c)
         self._raw_stream = torch._C._cuda_getCurrentRawStream
+        self._current = (torch._C._cuda_getDevice if self.device.type == "cuda"
+                         else lambda: self._index)
         self._ws, self._lock = {}, threading.Lock()
         self._types = {torch.float16: 0, torch.bfloat16: 1}
         self._scale = 1.0 / math.sqrt(D)
@@ -157,10 +159,32 @@ class Kv8Cache:
         return _ROWS.pack(*self._strided(t, name, shape, dtype))
 
     def _handle(self, stream):
-        """The HIP stream's handle: the caller's, or torch's current one."""
-        if stream is not None:
+        """The HIP stream's handle: the caller's, or torch's current one; of the cache's GPU."""
+        if stream is None:
+            if self.device.type == "cuda":
+                return self._raw_stream(self._index)
+        elif getattr(stream, "device", self.device) == self.device:
             return stream.cuda_stream
-        return self._raw_stream(self._index)
+        raise ValueError(f"the cache is on {self.device}: a GPU is wanted, and a stream of it")
+
+    def _launch(self, name, fn, stream, *args, need=None):
+        """fn(cache, *args, stream), or with `need` bytes of scratch fn(cache, *args, scratch, its
+        bytes, stream); with the cache's GPU as the current one, where a launch goes. Launches that
+        share scratch are made in one piece: another thread's on the same stream would find it half
+        used, or replace it."""
+        handle = self._handle(stream)
+        if self._current() != self._index:
+            with self.torch.cuda.device(self._index):
+                return self._launch(name, fn, stream, *args, need=need)
+        if need is None:
+            rc = fn(self._cp, *args, handle)
+        elif need == 0:
+            rc = fn(self._cp, *args, None, 0, handle)
+        else:
+            with self._lock:
+                ws = self._scratch(stream, handle, need)
+                rc = fn(self._cp, *args, ws[0], ws[1], handle)
+        _check(rc, name)
 
     def _new(self, make, shape, dtype, stream):
         """A tensor whose memory's reuse is ordered on the stream."""
@@ -184,17 +208,6 @@ class Kv8Cache:
         if ws is None or ws[1] < need:
             ws = self._ws[handle] = self._cleared(need, stream)
         return ws
-
-    def _with_scratch(self, name, fn, need, stream, *args):
-        """fn(cache, *args, scratch, its bytes, stream), its launches in one piece: another thread's
-        on the same stream would find the scratch half used, or replace it."""
-        handle = self._handle(stream)
-        if not need:
-            _check(fn(self._cp, *args, None, 0, handle), name)
-            return
-        with self._lock:
-            ws = self._scratch(stream, handle, need)
-            _check(fn(self._cp, *args, ws[0], ws[1], handle), name)
 
     def _cleared(self, need, stream):
         """Scratch of `need` bytes, of which the counters at its front have to be zero."""
@@ -223,11 +236,11 @@ class Kv8Cache:
               "n_heads, head_dim] is wanted")
         _need(starts is not None, "starts is missing")
         shape = (n, k.shape[1], self.n_heads, self.head_dim)
-        _check(_lib().cg_kv8_store(
-            self._cp, s, self._per_seq(starts, "starts", n), self._per_seq(counts, "counts", n),
-            shape[1], kind, self._rows(k, "k", shape, k.dtype), self._rows(v, "v", shape, k.dtype),
-            None if status is None else self._tensor(status, "status", self._i32, (1,)),
-            self._handle(stream)), "cg_kv8_store")
+        self._launch(
+            "cg_kv8_store", _lib().cg_kv8_store, stream, s, self._per_seq(starts, "starts", n),
+            self._per_seq(counts, "counts", n), shape[1], kind, self._rows(k, "k", shape, k.dtype),
+            self._rows(v, "v", shape, k.dtype),
+            None if status is None else self._tensor(status, "status", self._i32, (1,)))
 
     def load(self, table, starts, n_tokens, counts=None, dtype=None, k=None, v=None, stream=None):
         """(k, v) [n_seq, n_tokens, n_heads, head_dim]: the sequences' tokens from ``starts`` on,
@@ -248,9 +261,9 @@ class Kv8Cache:
             rows = self._rows(k, "k", shape, k.dtype), self._rows(v, "v", shape, k.dtype)
         _need(kind is not None, "k: float16 or bfloat16 is wanted")
         _need(starts is not None, "starts is missing")
-        _check(_lib().cg_kv8_load(
-            self._cp, s, self._per_seq(starts, "starts", n), self._per_seq(counts, "counts", n),
-            T, kind, *rows, self._handle(stream)), "cg_kv8_load")
+        self._launch("cg_kv8_load", _lib().cg_kv8_load, stream, s,
+                     self._per_seq(starts, "starts", n), self._per_seq(counts, "counts", n), T,
+                     kind, *rows)
         return k, v
 
     # ---- attention -----------------------------------------------------------------------
@@ -297,8 +310,8 @@ class Kv8Cache:
                        0 if lse is None else self._tensor(lse, "lse", self._f32, shape[:3]),
                        picks_p, n_picks, mass_p, mass_out_p, decay)
         L = _lib()
-        self._with_scratch("cg_kv8_attend", L.cg_kv8_attend,
-                           L.cg_kv8_attend_workspace_bytes(self._cp, s, a), stream, s, a)
+        self._launch("cg_kv8_attend", L.cg_kv8_attend, stream, s, a,
+                     need=L.cg_kv8_attend_workspace_bytes(self._cp, s, a))
         return out
 
     def select(self, q, table, lengths, n_picks, recent=1, q_lens=None, max_len=None, out=None,
@@ -317,9 +330,9 @@ class Kv8Cache:
                        width * PAGE if max_len is None else max_len,
                        self._per_seq(q_lens, "q_lens", n), *rows, *rows, 0, 0, n_picks, 0, 0, 0.0)
         L = _lib()
-        self._with_scratch("cg_kv8_select", L.cg_kv8_select,
-                           L.cg_kv8_select_workspace_bytes(self._cp, s, a), stream, s, a, recent,
-                           self._tensor(out, "out", self._i32, want))
+        self._launch("cg_kv8_select", L.cg_kv8_select, stream, s, a, recent,
+                     self._tensor(out, "out", self._i32, want),
+                     need=L.cg_kv8_select_workspace_bytes(self._cp, s, a))
         return out
 
     # ---- eviction ------------------------------------------------------------------------
@@ -333,10 +346,9 @@ class Kv8Cache:
         _need(lengths is not None and mass is not None, "lengths and mass are wanted")
         kept = self._empty((n, self.n_heads, max(0, keep)), self._i32, stream)
         new_lengths = self._empty((n,), self._i32, stream)
-        _check(_lib().cg_kv8_evict(
-            self._cp, s, self._per_seq(lengths, "lengths", n),
+        self._launch(
+            "cg_kv8_evict", _lib().cg_kv8_evict, stream, s, self._per_seq(lengths, "lengths", n),
             width * PAGE if max_len is None else max_len,
             self._tensor(mass, "mass", self._f32, (self.n_pages, self.n_heads, PAGE)), keep,
-            recent, to, kept.data_ptr(), new_lengths.data_ptr(), self._handle(stream)),
-            "cg_kv8_evict")
+            recent, to, kept.data_ptr(), new_lengths.data_ptr())
         return kept, new_lengths

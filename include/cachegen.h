@@ -420,6 +420,8 @@ typedef struct cg_kv8_cache {
   int8_t* k_bounds;       /* [P][H][2][D], 16-byte aligned: lowest and highest K code of each
                              channel over the page's tokens; NULL: not kept (cg_kv8_select
                              needs them) */
+  float* mass;            /* [P][H][64]: token weights as cg_kv8_attend adds them up, which
+                             cg_kv8_store clears for the tokens it writes; NULL: it clears none */
 } cg_kv8_cache;
 
 typedef struct cg_kv8_seqs {
@@ -445,8 +447,11 @@ typedef struct cg_kv8_rows {
  * Per page, head and K/V, with m the largest |x| of the page's new rows: scale s = m / 127, or the
  * page's own if that is larger and earlier tokens stay in it; code = rint(clamp(x / s, +-127))
  * (s = 0: code 0). Where s grows, the earlier tokens are coded again from code * old scale. All
- * quotients and products are IEEE fp32, as in the codec. Pages are shared with no other sequence
- * of the call, or the result is undefined. Asynchronous. */
+ * quotients and products are IEEE fp32, as in the codec. With c->mass, the weights of a written
+ * page become 0 from its first new row on: a token starts without weight, whoever had the page
+ * before. (A caller that passes no mass clears the weights of a page itself, when the page goes to
+ * another sequence.) Pages are shared with no other sequence of the call, or the result is
+ * undefined. Asynchronous. */
 int cg_kv8_store(const cg_kv8_cache* c, const cg_kv8_seqs* s, const int32_t* starts,
                  const int32_t* counts, int32_t n_tokens, int32_t dtype, const cg_kv8_rows* k,
                  const cg_kv8_rows* v, uint32_t* status, hipStream_t stream);
@@ -482,7 +487,8 @@ typedef struct cg_kv8_attn {
   /* The weight each token got: mass_out [P][H][64] receives, for every token of the sequences,
    * decay * mass_in + the sum over the query tokens and the heads of its group of their softmax
    * weight on it. mass_in NULL: the sum alone; it may be mass_out. mass_out NULL: no weights. Not
-   * together with picks, nor for sequences that share pages. */
+   * together with picks, nor for sequences that share pages. What mass_in holds for a token counts,
+   * also for one that has got no weight yet: see cg_kv8_store. */
   const float* mass_in;
   float* mass_out;
   float decay;

@@ -31,6 +31,7 @@ struct KvPool {
   float* ks;
   float* vs;
   int8_t* bounds;               // may be null
+  float* mass;                  // weights that store clears; may be null
 };
 
 struct KvSeqs {

@@ -14,10 +14,10 @@ int check_cache(const cg_kv8_cache* c, KvPool* out) {
   if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return CG_ERR_SHAPE;
   if (!c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale) return CG_ERR_ARG;
   if (!aligned(c->k_codes, 16) || !aligned(c->v_codes, 16) || !aligned(c->k_scale, 4) ||
-      !aligned(c->v_scale, 4) || !aligned(c->k_bounds, 16))
+      !aligned(c->v_scale, 4) || !aligned(c->k_bounds, 16) || !aligned(c->mass, 4))
     return CG_ERR_ARG;
   *out = KvPool{c->n_pages, c->n_heads, c->k_codes, c->v_codes, c->k_scale, c->v_scale,
-                c->k_bounds};
+                c->k_bounds, c->mass};
   return CG_OK;
 }
 

@@ -168,6 +168,8 @@ __global__ __launch_bounds__(2 * D, WHICH == kNew ? 4 : 2) void store_kernel(KvP
     const int page = j < S.width ? kv_page(S, pool.P, seq, (int)j) : -1;
     if (page < 0) continue;                           // no such page: nothing is written
     const int last = end - j * kPage < kPage ? (int)(end - j * kPage) : kPage;
+    if (pool.mass && tid >= held && tid < kPage)
+      pool.mass[((int64_t)page * pool.H + h) * kPage + tid] = 0.0f;
     const int64_t row0 = j * kPage - start;           // row of the page's first token
     const uint16_t* kp = static_cast<const uint16_t*>(k.p) + seq * k.seq + row0 * k.tok + h * k.head;
     const uint16_t* vp = static_cast<const uint16_t*>(v.p) + seq * v.seq + row0 * v.tok + h * v.head;

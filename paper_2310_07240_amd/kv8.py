@@ -26,7 +26,7 @@ _I32 = ctypes.c_int32
 
 class _Cache(ctypes.Structure):
     _fields_ = [("n_pages", _I32), ("n_heads", _I32), ("head_dim", _I32), ("k_codes", _P),
-                ("v_codes", _P), ("k_scale", _P), ("v_scale", _P), ("k_bounds", _P)]
+                ("v_codes", _P), ("k_scale", _P), ("v_scale", _P), ("k_bounds", _P), ("mass", _P)]
 
 
 class _Seqs(ctypes.Structure):
@@ -167,7 +167,7 @@ class Kv8Cache:
             return stream.cuda_stream
         raise ValueError(f"the cache is on {self.device}: a GPU is wanted, and a stream of it")
 
-    def _launch(self, name, fn, stream, *args, need=None):
+    def _launch(self, name, fn, stream, *args, need=None, cache=None):
         """fn(cache, *args, stream), or with `need` bytes of scratch fn(cache, *args, scratch, its
         bytes, stream); with the cache's GPU as the current one, where a launch goes. Launches that
         share scratch are made in one piece: another thread's on the same stream would find it half
@@ -175,9 +175,9 @@ class Kv8Cache:
         handle = self._handle(stream)
         if self._current() != self._index:
             with self.torch.cuda.device(self._index):
-                return self._launch(name, fn, stream, *args, need=need)
+                return self._launch(name, fn, stream, *args, need=need, cache=cache)
         if need is None:
-            rc = fn(self._cp, *args, handle)
+            rc = fn(cache or self._cp, *args, handle)
         elif need == 0:
             rc = fn(self._cp, *args, None, 0, handle)
         else:
@@ -225,11 +225,22 @@ class Kv8Cache:
         with self.torch.cuda.stream(stream):
             return self.torch.cuda.is_current_stream_capturing()
 
+    def _mass(self, mass):
+        return self._tensor(mass, "mass", self._f32, (self.n_pages, self.n_heads, PAGE))
+
+    def _clearing(self, mass):
+        """The cache with these weights, for a store."""
+        c = _Cache.from_buffer_copy(self._c)
+        c.mass = self._mass(mass)
+        return ctypes.byref(c)
+
     # ---- rows in and out -----------------------------------------------------------------
-    def store(self, k, v, table, starts, counts=None, status=None, stream=None):
+    def store(self, k, v, table, starts, counts=None, status=None, stream=None, mass=None):
         """Rows k, v [n_seq, n_tokens, n_heads, head_dim] become the sequences' tokens from
         ``starts`` on (``counts``: how many of each; default all). ``status``: an int32 tensor of
-        one element that receives 0, or non-zero for NaN / Inf."""
+        one element that receives 0, or non-zero for NaN / Inf. ``mass``: the weights of ``attend``
+        and ``evict``, in which the new tokens start from 0; without it what their places held
+        stays, the weights of the pages' last owner as a rule."""
         s, n, _ = self._seqs(table)
         kind = self._types.get(k.dtype)
         _need(kind is not None and k.dim() == 4, "k: float16 or bfloat16 [n_seq, n_tokens, "
@@ -240,7 +251,8 @@ class Kv8Cache:
             "cg_kv8_store", _lib().cg_kv8_store, stream, s, self._per_seq(starts, "starts", n),
             self._per_seq(counts, "counts", n), shape[1], kind, self._rows(k, "k", shape, k.dtype),
             self._rows(v, "v", shape, k.dtype),
-            None if status is None else self._tensor(status, "status", self._i32, (1,)))
+            None if status is None else self._tensor(status, "status", self._i32, (1,)),
+            cache=None if mass is None else self._clearing(mass))
 
     def load(self, table, starts, n_tokens, counts=None, dtype=None, k=None, v=None, stream=None):
         """(k, v) [n_seq, n_tokens, n_heads, head_dim]: the sequences' tokens from ``starts`` on,
@@ -298,10 +310,10 @@ class Kv8Cache:
             n_picks = picks.shape[3]
             picks_p = self._tensor(picks, "picks", self._i32, (n, nq, self.n_heads, n_picks))
         if mass is not None or mass_out is not None:
-            pool = (self.n_pages, self.n_heads, PAGE)
             mass_out = mass if mass_out is None else mass_out
-            mass_p = 0 if mass is None else self._tensor(mass, "mass", self._f32, pool)
-            mass_out_p = self._tensor(mass_out, "mass_out", self._f32, pool)
+            mass_p = 0 if mass is None else self._mass(mass)
+            mass_out_p = self._tensor(mass_out, "mass_out", self._f32,
+                                      (self.n_pages, self.n_heads, PAGE))
         a = _ATTN.pack(nq, heads, kind, self._scale if scale is None else scale,
                        self._per_seq(lengths, "lengths", n),
                        width * PAGE if max_len is None else max_len,
@@ -349,6 +361,5 @@ class Kv8Cache:
         self._launch(
             "cg_kv8_evict", _lib().cg_kv8_evict, stream, s, self._per_seq(lengths, "lengths", n),
             width * PAGE if max_len is None else max_len,
-            self._tensor(mass, "mass", self._f32, (self.n_pages, self.n_heads, PAGE)), keep,
-            recent, to, kept.data_ptr(), new_lengths.data_ptr())
+            self._mass(mass), keep, recent, to, kept.data_ptr(), new_lengths.data_ptr())
         return kept, new_lengths

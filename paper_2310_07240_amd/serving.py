@@ -80,7 +80,8 @@ def run(w, kv_heads=8, q_heads=32, question=100, tokens=16, keep=0.25, picks=16,
     mass = torch.zeros((cache.n_pages, H, PAGE), dtype=torch.float32, device=device)
     lengths = torch.full((n,), T, dtype=torch.int32, device=device)
     k, v = rows(kv)
-    _timed(torch, "store", times, lambda: cache.store(k, v, table, torch.zeros_like(lengths)))
+    _timed(torch, "store", times, lambda: cache.store(k, v, table, torch.zeros_like(lengths),
+                                                      mass=mass))
 
     # the question, then token after token: new rows behind the old ones, attention with weights
     g = torch.Generator(device=device).manual_seed(seed)
@@ -98,7 +99,7 @@ def run(w, kv_heads=8, q_heads=32, question=100, tokens=16, keep=0.25, picks=16,
         lengths += count
 
         def one():
-            cache.store(kn, vn, table, starts)
+            cache.store(kn, vn, table, starts, mass=mass)
             return cache.attend(q, table, lengths, max_len=at + count, mass=mass, decay=0.98)
         out = _timed(torch, what, times, one)
         if step == 0:

@@ -623,12 +623,14 @@ __global__ __launch_bounds__(256) void mass_scores_kernel(KvPool pool, KvSeqs S,
 // The weights of a page enter the second product times the page's V scale, relative to a running
 // reference of that product (`ref`, log2), so O needs no further factor, and l sums them without
 // the scale. No maximum is taken: the weights go by the reference that is there, and only where
-// they sum to more than kMost (less than fp16 holds) a tile's maximum is found, the accumulators
-// move to it, and the weights are taken again; a row's first tile does that. What fp16 holds is
-// normal down to 2^-(14 + kLift) of the reference (and steps of 2^-(24 + kLift) below), far
-// under what a sum around 1 shows.
-constexpr int kLift = 4;
-constexpr float kMost = 32768.0f;
+// 16 of them sum to more than fp16 holds a tile's maximum is found, the accumulators move to it, and
+// the weights are taken again; a row's first tile does that. Behind a move the heaviest weight is
+// 2^kLift, so that 16 as heavy still pass and nothing moves before one is 2^(16 - kLift) times as
+// heavy; below, a weight keeps 11 bits down to 2^-(14 + kLift) of the heaviest and is off by
+// 2^-(25 + kLift) of it under that. What a light weight keeps shows in the channels where the heavy
+// ones have nothing, so kLift is the largest that equal weights pass.
+constexpr int kLift = 11;
+constexpr float kMost = 65504.0f;
 
 __device__ __forceinline__ int tile_row(int t) {       // of token t of 32: its row in the K tile
   return 8 * ((t & 15) >> 2) + 4 * (t >> 4) + (t & 3);
@@ -878,47 +880,55 @@ void prompt_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles, int splits, int64
     mask(x, 0.0f);
 #pragma unroll
     for (int e = 0; e < 16; ++e) sum += x[e];
-    half8 a[D / 32][2];
     if (__builtin_expect(__any(!(sum <= kMost)) || !with_v, 0)) {
-      const float16v z = tile_scores<D>(k, q);
-      float16v seen = z;
-      mask(seen, kNegInf);
-      float t = seen[0];
+      float g;
+      if (with_v && !__any(!(sum < __builtin_inff()))) {
+        // weights that 32 bits hold move by a power of two
+        float t = x[0];
 #pragma unroll
-      for (int e = 1; e < 16; ++e) t = max2(t, seen[e]);
-      t = half_max(t);
-      t = t == kNegInf ? t : t * f;
-      if (with_v) {
-        const float now = fmaxf(ref, t + lv - (float)kLift);
-        const float g = __builtin_amdgcn_exp2f(ref - now);
-        ref = now;
-        l *= g;
+        for (int e = 1; e < 16; ++e) t = max2(t, x[e]);
+        const int up = __builtin_amdgcn_frexp_expf(half_max(t)) - kLift;
+        const int by = up > 0 ? up : 0;
+        g = __builtin_ldexpf(1.0f, -by);
+        ref += (float)by;
+        sum *= g;
 #pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt)
+        for (int e = 0; e < 16; ++e) x[e] *= g;
+      } else {
+        x = tile_scores<D>(k, q);
+        float t = kNegInf;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) o[dt][e] *= g;
+        for (int e = 0; e < 16; ++e) t = max2(t, !cut || e < seen_here ? x[e] : kNegInf);
+        t = half_max(t);
+        t = t == kNegInf ? t : t * f;
+        const float was = with_v ? ref : ref0;
+        const float now = fmaxf(was, with_v ? t + lv - (float)kLift : t);
+        g = __builtin_amdgcn_exp2f(was - now);
+        const float by = with_v ? lv - now : -now;
         sum = 0.0f;
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[e], f, lv - ref));
+        for (int e = 0; e < 16; ++e) x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], f, by));
         mask(x, 0.0f);
 #pragma unroll
         for (int e = 0; e < 16; ++e) sum += x[e];
-      } else {
-        const float now = fmaxf(ref0, t);
-        l0 *= __builtin_amdgcn_exp2f(ref0 - now);
-        ref0 = now;
-        float16v w;
+        if (with_v) {
+          ref = now;
+        } else {
+          ref0 = now;
+          l0 = __builtin_fmaf(l0, g, sum);
+          g = 1.0f;
+          sum = 0.0f;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[e], f, -now));
-        mask(w, 0.0f);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) l0 += w[e];
-        sum = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = 0.0f;
+          for (int e = 0; e < 16; ++e) x[e] = 0.0f;
+        }
       }
+      l *= g;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[dt][e] *= g;
     }
+    half8 a[D / 32][2];
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll

@@ -839,7 +839,11 @@ void prompt_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles, int splits, int64
     for (int e = 0; e < 16; ++e) o[dt][e] = 0.0f;
   float ref = -1e30f, l = 0.0f;      // O and l in units of 2^(ref - kLift)
   float ref0 = -1e30f, l0 = 0.0f;    // l of the pages without V, in units of 2^ref0
-  float v_top = 0x1p-40f;            // the largest V scale so far; below 2^-100 counts as none
+  // l has no V scale in it: where all of them are tiny it is kept 2^64 times smaller, or it would
+  // overflow.
+  bool tiny = false;
+  float l_unit = 1.0f;
+  float v_top = 0x1p-40f;            // the largest V scale so far; what is 2^-60 of it counts as none
 
   // The pages in turn, those that do not exist left out.
   int jn = j0;
@@ -934,7 +938,7 @@ void prompt_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles, int splits, int64
 #pragma unroll
       for (int e = 0; e < 2; ++e)
         a[dt][e] = *reinterpret_cast<const half8*>(&v[32 * dt + m][16 * half + 8 * e]);
-    l = sum == 0.0f ? l : __builtin_fmaf(sum, __builtin_amdgcn_rcpf(vs), l);
+    l = sum == 0.0f ? l : __builtin_fmaf(sum, __builtin_amdgcn_rcpf(vs) * l_unit, l);
     half8 p[2];
 #pragma unroll
     for (int e = 0; e < 16; e += 2) {
@@ -979,6 +983,17 @@ void prompt_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles, int splits, int64
   if (at[0] >= 0) {
     fetch_k(at[0]);
     fetch_v(at[0]);
+    float v_most = 0.0f;
+    for (int jb = j0; jb < j1; jb += 64) {
+      const int page = jb + lane < j1 ? kv_page(S, pool.P, seq, jb + lane) : -1;
+      const float v = page >= 0 ? pool.vs[(int64_t)page * pool.H + h] : 0.0f;
+      v_most = v < __builtin_inff() ? fmaxf(v_most, v) : v_most;
+    }
+    tiny = !__any(v_most >= 0x1p-40f);
+    if (tiny) {
+      l_unit = 0x1p-64f;
+      v_top = 0x1p-66f;
+    }
     ks = ks_n;
     vs = vs_n;
     widen_k<D, NT>(kr, L.k[0]);
@@ -1023,13 +1038,13 @@ void prompt_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles, int splits, int64
   l0 = half_sum(l0);
   if (row >= rows) return;
   // both sums to one reference, and O with them
-  ref -= (float)kLift;
+  const float l_ref = ref - (float)kLift + (tiny ? 64.0f : 0.0f);
   const bool some = l > 0.0f || l != l, some0 = l0 > 0.0f || l0 != l0;
   const bool empty = see <= 0 || !(some || some0);
-  const float top = fmaxf(some ? ref : -1e30f, some0 ? ref0 : -1e30f);
-  const float to_top = some ? __builtin_amdgcn_exp2f(ref - top) : 0.0f;
+  const float top = fmaxf(some ? l_ref : -1e30f, some0 ? ref0 : -1e30f);
+  const float to_top = some ? __builtin_amdgcn_exp2f(l_ref - top) : 0.0f;
   const float sum = l * to_top + (some0 ? l0 * __builtin_amdgcn_exp2f(ref0 - top) : 0.0f);
-  const float g = empty ? 0.0f : splits > 1 ? to_top : to_top / sum;
+  const float g = empty ? 0.0f : (splits > 1 ? to_top : to_top / sum) * l_unit;
   const int64_t u16 = ((int64_t)seq * pool.H + h) * ((rows + 15) / 16) + row / 16;
   float* dst = splits > 1 ? part + (u16 * splits + split) * kPart<D> : nullptr;
 #pragma unroll

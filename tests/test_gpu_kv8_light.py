@@ -70,3 +70,41 @@ def test_light_weights_of_whole_prompts(D, steps, vs, kind):
     q = torch.full((40, 100, 16, D), 1 / D, dtype=getattr(torch, kind), device="cuda")
     out = cache.attend(q, torch.from_numpy(t).cuda(), ints(torch, [192] * 40), scale=1.0)
     close(cache, out, q, t, 192, kind)
+
+
+@pytest.mark.parametrize("vs", [1e-30, 1e-33, 1e-36])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("split", [True, False])
+def test_tiny_values_of_prompts(D, vs, split):
+    """V scales that bf16 results hold and that are far below 1."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(D)
+    t, _, n = tables(torch, rng, 1, 3)
+    cache = light_cache(torch, t, n, D, vs, (6, 10, 1))
+    B = 1 if split else 40
+    if split:
+        t, table = much_room(torch, t)
+    else:
+        t = np.repeat(t, B, 0)
+        table = torch.from_numpy(t).cuda()
+    q = torch.full((B, 100, 16, D), 1 / D, device="cuda").bfloat16()
+    lse = torch.empty((B, 100, 16), device="cuda")
+    out = cache.attend(q, table, ints(torch, [192] * B), scale=1.0, lse=lse)
+    close(cache, out, q, t, 192, "bfloat16")
+    want = R.attend(R.Ref(cache), q[:1, :, :1].float().cpu().numpy(), t[:1], [192], [100], 1.0)[1]
+    assert np.abs(lse[:1, :, :1].cpu().numpy() - want).max() <= 1e-4
+
+
+def test_tiny_values_beside_ordinary_ones():
+    """Pages of V scales from 1e-36 to 1 in one prompt, in both orders."""
+    torch = torch_cuda()
+    for scales in ((1e-36, 1e-20, 1.0), (1.0, 1e-10, 1e-36), (0.0, 1e-36, 0.0), (1e-36, 0.0, 1e-14)):
+        rng = np.random.default_rng(3)
+        t, _, n = tables(torch, rng, 1, 3)
+        cache = light_cache(torch, t, n, 64, 1.0, (3, 5, 4))
+        for j, x in enumerate(scales):
+            cache.v_scale[int(t[0, j])] = x
+        t = np.repeat(t, 40, 0)
+        q = torch.full((40, 100, 16, 64), 1 / 64, device="cuda").bfloat16()
+        out = cache.attend(q, torch.from_numpy(t).cuda(), ints(torch, [192] * 40), scale=1.0)
+        close(cache, out, q, t, 192, "bfloat16")

@@ -519,7 +519,8 @@ uint64_t cg_kv8_select_workspace_bytes(const cg_kv8_cache* c, const cg_kv8_seqs*
  *   score(page) = fp32(sum over the group's heads and the channels of max(q8 lo, q8 hi)) * k_scale
  * with q8 = rint(clamp(q * 2^(6 - e), +-127)), 2^e the power of two at or below the largest |q| of
  * the group, and lo, hi the page's bounds: an upper bound of the page's summed q . k, in whole
- * numbers. Equal scores go to the lower column. Uses q, lengths, max_len, q_lens, n_picks and
+ * numbers (of at most 31 bits: groups past 520 heads of 256 channels, 1040 of 128, 2080 of 64 are
+ * CG_ERR_SHAPE). Equal scores go to the lower column. Uses q, lengths, max_len, q_lens, n_picks and
  * dtype of `a`; the workspace as for cg_kv8_attend. Asynchronous. */
 int cg_kv8_select(const cg_kv8_cache* c, const cg_kv8_seqs* s, const cg_kv8_attn* a,
                   int32_t recent, int32_t* picks_out, void* workspace, uint64_t workspace_bytes,

@@ -89,6 +89,9 @@ int check_attend(const cg_kv8_cache* c, const cg_kv8_seqs* s, const cg_kv8_attn*
   return CG_OK;
 }
 
+// A page's score is a sum over the group's channels of products of two codes, in 32 bits.
+bool score_fits(int64_t group, int64_t D) { return group * D * (127 * 127) <= INT32_MAX; }
+
 int hip_rc(hipError_t e) { return e == hipSuccess ? CG_OK : CG_ERR_HIP; }
 
 }  // namespace
@@ -156,7 +159,7 @@ uint64_t cg_kv8_select_workspace_bytes(const cg_kv8_cache* c, const cg_kv8_seqs*
   KvSeqs S;
   KvAttn A;
   if (check_cache(c, &pool) != CG_OK || check_seqs(s, pool, &S) != CG_OK ||
-      check_queries(a, pool, S, &A) != CG_OK)
+      check_queries(a, pool, S, &A) != CG_OK || !score_fits(A.group, c->head_dim))
     return 0;
   return cg_kv8_select_ws(S, pool.H, A.nq, A.max_len);
 }
@@ -171,7 +174,7 @@ int cg_kv8_select(const cg_kv8_cache* c, const cg_kv8_seqs* s, const cg_kv8_attn
   if (rc == CG_OK) rc = check_seqs(s, pool, &S);
   if (rc == CG_OK) rc = check_queries(a, pool, S, &A);
   if (rc != CG_OK) return rc;
-  if (a->n_picks <= 0 || recent < 0) return CG_ERR_SHAPE;
+  if (a->n_picks <= 0 || recent < 0 || !score_fits(A.group, c->head_dim)) return CG_ERR_SHAPE;
   if (!pool.bounds || !picks_out || !aligned(picks_out, 4)) return CG_ERR_ARG;
   const uint64_t need = cg_kv8_select_ws(S, pool.H, A.nq, A.max_len);
   if (need && (!workspace || !aligned(workspace, 256))) return CG_ERR_ARG;

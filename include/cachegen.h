@@ -398,8 +398,8 @@ int cg_decode_tokens(const cg_params* p, const uint32_t* words, const uint64_t* 
  * memory of the caller. Page numbers and lengths are read on the device and never trusted: a page
  * number outside [0, n_pages) is a page without tokens, a length is cut to the table's row and to
  * the caller's bound. Every call is asynchronous on the given stream and none allocates. Rows of
- * K, V, queries and outputs are fp16 or bf16 with any strides (the last dimension contiguous);
- * 16-byte aligned rows are read and written 16 bytes at a time. */
+ * K, V, queries and outputs are fp16 or bf16 with any strides (the last dimension contiguous); where
+ * they are 16-byte aligned, K, V and queries move 16 bytes at a time. */
 #define CG_KV8_PAGE 64
 
 /* The workspaces of cg_kv8_attend and cg_kv8_select start with this many bytes of counters, which

@@ -361,7 +361,7 @@ struct KvAttn {
   KvRows q, out;
   int32_t max_len, nq, group, n_picks;
   float scale, decay;
-  bool wide_q, wide_out;        // rows on 16-byte boundaries
+  bool wide_q;                  // q's rows on 16-byte boundaries
 };
 
 // The workspaces' first bytes: a counter for each tile whose pages are split, zero between calls

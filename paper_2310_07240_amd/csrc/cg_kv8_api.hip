@@ -79,7 +79,6 @@ int check_attend(const cg_kv8_cache* c, const cg_kv8_seqs* s, const cg_kv8_attn*
     return CG_ERR_ARG;
   if ((a->mass_in && !a->mass_out) || (a->mass_out && a->picks)) return CG_ERR_ARG;
   A->out = rows(a->out);
-  A->wide_out = wide(a->out);
   A->lse = a->lse;
   A->picks = a->picks;
   A->mass_in = a->mass_in;

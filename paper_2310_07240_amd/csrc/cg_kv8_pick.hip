@@ -447,15 +447,14 @@ template <int D, bool BF16>
 __global__ __launch_bounds__(kSelectThreads) void select_kernel(KvPool pool, KvSeqs S, KvAttn A,
                                                                 int recent, int splits,
                                                                 int32_t* out, uint32_t* keys,
-                                                                int np, uint32_t* arrived,
-                                                                int64_t row0) {
+                                                                int np, uint32_t* arrived) {
   __shared__ PickLds<kSelectThreads> L;
   __shared__ float red[kSelectThreads / 64];
   __shared__ uint32_t w0[2 * D / 4], w1[2 * D / 4];    // of the lowest codes, then the highest
   __shared__ uint32_t others;
   const int tid = threadIdx.x;
   const int split = blockIdx.x % splits;
-  const int64_t row = row0 + blockIdx.x / splits;
+  const int64_t row = blockIdx.x / splits;
   const int h = (int)(row % pool.H), vseq = (int)(row / pool.H);
   const int seq = vseq / A.nq, i = vseq % A.nq;
   int32_t* picks = out + row * A.n_picks;
@@ -595,13 +594,10 @@ void select_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, int recent, 
   if (splits > (np + round - 1) / round) splits = (np + round - 1) / round;
   if (splits < 1) splits = 1;
   uint32_t* keys = reinterpret_cast<uint32_t*>(ws + kKv8Front);
-  constexpr int64_t kMost = 1 << 23;                   // workgroups a launch, below 2^32 threads
-  for (int64_t row0 = 0; row0 < rows; row0 += kMost) {
-    const int64_t n = rows - row0 < kMost ? rows - row0 : kMost;
-    hipLaunchKernelGGL((select_kernel<D, BF16>), dim3((unsigned)(n * splits)),
-                       dim3(kSelectThreads), 0, st, pool, S, A, recent, (int)splits, picks, keys,
-                       np, reinterpret_cast<uint32_t*>(ws), row0);
-  }
+  // (the C ABI takes at most 2^23 rows: below 2^32 threads)
+  hipLaunchKernelGGL((select_kernel<D, BF16>), dim3((unsigned)(rows * splits)),
+                     dim3(kSelectThreads), 0, st, pool, S, A, recent, (int)splits, picks, keys, np,
+                     reinterpret_cast<uint32_t*>(ws));
 }
 
 }  // namespace

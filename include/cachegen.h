@@ -494,7 +494,9 @@ typedef struct cg_kv8_attn {
   float decay;
 } cg_kv8_attn;
 
-/* Device scratch that cg_kv8_attend needs (bytes); 0 if an argument is invalid or none is needed. */
+/* Device scratch that cg_kv8_attend needs (bytes); 0 if an argument is invalid or none is needed. It
+ * follows max_len (or the table's row, if that is shorter), not the lengths, which only the device
+ * knows. */
 uint64_t cg_kv8_attend_workspace_bytes(const cg_kv8_cache* c, const cg_kv8_seqs* s,
                                        const cg_kv8_attn* a);
 

@@ -31,6 +31,14 @@ int check_seqs(const cg_kv8_seqs* s, const KvPool& pool, KvSeqs* out) {
   return CG_OK;
 }
 
+// The caller's bound of the lengths, or the table's row where that is the smaller: no sequence is
+// longer, and work and scratch are laid out for it. (The kernels round tokens up to pages in 32 bits.)
+int32_t most_tokens(int32_t max_len, const KvSeqs& S) {
+  int64_t room = (int64_t)S.width * kPage;
+  if (room > INT32_MAX - (kPage - 1)) room = INT32_MAX - (kPage - 1);
+  return max_len < room ? max_len : (int32_t)room;
+}
+
 bool bad_rows(const cg_kv8_rows* r) { return !r || !r->data || !aligned(r->data, 2); }
 
 KvRows rows(const cg_kv8_rows& r) {
@@ -59,7 +67,7 @@ int check_queries(const cg_kv8_attn* a, const KvPool& pool, const KvSeqs& S, KvA
   out->q_lens = a->q_lens;
   out->q = rows(a->q);
   out->wide_q = wide(a->q);
-  out->max_len = a->max_len;
+  out->max_len = most_tokens(a->max_len, S);
   out->nq = a->n_q;
   out->group = a->n_q_heads / pool.H;
   out->n_picks = a->n_picks;
@@ -195,6 +203,7 @@ int cg_kv8_evict(const cg_kv8_cache* c, const cg_kv8_seqs* s, const int32_t* len
   if (!lengths || !aligned(lengths, 4) || !mass || !aligned(mass, 4) || !kept ||
       !aligned(kept, 4) || !new_lengths || !aligned(new_lengths, 4))
     return CG_ERR_ARG;
+  max_len = most_tokens(max_len, S);
   const int64_t most = keep < max_len ? keep : max_len;
   if ((most + kPage - 1) / kPage > T.width) return CG_ERR_CAPACITY;
   return hip_rc(cg_launch_kv8_evict(pool, S, c->head_dim, lengths, max_len, mass, keep, recent, T,

@@ -80,6 +80,11 @@ def _need(ok, what):
         raise ValueError(what)
 
 
+def _bound(max_len, width):
+    """The bound of the lengths: the caller's, or what the table's row holds."""
+    return min(width * PAGE, 0x7fffffff) if max_len is None else max_len
+
+
 class Kv8Cache:
     """A pool of pages on one GPU and the operators on it.
 
@@ -316,7 +321,7 @@ class Kv8Cache:
                                       (self.n_pages, self.n_heads, PAGE))
         a = _ATTN.pack(nq, heads, kind, self._scale if scale is None else scale,
                        self._per_seq(lengths, "lengths", n),
-                       width * PAGE if max_len is None else max_len,
+                       _bound(max_len, width),
                        self._per_seq(q_lens, "q_lens", n), *self._strided(q, "q", shape, q.dtype),
                        *self._strided(out, "out", shape, q.dtype),
                        0 if lse is None else self._tensor(lse, "lse", self._f32, shape[:3]),
@@ -339,7 +344,7 @@ class Kv8Cache:
             out = self._empty(want, self._i32, stream)
         rows = self._strided(q, "q", shape, q.dtype)
         a = _ATTN.pack(nq, heads, kind, 0.0, self._per_seq(lengths, "lengths", n),
-                       width * PAGE if max_len is None else max_len,
+                       _bound(max_len, width),
                        self._per_seq(q_lens, "q_lens", n), *rows, *rows, 0, 0, n_picks, 0, 0, 0.0)
         L = _lib()
         self._launch("cg_kv8_select", L.cg_kv8_select, stream, s, a, recent,
@@ -360,6 +365,6 @@ class Kv8Cache:
         new_lengths = self._empty((n,), self._i32, stream)
         self._launch(
             "cg_kv8_evict", _lib().cg_kv8_evict, stream, s, self._per_seq(lengths, "lengths", n),
-            width * PAGE if max_len is None else max_len,
+            _bound(max_len, width),
             self._mass(mass), keep, recent, to, kept.data_ptr(), new_lengths.data_ptr())
         return kept, new_lengths

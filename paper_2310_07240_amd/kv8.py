@@ -211,7 +211,8 @@ class Kv8Cache:
             return self._cleared(need, stream)
         ws = self._ws.get(handle)
         if ws is None or ws[1] < need:
-            ws = self._ws[handle] = self._cleared(need, stream)
+            # (a quarter more: a decode's need grows with every page)
+            ws = self._ws[handle] = self._cleared(need + need // 4, stream)
         return ws
 
     def _cleared(self, need, stream):

@@ -50,3 +50,14 @@ def test_captures_leave_nothing_behind(cache):
     t = weakref.ref(cache._scratch(None, STREAM, 5000)[2])
     gc.collect()
     assert t() is None and not cache._ws
+
+
+def test_a_need_that_grows_by_steps_is_not_met_step_by_step(cache):
+    """A sequence of tokens needs a little more with every page."""
+    need, seen = 100000, set()
+    for _ in range(200):
+        ws = cache._scratch(None, STREAM, need)
+        assert ws[1] >= need
+        seen.add(ws[1])
+        need += 4096
+    assert len(seen) <= 12                     # 9 times as much at the end: quarters, ten of them

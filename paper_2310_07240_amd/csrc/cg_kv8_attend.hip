@@ -1244,6 +1244,7 @@ void mass_rows_kernel(KvPool pool, KvSeqs S, KvAttn A, int np, int shares, int64
 #pragma unroll
       for (int c = 0; c < CH; ++c)
         *reinterpret_cast<uint4v*>(&mine[c * RC + lane / LR][lane % LR * 8]) = u[c];
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // the other lanes' rows are read
       const float c0 = -z * kLog2e;
       const int seen = see;
       if (32 * (tile + shares) < rows) fetch(tile + shares);
@@ -1259,6 +1260,7 @@ void mass_rows_kernel(KvPool pool, KvSeqs S, KvAttn A, int np, int shares, int64
 #pragma unroll
         for (int t = 0; t < 2; ++t) x[t] = mfma32<BF16>(k[t][s], q, x[t]);
       }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // before the next tile's overwrite them
       if (__any(seen < pos0 + kPage)) {          // some row sees the page in part or not at all
 #pragma unroll
         for (int t = 0; t < 2; ++t)

@@ -138,8 +138,12 @@ __device__ __forceinline__ bool store_page(const KvPool& pool, int page, int h, 
 // Which pages a launch is for: those that keep tokens (a sequence's first, if any), those that do
 // not, or both. Keeping takes 187 registers where coding new rows takes 128, so one kernel for both
 // leaves two waves on a SIMD: 217 us for 805 MB of rows and codes, against 176 (4.6 TB/s) and 5 for
-// the second launch with one for each. Up to kFewPages pages all run at once anyway, and one launch
-// for both is the shorter.
+// the second launch with one for each. Up to kFewPages pages (of heads) all run at once anyway, and
+// one launch for both is the shorter. (One / two, us, 8 heads of 128 channels. Rows behind 100
+// tokens: 8192 of one sequence, 1032 pages, 17.6 / 22.3; 16384, 2056, 27.5 / 29.8; 32768, 4104, 47.2 /
+// 43.3. 4096 rows from a sequence's start: of 4, 2080 pages, 27.2 / 24.0; of 8, 4160, 47.3 / 37.4. One
+// row behind 100 tokens of 256 sequences, 2048 pages, 33.8 / 36.9, of 512, 4096, 62.5 / 67.8: where
+// nearly all pages keep tokens the second launch never pays.)
 enum Pages { kBoth, kNew, kKept };
 
 template <int D, bool BF16, bool VEC, Pages WHICH>

@@ -69,6 +69,8 @@ def _lib():
         L.cg_kv8_select_workspace_bytes.restype = U64
         L.cg_kv8_select.argtypes = [_P, _P, _P, _I32, _P, _P, U64, _P]
         L.cg_kv8_evict.argtypes = [_P, _P, _P, _I32, _P, _I32, _I32, _P, _P, _P, _P]
+        L.hipStreamIsCapturing.argtypes = [_P, _P]        # of the runtime that the library links
+        L.hipStreamIsCapturing.restype = ctypes.c_int
         for n in ("store", "load", "attend", "select", "evict"):
             getattr(L, "cg_kv8_" + n).restype = ctypes.c_int
         _LIB = L
@@ -124,9 +126,11 @@ class Kv8Cache:
                                     for n in want))
         self._cp = ctypes.addressof(self._c)
         self._raw_stream = torch._C._cuda_getCurrentRawStream
-        self._current = (torch._C._cuda_getDevice if self.device.type == "cuda"
-                         else lambda: self._index)
+        self._on_gpu = self.device.type == "cuda"
+        self._current = torch._C._cuda_getDevice if self._on_gpu else lambda: self._index
         self._ws, self._lock = {}, threading.Lock()
+        self._status = _I32()
+        self._status_p = ctypes.addressof(self._status)
         self._types = {torch.float16: 0, torch.bfloat16: 1}
         self._scale = 1.0 / math.sqrt(D)
 
@@ -166,7 +170,7 @@ class Kv8Cache:
     def _handle(self, stream):
         """The HIP stream's handle: the caller's, or torch's current one; of the cache's GPU."""
         if stream is None:
-            if self.device.type == "cuda":
+            if self._on_gpu:
                 return self._raw_stream(self._index)
         elif getattr(stream, "device", self.device) == self.device:
             return stream.cuda_stream
@@ -207,7 +211,7 @@ class Kv8Cache:
         one needs more, and may be at work when the graph is replayed. It comes from the graph's
         memory pool, which lives as long as the graph (and may give it to a later call of the same
         capture, which runs behind this one); the graph clears its counters."""
-        if self._capturing(stream, handle):
+        if self._capturing(handle):
             return self._cleared(need, stream)
         ws = self._ws.get(handle)
         if ws is None or ws[1] < need:
@@ -225,11 +229,10 @@ class Kv8Cache:
                 t[:ZEROED].zero_()
         return t.data_ptr(), need, t
 
-    def _capturing(self, stream, handle):
-        if stream is None or handle == self._raw_stream(self._index):
-            return self.torch.cuda.is_current_stream_capturing()
-        with self.torch.cuda.stream(stream):
-            return self.torch.cuda.is_current_stream_capturing()
+    def _capturing(self, handle):
+        """Whether the stream is being captured (the null stream cannot be); under the lock."""
+        return handle != 0 and (_lib().hipStreamIsCapturing(handle, self._status_p) != 0
+                                or self._status.value != 0)
 
     def _mass(self, mass):
         return self._tensor(mass, "mass", self._f32, (self.n_pages, self.n_heads, PAGE))

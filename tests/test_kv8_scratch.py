@@ -61,3 +61,22 @@ def test_a_need_that_grows_by_steps_is_not_met_step_by_step(cache):
         seen.add(ws[1])
         need += 4096
     assert len(seen) <= 12                     # 9 times as much at the end: quarters, ten of them
+
+
+def test_which_streams_are_captured(monkeypatch):
+    """The runtime is asked about the call's own stream, whichever is current; what it cannot tell
+    counts as captured, the null stream never does."""
+    import ctypes
+    pytest.importorskip("torch")
+    states, asked = {5: (0, 0), 6: (0, 1), 7: (0, 2), 8: (900, 0)}, []
+
+    class Lib:
+        def hipStreamIsCapturing(self, handle, status):
+            asked.append(handle)
+            ctypes.c_int.from_address(status).value = states[handle][1]
+            return states[handle][0]
+
+    monkeypatch.setattr(kv8, "_lib", Lib)
+    c = kv8.Kv8Cache(4, 2, 64, device="cpu")
+    assert [c._capturing(h) for h in (0, 5, 6, 7, 8, 5)] == [False, False, True, True, True, False]
+    assert asked == [5, 6, 7, 8, 5]

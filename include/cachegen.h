@@ -500,10 +500,14 @@ typedef struct cg_kv8_attn {
 uint64_t cg_kv8_attend_workspace_bytes(const cg_kv8_cache* c, const cg_kv8_seqs* s,
                                        const cg_kv8_attn* a);
 
-/* The attention above. Products take fp16 operands (the codes and fp16 queries exactly, bf16
- * queries under a power of two per row, softmax weights rounded to fp16) and sum in 32 bits;
- * maxima, sums, lse and mass are 32-bit. Results do not depend on the order in which parts of the
- * work end.
+/* The attention above. Products take fp16 operands and sum in 32 bits; maxima, sums, lse and mass
+ * are 32-bit. The codes and fp16 queries are exact. bf16 queries go in under a power of two per row:
+ * exactly down to 2^-17 of the row's largest, off by 2^-25 of it at most below. Softmax weights are
+ * rounded to fp16, 2^-11 of a weight, down to 2^-29 of the heaviest in its page where there are few
+ * rows, and to 2^-25 of the row's heaviest (lighter ones are off by 2^-36 of it at most) where there
+ * are many; there, pages whose V scale is below 2^-60 of the sequence's largest, or subnormal, may
+ * add nothing to `out`. Which of the two a call takes follows its sizes and max_len. Results do not
+ * depend on the order in which parts of the work end.
  *   workspace   device scratch of workspace_bytes >= cg_kv8_attend_workspace_bytes, 256-byte
  *               aligned (may be NULL where that is 0), its first CG_KV8_WORKSPACE_ZEROED bytes
  *               zero.
@@ -520,7 +524,7 @@ uint64_t cg_kv8_select_workspace_bytes(const cg_kv8_cache* c, const cg_kv8_seqs*
  * its ceil(n / 64) pages are taken, and of the others the best by
  *   score(page) = fp32(sum over the group's heads and the channels of max(q8 lo, q8 hi)) * k_scale
  * with q8 = rint(clamp(q * 2^(6 - e), +-127)), 2^e the power of two at or below the largest |q| of
- * the group, and lo, hi the page's bounds: an upper bound of the page's summed q . k, in whole
+ * the group, and lo, hi the page's bounds: an upper bound of the page's summed q8 . k, in whole
  * numbers (of at most 31 bits: groups past 520 heads of 256 channels, 1040 of 128, 2080 of 64 are
  * CG_ERR_SHAPE). Equal scores go to the lower column. Uses q, lengths, max_len, q_lens, n_picks and
  * dtype of `a`; the workspace as for cg_kv8_attend. Asynchronous. */

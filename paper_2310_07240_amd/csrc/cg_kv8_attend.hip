@@ -4,8 +4,9 @@
 // S = q K^T and O = P V, with the softmax carried along: running maximum m, running sum l, and O
 // under the reference m, all in 32 bits. The codes go into the matrix units as fp16 (exact), the
 // scales of the page are applied to S and to the page's share of O in 32 bits, and P is rounded
-// to fp16 for the second product (relative 2^-11 of a weight down to 2^-29 of the page's largest,
-// the rounding that the fp16 result gets anyway; l sums the unrounded weights).
+// to fp16 for the second product, the rounding that the fp16 result gets anyway (attend_kernel:
+// relative 2^-11 of a weight down to 2^-29 of the page's largest; prompt_kernel, whose reference is
+// the row's: down to 2^-25 of the heaviest; l sums the unrounded weights).
 //
 // Operand layout (v_mfma_f32_16x16x32_f16; lane = 16 g + m): both products are taken transposed,
 // S^T = K q^T and O^T = V^T P^T, so a lane's results belong to one query row (m) throughout and
@@ -786,8 +787,8 @@ constexpr int kPromptWaves = D == 256 ? 4 : 8;
 // Workgroup = (sequence, KV head, tile of 32 rows a wave, split of the pages). `it0`: where this
 // launch starts (see in_launches). Bound by the matrix units and the vector instructions of the
 // softmax (32 exponentials a lane and page), which two waves on a SIMD overlap in part: 2 sequences
-// of 8K, 64 heads, 2048 queries, 962 GFLOP in 0.92 to 1.03 ms as the clock goes, 0.94 to 1.05
-// PFLOP/s (a library product of 8192 cubed: 1.23); 500 queries of 32 heads over 4K, 33 GFLOP, 48 us.
+// of 8K, 64 heads, 2048 queries, 962 GFLOP in 0.92 to 1.07 ms as the clock goes, 0.90 to 1.05
+// PFLOP/s (a library product of 8192 cubed: 1.23); 500 queries of 32 heads over 4K, 33 GFLOP, 51 us.
 template <int D, bool BF16>
 __global__ __launch_bounds__(64 * kPromptWaves<D>, kPromptWaves<D> / 4)
 void prompt_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles, int splits, int64_t it0,

@@ -404,7 +404,8 @@ int cg_decode_tokens(const cg_params* p, const uint32_t* words, const uint64_t* 
 
 /* The workspaces of cg_kv8_attend and cg_kv8_select start with this many bytes of counters, which
  * the caller clears once, before a workspace's first use; every call leaves them zero. The rest of
- * a workspace may hold anything. Calls that may overlap need workspaces of their own. */
+ * a workspace may hold anything. Calls that may overlap need workspaces of their own, and so do two
+ * host threads that call on one stream: a call is up to three launches. */
 #define CG_KV8_WORKSPACE_ZEROED 4096
 
 enum { CG_KV8_F16 = 0, CG_KV8_BF16 = 1 };

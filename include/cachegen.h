@@ -422,7 +422,8 @@ typedef struct cg_kv8_cache {
                              channel over the page's tokens; NULL: not kept (cg_kv8_select
                              needs them) */
   float* mass;            /* [P][H][64]: token weights as cg_kv8_attend adds them up, which
-                             cg_kv8_store clears for the tokens it writes; NULL: it clears none */
+                             cg_kv8_store clears for the tokens it writes, and which move with the
+                             pages in cg_kv8_reserve, copy and compact; NULL: none are touched */
 } cg_kv8_cache;
 
 typedef struct cg_kv8_seqs {
@@ -547,6 +548,143 @@ int cg_kv8_select(const cg_kv8_cache* c, const cg_kv8_seqs* s, const cg_kv8_attn
 int cg_kv8_evict(const cg_kv8_cache* c, const cg_kv8_seqs* s, const int32_t* lengths,
                  int32_t max_len, float* mass, int32_t keep, int32_t recent,
                  const cg_kv8_seqs* to, int32_t* kept, int32_t* new_lengths, hipStream_t stream);
+
+/* ---- Requests that share a context ---------------------------------------------------------
+ * Sequences may hold the same pages: refs [P] (int32, the caller's, on the device) counts the table
+ * rows that hold each page, and 0 marks it free. A context is forked into requests, which share its
+ * pages; before a request writes, cg_kv8_reserve gives it pages, and of a page that it shares a copy
+ * of its own; cg_kv8_release gives back what a request no longer needs, all of it or what lies
+ * behind a length (drafted tokens that were not accepted). Table entries outside [0, n_pages) are
+ * "no page" (-1 is written). Every call is asynchronous, allocates nothing, and gives the same
+ * result in whatever order its parts run. A page's weights (c->mass, if given) go where the page
+ * goes. */
+
+/* Children of sequences: row c of `to` receives the pages of sequence parents[c] of `s` that hold
+ * its first min(lengths[parent], ends[c]) tokens, -1 behind them, and each page's count goes up by
+ * one for each child.
+ *   parents      [to->n_seq]; one outside [0, s->n_seq) makes an empty sequence.
+ *   ends         [to->n_seq] tokens to share, or NULL: all.
+ *   to           its table is written: at least s->max_pages columns, no memory of a row of `s`
+ *                that is a parent's (else the result is undefined). What its rows held is not
+ *                released.
+ *   new_lengths  out [to->n_seq]. */
+int cg_kv8_fork(const cg_kv8_cache* c, const cg_kv8_seqs* s, const int32_t* lengths,
+                const int32_t* parents, const int32_t* ends, const cg_kv8_seqs* to,
+                int32_t* new_lengths, int32_t* refs, hipStream_t stream);
+
+/* Device scratch of cg_kv8_reserve (bytes): 4 a sequence's columns and up to 4 a page. 0 if an
+ * argument is invalid. */
+uint64_t cg_kv8_reserve_workspace_bytes(const cg_kv8_cache* c, const cg_kv8_seqs* s);
+
+/* Pages for tokens lengths[b] .. lengths[b] + counts[b] - 1 of every sequence (as far as its row of
+ * the table goes), which a cg_kv8_store will write. Of the columns they touch, one that holds earlier
+ * tokens keeps its page if its count is 1, and gets a copy of it if that is more (a lost page, -1,
+ * stays lost); any other keeps a page whose count is 1 and gets a free one otherwise. The i-th page
+ * wanted, by sequence and column, is the i-th free one; its count becomes 1, and that of the page it
+ * replaces goes down by one. Sequences of one call that share a page get a copy each, and pages that
+ * they all leave are free behind the call, not in it.
+ *   s        its table is written.
+ *   missing  out [1]: 0, or how many pages more it would have taken; then nothing is changed.
+ *   workspace as for cg_kv8_attend. */
+int cg_kv8_reserve(const cg_kv8_cache* c, const cg_kv8_seqs* s, const int32_t* lengths,
+                   const int32_t* counts, int32_t* refs, int32_t* missing, void* workspace,
+                   uint64_t workspace_bytes, hipStream_t stream);
+
+/* Gives back the pages of every sequence from column ceil(keep[b] / 64) on (keep NULL: all): their
+ * counts go down by one (never below 0), the entries become -1. What the pages hold stays until
+ * someone else gets them. */
+int cg_kv8_release(const cg_kv8_cache* c, const cg_kv8_seqs* s, const int32_t* keep, int32_t* refs,
+                   hipStream_t stream);
+
+/* Page src[i] to page dst[i] for i < n, codes, scales, bounds and weights. Pairs outside the pool
+ * are skipped. No page is the target of two pairs, or of one and the source of another, or the
+ * result is undefined. */
+int cg_kv8_copy(const cg_kv8_cache* c, const int32_t* src, const int32_t* dst, int32_t n,
+                hipStream_t stream);
+
+/* Device scratch of cg_kv8_compact (bytes), 8 a page. 0 if c is invalid. */
+uint64_t cg_kv8_compact_workspace_bytes(const cg_kv8_cache* c);
+
+/* The pages in use (count above 0) move to the front of the pool: with L of them, the i-th that lies
+ * at L or behind goes to the i-th free page before L. The others stay.
+ *   s            the sequences' table as it was.
+ *   new_table    out [n_seq][max_pages]: the same with the pages' new numbers (may be s->table).
+ *   new_refs     out [P]: the counts as the pages lie now (not refs itself).
+ *   moved        out [P]: the new number of each page, -1 of one that was free: for other tables.
+ *   n_live       out [1]: L. */
+int cg_kv8_compact(const cg_kv8_cache* c, const cg_kv8_seqs* s, const int32_t* refs,
+                   int32_t* new_table, int32_t* new_refs, int32_t* moved, int32_t* n_live,
+                   void* workspace, uint64_t workspace_bytes, hipStream_t stream);
+
+/* The contexts of cg_kv8_attend_shared. */
+typedef struct cg_kv8_contexts {
+  cg_kv8_seqs seqs;             /* the contexts' pages */
+  const int32_t* lengths;       /* [seqs.n_seq] tokens of each */
+  int32_t max_len;              /* no length is above it (longer ones are cut to it) */
+  const int32_t* firsts;        /* [seqs.n_seq + 1], ascending: context p is read by sequences
+                                   firsts[p] .. firsts[p + 1] - 1 of the call */
+  int32_t max_users;            /* no context is read by more of them (those behind see none) */
+} cg_kv8_contexts;
+
+/* Device scratch that cg_kv8_attend_shared needs (bytes); 0 if an argument is invalid or none is
+ * needed. It follows max_users and the two max_len. */
+uint64_t cg_kv8_attend_shared_workspace_bytes(const cg_kv8_cache* c, const cg_kv8_contexts* x,
+                                              const cg_kv8_seqs* s, const cg_kv8_attn* a);
+
+/* Attention of sequences that share contexts, whose pages are read once for all that share them.
+ * The query tokens of a sequence see all of its context (none, if it has none) and, as in
+ * cg_kv8_attend, their sequence's own tokens up to their place: with S = scale * q . k over both,
+ *   out = softmax(S) v,   lse = log sum exp(S).
+ *   s    the sequences' own pages, behind the context; lengths and max_len of `a` are theirs. With
+ *        table NULL there are none (max_pages and a->lengths are not read): attention of n_seq
+ *        sequences over the contexts alone, as over the states of an encoder.
+ *   a    as for cg_kv8_attend; without picks and weights (CG_ERR_ARG).
+ * Precision, workspace and the rest as for cg_kv8_attend; what is said there of page scales within
+ * a sequence holds within a context and within a sequence's own pages. */
+int cg_kv8_attend_shared(const cg_kv8_cache* c, const cg_kv8_contexts* x, const cg_kv8_seqs* s,
+                         const cg_kv8_attn* a, void* workspace, uint64_t workspace_bytes,
+                         hipStream_t stream);
+
+/* Drafted tokens against the target's probabilities. Sequence b has drafts x_0 .. x_(counts[b] - 1);
+ * p_j is row j of its target probabilities (n_drafts + 1 rows: the last is behind all drafts), q_j
+ * row j of the draft's. x_j is accepted while u_j q_j(x_j) < p_j(x_j) (so with probability
+ * min(1, p / q)); the first that is not ends the drafts, and one more token is drawn, from the
+ * weights max(p_j - q_j, 0) there, or from p of the row behind the last accepted draft: the tokens
+ * are distributed as the target's. */
+#define CG_VERIFY_MAX_VOCAB (1 << 20)
+#define CG_VERIFY_MAX_DRAFTS 1024
+enum { CG_KV8_F32 = 2 };        /* a type of probabilities, beside CG_KV8_F16 and CG_KV8_BF16 */
+
+typedef struct cg_verify {
+  int32_t n_seq, n_drafts, vocab, dtype;
+  const void* target;           /* [n_seq][n_drafts + 1][vocab], rows t_row_stride apart */
+  int64_t t_seq_stride, t_row_stride;          /* in elements */
+  const void* draft;            /* [n_seq][n_drafts][vocab], or NULL: each draft was sure (q = 1 for
+                                   it, 0 for the others) */
+  int64_t d_seq_stride, d_row_stride;
+  const int32_t* drafts;        /* [n_seq][n_drafts]; a token outside [0, vocab) is not accepted */
+  const int32_t* counts;        /* [n_seq], at most n_drafts; below 0 the sequence sits out; NULL:
+                                   n_drafts */
+  const float* u;               /* [n_seq][n_drafts + 1] in [0, 1): u_j for draft j, the last for the
+                                   token that is drawn */
+  int32_t* tokens;              /* out [n_seq][n_drafts + 1]: the accepted drafts and the token
+                                   drawn, -1 behind it */
+  int32_t* accepted;            /* out [n_seq] drafts accepted; 0 of one that sits out */
+  const int32_t* lengths;       /* [n_seq] tokens held, the drafts' own among them, and out: */
+  int32_t* new_lengths;         /* those less the drafts not accepted (may be lengths), or NULL */
+} cg_verify;
+
+/* Device scratch of cg_verify_drafts (bytes); 0 if the sizes are invalid. */
+uint64_t cg_verify_workspace_bytes(const cg_verify* v);
+
+/* The above. A probability counts as 0 where it is NaN or below 0 and as 1 above 1; the acceptance
+ * is decided exactly; a weight is a difference of probabilities rounded to multiples of 2^-42, and of
+ * a row whose weights sum to W such multiples the token drawn is the first with
+ * (weights up to it) > floor(floor(u 2^24) W / 2^24), all in whole numbers. Where nothing of p is
+ * above q the weights are p's own, and -1 is drawn where those are all 0. n_drafts may be 0. The
+ * workspace as for cg_kv8_attend. Asynchronous. */
+int cg_verify_drafts(const cg_verify* v, void* workspace, uint64_t workspace_bytes,
+                     hipStream_t stream);
 
 /* Static description of a return code; never NULL. */
 const char* cg_strerror(int code);

@@ -378,6 +378,26 @@ struct KvAttnPlan {
 };
 
 KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& seqs, const KvAttn& a, int D);
+
+// Which requests read a context: context p those from firsts[p] on, `most` at most, of `n_seq` with
+// `per` query tokens each.
+struct KvUsers {
+  const int32_t* firsts;
+  int32_t n_seq, most, per;
+};
+
+// A call over contexts and the requests' own pages: the plan of each (own.tiles = 0: no own pages),
+// and where their partial states lie.
+struct KvSharedPlan {
+  KvAttnPlan shared, own;
+  uint64_t shared_off, own_off, total;
+};
+
+KvSharedPlan cg_kv8_shared_plan(const KvPool&, const KvSeqs& contexts, const KvAttn& over_contexts,
+                                const KvSeqs& own, const KvAttn& over_own, int D);
+hipError_t cg_launch_kv8_shared(const KvPool&, const KvSeqs& contexts, const KvAttn& over_contexts,
+                                const KvUsers&, const KvSeqs& own, const KvAttn& over_own, int D,
+                                bool bf16, void* ws, hipStream_t);
 hipError_t cg_launch_kv8_store(const KvPool&, const KvSeqs&, int D, bool bf16,
                                const int32_t* starts, const int32_t* counts, int n_tokens,
                                const KvRows& k, const KvRows& v, uint32_t* status, hipStream_t);
@@ -393,3 +413,30 @@ hipError_t cg_launch_kv8_evict(const KvPool&, const KvSeqs&, int D, const int32_
                                int max_len, float* mass, int keep, int recent,
                                const KvSeqs& to, int32_t* kept, int32_t* new_lengths,
                                hipStream_t);
+hipError_t cg_launch_kv8_fork(const KvPool&, const KvSeqs&, const int32_t* lengths,
+                              const int32_t* parents, const int32_t* ends, int n, int width,
+                              int32_t* table, int32_t* new_lengths, int32_t* refs, hipStream_t);
+uint64_t cg_kv8_reserve_ws(int P, int n, int width);
+hipError_t cg_launch_kv8_reserve(const KvPool&, int D, int n, int width, int32_t* table,
+                                 const int32_t* lengths, const int32_t* counts, int32_t* refs,
+                                 int32_t* missing, void* ws, hipStream_t);
+hipError_t cg_launch_kv8_release(const KvPool&, int n, int width, int32_t* table,
+                                 const int32_t* keep, int32_t* refs, hipStream_t);
+hipError_t cg_launch_kv8_copy(const KvPool&, int D, const int32_t* src, const int32_t* dst, int n,
+                              hipStream_t);
+uint64_t cg_kv8_compact_ws(int P);
+hipError_t cg_launch_kv8_compact(const KvPool&, const KvSeqs&, int D, const int32_t* refs,
+                                 int32_t* new_table, int32_t* new_refs, int32_t* moved,
+                                 int32_t* n_live, void* ws, hipStream_t);
+
+struct CgVerify {
+  int32_t n, n_drafts, vocab;
+  const void *target, *draft;   // rows of probabilities; draft may be null
+  int64_t t_seq, t_row, d_seq, d_row;
+  const int32_t *drafts, *counts;
+  const float* u;
+  const int32_t* lengths;
+  int32_t *tokens, *accepted, *new_lengths;
+};
+uint64_t cg_verify_ws(int n, int vocab);
+hipError_t cg_launch_verify(const CgVerify&, int dtype, void* ws, hipStream_t);

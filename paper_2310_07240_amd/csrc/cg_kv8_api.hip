@@ -96,8 +96,56 @@ int check_attend(const cg_kv8_cache* c, const cg_kv8_seqs* s, const cg_kv8_attn*
   return CG_OK;
 }
 
+// Contexts X with their users as one sequence each, and the sequences' own pages (S.table null:
+// none).
+int check_shared(const cg_kv8_cache* c, const cg_kv8_contexts* x, const cg_kv8_seqs* s,
+                 const cg_kv8_attn* a, KvPool* pool, KvSeqs* X, KvAttn* XA, KvUsers* U, KvSeqs* S,
+                 KvAttn* A) {
+  if (!x || !s || !a) return CG_ERR_ARG;
+  cg_kv8_seqs own = *s;
+  cg_kv8_attn b = *a;
+  if (!s->table) {                     // (checked as one column of something that is there)
+    own.max_pages = 1;
+    own.table = x->seqs.table;
+    b.lengths = x->lengths;
+    b.max_len = 0;
+  }
+  int rc = check_attend(c, &own, &b, pool, S, A);
+  if (rc == CG_OK) rc = check_seqs(&x->seqs, *pool, X);
+  if (rc != CG_OK) return rc;
+  if (a->picks || a->mass_in || a->mass_out || !x->lengths || !aligned(x->lengths, 4) ||
+      !x->firsts || !aligned(x->firsts, 4))
+    return CG_ERR_ARG;
+  if (x->max_users <= 0 || x->max_len < 0) return CG_ERR_SHAPE;
+  U->firsts = x->firsts;
+  U->n_seq = S->n;
+  U->most = x->max_users < S->n ? x->max_users : S->n;
+  U->per = A->nq;
+  const int64_t tokens = (int64_t)X->n * U->most * A->nq;
+  if (tokens * A->group * pool->H > (1LL << 30) || tokens * pool->H > (1 << 23))
+    return CG_ERR_SHAPE;
+  *XA = *A;
+  XA->lengths = x->lengths;
+  XA->max_len = most_tokens(x->max_len, *X);
+  XA->nq = U->most * A->nq;
+  if (!s->table) *S = KvSeqs{s->n_seq, 0, nullptr};
+  return CG_OK;
+}
+
 // A page's score is a sum over the group's channels of products of two codes, in 32 bits.
 bool score_fits(int64_t group, int64_t D) { return group * D * (127 * 127) <= INT32_MAX; }
+
+bool bad_ints(const int32_t* p) { return !p || !aligned(p, 4); }
+
+int check_workspace(const void* ws, uint64_t bytes, uint64_t need) {
+  if (!ws || !aligned(ws, 256)) return CG_ERR_ARG;
+  return bytes < need ? CG_ERR_CAPACITY : CG_OK;
+}
+
+bool bad_verify_sizes(const cg_verify* v) {
+  return !v || v->n_seq <= 0 || v->n_seq > (1 << 21) || v->n_drafts < 0 ||
+         v->n_drafts > CG_VERIFY_MAX_DRAFTS || v->vocab <= 0 || v->vocab > CG_VERIFY_MAX_VOCAB;
+}
 
 int hip_rc(hipError_t e) { return e == hipSuccess ? CG_OK : CG_ERR_HIP; }
 
@@ -160,6 +208,32 @@ int cg_kv8_attend(const cg_kv8_cache* c, const cg_kv8_seqs* s, const cg_kv8_attn
                                      stream));
 }
 
+uint64_t cg_kv8_attend_shared_workspace_bytes(const cg_kv8_cache* c, const cg_kv8_contexts* x,
+                                              const cg_kv8_seqs* s, const cg_kv8_attn* a) {
+  KvPool pool;
+  KvSeqs X, S;
+  KvAttn XA, A;
+  KvUsers U;
+  if (check_shared(c, x, s, a, &pool, &X, &XA, &U, &S, &A) != CG_OK) return 0;
+  return cg_kv8_shared_plan(pool, X, XA, S, A, c->head_dim).total;
+}
+
+int cg_kv8_attend_shared(const cg_kv8_cache* c, const cg_kv8_contexts* x, const cg_kv8_seqs* s,
+                         const cg_kv8_attn* a, void* workspace, uint64_t workspace_bytes,
+                         hipStream_t stream) {
+  KvPool pool;
+  KvSeqs X, S;
+  KvAttn XA, A;
+  KvUsers U;
+  const int rc = check_shared(c, x, s, a, &pool, &X, &XA, &U, &S, &A);
+  if (rc != CG_OK) return rc;
+  const uint64_t need = cg_kv8_shared_plan(pool, X, XA, S, A, c->head_dim).total;
+  if (need && (!workspace || !aligned(workspace, 256))) return CG_ERR_ARG;
+  if (workspace_bytes < need) return CG_ERR_CAPACITY;
+  return hip_rc(cg_launch_kv8_shared(pool, X, XA, U, S, A, c->head_dim, a->dtype == CG_KV8_BF16,
+                                     workspace, stream));
+}
+
 uint64_t cg_kv8_select_workspace_bytes(const cg_kv8_cache* c, const cg_kv8_seqs* s,
                                        const cg_kv8_attn* a) {
   KvPool pool;
@@ -208,6 +282,113 @@ int cg_kv8_evict(const cg_kv8_cache* c, const cg_kv8_seqs* s, const int32_t* len
   if ((most + kPage - 1) / kPage > T.width) return CG_ERR_CAPACITY;
   return hip_rc(cg_launch_kv8_evict(pool, S, c->head_dim, lengths, max_len, mass, keep, recent, T,
                                     kept, new_lengths, stream));
+}
+
+int cg_kv8_fork(const cg_kv8_cache* c, const cg_kv8_seqs* s, const int32_t* lengths,
+                const int32_t* parents, const int32_t* ends, const cg_kv8_seqs* to,
+                int32_t* new_lengths, int32_t* refs, hipStream_t stream) {
+  KvPool pool;
+  KvSeqs S, T;
+  int rc = check_cache(c, &pool);
+  if (rc == CG_OK) rc = check_seqs(s, pool, &S);
+  if (rc == CG_OK) rc = check_seqs(to, pool, &T);
+  if (rc != CG_OK) return rc;
+  if (bad_ints(lengths) || bad_ints(parents) || !aligned(ends, 4) || bad_ints(new_lengths) ||
+      bad_ints(refs))
+    return CG_ERR_ARG;
+  if (T.width < S.width) return CG_ERR_CAPACITY;
+  return hip_rc(cg_launch_kv8_fork(pool, S, lengths, parents, ends, T.n, T.width,
+                                   const_cast<int32_t*>(T.table), new_lengths, refs, stream));
+}
+
+uint64_t cg_kv8_reserve_workspace_bytes(const cg_kv8_cache* c, const cg_kv8_seqs* s) {
+  KvPool pool;
+  KvSeqs S;
+  if (check_cache(c, &pool) != CG_OK || check_seqs(s, pool, &S) != CG_OK) return 0;
+  return cg_kv8_reserve_ws(pool.P, S.n, S.width);
+}
+
+int cg_kv8_reserve(const cg_kv8_cache* c, const cg_kv8_seqs* s, const int32_t* lengths,
+                   const int32_t* counts, int32_t* refs, int32_t* missing, void* workspace,
+                   uint64_t workspace_bytes, hipStream_t stream) {
+  KvPool pool;
+  KvSeqs S;
+  int rc = check_cache(c, &pool);
+  if (rc == CG_OK) rc = check_seqs(s, pool, &S);
+  if (rc != CG_OK) return rc;
+  if (bad_ints(lengths) || bad_ints(counts) || bad_ints(refs) || bad_ints(missing))
+    return CG_ERR_ARG;
+  rc = check_workspace(workspace, workspace_bytes, cg_kv8_reserve_ws(pool.P, S.n, S.width));
+  if (rc != CG_OK) return rc;
+  return hip_rc(cg_launch_kv8_reserve(pool, c->head_dim, S.n, S.width,
+                                      const_cast<int32_t*>(S.table), lengths, counts, refs, missing,
+                                      workspace, stream));
+}
+
+int cg_kv8_release(const cg_kv8_cache* c, const cg_kv8_seqs* s, const int32_t* keep, int32_t* refs,
+                   hipStream_t stream) {
+  KvPool pool;
+  KvSeqs S;
+  int rc = check_cache(c, &pool);
+  if (rc == CG_OK) rc = check_seqs(s, pool, &S);
+  if (rc != CG_OK) return rc;
+  if (!aligned(keep, 4) || bad_ints(refs)) return CG_ERR_ARG;
+  return hip_rc(cg_launch_kv8_release(pool, S.n, S.width, const_cast<int32_t*>(S.table), keep, refs,
+                                      stream));
+}
+
+int cg_kv8_copy(const cg_kv8_cache* c, const int32_t* src, const int32_t* dst, int32_t n,
+                hipStream_t stream) {
+  KvPool pool;
+  const int rc = check_cache(c, &pool);
+  if (rc != CG_OK) return rc;
+  if (n <= 0 || pool.H > (1 << 21)) return CG_ERR_SHAPE;
+  if (bad_ints(src) || bad_ints(dst)) return CG_ERR_ARG;
+  return hip_rc(cg_launch_kv8_copy(pool, c->head_dim, src, dst, n, stream));
+}
+
+uint64_t cg_kv8_compact_workspace_bytes(const cg_kv8_cache* c) {
+  KvPool pool;
+  return check_cache(c, &pool) == CG_OK ? cg_kv8_compact_ws(pool.P) : 0;
+}
+
+int cg_kv8_compact(const cg_kv8_cache* c, const cg_kv8_seqs* s, const int32_t* refs,
+                   int32_t* new_table, int32_t* new_refs, int32_t* moved, int32_t* n_live,
+                   void* workspace, uint64_t workspace_bytes, hipStream_t stream) {
+  KvPool pool;
+  KvSeqs S;
+  int rc = check_cache(c, &pool);
+  if (rc == CG_OK) rc = check_seqs(s, pool, &S);
+  if (rc != CG_OK) return rc;
+  if (bad_ints(refs) || bad_ints(new_table) || bad_ints(new_refs) || bad_ints(moved) ||
+      bad_ints(n_live) || new_refs == refs)
+    return CG_ERR_ARG;
+  rc = check_workspace(workspace, workspace_bytes, cg_kv8_compact_ws(pool.P));
+  if (rc != CG_OK) return rc;
+  return hip_rc(cg_launch_kv8_compact(pool, S, c->head_dim, refs, new_table, new_refs, moved, n_live,
+                                      workspace, stream));
+}
+
+uint64_t cg_verify_workspace_bytes(const cg_verify* v) {
+  return bad_verify_sizes(v) ? 0 : cg_verify_ws(v->n_seq, v->vocab);
+}
+
+int cg_verify_drafts(const cg_verify* v, void* workspace, uint64_t workspace_bytes,
+                     hipStream_t stream) {
+  if (!v) return CG_ERR_ARG;
+  if (bad_verify_sizes(v)) return CG_ERR_SHAPE;
+  const size_t size = v->dtype == CG_KV8_F32 ? 4 : 2;
+  if ((bad_dtype(v->dtype) && v->dtype != CG_KV8_F32) || !v->target || !aligned(v->target, size) ||
+      !aligned(v->draft, size) || (v->n_drafts && bad_ints(v->drafts)) || !aligned(v->counts, 4) ||
+      !v->u || !aligned(v->u, 4) || bad_ints(v->tokens) || bad_ints(v->accepted) ||
+      !aligned(v->lengths, 4) || !aligned(v->new_lengths, 4) || (v->new_lengths && !v->lengths))
+    return CG_ERR_ARG;
+  const int rc = check_workspace(workspace, workspace_bytes, cg_verify_ws(v->n_seq, v->vocab));
+  if (rc != CG_OK) return rc;
+  const CgVerify A = {v->n_seq, v->n_drafts, v->vocab, v->target, v->n_drafts ? v->draft : nullptr,
+                      v->t_seq_stride, v->t_row_stride, v->d_seq_stride, v->d_row_stride, v->drafts,
+                      v->counts, v->u, v->lengths, v->tokens, v->accepted, v->new_lengths};
+  return hip_rc(cg_launch_verify(A, v->dtype, workspace, stream));
 }
 
 }  // extern "C"

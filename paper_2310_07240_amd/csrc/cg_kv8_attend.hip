@@ -73,6 +73,26 @@ __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirs
 struct RowsOf {
   int seq, i0, nq;   // sequence, first query token, query tokens
   int len, q_len;
+
+  // Tokens that query token i sees: those up to its own place, the last q_len tokens being the
+  // queries' own.
+  __device__ __forceinline__ int visible(int i) const {
+    if (i >= q_len) return 0;
+    const int64_t n = (int64_t)len - q_len + i + 1;
+    return n > 0 ? (int)n : 0;
+  }
+  // Tokens that any of the query tokens first .. last sees.
+  __device__ __forceinline__ int most(int first, int last) const {
+    return q_len > 0 ? visible(last < q_len ? last : q_len - 1) : 0;
+  }
+  __device__ __forceinline__ int64_t at(const KvRows& r, int i) const {
+    return seq * r.seq + (int64_t)i * r.tok;
+  }
+  // Index of query token i among all sequences' (of A.nq each), and whether it is one.
+  __device__ __forceinline__ int64_t token(int nq_all, int i) const {
+    return (int64_t)seq * nq_all + i;
+  }
+  __device__ __forceinline__ bool exists(int) const { return true; }
 };
 
 __device__ __forceinline__ RowsOf rows_of(const KvSeqs& S, const KvAttn& A, int vseq) {
@@ -91,27 +111,81 @@ __device__ __forceinline__ RowsOf rows_of(const KvSeqs& S, const KvAttn& A, int 
   return r;
 }
 
-// Tokens that query token i sees: those up to its own place, the last q_len tokens being the
-// queries' own.
-__device__ __forceinline__ int visible_of(const RowsOf& r, int i) {
-  if (i >= r.q_len) return 0;
-  const int64_t n = (int64_t)r.len - r.q_len + i + 1;
-  return n > 0 ? (int)n : 0;
+// The requests of a shared context, as one sequence whose query tokens are theirs one after the
+// other: token i is token i % per of request first + i / per. All of them see the whole context.
+struct SharedRows {
+  int seq;           // the context, whose pages are read
+  int nq, i0;        // query tokens that there is room for; 0
+  int len, q_len;    // the context's tokens; query tokens of the requests that there are
+  int first, per;
+  const int32_t* q_lens;
+
+  __device__ __forceinline__ int visible(int i) const {
+    if (i >= q_len) return 0;
+    return !q_lens || i % per < q_lens[first + i / per] ? len : 0;
+  }
+  __device__ __forceinline__ int most(int from, int) const { return from < q_len ? len : 0; }
+  __device__ __forceinline__ int64_t at(const KvRows& r, int i) const {
+    return (int64_t)(first + i / per) * r.seq + (int64_t)(i % per) * r.tok;
+  }
+  __device__ __forceinline__ int64_t token(int, int i) const {
+    return (int64_t)first * per + i;
+  }
+  __device__ __forceinline__ bool exists(int i) const { return i < q_len; }
+};
+
+// Requests first .. first + count - 1 read context p: what `firsts` says, cut to the requests that
+// exist and to the bound of them.
+struct Requests {
+  int first, count;
+};
+
+__device__ __forceinline__ Requests requests_of(const KvUsers& U, int p) {
+  int a = U.firsts[p], b = U.firsts[p + 1];
+  a = a < 0 ? 0 : a < U.n_seq ? a : U.n_seq;
+  b = b < a ? a : b < U.n_seq ? b : U.n_seq;
+  return Requests{a, b - a < U.most ? b - a : U.most};
+}
+
+__device__ __forceinline__ SharedRows rows_of(const KvSeqs& S, const KvAttn& A, const KvUsers& U,
+                                              int p) {
+  SharedRows r;
+  const Requests q = requests_of(U, p);
+  r.seq = p;
+  r.i0 = 0;
+  r.nq = A.nq;
+  r.per = U.per;
+  r.first = q.first;
+  r.q_len = q.count * U.per;
+  r.q_lens = A.q_lens;
+  int len = A.lengths[p];
+  const int64_t room = (int64_t)S.width * kPage;
+  if (len > A.max_len) len = A.max_len;
+  if (len > room) len = (int)room;
+  r.len = len > 0 ? len : 0;
+  return r;
+}
+
+// The same of either kind.
+template <class Rows>
+__device__ __forceinline__ Rows rows_in(const KvSeqs& S, const KvAttn& A, const KvUsers& U, int i) {
+  if constexpr (__is_same(Rows, SharedRows)) return rows_of(S, A, U, i);
+  else return rows_of(S, A, i);
 }
 
 // Rows 16 tile .. 16 tile + 15 of the group's queries; rows past the last one see nothing.
 // bf16 rows are scaled by a power of two to [1, 2) at their largest, so that fp16 holds them to
 // 2^-25 of it; fp16 rows go as they are.
-template <int D, bool BF16>
-__device__ __forceinline__ void load_q(const KvAttn& A, const RowsOf& R, int h, int tile,
+template <int D, bool BF16, class Rows>
+__device__ __forceinline__ void load_q(const KvAttn& A, const Rows& R, int h, int tile,
                                        QTile<D>& Q) {
   const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
   const int row = tile * 16 + m;
   const int i = R.i0 + row / A.group, head = h * A.group + row % A.group;
   const bool live = row < R.nq * A.group;
-  Q.visible = live ? visible_of(R, i) : 0;
-  const uint16_t* src = static_cast<const uint16_t*>(A.q.p) + R.seq * A.q.seq +
-                        (int64_t)i * A.q.tok + (int64_t)head * A.q.head;
+  Q.visible = live ? R.visible(i) : 0;
+  const uint16_t* src = static_cast<const uint16_t*>(A.q.p) + R.at(A.q, i) +
+                        (int64_t)head * A.q.head;
   uint16_t u[D / 32][8];
 #pragma unroll
   for (int s = 0; s < D / 32; ++s) *reinterpret_cast<uint4v*>(u[s]) = uint4v{0, 0, 0, 0};
@@ -264,19 +338,25 @@ __device__ __forceinline__ void page_values(const VRegs<D>& V, const half8 p[2],
   }
 }
 
-template <int D, bool BF16>
-__device__ __forceinline__ void put_out(const KvAttn& A, const RowsOf& R, int h, int row, int d,
+template <int D, bool BF16, class Rows>
+__device__ __forceinline__ void put_out(const KvAttn& A, const Rows& R, int h, int row, int d,
                                         const float* o, int n) {
   const int i = R.i0 + row / A.group, head = h * A.group + row % A.group;
-  uint16_t* p = static_cast<uint16_t*>(A.out.p) + R.seq * A.out.seq + (int64_t)i * A.out.tok +
-                (int64_t)head * A.out.head + d;
+  if (!R.exists(i)) return;
+  uint16_t* p = static_cast<uint16_t*>(A.out.p) + R.at(A.out, i) + (int64_t)head * A.out.head + d;
   for (int c = 0; c < n; ++c) p[c] = kv_narrow<BF16>(o[c]);
 }
 
-__device__ __forceinline__ int64_t lse_at(const KvAttn& A, const RowsOf& R, int H, int h,
-                                          int row) {
+template <class Rows>
+__device__ __forceinline__ int64_t lse_at(const KvAttn& A, const Rows& R, int H, int h, int row) {
   const int i = R.i0 + row / A.group, head = h * A.group + row % A.group;
-  return ((int64_t)R.seq * A.nq + i) * ((int64_t)H * A.group) + head;
+  return R.token(A.nq, i) * ((int64_t)H * A.group) + head;
+}
+
+template <class Rows>
+__device__ __forceinline__ void put_lse(const KvAttn& A, const Rows& R, int H, int h, int row,
+                                        float* lse, float x) {
+  if (lse && R.exists(R.i0 + row / A.group)) lse[lse_at(A, R, H, h, row)] = x;
 }
 
 // Partial states of one 16-row tile in 32 bits: O [16][D], then (m, l) [16].
@@ -305,8 +385,8 @@ __device__ __forceinline__ void get_pair(const float* p, float& a, float& b) {
 // out: the 256 threads first fetch every state's (m, l) at once, then each takes pairs of channels
 // through all states. FAR: written by other workgroups of this launch. w [n][16]: LDS. rows0: rows
 // of the tile that exist.
-template <int D, bool BF16, bool FAR, int kAhead>
-__device__ __forceinline__ void join_tile(const KvAttn& A, const RowsOf& R, int H, int h, int tile,
+template <int D, bool BF16, bool FAR, int kAhead, class Rows>
+__device__ __forceinline__ void join_tile(const KvAttn& A, const Rows& R, int H, int h, int tile,
                                           int rows0, const float* p, int n, float* w, float* lse) {
   const int tid = threadIdx.x;
   const int row = tid >> 4, sub = tid & 15;            // 16 threads a row
@@ -340,8 +420,7 @@ __device__ __forceinline__ void join_tile(const KvAttn& A, const RowsOf& R, int 
     const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
     for (int i = sub; i < n; i += 16)
       w[i * 16 + row] = __builtin_amdgcn_exp2f(w[i * 16 + row] - ref) * inv;
-    if (lse && sub == 0)
-      lse[lse_at(A, R, H, h, tile * 16 + row)] = (top + __builtin_amdgcn_logf(l)) * kLn2;
+    if (sub == 0) put_lse(A, R, H, h, tile * 16 + row, lse, (top + __builtin_amdgcn_logf(l)) * kLn2);
   }
   __syncthreads();
   for (int e = tid; e < rows0 * (D / 2); e += 256) {
@@ -369,15 +448,37 @@ __device__ __forceinline__ void join_tile(const KvAttn& A, const RowsOf& R, int 
 }
 
 // One joined row's channels to `out`, and its log-sum-exp.
-template <int D, bool BF16, int N>
-__device__ __forceinline__ void finish_row(const KvAttn& A, const RowsOf& R, int H, int h, int row,
+template <int D, bool BF16, int N, class Rows>
+__device__ __forceinline__ void finish_row(const KvAttn& A, const Rows& R, int H, int h, int row,
                                            int d0, float* o, float top, float l, float* lse) {
   const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
 #pragma unroll
   for (int c = 0; c < N; ++c) o[c] *= inv;
   put_out<D, BF16>(A, R, h, row, d0, o, N);
-  if (lse && d0 == 0)
-    lse[lse_at(A, R, H, h, row)] = (top + __builtin_amdgcn_logf(l)) * kLn2;
+  if (d0 == 0) put_lse(A, R, H, h, row, lse, (top + __builtin_amdgcn_logf(l)) * kLn2);
+}
+
+// Requests that have no context see nothing: those before the first context's, between the bound of
+// a context's requests and the next one's, and behind the last. Context p's workgroup fills in the
+// ones behind p's own.
+template <int NT>
+__device__ __forceinline__ void fill_without(const KvAttn& A, const KvUsers& U, int contexts, int p,
+                                             int H, int D, float* lse) {
+  const Requests q = requests_of(U, p);
+  int to = U.firsts[p + 1];
+  to = to < U.n_seq && p + 1 < contexts ? to : U.n_seq;
+  const int before = p == 0 ? q.first : 0;               // [0, before) and [q.first + q.count, to)
+  const int from = q.first + q.count, n = before + (to > from ? to - from : 0);
+  const int heads = H * A.group;
+  for (int k = 0; k < n; ++k) {
+    const int64_t b = k < before ? k : from + (k - before);
+    for (int64_t e = threadIdx.x; e < (int64_t)U.per * heads * D; e += NT) {
+      const int64_t row = e / D;
+      const int i = (int)(row / heads), head = (int)(row % heads), d = (int)(e % D);
+      static_cast<uint16_t*>(A.out.p)[b * A.out.seq + i * A.out.tok + head * A.out.head + d] = 0;
+      if (lse && d == 0) lse[(b * U.per + i) * heads + head] = kNegInf;
+    }
+  }
 }
 
 // Workgroup = (virtual sequence, KV head, 16-row tile, split of the pages); its four waves take
@@ -391,9 +492,12 @@ __device__ __forceinline__ void finish_row(const KvAttn& A, const RowsOf& R, int
 // Bound by the codes' bytes where there are many: 4 sequences of 8K on 32 heads, 269 MB in 51 us, 5.3
 // TB/s (a copy of 1 GiB: 5.1); one sequence of 4K on 8 heads, 8 MB, 11 us, is a chain of dependent
 // reads (length, table, codes) and the join, 6 us with a single page.
-template <int D, bool BF16>
-__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles,
-                                                        int splits, int64_t items, float* part,
+// With SharedRows the sequences are contexts that requests share; with PARTS every split's state
+// stays in memory, for a join with those of another launch.
+template <int D, bool BF16, class Rows, bool PARTS>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_kernel(KvPool pool, KvSeqs S, KvAttn A,
+                                                        KvUsers U, int tiles, int splits,
+                                                        int64_t items, float* part,
                                                         uint32_t* arrived, float* lse,
                                                         float* scores, int np) {
   __shared__ float os[4][16][D + 4];
@@ -406,12 +510,13 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_kernel(KvPool po
     const int tile = (int)(unit % tiles);
     const int h = (int)(unit / tiles % pool.H);
     const int vseq = (int)(unit / tiles / pool.H);
-    const RowsOf R = rows_of(S, A, vseq);
+    const Rows R = rows_in<Rows>(S, A, U, vseq);
+    if constexpr (__is_same(Rows, SharedRows) && !PARTS)
+      if (split == 0 && tile == 0 && h == 0) fill_without<256>(A, U, S.n, vseq, pool.H, D, lse);
     // the pages that any row of the tile sees
     const int rows = R.nq * A.group;
-    int last = tile * 16 + 15 < rows ? tile * 16 + 15 : rows - 1;
-    last = R.i0 + last / A.group;
-    const int most = R.q_len > 0 ? visible_of(R, last < R.q_len ? last : R.q_len - 1) : 0;
+    const int last = tile * 16 + 15 < rows ? tile * 16 + 15 : rows - 1;
+    const int most = R.most(R.i0 + tile * 16 / A.group, R.i0 + last / A.group);
     const int n = A.picks ? A.n_picks : (most + kPage - 1) / kPage;
     const int per = (n + splits - 1) / splits;
     const int j0 = split * per, j1 = j0 + per < n ? j0 + per : n;
@@ -490,7 +595,16 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_kernel(KvPool po
         for (int c = 0; c < N; ++c) o[c] = __builtin_fmaf(os[w][row][d0 + c], f, o[c]);
       }
     }
-    if (splits == 1) {
+    if (PARTS) {
+      float* mine = part + it * kPart<D>;
+      if (live) {
+#pragma unroll
+        for (int c = 0; c < N; c += 2)
+          *reinterpret_cast<float2v*>(mine + row * D + d0 + c) = float2v{o[c], o[c + 1]};
+        if (d0 == 0)
+          *reinterpret_cast<float2v*>(mine + 16 * D + 2 * row) = float2v{top, l};
+      }
+    } else if (splits == 1) {
       if (live) finish_row<D, BF16, N>(A, R, pool.H, h, tile * 16 + row, d0, o, top, l, lse);
     } else {
       float* mine = part + it * kPart<D>;
@@ -519,16 +633,16 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_kernel(KvPool po
 
 // The splits of prompt_kernel joined: a workgroup a 16-row tile. Bound by the states' bytes: 33 MB of
 // 2000 rows of 8 heads in 4 splits, 9 us, 3.7 TB/s.
-template <int D, bool BF16>
-__global__ __launch_bounds__(256) void join_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles,
-                                                   int splits, int64_t items, const float* part,
-                                                   float* lse) {
+template <int D, bool BF16, class Rows>
+__global__ __launch_bounds__(256) void join_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U,
+                                                   int tiles, int splits, int64_t items,
+                                                   const float* part, float* lse) {
   __shared__ float w[kMostSplits * 16];
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const int tile = (int)(it % tiles);
     const int64_t r = it / tiles;
     const int h = (int)(r % pool.H);
-    const RowsOf R = rows_of(S, A, (int)(r / pool.H));
+    const Rows R = rows_in<Rows>(S, A, U, (int)(r / pool.H));
     const int rows = R.nq * A.group - tile * 16;
     join_tile<D, BF16, false, 4>(A, R, pool.H, h, tile, rows < 16 ? rows : 16,
                               part + it * splits * kPart<D>, splits, w, lse);
@@ -602,7 +716,7 @@ __global__ __launch_bounds__(256) void mass_scores_kernel(KvPool pool, KvSeqs S,
     float sum = 0.0f;
 #pragma unroll 4
     for (int row = 0; row < rows; ++row) {
-      const int see = visible_of(R, row / A.group);
+      const int see = R.visible(row / A.group);
       const float z = lse[lse_at(A, R, pool.H, h, row)] * kLog2e;
       if (t < see) sum += __builtin_amdgcn_exp2f(x[(int64_t)row * np * kPage] - z);
     }
@@ -789,9 +903,10 @@ constexpr int kPromptWaves = D == 256 ? 4 : 8;
 // softmax (32 exponentials a lane and page), which two waves on a SIMD overlap in part: 2 sequences
 // of 8K, 64 heads, 2048 queries, 962 GFLOP in 0.92 to 1.07 ms as the clock goes, 0.90 to 1.05
 // PFLOP/s (a library product of 8192 cubed: 1.23); 500 queries of 32 heads over 4K, 33 GFLOP, 51 us.
-template <int D, bool BF16>
+// `part`: where the splits' states go; null: there is one, and it is the result.
+template <int D, bool BF16, class Rows>
 __global__ __launch_bounds__(64 * kPromptWaves<D>, kPromptWaves<D> / 4)
-void prompt_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles, int splits, int64_t it0,
+void prompt_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, int tiles, int splits, int64_t it0,
                    float* part, float* lse) {
   constexpr int NT = 64 * kPromptWaves<D>;
   __shared__ PromptLds<D> L;
@@ -803,19 +918,24 @@ void prompt_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles, int splits, int64
   r /= splits;
   const int tile = uniform(tiles - 1 - (int)(r % tiles));   // the tiles that see most go first
   const int seq = uniform((int)(r / tiles));
-  RowsOf R = rows_of(S, A, seq);
+  Rows R = rows_in<Rows>(S, A, U, seq);
   R.len = uniform(R.len);
   R.q_len = uniform(R.q_len);
+  if constexpr (__is_same(Rows, SharedRows)) {
+    R.first = uniform(R.first);
+    if (!part && split == 0 && tile == 0 && h == 0)
+      fill_without<NT>(A, U, S.n, seq, pool.H, D, lse);
+  }
   const int rows = R.nq * A.group, row = (tile * kPromptWaves<D> + wave) * 32 + m;
 
   half8 q[D / 16];
   // a row that sees nothing is not masked tile by tile: it is written as empty at the end
   const int i_row = row / A.group, head = h * A.group + row % A.group;
-  const int see = row < rows ? visible_of(R, i_row) : 0;
+  const int see = row < rows ? R.visible(i_row) : 0;
   const int visible = see > 0 ? see : 0x7fffffff;
   const float unit = load_row32<D, BF16>(
-      A, static_cast<const uint16_t*>(A.q.p) + R.seq * A.q.seq + (int64_t)i_row * A.q.tok +
-             (int64_t)head * A.q.head, see > 0, q);
+      A, static_cast<const uint16_t*>(A.q.p) + R.at(A.q, i_row) + (int64_t)head * A.q.head, see > 0,
+      q);
   int low = visible;                                   // what every row of the wave sees
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -826,9 +946,7 @@ void prompt_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles, int splits, int64
   // the workgroup's pages: up to what its last live row sees
   int last = (tile + 1) * (32 * kPromptWaves<D>) - 1;
   last = last < rows ? last : rows - 1;
-  int top_token = last / A.group;
-  if (top_token >= R.q_len) top_token = R.q_len - 1;
-  const int most = top_token >= 0 ? visible_of(R, top_token) : 0;
+  const int most = R.most(tile * (32 * kPromptWaves<D>) / A.group, last / A.group);
   const int n = (most + kPage - 1) / kPage;
   const int per = (n + splits - 1) / splits;
   const int j0 = split * per, j1 = j0 + per < n ? j0 + per : n;
@@ -1045,9 +1163,9 @@ void prompt_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles, int splits, int64
   const float top = fmaxf(some ? l_ref : -1e30f, some0 ? ref0 : -1e30f);
   const float to_top = some ? __builtin_amdgcn_exp2f(l_ref - top) : 0.0f;
   const float sum = l * to_top + (some0 ? l0 * __builtin_amdgcn_exp2f(ref0 - top) : 0.0f);
-  const float g = empty ? 0.0f : (splits > 1 ? to_top : to_top / sum) * l_unit;
+  const float g = empty ? 0.0f : (part ? to_top : to_top / sum) * l_unit;
   const int64_t u16 = ((int64_t)seq * pool.H + h) * ((rows + 15) / 16) + row / 16;
-  float* dst = splits > 1 ? part + (u16 * splits + split) * kPart<D> : nullptr;
+  float* dst = part ? part + (u16 * splits + split) * kPart<D> : nullptr;
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -1065,9 +1183,9 @@ void prompt_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles, int splits, int64
   if (dst) {
     dst[16 * D + 2 * (row & 15)] = empty ? kNegInf : top;
     dst[16 * D + 2 * (row & 15) + 1] = empty ? 0.0f : sum;
-  } else if (lse) {
-    lse[lse_at(A, R, pool.H, h, row)] =
-        empty ? kNegInf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+  } else {
+    put_lse(A, R, pool.H, h, row, lse,
+            empty ? kNegInf : (top + __builtin_amdgcn_logf(sum)) * kLn2);
   }
 }
 
@@ -1197,7 +1315,7 @@ void mass_rows_kernel(KvPool pool, KvSeqs S, KvAttn A, int np, int shares, int64
         if (32 * t + 32 <= rows) {
 #pragma unroll
           for (int c = 0; c < CH; ++c) u[c] = *reinterpret_cast<const uint4v*>(tile_q + q_off[c]);
-          see = visible_of(R, own_i);
+          see = R.visible(own_i);
           z = tile_lse[lse_off];
         } else {                     // (behind the last row the tile's first, of no use)
 #pragma unroll
@@ -1205,7 +1323,7 @@ void mass_rows_kernel(KvPool pool, KvSeqs S, KvAttn A, int np, int shares, int64
             u[c] = *reinterpret_cast<const uint4v*>(
                 tile_q + (32 * t + c * RC + lane / LR < rows ? q_off[c] : 0u));
           const bool live = 32 * t + m < rows;
-          see = live ? visible_of(R, own_i) : 0;
+          see = live ? R.visible(own_i) : 0;
           z = tile_lse[live ? lse_off : 0u];
         }
         tile_q += step_off * 2;
@@ -1229,7 +1347,7 @@ void mass_rows_kernel(KvPool pool, KvSeqs S, KvAttn A, int np, int shares, int64
         for (int c = 0; c < CH; ++c) u[c] = load8(src[c], false);
       }
       const bool live = 32 * t + m < rows;
-      see = live ? visible_of(R, own_i) : 0;
+      see = live ? R.visible(own_i) : 0;
       z = lse0[live ? own_i * lse_tok + own_g : 0];
       from.move(step_off, step_g, A.group, wrap);
       own_i += step_i;
@@ -1291,6 +1409,107 @@ void mass_rows_kernel(KvPool pool, KvSeqs S, KvAttn A, int np, int shares, int64
   }
 }
 
+// ---- a shared context and the requests' own tokens ------------------------------------------------
+// The partial states of both, in 32 bits, joined: a workgroup a request's 16-row tile. The context's
+// states of the tile lie in rows of its own tiles, from the request's first on. Bound by the states'
+// bytes.
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void shared_join_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U,
+                                                          int contexts, int tiles, int shared_tiles,
+                                                          int shared_splits, int splits,
+                                                          int64_t items, const float* shared_part,
+                                                          const float* part, float* lse) {
+  constexpr int kAhead = 8;
+  __shared__ float w[2 * kMostSplits * 16];
+  const int tid = threadIdx.x, row = tid >> 4, sub = tid & 15;
+  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const int tile = (int)(it % tiles);
+    const int64_t r = it / tiles;
+    const int h = (int)(r % pool.H);
+    const RowsOf R = rows_of(S, A, (int)(r / pool.H));
+    const int rows = R.nq * A.group, rows0 = rows - tile * 16 < 16 ? rows - tile * 16 : 16;
+    // the context: the last one whose requests start at this one or before
+    int lo = 0, hi = contexts;                         // firsts[lo - 1] <= seq < firsts[hi]
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (U.firsts[mid] <= R.seq) lo = mid + 1;
+      else hi = mid;
+    }
+    const int p = lo - 1;
+    int n0 = 0, from = 0;                              // the context's states; its row of row 0
+    if (p >= 0) {
+      const Requests q = requests_of(U, p);
+      if (R.seq - q.first < q.count) {
+        n0 = shared_splits;
+        from = (R.seq - q.first) * rows + tile * 16;
+      }
+    }
+    const int n = n0 + splits;
+    // state i of row x: the context's first, then the request's own
+    const float* const s0 = n0 ? shared_part + ((int64_t)p * pool.H + h) * shared_tiles *
+                                                   shared_splits * kPart<D> : nullptr;
+    const auto state = [&](int i, int x, int& in) -> const float* {
+      if (i < n0) {
+        in = (from + x) & 15;
+        return s0 + ((int64_t)((from + x) >> 4) * shared_splits + i) * kPart<D>;
+      }
+      in = x;
+      return part + (it * splits + (i - n0)) * kPart<D>;
+    };
+    float top = kNegInf, l = 0.0f;
+    if (row < rows0) {
+      for (int i = sub; i < n; i += 16) {
+        int in;
+        const float* const s = state(i, row, in);
+        const float2v ml = *reinterpret_cast<const float2v*>(s + 16 * D + 2 * in);
+        w[i * 16 + row] = ml[0];
+        const float both = fmaxf(top, ml[0]), ref = both == kNegInf ? 0.0f : both;
+        l = l * __builtin_amdgcn_exp2f(top - ref) + ml[1] * __builtin_amdgcn_exp2f(ml[0] - ref);
+        top = both;
+      }
+    }
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) {
+      const float m = __shfl_xor(top, o), x = __shfl_xor(l, o);
+      const float both = fmaxf(top, m), ref = both == kNegInf ? 0.0f : both;
+      l = l * __builtin_amdgcn_exp2f(top - ref) + x * __builtin_amdgcn_exp2f(m - ref);
+      top = both;
+    }
+    const float ref = top == kNegInf ? 0.0f : top;
+    if (row < rows0) {
+      const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+      for (int i = sub; i < n; i += 16)
+        w[i * 16 + row] = __builtin_amdgcn_exp2f(w[i * 16 + row] - ref) * inv;
+      if (sub == 0)
+        put_lse(A, R, pool.H, h, tile * 16 + row, lse, (top + __builtin_amdgcn_logf(l)) * kLn2);
+    }
+    __syncthreads();
+    for (int e = tid; e < rows0 * (D / 2); e += 256) {
+      const int x = e / (D / 2), d = e % (D / 2) * 2;
+      float o[2] = {0.0f, 0.0f};
+      for (int i0 = 0; i0 < n; i0 += kAhead) {
+        float2v v[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          int in;
+          const float* const s = state(i0 + i < n ? i0 + i : n - 1, x, in);
+          v[i] = *reinterpret_cast<const float2v*>(s + in * D + d);
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          if (i0 + i < n) {
+            const float f = w[(i0 + i) * 16 + x];
+            o[0] = __builtin_fmaf(v[i][0], f, o[0]);
+            o[1] = __builtin_fmaf(v[i][1], f, o[1]);
+          }
+        }
+      }
+      put_out<D, BF16>(A, R, h, tile * 16 + x, d, o, 2);
+    }
+    __syncthreads();
+  }
+}
+
 unsigned grid_of(int64_t items) { return (unsigned)(items < (1 << 22) ? items : (1 << 22)); }
 
 // Kernels of one workgroup per item: as many launches as keep each below 2^32 threads.
@@ -1301,12 +1520,12 @@ void in_launches(int64_t items, Launch launch) {
     launch(it0, (unsigned)(items - it0 < kMost ? items - it0 : kMost));
 }
 
-template <int D, bool BF16>
-void prompt_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, const KvAttnPlan& P,
-              float* part, float* lse, hipStream_t st) {
+template <int D, bool BF16, class Rows>
+void prompt_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, const KvUsers& U,
+              const KvAttnPlan& P, float* part, float* lse, hipStream_t st) {
   in_launches((int64_t)S.n * pool.H * P.big * P.splits, [&](int64_t it0, unsigned n) {
-    hipLaunchKernelGGL((prompt_kernel<D, BF16>), dim3(n), dim3(64 * kPromptWaves<D>), 0, st, pool,
-                       S, A, P.big, P.splits, it0, part, lse);
+    hipLaunchKernelGGL((prompt_kernel<D, BF16, Rows>), dim3(n), dim3(64 * kPromptWaves<D>), 0, st,
+                       pool, S, A, U, P.big, P.splits, it0, part, lse);
   });
 }
 
@@ -1347,14 +1566,14 @@ hipError_t attend_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, void* 
   const int vseqs = A.picks ? S.n * A.nq : S.n;
   const int64_t units = (int64_t)vseqs * pool.H * P.tiles;
   if (P.big)
-    prompt_d<D, BF16>(pool, S, A, P, part, lse, st);
+    prompt_d<D, BF16, RowsOf>(pool, S, A, KvUsers{}, P, P.splits > 1 ? part : nullptr, lse, st);
   else
-    hipLaunchKernelGGL((attend_kernel<D, BF16>), dim3(grid_of(units * P.splits)), dim3(256), 0,
-                       st, pool, S, A, P.tiles, P.splits, units * P.splits, part,
-                       reinterpret_cast<uint32_t*>(base), lse, scores, np);
+    hipLaunchKernelGGL((attend_kernel<D, BF16, RowsOf, false>), dim3(grid_of(units * P.splits)),
+                       dim3(256), 0, st, pool, S, A, KvUsers{}, P.tiles, P.splits,
+                       units * P.splits, part, reinterpret_cast<uint32_t*>(base), lse, scores, np);
   if (P.splits > 1 && P.big)
-    hipLaunchKernelGGL((join_kernel<D, BF16>), dim3(grid_of(units)), dim3(256), 0, st, pool, S, A,
-                       P.tiles, P.splits, units, part, lse);
+    hipLaunchKernelGGL((join_kernel<D, BF16, RowsOf>), dim3(grid_of(units)), dim3(256), 0, st, pool,
+                       S, A, KvUsers{}, P.tiles, P.splits, units, part, lse);
   if (A.mass_out && np) {
     const int64_t items = (int64_t)S.n * pool.H * np;
     if (P.many)
@@ -1369,7 +1588,81 @@ hipError_t attend_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, void* 
   return hipGetLastError();
 }
 
+template <int D, bool BF16>
+hipError_t shared_d(const KvPool& pool, const KvSeqs& C, const KvAttn& CA, const KvUsers& U,
+                    const KvSeqs& S, const KvAttn& A, void* ws, hipStream_t st) {
+  const KvSharedPlan P = cg_kv8_shared_plan(pool, C, CA, S, A, D);
+  char* base = static_cast<char*>(ws);
+  float* const part0 = reinterpret_cast<float*>(base + P.shared_off);
+  const int64_t units0 = (int64_t)C.n * pool.H * P.shared.tiles;
+  const int splits0 = P.shared.splits;
+  if (P.own.tiles == 0) {
+    // the context alone
+    if (P.shared.big) {
+      prompt_d<D, BF16, SharedRows>(pool, C, CA, U, P.shared, splits0 > 1 ? part0 : nullptr, A.lse,
+                                    st);
+      if (splits0 > 1)
+        hipLaunchKernelGGL((join_kernel<D, BF16, SharedRows>), dim3(grid_of(units0)), dim3(256), 0,
+                           st, pool, C, CA, U, P.shared.tiles, splits0, units0, part0, A.lse);
+    } else {
+      hipLaunchKernelGGL((attend_kernel<D, BF16, SharedRows, false>),
+                         dim3(grid_of(units0 * splits0)), dim3(256), 0, st, pool, C, CA, U,
+                         P.shared.tiles, splits0, units0 * splits0, part0,
+                         reinterpret_cast<uint32_t*>(base), A.lse, nullptr, 0);
+    }
+    return hipGetLastError();
+  }
+  if (P.shared.big)
+    prompt_d<D, BF16, SharedRows>(pool, C, CA, U, P.shared, part0, nullptr, st);
+  else
+    hipLaunchKernelGGL((attend_kernel<D, BF16, SharedRows, true>), dim3(grid_of(units0 * splits0)),
+                       dim3(256), 0, st, pool, C, CA, U, P.shared.tiles, splits0, units0 * splits0,
+                       part0, nullptr, nullptr, nullptr, 0);
+  float* const part = reinterpret_cast<float*>(base + P.own_off);
+  const int64_t units = (int64_t)S.n * pool.H * P.own.tiles;
+  if (P.own.big)
+    prompt_d<D, BF16, RowsOf>(pool, S, A, KvUsers{}, P.own, part, nullptr, st);
+  else
+    hipLaunchKernelGGL((attend_kernel<D, BF16, RowsOf, true>), dim3(grid_of(units * P.own.splits)),
+                       dim3(256), 0, st, pool, S, A, KvUsers{}, P.own.tiles, P.own.splits,
+                       units * P.own.splits, part, nullptr, nullptr, nullptr, 0);
+  hipLaunchKernelGGL((shared_join_kernel<D, BF16>), dim3(grid_of(units)), dim3(256), 0, st, pool, S,
+                     A, U, C.n, P.own.tiles, P.shared.tiles, splits0, P.own.splits, units, part0,
+                     part, A.lse);
+  return hipGetLastError();
+}
+
 }  // namespace
+
+KvSharedPlan cg_kv8_shared_plan(const KvPool& pool, const KvSeqs& C, const KvAttn& CA,
+                                const KvSeqs& S, const KvAttn& A, int D) {
+  KvSharedPlan P = {};
+  P.shared = cg_kv8_plan(pool, C, CA, D);
+  const uint64_t state = 16ull * (D + 2) * 4;
+  const bool own = S.table != nullptr;
+  uint64_t at = own || P.shared.splits > 1 ? kKv8Front : 0;
+  P.shared_off = at;
+  if (own || P.shared.splits > 1)
+    at += (uint64_t)C.n * pool.H * P.shared.tiles * P.shared.splits * state;
+  at = (at + 255) & ~255ull;
+  P.own_off = at;
+  if (own) {
+    P.own = cg_kv8_plan(pool, S, A, D);
+    at += (uint64_t)S.n * pool.H * P.own.tiles * P.own.splits * state;
+  }
+  P.total = (at + 255) & ~255ull;
+  return P;
+}
+
+hipError_t cg_launch_kv8_shared(const KvPool& pool, const KvSeqs& C, const KvAttn& CA,
+                                const KvUsers& U, const KvSeqs& S, const KvAttn& A, int D, bool bf16,
+                                void* ws, hipStream_t st) {
+  switch (D) {
+    case 64: return (bf16 ? shared_d<64, true> : shared_d<64, false>)(pool, C, CA, U, S, A, ws, st);
+    case 128: return (bf16 ? shared_d<128, true> : shared_d<128, false>)(pool, C, CA, U, S, A, ws, st);
+    default: return (bf16 ? shared_d<256, true> : shared_d<256, false>)(pool, C, CA, U, S, A, ws, st);
+  }
+}
 
 KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& S, const KvAttn& A, int D) {
   KvAttnPlan P;

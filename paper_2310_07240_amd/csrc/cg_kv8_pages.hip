@@ -1,0 +1,609 @@
+// cg_kv8_pages.hip — who holds which page of the 8-bit cache: sequences that share another's pages
+// (cg_kv8_fork), pages for what comes (cg_kv8_reserve), pages given back (cg_kv8_release), moved
+// together (cg_kv8_compact) and copied (cg_kv8_copy).
+//
+// Free pages are found by rank: the pages' counts are taken in chunks of 4096, a workgroup each; the
+// last workgroup to arrive sums the chunks up (with what each sequence wants), and the pages of a
+// chunk then know their place among all. So the i-th page wanted gets the i-th free one, and no
+// result depends on an order of arrival. Values that workgroups of one launch hand to each other are
+// written and read past the XCDs' own caches (agent scope).
+#include "cg_kv8.h"
+
+namespace {
+
+constexpr int kRounds = 16, kChunk = 256 * kRounds;
+
+__device__ __forceinline__ void put_far(int32_t* p, int32_t v) {
+  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ int32_t get_far(const int32_t* p) {
+  return __hip_atomic_load(const_cast<int32_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ int below(uint64_t mask) {     // set bits under the lane's own
+  return __popcll(mask & ((1ull << (threadIdx.x & 63)) - 1));
+}
+
+// Whether this workgroup is the last of the launch to come here; all that it wrote has arrived
+// before it counts itself in. The counter is left at zero.
+__device__ __forceinline__ bool last_here(uint32_t* counter, uint32_t* lds) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    *lds = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (*lds == gridDim.x - 1)
+      __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  return *lds == gridDim.x - 1;
+}
+
+// Exclusive sum over the workgroup's 256 threads; `total` receives the whole. lds: 4 words.
+__device__ __forceinline__ int64_t scan256(int64_t x, int64_t* lds, int64_t& total) {
+  int64_t s = x;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t y = __shfl_up(s, o);
+    s += (int)(threadIdx.x & 63) >= o ? y : 0;
+  }
+  __syncthreads();
+  if ((threadIdx.x & 63) == 63) lds[threadIdx.x >> 6] = s;
+  __syncthreads();
+  int64_t before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    before += w < (int)(threadIdx.x >> 6) ? lds[w] : 0;
+    total += lds[w];
+  }
+  return before + s - x;
+}
+
+// In place: values [n] another workgroup of the launch wrote become their exclusive sums. Returns
+// the whole. (Sums past 32 bits are of no use to anyone: more pages than a pool can have.)
+__device__ __forceinline__ int64_t scan_far(int32_t* v, int n, int64_t* lds) {
+  constexpr int N = 8;
+  int64_t run = 0;
+  for (int64_t i0 = 0; i0 < n; i0 += 256 * N) {
+    int32_t x[N];
+    int64_t sum = 0, total;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int64_t i = i0 + threadIdx.x * N + k;
+      x[k] = i < n ? get_far(v + i) : 0;
+      sum += x[k];
+    }
+    int64_t at = run + scan256(sum, lds, total);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int64_t i = i0 + threadIdx.x * N + k;
+      if (i < n) v[i] = (int32_t)at;
+      at += x[k];
+    }
+    run += total;
+  }
+  return run;
+}
+
+struct ChunkLds {
+  int32_t at[4 * kRounds];           // pages in use before round k's wave w: [k][w]
+  int32_t total;
+};
+
+// Calls f(page, in use, pages of the chunk in use before it) for every page of a chunk, a thread
+// each, and returns the chunk's pages in use.
+template <class F>
+__device__ __forceinline__ int walk_chunk(const int32_t* refs, int P, int chunk, ChunkLds& L, F f) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint32_t used = 0;                 // this thread's pages, bit k for round k
+  const int64_t p0 = (int64_t)chunk * kChunk + threadIdx.x;
+  int32_t r[kRounds];
+#pragma unroll
+  for (int k = 0; k < kRounds; ++k) r[k] = p0 + k * 256 < P ? refs[p0 + k * 256] : 0;
+  uint64_t mask[kRounds];
+#pragma unroll
+  for (int k = 0; k < kRounds; ++k) {
+    used |= (r[k] > 0 ? 1u : 0u) << k;
+    mask[k] = __ballot(r[k] > 0);
+    if (lane == 0) L.at[4 * k + wave] = __popcll(mask[k]);
+  }
+  __syncthreads();
+  if (wave == 0) {
+    const int x = L.at[lane];
+    int s = x;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(s, o);
+      s += lane >= o ? y : 0;
+    }
+    L.at[lane] = s - x;
+    if (lane == 63) L.total = s;
+  }
+  __syncthreads();
+  const int total = L.total;
+#pragma unroll
+  for (int k = 0; k < kRounds; ++k)
+    if (p0 + k * 256 < P)
+      f((int)(p0 + k * 256), (used >> k & 1) != 0, L.at[4 * k + wave] + below(mask[k]));
+  __syncthreads();                   // the LDS may be used again
+  return total;
+}
+
+static_assert(4 * kRounds == 64, "one lane a (round, wave)");
+
+// ---- copies -----------------------------------------------------------------------------------
+// A page is copied in pieces of 16 KB of its codes, K's and then V's, a workgroup each, with four
+// 16-byte loads of a thread on their way together; the pieces share its scales, bounds and weights.
+// Bound by those bytes.
+constexpr int kUnits = 1024;           // of 16 bytes, a piece
+
+__host__ __device__ inline int pieces_of(int H, int D) {
+  return (int)(((int64_t)8 * H * D + kUnits - 1) / kUnits);
+}
+
+__device__ __forceinline__ void copy_piece(const KvPool& pool, int D, int src, int dst, int piece,
+                                           int pieces) {
+  const int64_t half = (int64_t)4 * pool.H * D;                // 16-byte units of K (and of V)
+  const uint4v* k = reinterpret_cast<const uint4v*>(pool.k);
+  const uint4v* v = reinterpret_cast<const uint4v*>(pool.v);
+  uint4v x[kUnits / 256];
+  const int64_t u0 = (int64_t)piece * kUnits + threadIdx.x;
+#pragma unroll
+  for (int i = 0; i < kUnits / 256; ++i) {
+    const int64_t u = u0 + 256 * i;
+    if (u < half) x[i] = k[src * half + u];
+    else if (u < 2 * half) x[i] = v[src * half + u - half];
+  }
+  // words of the scales, the bounds and the weights
+  const int H = pool.H, nb = pool.bounds ? H * (D / 2) : 0, nm = pool.mass ? H * kPage : 0;
+  uint32_t* const bounds = reinterpret_cast<uint32_t*>(pool.bounds);
+  for (int i = piece * 256 + threadIdx.x; i < 2 * H + nb + nm; i += pieces * 256) {
+    if (i < H) {
+      pool.ks[(int64_t)dst * H + i] = pool.ks[(int64_t)src * H + i];
+    } else if (i < 2 * H) {
+      pool.vs[(int64_t)dst * H + i - H] = pool.vs[(int64_t)src * H + i - H];
+    } else if (i < 2 * H + nb) {
+      const int64_t w = i - 2 * H, n = H * (D / 2);
+      bounds[dst * n + w] = bounds[src * n + w];
+    } else {
+      const int64_t w = i - 2 * H - nb, n = H * kPage;
+      pool.mass[dst * n + w] = pool.mass[src * n + w];
+    }
+  }
+  uint4v* const k_to = reinterpret_cast<uint4v*>(pool.k);
+  uint4v* const v_to = reinterpret_cast<uint4v*>(pool.v);
+#pragma unroll
+  for (int i = 0; i < kUnits / 256; ++i) {
+    const int64_t u = u0 + 256 * i;
+    if (u < half) k_to[dst * half + u] = x[i];
+    else if (u < 2 * half) v_to[dst * half + u - half] = x[i];
+  }
+}
+
+__global__ __launch_bounds__(256) void copy_kernel(KvPool pool, int D, const int32_t* src,
+                                                   const int32_t* dst, int pieces, int64_t items) {
+  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const int64_t i = it / pieces;
+    const int a = src[i], b = dst[i];
+    if (a >= 0 && a < pool.P && b >= 0 && b < pool.P && a != b)
+      copy_piece(pool, D, a, b, (int)(it % pieces), pieces);
+  }
+}
+
+// ---- sharing and giving back --------------------------------------------------------------------
+__device__ __forceinline__ bool names_page(int32_t p, int P) { return p >= 0 && p < P; }
+
+// One holder less; a count that is 0 stays. (However many threads do so at once, the count ends at
+// what it was less the holders, or 0.)
+__device__ __forceinline__ void drop(int32_t* refs, int p) {
+  if (atomicSub(refs + p, 1) <= 0) atomicAdd(refs + p, 1);
+}
+
+__device__ __forceinline__ int clamp_len(int64_t n, int width) {
+  const int64_t room = (int64_t)width * kPage;
+  n = n < room ? n : room;
+  n = n < INT32_MAX ? n : INT32_MAX;
+  return n > 0 ? (int)n : 0;
+}
+
+__global__ __launch_bounds__(256) void fork_kernel(int P, KvSeqs S, const int32_t* lengths,
+                                                   const int32_t* parents, const int32_t* ends,
+                                                   int n, int width, int32_t* table,
+                                                   int32_t* new_lengths, int32_t* refs) {
+  const int64_t items = (int64_t)n * width;
+  for (int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x; it < items;
+       it += (int64_t)gridDim.x * 256) {
+    const int row = (int)(it / width), j = (int)(it % width), p = parents[row];
+    int len = 0;
+    if (p >= 0 && p < S.n) {
+      len = clamp_len(lengths[p], S.width);
+      if (ends) len = ends[row] < len ? (ends[row] > 0 ? ends[row] : 0) : len;
+    }
+    int32_t page = -1;
+    if ((int64_t)j * kPage < len) page = kv_page(S, P, p, j);
+    table[it] = page;
+    if (page >= 0) atomicAdd(refs + page, 1);
+    if (j == 0) new_lengths[row] = len;
+  }
+}
+
+__global__ __launch_bounds__(256) void release_kernel(int P, int n, int width, int32_t* table,
+                                                      const int32_t* keep, int32_t* refs) {
+  const int64_t items = (int64_t)n * width;
+  for (int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x; it < items;
+       it += (int64_t)gridDim.x * 256) {
+    const int row = (int)(it / width), j = (int)(it % width);
+    if (keep && (int64_t)j * kPage < keep[row]) continue;
+    const int32_t p = table[it];
+    if (names_page(p, P)) drop(refs, p);
+    table[it] = -1;
+  }
+}
+
+// ---- pages for what comes -----------------------------------------------------------------------
+// The workspace of reserve behind the counters.
+struct Reserve {
+  int32_t* chunks;                   // [chunks] free pages of each, then before each
+  int32_t* need;                     // [n] pages that each sequence wants, then those before it
+  int32_t* source;                   // [n] the page that a sequence's first wanted one copies, or -1
+  uint64_t* wants;                   // [n][words][2] which columns from its first on, and which of
+                                     // them name a page that the sequence holds with others
+  int32_t* state;                    // pages wanted by all, or -1: there are not as many
+  int32_t* list;                     // [at most P] the free pages in order
+};
+
+struct Span {                        // columns that a sequence will write to
+  int first, last, start;            // (last: one behind)
+};
+
+__device__ __forceinline__ Span span_of(const int32_t* lengths, const int32_t* counts, int width,
+                                        int b) {
+  const int start = clamp_len(lengths[b], width);
+  const int64_t end = clamp_len((int64_t)start + (counts[b] > 0 ? counts[b] : 0), width);
+  Span s;
+  s.start = start;
+  s.first = start / kPage;
+  s.last = end > start ? (int)((end + kPage - 1) / kPage) : s.first;
+  return s;
+}
+
+// The free pages of a chunk to their places in the list, as far as they are wanted.
+__device__ __forceinline__ void list_chunk(const int32_t* refs, int P, int chunk, int before,
+                                           int wanted, int32_t* list, ChunkLds& L) {
+  walk_chunk(refs, P, chunk, L, [&](int page, bool used, int used_before) {
+    const int64_t rank = (int64_t)before + (page - chunk * kChunk - used_before);
+    if (!used && rank < wanted) list[rank] = page;
+  });
+}
+
+// Workgroups 0 .. chunks - 1 count the free pages of their chunks, the others what four sequences
+// want, a wave each; the last to come sums both up and, where `lists`, writes the list as well: with
+// few chunks that takes less than another launch.
+__global__ __launch_bounds__(256) void want_kernel(int P, int n, int width, const int32_t* table,
+                                                   const int32_t* lengths, const int32_t* counts,
+                                                   const int32_t* refs, int chunks, int words,
+                                                   bool lists, Reserve R, int32_t* missing,
+                                                   uint32_t* counter) {
+  __shared__ ChunkLds L;
+  __shared__ int64_t sums[4];
+  __shared__ uint32_t order;
+  const int lane = threadIdx.x & 63;
+  if ((int)blockIdx.x < chunks) {
+    const int chunk = blockIdx.x;
+    const int used = walk_chunk(refs, P, chunk, L, [](int, bool, int) {});
+    const int64_t left = (int64_t)P - (int64_t)chunk * kChunk;
+    if (threadIdx.x == 0) put_far(R.chunks + chunk, (int)(left < kChunk ? left : kChunk) - used);
+  } else {
+    const int b = ((int)blockIdx.x - chunks) * 4 + (threadIdx.x >> 6);
+    if (b < n) {
+      const Span s = span_of(lengths, counts, width, b);
+      int need = 0, source = -1;
+      for (int j0 = s.first; j0 < s.last; j0 += 64) {
+        const int j = j0 + lane;
+        bool want = false, drops = false;
+        if (j < s.last) {
+          const int32_t p = table[(int64_t)b * width + j];
+          const int held = names_page(p, P) ? refs[p] : 0;
+          // a page with tokens that stay is copied if others hold it too (one that is lost stays
+          // so); behind them a page has to be the sequence's alone
+          const bool keeps = (int64_t)j * kPage < s.start;
+          want = keeps ? held > 1 : held != 1;
+          drops = held > 1;
+          if (keeps && want) source = p;
+        }
+        const uint64_t mask = __ballot(want), shared = __ballot(drops);
+        if (lane == 0) {
+          uint64_t* const w = R.wants + 2 * ((int64_t)b * words + (j0 - s.first) / 64);
+          w[0] = mask;
+          w[1] = shared;
+        }
+        need += __popcll(mask);
+      }
+      if (lane == 0) {                 // (a page that is copied is in the first column: lane 0's)
+        R.source[b] = source;
+        put_far(R.need + b, need);
+      }
+    }
+  }
+  if (!last_here(counter, &order)) return;
+  const int64_t free = scan_far(R.chunks, chunks, sums);
+  const int64_t wanted = scan_far(R.need, n, sums);
+  const bool ok = wanted <= free;
+  if (threadIdx.x == 0) {
+    *R.state = ok ? (int32_t)wanted : -1;
+    *missing = ok ? 0 : wanted - free < INT32_MAX ? (int32_t)(wanted - free) : INT32_MAX;
+  }
+  if (!lists || !ok) return;
+  int before = 0;
+  for (int c = 0; c < chunks; ++c) {
+    const int64_t left = (int64_t)P - (int64_t)c * kChunk;
+    int used = 0;
+    if (before < wanted)
+      used = walk_chunk(refs, P, c, L, [&](int page, bool in_use, int used_before) {
+        const int64_t rank = (int64_t)before + (page - c * kChunk - used_before);
+        if (!in_use && rank < wanted) R.list[rank] = page;
+      });
+    before += (int)(left < kChunk ? left : kChunk) - used;
+  }
+}
+
+__global__ __launch_bounds__(256) void list_kernel(int P, const int32_t* refs, Reserve R) {
+  __shared__ ChunkLds L;
+  const int wanted = *R.state, before = R.chunks[blockIdx.x];
+  if (before < wanted) list_chunk(refs, P, blockIdx.x, before, wanted, R.list, L);
+}
+
+// Workgroup = (sequence, piece of a page): the first piece's first wave hands the pages out, all
+// pieces copy the sequence's shared page.
+__global__ __launch_bounds__(256) void hand_out_kernel(KvPool pool, int D, int n, int width,
+                                                       int32_t* table, const int32_t* lengths,
+                                                       const int32_t* counts, int32_t* refs,
+                                                       int words, int pieces, int64_t items,
+                                                       Reserve R) {
+  if (*R.state <= 0) return;
+  const int lane = threadIdx.x & 63;
+  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const int b = (int)(it / pieces), piece = (int)(it % pieces);
+    const int source = R.source[b];
+    int rank = R.need[b];
+    if (source >= 0) copy_piece(pool, D, source, R.list[rank], piece, pieces);
+    if (piece != 0 || threadIdx.x >= 64) continue;
+    const Span s = span_of(lengths, counts, width, b);
+    for (int j0 = s.first; j0 < s.last; j0 += 64) {
+      const uint64_t* const w = R.wants + 2 * ((int64_t)b * words + (j0 - s.first) / 64);
+      const uint64_t mask = w[0];
+      if (mask >> lane & 1) {
+        int32_t* const at = table + (int64_t)b * width + j0 + lane;
+        const int32_t page = R.list[rank + below(mask)];
+        if (w[1] >> lane & 1) drop(refs, *at);
+        *at = page;
+        refs[page] = 1;
+      }
+      rank += __popcll(mask);
+    }
+  }
+}
+
+// ---- pages moved together -----------------------------------------------------------------------
+struct Compact {
+  int32_t* chunks;                   // [chunks] pages in use of each, then before each
+  int32_t* state;                    // pages in use, those of them that lie in front, moves
+  int32_t* holes;                    // [P / 2 + 1] free pages in front, in order
+  int32_t* late;                     // [P / 2 + 1] pages in use behind, in order
+  int32_t* key;                      // [P] a page's new number, -1 (free), or -2 - i: the i-th hole
+};
+
+// What becomes of each page of a chunk; `before` pages in use lie in the chunks before it.
+__device__ __forceinline__ void place_chunk(const int32_t* refs, int P, int chunk, int before,
+                                            int live, int front, const Compact& C, int32_t* moved,
+                                            int32_t* new_refs, ChunkLds& L) {
+  walk_chunk(refs, P, chunk, L, [&](int page, bool used, int used_before) {
+    const int rank = before + used_before;             // pages in use before this one
+    int key = used ? page : -1;
+    if (page < live) {
+      if (!used) C.holes[page - rank] = page;
+      else new_refs[page] = refs[page];
+    } else {
+      if (used) {
+        C.late[rank - front] = page;
+        key = -2 - (rank - front);
+      }
+      new_refs[page] = 0;
+    }
+    C.key[page] = key;
+    if (key >= -1) moved[page] = key;
+  });
+}
+
+__global__ __launch_bounds__(256) void used_kernel(int P, const int32_t* refs, int chunks,
+                                                   bool places, Compact C, int32_t* moved,
+                                                   int32_t* new_refs, int32_t* n_live,
+                                                   uint32_t* counter) {
+  __shared__ ChunkLds L;
+  __shared__ int64_t sums[4];
+  __shared__ uint32_t order;
+  __shared__ int32_t in_front;
+  const int used = walk_chunk(refs, P, blockIdx.x, L, [](int, bool, int) {});
+  if (threadIdx.x == 0) put_far(C.chunks + blockIdx.x, used);
+  if (!last_here(counter, &order)) return;
+  const int live = (int)scan_far(C.chunks, chunks, sums);
+  __syncthreads();                   // (scan_far's writes are this workgroup's own)
+  if (threadIdx.x == 0) in_front = live;               // (all of them, where live == P)
+  __syncthreads();
+  if (live < P) {
+    // pages in use before page `live`
+    const int c = live / kChunk, before = C.chunks[c];
+    walk_chunk(refs, P, c, L, [&](int page, bool, int used_before) {
+      if (page == live) in_front = before + used_before;
+    });
+  }
+  const int front = in_front;
+  if (threadIdx.x == 0) {
+    C.state[0] = live;
+    C.state[1] = front;
+    C.state[2] = live - front;
+    *n_live = live;
+  }
+  if (places)
+    for (int c = 0; c < chunks; ++c)
+      place_chunk(refs, P, c, C.chunks[c], live, front, C, moved, new_refs, L);
+}
+
+__global__ __launch_bounds__(256) void place_kernel(int P, const int32_t* refs, Compact C,
+                                                    int32_t* moved, int32_t* new_refs) {
+  __shared__ ChunkLds L;
+  place_chunk(refs, P, blockIdx.x, C.chunks[blockIdx.x], C.state[0], C.state[1], C, moved, new_refs,
+              L);
+}
+
+// The moves, and the table: workgroups 0 .. movers - 1 copy, the others rewrite entries.
+__global__ __launch_bounds__(256) void move_kernel(KvPool pool, int D, const int32_t* refs,
+                                                   int64_t entries, const int32_t* table,
+                                                   int32_t* new_table, int movers, int pieces,
+                                                   Compact C, int32_t* moved, int32_t* new_refs) {
+  if ((int)blockIdx.x < movers) {
+    const int64_t items = (int64_t)C.state[2] * pieces;
+    for (int64_t it = blockIdx.x; it < items; it += movers) {
+      const int i = (int)(it / pieces), piece = (int)(it % pieces);
+      const int src = C.late[i], dst = C.holes[i];
+      copy_piece(pool, D, src, dst, piece, pieces);
+      if (piece == 0 && threadIdx.x == 0) {
+        moved[src] = dst;
+        new_refs[dst] = refs[src];
+      }
+    }
+    return;
+  }
+  for (int64_t e = (int64_t)(blockIdx.x - movers) * 256 + threadIdx.x; e < entries;
+       e += (int64_t)(gridDim.x - movers) * 256) {
+    const int32_t p = table[e];
+    int32_t to = names_page(p, pool.P) ? C.key[p] : -1;
+    if (to < -1) to = C.holes[-2 - to];
+    new_table[e] = to;
+  }
+}
+
+unsigned grid_of(int64_t items) { return (unsigned)(items < (1 << 20) ? items : (1 << 20)); }
+
+// The one workgroup that comes last writes the list itself for up to this many chunks; past them a
+// launch of a workgroup a chunk does.
+constexpr int kOwnChunks = 2;
+
+int chunks_of(int P) { return (int)(((int64_t)P + kChunk - 1) / kChunk); }
+
+// The words of `wants`: a sequence's columns from its first on, 64 a word.
+int words_of(int width) { return (width + 63) / 64; }
+
+struct Carve {                         // pieces of a workspace, each 256-byte aligned
+  char* base;
+  uint64_t at;
+  template <class T>
+  T* take(int64_t n) {
+    T* p = reinterpret_cast<T*>(base + at);
+    at = (at + (uint64_t)n * sizeof(T) + 255) & ~255ull;
+    return p;
+  }
+};
+
+Reserve reserve_of(void* ws, int P, int n, int width, uint64_t* total) {
+  Carve c = {static_cast<char*>(ws), kKv8Front};
+  Reserve R;
+  R.chunks = c.take<int32_t>(chunks_of(P));
+  R.need = c.take<int32_t>(n);
+  R.source = c.take<int32_t>(n);
+  R.wants = c.take<uint64_t>(2 * (int64_t)n * words_of(width));
+  R.state = c.take<int32_t>(1);
+  const int64_t most = (int64_t)n * width;
+  R.list = c.take<int32_t>(most < P ? most : P);
+  *total = c.at;
+  return R;
+}
+
+Compact compact_of(void* ws, int P, uint64_t* total) {
+  Carve c = {static_cast<char*>(ws), kKv8Front};
+  Compact C;
+  C.chunks = c.take<int32_t>(chunks_of(P));
+  C.state = c.take<int32_t>(3);
+  C.holes = c.take<int32_t>(P / 2 + 1);
+  C.late = c.take<int32_t>(P / 2 + 1);
+  C.key = c.take<int32_t>(P);
+  *total = c.at;
+  return C;
+}
+
+}  // namespace
+
+hipError_t cg_launch_kv8_fork(const KvPool& pool, const KvSeqs& S, const int32_t* lengths,
+                              const int32_t* parents, const int32_t* ends, int n, int width,
+                              int32_t* table, int32_t* new_lengths, int32_t* refs, hipStream_t st) {
+  hipLaunchKernelGGL(fork_kernel, dim3(grid_of(((int64_t)n * width + 255) / 256)), dim3(256), 0, st,
+                     pool.P, S, lengths, parents, ends, n, width, table, new_lengths, refs);
+  return hipGetLastError();
+}
+
+hipError_t cg_launch_kv8_release(const KvPool& pool, int n, int width, int32_t* table,
+                                 const int32_t* keep, int32_t* refs, hipStream_t st) {
+  hipLaunchKernelGGL(release_kernel, dim3(grid_of(((int64_t)n * width + 255) / 256)), dim3(256), 0,
+                     st, pool.P, n, width, table, keep, refs);
+  return hipGetLastError();
+}
+
+hipError_t cg_launch_kv8_copy(const KvPool& pool, int D, const int32_t* src, const int32_t* dst,
+                              int n, hipStream_t st) {
+  const int pieces = pieces_of(pool.H, D);
+  const int64_t items = (int64_t)n * pieces;
+  hipLaunchKernelGGL(copy_kernel, dim3(grid_of(items)), dim3(256), 0, st, pool, D, src, dst, pieces,
+                     items);
+  return hipGetLastError();
+}
+
+uint64_t cg_kv8_reserve_ws(int P, int n, int width) {
+  uint64_t total;
+  reserve_of(nullptr, P, n, width, &total);
+  return total;
+}
+
+hipError_t cg_launch_kv8_reserve(const KvPool& pool, int D, int n, int width, int32_t* table,
+                                 const int32_t* lengths, const int32_t* counts, int32_t* refs,
+                                 int32_t* missing, void* ws, hipStream_t st) {
+  uint64_t total;
+  const Reserve R = reserve_of(ws, pool.P, n, width, &total);
+  const int chunks = chunks_of(pool.P), words = words_of(width), pieces = pieces_of(pool.H, D);
+  const bool lists = chunks <= kOwnChunks;
+  hipLaunchKernelGGL(want_kernel, dim3(chunks + (n + 3) / 4), dim3(256), 0, st, pool.P, n, width,
+                     table, lengths, counts, refs, chunks, words, lists, R, missing,
+                     static_cast<uint32_t*>(ws));
+  if (!lists)
+    hipLaunchKernelGGL(list_kernel, dim3(chunks), dim3(256), 0, st, pool.P, refs, R);
+  const int64_t items = (int64_t)n * pieces;
+  hipLaunchKernelGGL(hand_out_kernel, dim3(grid_of(items)), dim3(256), 0, st, pool, D, n, width,
+                     table, lengths, counts, refs, words, pieces, items, R);
+  return hipGetLastError();
+}
+
+uint64_t cg_kv8_compact_ws(int P) {
+  uint64_t total;
+  compact_of(nullptr, P, &total);
+  return total;
+}
+
+hipError_t cg_launch_kv8_compact(const KvPool& pool, const KvSeqs& S, int D, const int32_t* refs,
+                                 int32_t* new_table, int32_t* new_refs, int32_t* moved,
+                                 int32_t* n_live, void* ws, hipStream_t st) {
+  uint64_t total;
+  const Compact C = compact_of(ws, pool.P, &total);
+  const int chunks = chunks_of(pool.P), pieces = pieces_of(pool.H, D);
+  const bool places = chunks <= kOwnChunks;
+  hipLaunchKernelGGL(used_kernel, dim3(chunks), dim3(256), 0, st, pool.P, refs, chunks, places, C,
+                     moved, new_refs, n_live, static_cast<uint32_t*>(ws));
+  if (!places)
+    hipLaunchKernelGGL(place_kernel, dim3(chunks), dim3(256), 0, st, pool.P, refs, C, moved,
+                       new_refs);
+  // as many copying workgroups as the card holds at once, or as there can be pieces to move
+  const int64_t most = (int64_t)(pool.P / 2 + 1) * pieces, entries = (int64_t)S.n * S.width;
+  const int movers = (int)(most < 2048 ? most : 2048);
+  const int64_t rest = (entries + 255) / 256;
+  hipLaunchKernelGGL(move_kernel, dim3(movers + (unsigned)(rest < 4096 ? rest : 4096)), dim3(256), 0,
+                     st, pool, D, refs, entries, S.table, new_table, movers, pieces, C, moved,
+                     new_refs);
+  return hipGetLastError();
+}

@@ -2,7 +2,9 @@
 pages that holds decoded contexts as int8 codes under a scale per page and head, and the operators
 on it — rows in and out (``store``, ``load``), attention of one or many query tokens
 (``attend``), eviction by accumulated weight (``evict``) and the choice of the pages a query reads
-(``select``).
+(``select``); and what requests that share a context need: pages shared, handed out, given back,
+copied and moved together (``fork``, ``reserve``, ``release``, ``copy``, ``compact``), attention that
+reads a shared context once (``attend_shared``), drafted tokens accepted or not (``verify``).
 
 Argument marshalling only, as in ``cachegen``: every step runs in the HIP kernels of
 ``libcachegen.so``, torch supplies buffers and the stream handle, and there is no CPU fallback.
@@ -45,12 +47,27 @@ class _Attn(ctypes.Structure):
                 ("decay", ctypes.c_float)]
 
 
+class _Contexts(ctypes.Structure):
+    _fields_ = [("seqs", _Seqs), ("lengths", _P), ("max_len", _I32), ("firsts", _P),
+                ("max_users", _I32)]
+
+
+class _Verify(ctypes.Structure):
+    _fields_ = [("n_seq", _I32), ("n_drafts", _I32), ("vocab", _I32), ("dtype", _I32),
+                ("target", _P), ("t_seq_stride", _I64), ("t_row_stride", _I64), ("draft", _P),
+                ("d_seq_stride", _I64), ("d_row_stride", _I64), ("drafts", _P), ("counts", _P),
+                ("u", _P), ("tokens", _P), ("accepted", _P), ("lengths", _P), ("new_lengths", _P)]
+
+
 # The same structures as bytes: a call of one token takes a few microseconds on the GPU, and packing
 # a structure at once takes a fraction of setting it field by field.
 _SEQS = struct.Struct("@iiP")
 _ROWS = struct.Struct("@Pqqq")
 _ATTN = struct.Struct("@iiifPiPPqqqPqqqPPiPPf0P")
-assert (_SEQS.size, _ROWS.size, _ATTN.size) == tuple(map(ctypes.sizeof, (_Seqs, _Rows, _Attn)))
+_CONTEXTS = struct.Struct("@iiPPiPi0P")
+_VERIFY = struct.Struct("@iiiiPqqPqqPPPPPPP")
+assert (_SEQS.size, _ROWS.size, _ATTN.size, _CONTEXTS.size, _VERIFY.size) == tuple(
+    map(ctypes.sizeof, (_Seqs, _Rows, _Attn, _Contexts, _Verify)))
 
 _LIB = None
 
@@ -69,9 +86,26 @@ def _lib():
         L.cg_kv8_select_workspace_bytes.restype = U64
         L.cg_kv8_select.argtypes = [_P, _P, _P, _I32, _P, _P, U64, _P]
         L.cg_kv8_evict.argtypes = [_P, _P, _P, _I32, _P, _I32, _I32, _P, _P, _P, _P]
+        L.cg_kv8_attend_shared_workspace_bytes.argtypes = [_P, _P, _P, _P]
+        L.cg_kv8_attend_shared_workspace_bytes.restype = U64
+        L.cg_kv8_attend_shared.argtypes = [_P, _P, _P, _P, _P, U64, _P]
+        L.cg_kv8_fork.argtypes = [_P, _P, _P, _P, _P, _P, _P, _P, _P]
+        L.cg_kv8_reserve_workspace_bytes.argtypes = [_P, _P]
+        L.cg_kv8_reserve_workspace_bytes.restype = U64
+        L.cg_kv8_reserve.argtypes = [_P, _P, _P, _P, _P, _P, _P, U64, _P]
+        L.cg_kv8_release.argtypes = [_P, _P, _P, _P, _P]
+        L.cg_kv8_copy.argtypes = [_P, _P, _P, _I32, _P]
+        L.cg_kv8_compact_workspace_bytes.argtypes = [_P]
+        L.cg_kv8_compact_workspace_bytes.restype = U64
+        L.cg_kv8_compact.argtypes = [_P, _P, _P, _P, _P, _P, _P, _P, U64, _P]
+        L.cg_verify_workspace_bytes.argtypes = [_P]
+        L.cg_verify_workspace_bytes.restype = U64
+        L.cg_verify_drafts.argtypes = [_P, _P, U64, _P]
+        L.cg_verify_drafts.restype = ctypes.c_int
         L.hipStreamIsCapturing.argtypes = [_P, _P]        # of the runtime that the library links
         L.hipStreamIsCapturing.restype = ctypes.c_int
-        for n in ("store", "load", "attend", "select", "evict"):
+        for n in ("store", "load", "attend", "select", "evict", "attend_shared", "fork", "reserve",
+                  "release", "copy", "compact"):
             getattr(L, "cg_kv8_" + n).restype = ctypes.c_int
         _LIB = L
     return _LIB
@@ -188,11 +222,11 @@ class Kv8Cache:
         if need is None:
             rc = fn(cache or self._cp, *args, handle)
         elif need == 0:
-            rc = fn(self._cp, *args, None, 0, handle)
+            rc = fn(cache or self._cp, *args, None, 0, handle)
         else:
             with self._lock:
                 ws = self._scratch(stream, handle, need)
-                rc = fn(self._cp, *args, ws[0], ws[1], handle)
+                rc = fn(cache or self._cp, *args, ws[0], ws[1], handle)
         _check(rc, name)
 
     def _new(self, make, shape, dtype, stream):
@@ -237,8 +271,10 @@ class Kv8Cache:
     def _mass(self, mass):
         return self._tensor(mass, "mass", self._f32, (self.n_pages, self.n_heads, PAGE))
 
-    def _clearing(self, mass):
-        """The cache with these weights, for a store."""
+    def _with(self, mass):
+        """The cache with these weights, for a call that clears or moves them; None without."""
+        if mass is None:
+            return None
         c = _Cache.from_buffer_copy(self._c)
         c.mass = self._mass(mass)
         return ctypes.byref(c)
@@ -261,7 +297,7 @@ class Kv8Cache:
             self._per_seq(counts, "counts", n), shape[1], kind, self._rows(k, "k", shape, k.dtype),
             self._rows(v, "v", shape, k.dtype),
             None if status is None else self._tensor(status, "status", self._i32, (1,)),
-            cache=None if mass is None else self._clearing(mass))
+            cache=self._with(mass))
 
     def load(self, table, starts, n_tokens, counts=None, dtype=None, k=None, v=None, stream=None):
         """(k, v) [n_seq, n_tokens, n_heads, head_dim]: the sequences' tokens from ``starts`` on,
@@ -372,3 +408,185 @@ class Kv8Cache:
             _bound(max_len, width),
             self._mass(mass), keep, recent, to, kept.data_ptr(), new_lengths.data_ptr())
         return kept, new_lengths
+
+    # ---- requests that share a context -----------------------------------------------------
+    def _refs(self, refs):
+        return self._tensor(refs, "refs", self._i32, (self.n_pages,))
+
+    def fork(self, table, lengths, parents, refs, ends=None, new_table=None, stream=None):
+        """Children of the table's sequences, which share their pages: child i holds the first
+        ``ends[i]`` tokens (default: all) of sequence ``parents[i]``. Returns (new_table, new_lengths).
+
+        refs       int32 [n_pages]: how many table rows hold each page (0: it is free), kept by the
+                   caller and brought up to date by the calls that take it.
+        new_table  int32 [children, columns] to write into, at least as wide as ``table`` and none
+                   of its memory a parent's row; what it held is not released. Default: a new one,
+                   as wide as ``table``. A child that will outgrow its parent's row wants a wider
+                   one."""
+        s, n, width = self._seqs(table)
+        _need(lengths is not None and parents is not None, "lengths and parents are wanted")
+        _need(parents.dim() == 1, "parents: [children] is wanted")
+        m = parents.shape[0]
+        if new_table is None:
+            new_table = self._empty((m, width), self._i32, stream)
+        to, rows, _ = self._seqs(new_table)
+        _need(rows == m, f"new_table: {m} rows are wanted")
+        new_lengths = self._empty((m,), self._i32, stream)
+        self._launch("cg_kv8_fork", _lib().cg_kv8_fork, stream, s,
+                     self._per_seq(lengths, "lengths", n), self._per_seq(parents, "parents", m),
+                     self._per_seq(ends, "ends", m), to, new_lengths.data_ptr(), self._refs(refs))
+        return new_table, new_lengths
+
+    def reserve(self, table, lengths, counts, refs, mass=None, missing=None, stream=None):
+        """Pages for ``counts[i]`` tokens behind the ``lengths[i]`` that sequence i holds, for a
+        ``store`` that follows: free ones (lowest number first) where its row of ``table`` has none
+        of its own, and a copy of a page that it shares and would write to. ``table`` and ``refs``
+        are updated. Returns ``missing`` (int32 [1]): 0, or how many free pages too few there are;
+        then nothing has changed, and the sequences must not be written to. ``mass``: weights that
+        go with a copied page."""
+        s, n, _ = self._seqs(table)
+        _need(lengths is not None and counts is not None, "lengths and counts are wanted")
+        if missing is None:
+            missing = self._empty((1,), self._i32, stream)
+        L, cache = _lib(), self._with(mass)
+        self._launch("cg_kv8_reserve", L.cg_kv8_reserve, stream, s,
+                     self._per_seq(lengths, "lengths", n), self._per_seq(counts, "counts", n),
+                     self._refs(refs), self._tensor(missing, "missing", self._i32, (1,)),
+                     need=L.cg_kv8_reserve_workspace_bytes(self._cp, s), cache=cache)
+        return missing
+
+    def release(self, table, refs, keep=None, stream=None):
+        """Gives back the pages of the table's sequences, or those that lie behind the first
+        ``keep[i]`` tokens of sequence i; their entries become -1."""
+        s, n, _ = self._seqs(table)
+        self._launch("cg_kv8_release", _lib().cg_kv8_release, stream, s,
+                     self._per_seq(keep, "keep", n), self._refs(refs))
+
+    def copy(self, src, dst, mass=None, stream=None):
+        """Page ``src[i]`` to page ``dst[i]`` (int32 [n]; no page twice in ``dst``, nor in both),
+        with its weights if ``mass`` is given."""
+        _need(src.dim() == 1, "src: [n] is wanted")
+        n = src.shape[0]
+        pages = self._tensor(src, "src", self._i32), self._tensor(dst, "dst", self._i32, (n,))
+        cache = self._with(mass)
+        if n:
+            self._launch("cg_kv8_copy", _lib().cg_kv8_copy, stream, *pages, n, cache=cache)
+
+    def compact(self, table, refs, mass=None, stream=None):
+        """Moves the pages in use to the front of the pool. Returns (new_table, new_refs, moved,
+        n_live): the table and the counts as the pages lie now, the new number of each page (int32
+        [n_pages], -1 of a free one) for other tables, and how many are in use (int32 [1]).
+        ``table`` and ``refs`` are left as they were."""
+        s, n, width = self._seqs(table)
+        new_table = self._empty((n, width), self._i32, stream)
+        new_refs = self._empty((self.n_pages,), self._i32, stream)
+        moved = self._empty((self.n_pages,), self._i32, stream)
+        live = self._empty((1,), self._i32, stream)
+        L, cache = _lib(), self._with(mass)
+        self._launch("cg_kv8_compact", L.cg_kv8_compact, stream, s, self._refs(refs),
+                     new_table.data_ptr(), new_refs.data_ptr(), moved.data_ptr(), live.data_ptr(),
+                     need=L.cg_kv8_compact_workspace_bytes(self._cp), cache=cache)
+        return new_table, new_refs, moved, live
+
+    def attend_shared(self, q, shared, shared_lengths, firsts, table=None, lengths=None, scale=None,
+                      q_lens=None, max_shared=None, max_len=None, max_users=None, out=None,
+                      lse=None, stream=None):
+        """Attention of the queries q [n_seq, n_q, n_q_heads, head_dim] over contexts that sequences
+        share, read once for all of them, and over the sequences' own tokens behind; returns ``out``.
+
+        shared         int32 [contexts, columns]: the contexts' pages; ``shared_lengths`` [contexts].
+        firsts         int32 [contexts + 1], ascending: context p is that of sequences firsts[p] ..
+                       firsts[p + 1] - 1. Every query token sees all of its sequence's context.
+        table, lengths the sequences' own pages and tokens, seen causally as in ``attend`` (the
+                       queries are the last of them). Without: attention over the contexts alone,
+                       as over an encoder's states.
+        max_shared, max_len, max_users  bounds that the host knows of shared_lengths, of lengths and
+                       of the sequences that share a context (default: the tables' widths, n_seq);
+                       the work is laid out for them.
+        scale, q_lens, lse  as in ``attend``."""
+        x, contexts, x_width = self._seqs(shared)
+        _need(q.dim() == 4, "q: [n_seq, n_q, n_q_heads, head_dim] is wanted")
+        n = q.shape[0]
+        kind, nq, heads, shape = self._queries(q, n)
+        _need(shared_lengths is not None and firsts is not None,
+              "shared_lengths and firsts are wanted")
+        _need((table is None) == (lengths is None), "table and lengths go together")
+        if table is None:
+            s, width = _SEQS.pack(n, 0, 0), 0
+        else:
+            s, rows, width = self._seqs(table)
+            _need(rows == n, f"table: {n} rows are wanted")
+        if out is None:
+            out = self._empty(q.shape, q.dtype, stream)
+        c = _CONTEXTS.pack(contexts, x_width, shared.data_ptr(),
+                           self._per_seq(shared_lengths, "shared_lengths", contexts),
+                           _bound(max_shared, x_width),
+                           self._per_seq(firsts, "firsts", contexts + 1),
+                           n if max_users is None else max_users)
+        a = _ATTN.pack(nq, heads, kind, self._scale if scale is None else scale,
+                       self._per_seq(lengths, "lengths", n), _bound(max_len, width),
+                       self._per_seq(q_lens, "q_lens", n), *self._strided(q, "q", shape, q.dtype),
+                       *self._strided(out, "out", shape, q.dtype),
+                       0 if lse is None else self._tensor(lse, "lse", self._f32, shape[:3]),
+                       0, 0, 0, 0, 1.0)
+        L = _lib()
+        self._launch("cg_kv8_attend_shared", L.cg_kv8_attend_shared, stream, c, s, a,
+                     need=L.cg_kv8_attend_shared_workspace_bytes(self._cp, c, s, a))
+        return out
+
+    # ---- drafted tokens --------------------------------------------------------------------
+    def _probabilities(self, t, name, shape, dtype):
+        """(address, strides of sequences and rows)"""
+        if t.dtype is dtype and t.shape == shape and t.device == self.device:
+            a, b, c = t.stride()
+            if c == 1:
+                return t.data_ptr(), a, b
+        raise ValueError(f"{name}: {dtype} probabilities {tuple(shape)} with a contiguous last "
+                         f"dimension on {self.device} are wanted, got {t.dtype} {tuple(t.shape)} "
+                         f"on {t.device}")
+
+    def verify(self, target, drafts, u, draft=None, counts=None, lengths=None, tokens=None,
+               accepted=None, new_lengths=None, stream=None):
+        """Drafted tokens accepted by the target's probabilities, and the token behind them.
+        Returns (tokens, accepted) or, with ``lengths``, (tokens, accepted, new_lengths).
+
+        target   [n_seq, n_drafts + 1, vocab] float32, float16 or bfloat16 probabilities of the
+                 target: row j for draft j, the last behind all drafts.
+        drafts   int32 [n_seq, n_drafts]; ``counts`` int32 [n_seq]: how many of each sequence
+                 (default: all; below 0: the sequence sits out).
+        draft    [n_seq, n_drafts, vocab] of the same type: the probabilities that the drafts were
+                 drawn from, or None: each draft was sure.
+        u        float32 [n_seq, n_drafts + 1] random numbers in [0, 1): one for each draft, the
+                 last for the token that is drawn.
+        lengths  int32 [n_seq] tokens that the cache holds, the drafts among them.
+        tokens   int32 [n_seq, n_drafts + 1]: the accepted drafts, the token drawn behind them, -1.
+        accepted     int32 [n_seq] drafts accepted.
+        new_lengths  int32 [n_seq] lengths less the drafts not accepted (may be ``lengths``): what
+                     ``release`` keeps."""
+        kind = {self.torch.float32: 2, **self._types}.get(target.dtype)
+        _need(target.dim() == 3 and kind is not None and target.shape[1] > 0,
+              "target: float32, float16 or bfloat16 [n_seq, n_drafts + 1, vocab] is wanted")
+        n, k, vocab = target.shape[0], target.shape[1] - 1, target.shape[2]
+        rows = self._probabilities(target, "target", target.shape, target.dtype)
+        near = (0, 0, 0) if draft is None or k == 0 else self._probabilities(
+            draft, "draft", (n, k, vocab), target.dtype)
+
+        def out(t, name, shape):
+            t = self._empty(shape, self._i32, stream) if t is None else t
+            return t, self._tensor(t, name, self._i32, shape)
+        tokens, tokens_p = out(tokens, "tokens", (n, k + 1))
+        accepted, accepted_p = out(accepted, "accepted", (n,))
+        lengths_p = new_p = 0
+        _need(lengths is not None or new_lengths is None, "lengths is missing")
+        if lengths is not None:
+            lengths_p = self._per_seq(lengths, "lengths", n)
+            new_lengths, new_p = out(new_lengths, "new_lengths", (n,))
+        v = _VERIFY.pack(n, k, vocab, kind, *rows, *near,
+                         self._tensor(drafts, "drafts", self._i32, (n, k)),
+                         self._per_seq(counts, "counts", n),
+                         self._tensor(u, "u", self._f32, (n, k + 1)), tokens_p, accepted_p,
+                         lengths_p, new_p)
+        L = _lib()
+        self._launch("cg_verify_drafts", L.cg_verify_drafts, stream,
+                     need=L.cg_verify_workspace_bytes(v), cache=v)
+        return (tokens, accepted) if lengths is None else (tokens, accepted, new_lengths)

@@ -2,16 +2,17 @@
 // (cg_kv8_fork), pages for what comes (cg_kv8_reserve), pages given back (cg_kv8_release), moved
 // together (cg_kv8_compact) and copied (cg_kv8_copy).
 //
-// Free pages are found by rank: the pages' counts are taken in chunks of 4096, a workgroup each; the
-// last workgroup to arrive sums the chunks up (with what each sequence wants), and the pages of a
-// chunk then know their place among all. So the i-th page wanted gets the i-th free one, and no
-// result depends on an order of arrival. Values that workgroups of one launch hand to each other are
-// written and read past the XCDs' own caches (agent scope).
+// Free pages are found by rank: sums over the pages' counts give each page its place among the free
+// ones (or those in use), so the i-th page wanted gets the i-th free one, and no result depends on
+// an order of arrival. Up to some tens of thousands of pages one workgroup does it all: a second one
+// would have to hand its sums over, which takes longer than the pages do. Of larger pools a workgroup
+// counts 4096 pages, and the last to arrive sums up; what workgroups of one launch hand to each other
+// is written and read past the XCDs' own caches (agent scope).
 #include "cg_kv8.h"
 
 namespace {
 
-constexpr int kRounds = 16, kChunk = 256 * kRounds;
+constexpr int kRounds = 16, kChunk = 256 * kRounds;   // (of a workgroup of 256)
 
 __device__ __forceinline__ void put_far(int32_t* p, int32_t v) {
   __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -37,23 +38,25 @@ __device__ __forceinline__ bool last_here(uint32_t* counter, uint32_t* lds) {
   return *lds == gridDim.x - 1;
 }
 
-// Exclusive sum over the workgroup's 256 threads; `total` receives the whole. lds: 4 words.
-__device__ __forceinline__ int64_t scan256(int64_t x, int64_t* lds, int64_t& total) {
-  int64_t s = x;
+// Exclusive sum over the workgroup's NT threads; `total` receives the whole. lds: a word a wave.
+template <int NT, class T>
+__device__ __forceinline__ T scan_wg(T x, T* lds, T& total) {
+  T s = x;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const int64_t y = __shfl_up(s, o);
+    const T y = __shfl_up(s, o);
     s += (int)(threadIdx.x & 63) >= o ? y : 0;
   }
   __syncthreads();
   if ((threadIdx.x & 63) == 63) lds[threadIdx.x >> 6] = s;
   __syncthreads();
-  int64_t before = 0;
+  T before = 0;
   total = 0;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    before += w < (int)(threadIdx.x >> 6) ? lds[w] : 0;
-    total += lds[w];
+  for (int w = 0; w < NT / 64; ++w) {
+    const T y = lds[w];
+    before += w < (int)(threadIdx.x >> 6) ? y : 0;
+    total += y;
   }
   return before + s - x;
 }
@@ -72,7 +75,7 @@ __device__ __forceinline__ int64_t scan_far(int32_t* v, int n, int64_t* lds) {
       x[k] = i < n ? get_far(v + i) : 0;
       sum += x[k];
     }
-    int64_t at = run + scan256(sum, lds, total);
+    int64_t at = run + scan_wg<256>(sum, lds, total);
 #pragma unroll
     for (int k = 0; k < N; ++k) {
       const int64_t i = i0 + threadIdx.x * N + k;
@@ -84,51 +87,68 @@ __device__ __forceinline__ int64_t scan_far(int32_t* v, int n, int64_t* lds) {
   return run;
 }
 
+template <int NT>
 struct ChunkLds {
-  int32_t at[4 * kRounds];           // pages in use before round k's wave w: [k][w]
+  int32_t at[kRounds * NT / 64];     // pages in use before round k's wave w: [k][w]
   int32_t total;
 };
 
-// Calls f(page, in use, pages of the chunk in use before it) for every page of a chunk, a thread
-// each, and returns the chunk's pages in use.
-template <class F>
-__device__ __forceinline__ int walk_chunk(const int32_t* refs, int P, int chunk, ChunkLds& L, F f) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint32_t used = 0;                 // this thread's pages, bit k for round k
-  const int64_t p0 = (int64_t)chunk * kChunk + threadIdx.x;
+// The pages of a chunk of 16 NT, a thread each in 16 rounds. Held: the counts, then f(page, count,
+// pages of the chunk in use before it) for every page.
+template <int NT>
+struct Chunk {
   int32_t r[kRounds];
-#pragma unroll
-  for (int k = 0; k < kRounds; ++k) r[k] = p0 + k * 256 < P ? refs[p0 + k * 256] : 0;
-  uint64_t mask[kRounds];
-#pragma unroll
-  for (int k = 0; k < kRounds; ++k) {
-    used |= (r[k] > 0 ? 1u : 0u) << k;
-    mask[k] = __ballot(r[k] > 0);
-    if (lane == 0) L.at[4 * k + wave] = __popcll(mask[k]);
-  }
-  __syncthreads();
-  if (wave == 0) {
-    const int x = L.at[lane];
-    int s = x;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(s, o);
-      s += lane >= o ? y : 0;
-    }
-    L.at[lane] = s - x;
-    if (lane == 63) L.total = s;
-  }
-  __syncthreads();
-  const int total = L.total;
-#pragma unroll
-  for (int k = 0; k < kRounds; ++k)
-    if (p0 + k * 256 < P)
-      f((int)(p0 + k * 256), (used >> k & 1) != 0, L.at[4 * k + wave] + below(mask[k]));
-  __syncthreads();                   // the LDS may be used again
-  return total;
-}
+  int64_t p0;
 
-static_assert(4 * kRounds == 64, "one lane a (round, wave)");
+  __device__ __forceinline__ void load(const int32_t* refs, int P, int chunk) {
+    p0 = (int64_t)chunk * (kRounds * NT) + threadIdx.x;
+#pragma unroll
+    for (int k = 0; k < kRounds; ++k) r[k] = p0 + k * NT < P ? refs[p0 + k * NT] : 0;
+  }
+  __device__ __forceinline__ bool past(int P, int k) const {   // no page of round k, in any lane
+    return p0 - threadIdx.x + k * NT >= P;
+  }
+  // Returns the chunk's pages in use.
+  __device__ __forceinline__ int count(int P, ChunkLds<NT>& L) const {
+    constexpr int W = NT / 64, E = kRounds * W / 64;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __syncthreads();                 // the LDS may have been used
+#pragma unroll
+    for (int k = 0; k < kRounds; ++k) {
+      const uint64_t mask = __ballot(r[k] > 0);
+      if (lane == 0) L.at[k * W + wave] = __popcll(mask);
+    }
+    __syncthreads();
+    if (wave == 0) {
+      int x[E], sum = 0;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        x[e] = sum;
+        sum += L.at[lane * E + e];
+      }
+      int s = sum;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(s, o);
+        s += lane >= o ? y : 0;
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) L.at[lane * E + e] = s - sum + x[e];
+      if (lane == 63) L.total = s;
+    }
+    __syncthreads();
+    return L.total;
+  }
+  template <class F>
+  __device__ __forceinline__ void each(int P, const ChunkLds<NT>& L, F f) const {
+#pragma unroll
+    for (int k = 0; k < kRounds; ++k) {
+      if (past(P, k)) break;
+      const int before = L.at[k * (NT / 64) + (threadIdx.x >> 6)] + below(__ballot(r[k] > 0));
+      if (p0 + k * NT < P) f((int)(p0 + k * NT), r[k], before);
+    }
+  }
+};
 
 // ---- copies -----------------------------------------------------------------------------------
 // A page is copied in pieces of 16 KB of its codes, K's and then V's, a workgroup each, with four
@@ -205,38 +225,34 @@ __device__ __forceinline__ int clamp_len(int64_t n, int width) {
   return n > 0 ? (int)n : 0;
 }
 
+// A workgroup = 256 columns of a row.
 __global__ __launch_bounds__(256) void fork_kernel(int P, KvSeqs S, const int32_t* lengths,
                                                    const int32_t* parents, const int32_t* ends,
-                                                   int n, int width, int32_t* table,
+                                                   int width, int per_row, int32_t* table,
                                                    int32_t* new_lengths, int32_t* refs) {
-  const int64_t items = (int64_t)n * width;
-  for (int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x; it < items;
-       it += (int64_t)gridDim.x * 256) {
-    const int row = (int)(it / width), j = (int)(it % width), p = parents[row];
-    int len = 0;
-    if (p >= 0 && p < S.n) {
-      len = clamp_len(lengths[p], S.width);
-      if (ends) len = ends[row] < len ? (ends[row] > 0 ? ends[row] : 0) : len;
-    }
-    int32_t page = -1;
-    if ((int64_t)j * kPage < len) page = kv_page(S, P, p, j);
-    table[it] = page;
-    if (page >= 0) atomicAdd(refs + page, 1);
-    if (j == 0) new_lengths[row] = len;
+  const int row = blockIdx.x / per_row, j = blockIdx.x % per_row * 256 + threadIdx.x;
+  const int p = parents[row];
+  int len = 0;
+  if (p >= 0 && p < S.n) {
+    len = clamp_len(lengths[p], S.width);
+    if (ends) len = ends[row] < len ? (ends[row] > 0 ? ends[row] : 0) : len;
   }
+  if (j == 0) new_lengths[row] = len;
+  if (j >= width) return;
+  int32_t page = -1;
+  if ((int64_t)j * kPage < len) page = kv_page(S, P, p, j);
+  table[(int64_t)row * width + j] = page;
+  if (page >= 0) atomicAdd(refs + page, 1);
 }
 
-__global__ __launch_bounds__(256) void release_kernel(int P, int n, int width, int32_t* table,
+__global__ __launch_bounds__(256) void release_kernel(int P, int width, int per_row, int32_t* table,
                                                       const int32_t* keep, int32_t* refs) {
-  const int64_t items = (int64_t)n * width;
-  for (int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x; it < items;
-       it += (int64_t)gridDim.x * 256) {
-    const int row = (int)(it / width), j = (int)(it % width);
-    if (keep && (int64_t)j * kPage < keep[row]) continue;
-    const int32_t p = table[it];
-    if (names_page(p, P)) drop(refs, p);
-    table[it] = -1;
-  }
+  const int row = blockIdx.x / per_row, j = blockIdx.x % per_row * 256 + threadIdx.x;
+  if (j >= width || (keep && (int64_t)j * kPage < keep[row])) return;
+  int32_t* const at = table + (int64_t)row * width + j;
+  const int32_t p = *at;
+  if (names_page(p, P)) drop(refs, p);
+  if (p != -1) *at = -1;
 }
 
 // ---- pages for what comes -----------------------------------------------------------------------
@@ -245,8 +261,9 @@ struct Reserve {
   int32_t* chunks;                   // [chunks] free pages of each, then before each
   int32_t* need;                     // [n] pages that each sequence wants, then those before it
   int32_t* source;                   // [n] the page that a sequence's first wanted one copies, or -1
-  uint64_t* wants;                   // [n][words][2] which columns from its first on, and which of
-                                     // them name a page that the sequence holds with others
+  uint64_t* wants;                   // [n][words] bits: the columns that want a page, by sequence,
+  uint64_t* drops;                   // and those that name a page which others hold too
+  int64_t* bits;                     // [n] where a sequence's first column lies in them
   int32_t* state;                    // pages wanted by all, or -1: there are not as many
   int32_t* list;                     // [at most P] the free pages in order
 };
@@ -266,30 +283,22 @@ __device__ __forceinline__ Span span_of(const int32_t* lengths, const int32_t* c
   return s;
 }
 
-// The free pages of a chunk to their places in the list, as far as they are wanted.
-__device__ __forceinline__ void list_chunk(const int32_t* refs, int P, int chunk, int before,
-                                           int wanted, int32_t* list, ChunkLds& L) {
-  walk_chunk(refs, P, chunk, L, [&](int page, bool used, int used_before) {
-    const int64_t rank = (int64_t)before + (page - chunk * kChunk - used_before);
-    if (!used && rank < wanted) list[rank] = page;
-  });
-}
-
 // Workgroups 0 .. chunks - 1 count the free pages of their chunks, the others what four sequences
-// want, a wave each; the last to come sums both up and, where `lists`, writes the list as well: with
-// few chunks that takes less than another launch.
+// want, a wave each; the last to come sums both up.
 __global__ __launch_bounds__(256) void want_kernel(int P, int n, int width, const int32_t* table,
                                                    const int32_t* lengths, const int32_t* counts,
                                                    const int32_t* refs, int chunks, int words,
-                                                   bool lists, Reserve R, int32_t* missing,
+                                                   Reserve R, int32_t* missing,
                                                    uint32_t* counter) {
-  __shared__ ChunkLds L;
+  __shared__ ChunkLds<256> L;
   __shared__ int64_t sums[4];
   __shared__ uint32_t order;
   const int lane = threadIdx.x & 63;
   if ((int)blockIdx.x < chunks) {
     const int chunk = blockIdx.x;
-    const int used = walk_chunk(refs, P, chunk, L, [](int, bool, int) {});
+    Chunk<256> c;
+    c.load(refs, P, chunk);
+    const int used = c.count(P, L);
     const int64_t left = (int64_t)P - (int64_t)chunk * kChunk;
     if (threadIdx.x == 0) put_far(R.chunks + chunk, (int)(left < kChunk ? left : kChunk) - used);
   } else {
@@ -312,14 +321,15 @@ __global__ __launch_bounds__(256) void want_kernel(int P, int n, int width, cons
         }
         const uint64_t mask = __ballot(want), shared = __ballot(drops);
         if (lane == 0) {
-          uint64_t* const w = R.wants + 2 * ((int64_t)b * words + (j0 - s.first) / 64);
-          w[0] = mask;
-          w[1] = shared;
+          const int64_t w = (int64_t)b * words + (j0 - s.first) / 64;
+          R.wants[w] = mask;
+          R.drops[w] = shared;
         }
         need += __popcll(mask);
       }
       if (lane == 0) {                 // (a page that is copied is in the first column: lane 0's)
         R.source[b] = source;
+        R.bits[b] = (int64_t)b * words * 64;
         put_far(R.need + b, need);
       }
     }
@@ -332,24 +342,119 @@ __global__ __launch_bounds__(256) void want_kernel(int P, int n, int width, cons
     *R.state = ok ? (int32_t)wanted : -1;
     *missing = ok ? 0 : wanted - free < INT32_MAX ? (int32_t)(wanted - free) : INT32_MAX;
   }
-  if (!lists || !ok) return;
-  int before = 0;
-  for (int c = 0; c < chunks; ++c) {
-    const int64_t left = (int64_t)P - (int64_t)c * kChunk;
-    int used = 0;
-    if (before < wanted)
-      used = walk_chunk(refs, P, c, L, [&](int page, bool in_use, int used_before) {
-        const int64_t rank = (int64_t)before + (page - c * kChunk - used_before);
-        if (!in_use && rank < wanted) R.list[rank] = page;
-      });
-    before += (int)(left < kChunk ? left : kChunk) - used;
+}
+
+// The free pages to their places in the list, as far as they are wanted.
+__global__ __launch_bounds__(256) void list_kernel(int P, const int32_t* refs, Reserve R) {
+  __shared__ ChunkLds<256> L;
+  const int wanted = *R.state, before = R.chunks[blockIdx.x], first = blockIdx.x * kChunk;
+  if (before >= wanted) return;
+  Chunk<256> c;
+  c.load(refs, P, blockIdx.x);
+  c.count(P, L);
+  c.each(P, L, [&](int page, int held, int used_before) {
+    const int64_t rank = (int64_t)before + (page - first - used_before);
+    if (held <= 0 && rank < wanted) R.list[rank] = page;
+  });
+}
+
+// All of the above in one workgroup. A thread takes a sequence's span of columns first; then the
+// spans' columns lie one after the other, a thread each, found by a search over the spans' sums in
+// LDS. Then the free pages, 16384 a step, until there are as many as wanted.
+constexpr int kPlanThreads = 1024, kPlanSeqs = 2048, kPlanPages = 16 * kPlanThreads;
+
+struct PlanLds {
+  int32_t at[kPlanSeqs + 1];           // columns before each sequence's
+  int32_t first[kPlanSeqs];            // its first column
+  int32_t keep[kPlanSeqs];             // tokens of its first column that stay
+  int32_t sums[kPlanThreads / 64];
+};
+
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(int P, int n, int width,
+                                                            const int32_t* table,
+                                                            const int32_t* lengths,
+                                                            const int32_t* counts,
+                                                            const int32_t* refs, Reserve R,
+                                                            int32_t* missing) {
+  __shared__ PlanLds L;
+  __shared__ ChunkLds<kPlanThreads> C;
+  const int tid = threadIdx.x, lane = tid & 63;
+  Chunk<kPlanThreads> c;
+  c.load(refs, P, 0);                                  // (on its way meanwhile)
+  int cols = 0, total;
+  for (int b0 = 0; b0 < n; b0 += kPlanThreads) {
+    const int b = b0 + tid;
+    Span s = {0, 0, 0};
+    if (b < n) s = span_of(lengths, counts, width, b);
+    const int at = cols + scan_wg<kPlanThreads>(s.last - s.first, L.sums, total);
+    if (b < n) {
+      L.at[b] = at;
+      L.first[b] = s.first;
+      L.keep[b] = s.start - s.first * kPage;
+      R.bits[b] = at;
+      if (s.first == s.last) R.source[b] = -1;         // (the others': with their first column)
+    }
+    cols += total;
+  }
+  if (tid == 0) L.at[n] = cols;
+  __syncthreads();
+  // which of the columns want a page
+  int wanted = 0;
+  for (int i0 = 0; i0 < cols; i0 += kPlanThreads) {
+    const int i = i0 + tid;
+    bool want = false, drops = false;
+    int b = 0, j = 0, page = -1;
+    if (i < cols) {
+      int lo = 0, hi = n;                              // at[lo] <= i < at[hi]
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (L.at[mid] <= i) lo = mid;
+        else hi = mid;
+      }
+      b = lo;
+      j = i - L.at[b];
+      page = table[(int64_t)b * width + L.first[b] + j];
+      const int held = names_page(page, P) ? refs[page] : 0;
+      drops = held > 1;
+      want = j == 0 && L.keep[b] > 0 ? drops : held != 1;
+    }
+    const uint64_t mask = __ballot(want), shared = __ballot(drops);
+    if (lane == 0 && i < cols) {
+      R.wants[i >> 6] = mask;
+      R.drops[i >> 6] = shared;
+    }
+    const int rank = wanted + scan_wg<kPlanThreads>(want ? 1 : 0, L.sums, total);
+    if (i < cols && j == 0) {
+      R.need[b] = rank;
+      R.source[b] = want && L.keep[b] > 0 ? page : -1;
+    }
+    wanted += total;
+  }
+  // the first free pages
+  int free = 0;
+  for (int chunk = 0; (int64_t)chunk * kPlanPages < P && (free < wanted || chunk == 0); ++chunk) {
+    if (chunk) c.load(refs, P, chunk);
+    const int first = chunk * kPlanPages, left = P - first, used = c.count(P, C);
+    c.each(P, C, [&](int page, int held, int used_before) {
+      const int rank = free + (page - first - used_before);
+      if (held <= 0 && rank < wanted) R.list[rank] = page;
+    });
+    free += (left < kPlanPages ? left : kPlanPages) - used;
+  }
+  if (tid == 0) {
+    const bool ok = wanted <= free;
+    *R.state = ok ? wanted : -1;
+    *missing = ok ? 0 : wanted - free;
   }
 }
 
-__global__ __launch_bounds__(256) void list_kernel(int P, const int32_t* refs, Reserve R) {
-  __shared__ ChunkLds L;
-  const int wanted = *R.state, before = R.chunks[blockIdx.x];
-  if (before < wanted) list_chunk(refs, P, blockIdx.x, before, wanted, R.list, L);
+// n <= 64 bits from bit `at` on.
+__device__ __forceinline__ uint64_t bits_at(const uint64_t* w, int64_t at, int n) {
+  const int off = (int)(at & 63);
+  uint64_t x = w[at >> 6] >> off;
+  if (n > 64) n = 64;
+  if (off + n > 64) x |= w[(at >> 6) + 1] << (64 - off);
+  return n < 64 ? x & ((1ull << n) - 1) : x;
 }
 
 // Workgroup = (sequence, piece of a page): the first piece's first wave hands the pages out, all
@@ -357,25 +462,25 @@ __global__ __launch_bounds__(256) void list_kernel(int P, const int32_t* refs, R
 __global__ __launch_bounds__(256) void hand_out_kernel(KvPool pool, int D, int n, int width,
                                                        int32_t* table, const int32_t* lengths,
                                                        const int32_t* counts, int32_t* refs,
-                                                       int words, int pieces, int64_t items,
-                                                       Reserve R) {
-  if (*R.state <= 0) return;
-  const int lane = threadIdx.x & 63;
+                                                       int pieces, int64_t items, Reserve R) {
+  const int lane = threadIdx.x & 63, wanted = *R.state;
+  if (wanted <= 0) return;
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const int b = (int)(it / pieces), piece = (int)(it % pieces);
     const int source = R.source[b];
-    int rank = R.need[b];
+    int rank = R.need[b];                              // (of no use where nothing is wanted)
     if (source >= 0) copy_piece(pool, D, source, R.list[rank], piece, pieces);
     if (piece != 0 || threadIdx.x >= 64) continue;
     const Span s = span_of(lengths, counts, width, b);
     for (int j0 = s.first; j0 < s.last; j0 += 64) {
-      const uint64_t* const w = R.wants + 2 * ((int64_t)b * words + (j0 - s.first) / 64);
-      const uint64_t mask = w[0];
+      const int64_t at = R.bits[b] + (j0 - s.first);
+      const int left = s.last - j0;
+      const uint64_t mask = bits_at(R.wants, at, left);
       if (mask >> lane & 1) {
-        int32_t* const at = table + (int64_t)b * width + j0 + lane;
+        int32_t* const entry = table + (int64_t)b * width + j0 + lane;
         const int32_t page = R.list[rank + below(mask)];
-        if (w[1] >> lane & 1) drop(refs, *at);
-        *at = page;
+        if (bits_at(R.drops, at, left) >> lane & 1) drop(refs, *entry);
+        *entry = page;
         refs[page] = 1;
       }
       rank += __popcll(mask);
@@ -392,37 +497,34 @@ struct Compact {
   int32_t* key;                      // [P] a page's new number, -1 (free), or -2 - i: the i-th hole
 };
 
-// What becomes of each page of a chunk; `before` pages in use lie in the chunks before it.
-__device__ __forceinline__ void place_chunk(const int32_t* refs, int P, int chunk, int before,
-                                            int live, int front, const Compact& C, int32_t* moved,
-                                            int32_t* new_refs, ChunkLds& L) {
-  walk_chunk(refs, P, chunk, L, [&](int page, bool used, int used_before) {
-    const int rank = before + used_before;             // pages in use before this one
-    int key = used ? page : -1;
-    if (page < live) {
-      if (!used) C.holes[page - rank] = page;
-      else new_refs[page] = refs[page];
-    } else {
-      if (used) {
-        C.late[rank - front] = page;
-        key = -2 - (rank - front);
-      }
-      new_refs[page] = 0;
+// What becomes of a page that `rank` pages in use lie before, of `live` in all and `front` before
+// page `live`.
+__device__ __forceinline__ void place(const Compact& C, int32_t* moved, int32_t* new_refs, int page,
+                                      int held, int rank, int live, int front) {
+  int key = held > 0 ? page : -1;
+  if (page < live) {
+    if (held <= 0) C.holes[page - rank] = page;
+    else new_refs[page] = held;
+  } else {
+    if (held > 0) {
+      C.late[rank - front] = page;
+      key = -2 - (rank - front);
     }
-    C.key[page] = key;
-    if (key >= -1) moved[page] = key;
-  });
+    new_refs[page] = 0;
+  }
+  C.key[page] = key;
+  if (key >= -1) moved[page] = key;
 }
 
-__global__ __launch_bounds__(256) void used_kernel(int P, const int32_t* refs, int chunks,
-                                                   bool places, Compact C, int32_t* moved,
-                                                   int32_t* new_refs, int32_t* n_live,
-                                                   uint32_t* counter) {
-  __shared__ ChunkLds L;
+__global__ __launch_bounds__(256) void used_kernel(int P, const int32_t* refs, int chunks, Compact C,
+                                                   int32_t* n_live, uint32_t* counter) {
+  __shared__ ChunkLds<256> L;
   __shared__ int64_t sums[4];
   __shared__ uint32_t order;
   __shared__ int32_t in_front;
-  const int used = walk_chunk(refs, P, blockIdx.x, L, [](int, bool, int) {});
+  Chunk<256> k;
+  k.load(refs, P, blockIdx.x);
+  const int used = k.count(P, L);
   if (threadIdx.x == 0) put_far(C.chunks + blockIdx.x, used);
   if (!last_here(counter, &order)) return;
   const int live = (int)scan_far(C.chunks, chunks, sums);
@@ -432,9 +534,12 @@ __global__ __launch_bounds__(256) void used_kernel(int P, const int32_t* refs, i
   if (live < P) {
     // pages in use before page `live`
     const int c = live / kChunk, before = C.chunks[c];
-    walk_chunk(refs, P, c, L, [&](int page, bool, int used_before) {
+    k.load(refs, P, c);
+    k.count(P, L);
+    k.each(P, L, [&](int page, int, int used_before) {
       if (page == live) in_front = before + used_before;
     });
+    __syncthreads();
   }
   const int front = in_front;
   if (threadIdx.x == 0) {
@@ -443,16 +548,45 @@ __global__ __launch_bounds__(256) void used_kernel(int P, const int32_t* refs, i
     C.state[2] = live - front;
     *n_live = live;
   }
-  if (places)
-    for (int c = 0; c < chunks; ++c)
-      place_chunk(refs, P, c, C.chunks[c], live, front, C, moved, new_refs, L);
 }
 
 __global__ __launch_bounds__(256) void place_kernel(int P, const int32_t* refs, Compact C,
                                                     int32_t* moved, int32_t* new_refs) {
-  __shared__ ChunkLds L;
-  place_chunk(refs, P, blockIdx.x, C.chunks[blockIdx.x], C.state[0], C.state[1], C, moved, new_refs,
-              L);
+  __shared__ ChunkLds<256> L;
+  const int before = C.chunks[blockIdx.x], live = C.state[0], front = C.state[1];
+  Chunk<256> c;
+  c.load(refs, P, blockIdx.x);
+  c.count(P, L);
+  c.each(P, L, [&](int page, int held, int used_before) {
+    place(C, moved, new_refs, page, held, before + used_before, live, front);
+  });
+}
+
+// Both in one workgroup, which holds all counts in registers.
+__global__ __launch_bounds__(kPlanThreads) void places_kernel(int P, const int32_t* refs, Compact C,
+                                                              int32_t* moved, int32_t* new_refs,
+                                                              int32_t* n_live) {
+  __shared__ ChunkLds<kPlanThreads> L;
+  __shared__ int32_t in_front;
+  Chunk<kPlanThreads> c;
+  c.load(refs, P, 0);
+  const int live = c.count(P, L);
+  if (threadIdx.x == 0) in_front = live;               // (all of them, where there are no others)
+  __syncthreads();
+  c.each(P, L, [&](int page, int, int before) {
+    if (page == live) in_front = before;
+  });
+  __syncthreads();
+  const int front = in_front;
+  c.each(P, L, [&](int page, int held, int before) {
+    place(C, moved, new_refs, page, held, before, live, front);
+  });
+  if (threadIdx.x == 0) {
+    C.state[0] = live;
+    C.state[1] = front;
+    C.state[2] = live - front;
+    *n_live = live;
+  }
 }
 
 // The moves, and the table: workgroups 0 .. movers - 1 copy, the others rewrite entries.
@@ -484,11 +618,16 @@ __global__ __launch_bounds__(256) void move_kernel(KvPool pool, int D, const int
 
 unsigned grid_of(int64_t items) { return (unsigned)(items < (1 << 20) ? items : (1 << 20)); }
 
-// The one workgroup that comes last writes the list itself for up to this many chunks; past them a
-// launch of a workgroup a chunk does.
-constexpr int kOwnChunks = 2;
-
 int chunks_of(int P) { return (int)(((int64_t)P + kChunk - 1) / kChunk); }
+
+// Launches of a workgroup for each 256 columns of a row, of below 2^32 threads each.
+template <class Launch>
+void in_rows(int n, int width, Launch launch) {
+  const int per_row = (int)(((int64_t)width + 255) / 256);
+  const int most = per_row < (1 << 22) ? (1 << 22) / per_row : 1;
+  for (int row0 = 0; row0 < n; row0 += most)
+    launch(row0, n - row0 < most ? n - row0 : most, per_row);
+}
 
 // The words of `wants`: a sequence's columns from its first on, 64 a word.
 int words_of(int width) { return (width + 63) / 64; }
@@ -510,7 +649,9 @@ Reserve reserve_of(void* ws, int P, int n, int width, uint64_t* total) {
   R.chunks = c.take<int32_t>(chunks_of(P));
   R.need = c.take<int32_t>(n);
   R.source = c.take<int32_t>(n);
-  R.wants = c.take<uint64_t>(2 * (int64_t)n * words_of(width));
+  R.wants = c.take<uint64_t>((int64_t)n * words_of(width));
+  R.drops = c.take<uint64_t>((int64_t)n * words_of(width));
+  R.bits = c.take<int64_t>(n);
   R.state = c.take<int32_t>(1);
   const int64_t most = (int64_t)n * width;
   R.list = c.take<int32_t>(most < P ? most : P);
@@ -535,15 +676,21 @@ Compact compact_of(void* ws, int P, uint64_t* total) {
 hipError_t cg_launch_kv8_fork(const KvPool& pool, const KvSeqs& S, const int32_t* lengths,
                               const int32_t* parents, const int32_t* ends, int n, int width,
                               int32_t* table, int32_t* new_lengths, int32_t* refs, hipStream_t st) {
-  hipLaunchKernelGGL(fork_kernel, dim3(grid_of(((int64_t)n * width + 255) / 256)), dim3(256), 0, st,
-                     pool.P, S, lengths, parents, ends, n, width, table, new_lengths, refs);
+  in_rows(n, width, [&](int row0, int rows, int per_row) {
+    hipLaunchKernelGGL(fork_kernel, dim3((unsigned)(rows * per_row)), dim3(256), 0, st, pool.P, S,
+                       lengths, parents + row0, ends ? ends + row0 : nullptr, width, per_row,
+                       table + (int64_t)row0 * width, new_lengths + row0, refs);
+  });
   return hipGetLastError();
 }
 
 hipError_t cg_launch_kv8_release(const KvPool& pool, int n, int width, int32_t* table,
                                  const int32_t* keep, int32_t* refs, hipStream_t st) {
-  hipLaunchKernelGGL(release_kernel, dim3(grid_of(((int64_t)n * width + 255) / 256)), dim3(256), 0,
-                     st, pool.P, n, width, table, keep, refs);
+  in_rows(n, width, [&](int row0, int rows, int per_row) {
+    hipLaunchKernelGGL(release_kernel, dim3((unsigned)(rows * per_row)), dim3(256), 0, st, pool.P,
+                       width, per_row, table + (int64_t)row0 * width, keep ? keep + row0 : nullptr,
+                       refs);
+  });
   return hipGetLastError();
 }
 
@@ -568,15 +715,18 @@ hipError_t cg_launch_kv8_reserve(const KvPool& pool, int D, int n, int width, in
   uint64_t total;
   const Reserve R = reserve_of(ws, pool.P, n, width, &total);
   const int chunks = chunks_of(pool.P), words = words_of(width), pieces = pieces_of(pool.H, D);
-  const bool lists = chunks <= kOwnChunks;
-  hipLaunchKernelGGL(want_kernel, dim3(chunks + (n + 3) / 4), dim3(256), 0, st, pool.P, n, width,
-                     table, lengths, counts, refs, chunks, words, lists, R, missing,
-                     static_cast<uint32_t*>(ws));
-  if (!lists)
+  if (pool.P <= 4 * kPlanPages && n <= kPlanSeqs && (int64_t)n * width <= 1 << 30) {
+    hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, pool.P, n, width, table,
+                       lengths, counts, refs, R, missing);
+  } else {
+    hipLaunchKernelGGL(want_kernel, dim3(chunks + (n + 3) / 4), dim3(256), 0, st, pool.P, n, width,
+                       table, lengths, counts, refs, chunks, words, R, missing,
+                       static_cast<uint32_t*>(ws));
     hipLaunchKernelGGL(list_kernel, dim3(chunks), dim3(256), 0, st, pool.P, refs, R);
+  }
   const int64_t items = (int64_t)n * pieces;
   hipLaunchKernelGGL(hand_out_kernel, dim3(grid_of(items)), dim3(256), 0, st, pool, D, n, width,
-                     table, lengths, counts, refs, words, pieces, items, R);
+                     table, lengths, counts, refs, pieces, items, R);
   return hipGetLastError();
 }
 
@@ -592,12 +742,15 @@ hipError_t cg_launch_kv8_compact(const KvPool& pool, const KvSeqs& S, int D, con
   uint64_t total;
   const Compact C = compact_of(ws, pool.P, &total);
   const int chunks = chunks_of(pool.P), pieces = pieces_of(pool.H, D);
-  const bool places = chunks <= kOwnChunks;
-  hipLaunchKernelGGL(used_kernel, dim3(chunks), dim3(256), 0, st, pool.P, refs, chunks, places, C,
-                     moved, new_refs, n_live, static_cast<uint32_t*>(ws));
-  if (!places)
+  if (pool.P <= kPlanPages) {
+    hipLaunchKernelGGL(places_kernel, dim3(1), dim3(kPlanThreads), 0, st, pool.P, refs, C, moved,
+                       new_refs, n_live);
+  } else {
+    hipLaunchKernelGGL(used_kernel, dim3(chunks), dim3(256), 0, st, pool.P, refs, chunks, C, n_live,
+                       static_cast<uint32_t*>(ws));
     hipLaunchKernelGGL(place_kernel, dim3(chunks), dim3(256), 0, st, pool.P, refs, C, moved,
                        new_refs);
+  }
   // as many copying workgroups as the card holds at once, or as there can be pieces to move
   const int64_t most = (int64_t)(pool.P / 2 + 1) * pieces, entries = (int64_t)S.n * S.width;
   const int movers = (int)(most < 2048 ? most : 2048);

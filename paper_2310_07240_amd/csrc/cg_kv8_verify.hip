@@ -4,10 +4,11 @@
 // the first one that is not: from max(p - q, 0), or from p behind the last. Probabilities count in
 // whole multiples of 2^-42, so a row's weights sum up exactly, in any order, and the drawn token is
 // that of the definition, whichever workgroups shared the row. A multiple comes from one addition:
-// p + 1536 in 64 bits is rounded to 2^-42, and lies in the low bits of the sum.
+// p + 1536 in 64 bits is rounded to 2^-42, and lies in the low bits of the sum; the differences of two
+// such sums, and a wave's 1024 of them added up, fit a 64-bit float as they are.
 //
-// Workgroup = (sequence, slice of 4096 probabilities of its row): each finds the row by itself (a
-// wave's lanes take a draft each), sums its slice, and the last of a sequence to arrive finds the
+// Workgroup = (sequence, slices of 4096 probabilities of its row): each finds the row by itself (a
+// wave's lanes take a draft each), sums its slices, and the last of a sequence to arrive finds the
 // slice of the drawn token, reads it again, and the token in it. Bound by the row's bytes of p and q
 // where there are many sequences; a single one is a chain of dependent reads: count and drafts,
 // their probabilities, the row, the other slices' sums, the slice.
@@ -38,25 +39,25 @@ struct Prob<kF32> {
 };
 
 // What a probability counts as: a NaN and what is below 0 as 0, what is above 1 as 1.
-__device__ __forceinline__ float counted(float x) {
-  x = x > 0.0f ? x : 0.0f;
-  return x < 1.0f ? x : 1.0f;
-}
+__device__ __forceinline__ float counted(float x) { return fminf(fmaxf(x, 0.0f), 1.0f); }
 
-// Multiples of 2^-42, to the nearest (halves to even).
+// A probability as 1536 + its multiple of 2^-42, to the nearest (halves to even).
+__device__ __forceinline__ double lifted(float x) { return (double)counted(x) + 1536.0; }
+
+// Its number of them.
 __device__ __forceinline__ int64_t units(float x) {
-  return __builtin_bit_cast(int64_t, (double)counted(x) + 1536.0) -
-         __builtin_bit_cast(int64_t, 1536.0);
+  return __builtin_bit_cast(int64_t, lifted(x)) - __builtin_bit_cast(int64_t, 1536.0);
 }
 
 __device__ __forceinline__ uint64_t lane_value(uint64_t x, int lane) {
   const uint32_t lo = __shfl((uint32_t)x, lane), hi = __shfl((uint32_t)(x >> 32), lane);
   return (uint64_t)hi << 32 | lo;
 }
-__device__ __forceinline__ uint64_t wave_sum(uint64_t x) {
+// The whole number of multiples of 2^-42 in the wave's sum of x, which is exact.
+__device__ __forceinline__ uint64_t wave_units(double x) {
 #pragma unroll
-  for (int o = 32; o; o >>= 1) x += (uint64_t)__shfl_xor((unsigned long long)x, o);
-  return x;
+  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
+  return (uint64_t)(x * 0x1p42);
 }
 __device__ __forceinline__ uint64_t wave_scan(uint64_t x) {       // inclusive
 #pragma unroll
@@ -68,7 +69,7 @@ __device__ __forceinline__ uint64_t wave_scan(uint64_t x) {       // inclusive
 }
 
 struct VerifyLds {
-  uint64_t part[2][16];              // per (chunk, wave) or wave: sums of the residual and of p
+  uint64_t part[2][16];              // sums of each wave, or of each (chunk, wave)
   uint32_t order;
   int32_t token;
 };
@@ -78,10 +79,11 @@ template <Kind K>
 __device__ __forceinline__ int accepted_of(const CgVerify& A, int b, int count) {
   typedef typename Prob<K>::Raw Raw;
   const int lane = threadIdx.x & 63;
-  for (int j0 = 0; j0 < count; j0 += 64) {
+  for (int j0 = 0; j0 < A.n_drafts; j0 += 64) {
+    // (all drafts that there is room for, whatever `count` says: it may not have arrived yet)
     const int j = j0 + lane;
     bool good = true;
-    if (j < count) {
+    if (j < A.n_drafts) {
       const int x = A.drafts[(int64_t)b * A.n_drafts + j];
       const float u = A.u[(int64_t)b * (A.n_drafts + 1) + j];
       good = x >= 0 && x < A.vocab;
@@ -96,12 +98,17 @@ __device__ __forceinline__ int accepted_of(const CgVerify& A, int b, int count) 
       }
     }
     const uint64_t bad = __ballot(!good);
-    if (bad) return j0 + __builtin_ctzll(bad);
+    if (bad) {
+      const int first = j0 + __builtin_ctzll(bad);
+      return first < count ? first : count;
+    }
+    if (j0 + 64 >= count) break;
   }
   return count;
 }
 
-// A thread's probabilities of a slice: N = 16 / size in each chunk, chunk c's at c 256 N + N thread.
+// A thread's probabilities of a slice: N = 16 / size in each of C chunks, chunk c's at c 256 N + N
+// thread.
 template <Kind K>
 struct SliceRegs {
   typedef typename Prob<K>::Raw Raw;
@@ -109,53 +116,118 @@ struct SliceRegs {
   Sixteen<Raw> p[C], q[C];
 };
 
+template <class Raw>
+__device__ __forceinline__ void read_some(const Raw* row, int e, int vocab, Sixteen<Raw>& to) {
+  constexpr int N = 16 / sizeof(Raw);
+  if (e + N <= vocab) {
+    to = *reinterpret_cast<const Sixteen<Raw>*>(row + e);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) to.x[i] = e + i < vocab ? row[e + i] : Raw(0);
+  }
+}
+
 template <Kind K>
 __device__ __forceinline__ void read_slice(const typename Prob<K>::Raw* p,
                                            const typename Prob<K>::Raw* q, int at, int vocab,
                                            SliceRegs<K>& r) {
   typedef typename Prob<K>::Raw Raw;
-  constexpr int N = SliceRegs<K>::N;
+  constexpr int N = SliceRegs<K>::N, C = SliceRegs<K>::C;
+  const int e = at + (int)threadIdx.x * N;
+  if (at + kSlice <= vocab) {        // (the whole workgroup's: the loads go out together)
 #pragma unroll
-  for (int c = 0; c < SliceRegs<K>::C; ++c) {
-    const int e = at + (c * 256 + (int)threadIdx.x) * N;
-    if (e + N <= vocab) {
-      r.p[c] = *reinterpret_cast<const Sixteen<Raw>*>(p + e);
-      if (q) r.q[c] = *reinterpret_cast<const Sixteen<Raw>*>(q + e);
-    } else {
+    for (int c = 0; c < C; ++c)
+      r.p[c] = *reinterpret_cast<const Sixteen<Raw>*>(p + e + c * 256 * N);
+    if (q) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        r.p[c].x[i] = e + i < vocab ? p[e + i] : Raw(0);
-        r.q[c].x[i] = q && e + i < vocab ? q[e + i] : Raw(0);
-      }
+      for (int c = 0; c < C; ++c)
+        r.q[c] = *reinterpret_cast<const Sixteen<Raw>*>(q + e + c * 256 * N);
+    }
+  } else {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      read_some(p, e + c * 256 * N, vocab, r.p[c]);
+      if (q) read_some(q, e + c * 256 * N, vocab, r.q[c]);
     }
   }
 }
 
-// Weights of chunk c: of p, or (residual) of p over q, or without the token `skip`.
+// This thread's weights of a chunk, or of the slice, together: of p over q, or of p.
 template <Kind K>
-__device__ __forceinline__ uint64_t weight(const SliceRegs<K>& r, int c, int i, bool with_q,
-                                           int at, int skip) {
-  const int64_t p = units(Prob<K>::value(r.p[c].x[i]));
-  if (with_q) {
-    const int64_t d = p - units(Prob<K>::value(r.q[c].x[i]));
-    return d > 0 ? d : 0;
+__device__ __forceinline__ double sum_chunk(const SliceRegs<K>& r, int c, bool with_q) {
+  double sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < SliceRegs<K>::N; ++i) {
+    const double p = lifted(Prob<K>::value(r.p[c].x[i]));
+    if (with_q) {
+      const double d = p - lifted(Prob<K>::value(r.q[c].x[i]));
+      sum += d > 0.0 ? d : 0.0;
+    } else {
+      sum += p - 1536.0;
+    }
   }
-  return at + (c * 256 + (int)threadIdx.x) * SliceRegs<K>::N + i == skip ? 0 : p;
+  return sum;
 }
 
 template <Kind K>
-__global__ __launch_bounds__(256) void verify_kernel(CgVerify A, int b0, int slices, uint64_t* parts,
-                                                     uint32_t* arrived) {
+__device__ __forceinline__ double sum_slice(const SliceRegs<K>& r, bool with_q) {
+  double sum = 0.0;
+#pragma unroll
+  for (int c = 0; c < SliceRegs<K>::C; ++c) sum += sum_chunk<K>(r, c, with_q);
+  return sum;
+}
+
+// A thread's weights of one chunk, whose first probability is e: of p over q, or (q null) of p, of
+// which the token `skip` has none.
+template <Kind K>
+struct ChunkWeights {
+  typedef typename Prob<K>::Raw Raw;
+  static constexpr int N = 16 / sizeof(Raw);
+  uint64_t w[N], sum;
+
+  __device__ __forceinline__ ChunkWeights(const Raw* p, const Raw* q, int e, int vocab, int skip) {
+    Sixteen<Raw> x, y;
+    read_some(p, e, vocab, x);
+    if (q) read_some(q, e, vocab, y);
+    sum = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      int64_t d = units(Prob<K>::value(x.x[i]));
+      if (q) d -= units(Prob<K>::value(y.x[i]));
+      w[i] = d > 0 && e + i != skip ? d : 0;
+      sum += w[i];
+    }
+  }
+};
+
+// The workgroup's sum in multiples of 2^-42; every wave adds up to 1024 weights. `turn`: another one
+// than the last call's, whose sums may still be read.
+__device__ __forceinline__ uint64_t wg_units(double x, VerifyLds& L, int turn) {
+  const uint64_t s = wave_units(x);
+  if ((threadIdx.x & 63) == 0) L.part[turn & 1][threadIdx.x >> 6] = s;
+  __syncthreads();
+  const uint64_t* const p = L.part[turn & 1];
+  return p[0] + p[1] + p[2] + p[3];
+}
+
+__device__ __forceinline__ void put_part(uint64_t* p, uint64_t x) {
+  __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+template <Kind K>
+__global__ __launch_bounds__(256) void verify_kernel(CgVerify A, int b0, int slices, int per,
+                                                     uint64_t* parts, uint32_t* arrived) {
   typedef typename Prob<K>::Raw Raw;
   constexpr int N = SliceRegs<K>::N, C = SliceRegs<K>::C;
   __shared__ VerifyLds L;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int row = blockIdx.x / slices, slice = blockIdx.x % slices, b = b0 + row;
+  const int groups = (slices + per - 1) / per;          // workgroups of a sequence
+  const int row = blockIdx.x / groups, group = blockIdx.x % groups, b = b0 + row;
   int count = A.counts ? A.counts[b] : A.n_drafts;
   if (count > A.n_drafts) count = A.n_drafts;
   int32_t* const tokens = A.tokens + (int64_t)b * (A.n_drafts + 1);
   if (count < 0) {                   // the sequence sits out
-    if (slice != 0) return;
+    if (group != 0) return;
     for (int j = threadIdx.x; j <= A.n_drafts; j += 256) tokens[j] = -1;
     if (threadIdx.x == 0) {
       A.accepted[b] = 0;
@@ -172,116 +244,110 @@ __global__ __launch_bounds__(256) void verify_kernel(CgVerify A, int b0, int sli
     else skip = A.drafts[(int64_t)b * A.n_drafts + took];
   }
 
-  // the slice's weights, and those of p alone
+  // the weights of the slices
   SliceRegs<K> r;
-  read_slice<K>(p, q, slice * kSlice, A.vocab, r);
-  uint64_t over = 0, plain = 0;
-#pragma unroll
-  for (int c = 0; c < C; ++c)
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      over += weight<K>(r, c, i, q != nullptr, slice * kSlice, skip);
-      plain += units(Prob<K>::value(r.p[c].x[i]));
-    }
-  over = wave_sum(over);
-  plain = wave_sum(plain);
-  if (lane == 0) {
-    L.part[0][wave] = over;
-    L.part[1][wave] = plain;
+  uint64_t* const parts_of = parts + (int64_t)row * slices;
+  for (int i = group * per; i < (group + 1) * per && i < slices; ++i) {
+    const int at = i * kSlice;
+    read_slice<K>(p, q, at, A.vocab, r);
+    double sum = q ? sum_slice<K>(r, true) : sum_slice<K>(r, false);
+    if (threadIdx.x == 0 && skip >= at && skip < at + kSlice && skip < A.vocab)
+      sum -= lifted(Prob<K>::value(p[skip])) - 1536.0;   // (the wave's sum has it)
+    const uint64_t part = wg_units(sum, L, i);
+    if (threadIdx.x == 0) put_part(parts_of + i, part);
   }
-  __syncthreads();
   if (threadIdx.x == 0) {
-    uint64_t* const mine = parts + 2 * ((int64_t)row * slices + slice);
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
-      __hip_atomic_store(mine + k, L.part[k][0] + L.part[k][1] + L.part[k][2] + L.part[k][3],
-                         __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // they have arrived
     L.order = __hip_atomic_fetch_add(&arrived[row], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (L.order == (uint32_t)slices - 1)
+    if (L.order == (uint32_t)groups - 1)
       __hip_atomic_store(&arrived[row], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     L.token = -1;
   }
   __syncthreads();
-  if (L.order != (uint32_t)slices - 1) return;
+  if (L.order != (uint32_t)groups - 1) return;
 
   // the last one: every wave finds the drawn token's slice, four slices a lane
-  uint64_t s[2][kMostSlices / 64], sum[2] = {0, 0};
-#pragma unroll
-  for (int k = 0; k < 2; ++k)
+  uint64_t s[kMostSlices / 64], before, all;
+  const auto sum_up = [&] {
+    uint64_t x = 0;
 #pragma unroll
     for (int i = 0; i < kMostSlices / 64; ++i) {
       const int at = lane * (kMostSlices / 64) + i;
-      s[k][i] = at < slices ? __hip_atomic_load(parts + 2 * ((int64_t)row * slices + at) + k,
-                                                __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)
-                            : 0;
-      sum[k] += s[k][i];
+      s[i] = at < slices ? __hip_atomic_load(parts_of + at, __ATOMIC_RELAXED,
+                                             __HIP_MEMORY_SCOPE_AGENT)
+                         : 0;
+      x += s[i];
     }
-  uint64_t before[2], total[2];
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    before[k] = wave_scan(sum[k]);
-    total[k] = lane_value(before[k], 63);
-    before[k] -= sum[k];
+    before = wave_scan(x);
+    all = lane_value(before, 63);
+    before -= x;
+  };
+  sum_up();
+  if (all == 0 && (q || skip >= 0)) {
+    // nothing of p is over q (or only the sure draft has weight): the token is drawn from p itself,
+    // whose slices are summed here, which is rare
+    q = nullptr;
+    skip = -1;
+    for (int i = 0; i < slices; ++i) {
+      read_slice<K>(p, nullptr, i * kSlice, A.vocab, r);
+      const uint64_t part = wg_units(sum_slice<K>(r, false), L, i);
+      if (threadIdx.x == 0) put_part(parts_of + i, part);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    sum_up();
   }
-  // nothing of p is over q (or nothing but the draft has weight): from p itself
-  const int k = total[0] > 0 ? 0 : 1;
-  const uint64_t all = k == 0 ? total[0] : total[1];
   if (all > 0) {
     const float u = A.u[(int64_t)b * (A.n_drafts + 1) + A.n_drafts];
-    uint32_t part = 0;                                  // floor(u 2^24), below 2^24
-    if (u > 0.0f) part = u < 1.0f ? (uint32_t)(u * 16777216.0f) : 16777215u;
-    uint64_t bar = part * (all >> 24) + (part * (all & 0xffffff) >> 24);
+    uint32_t share = 0;                                 // floor(u 2^24), below 2^24
+    if (u > 0.0f) share = u < 1.0f ? (uint32_t)(u * 16777216.0f) : 16777215u;
+    const uint64_t bar = share * (all >> 24) + (share * (all & 0xffffff) >> 24);
     // the slice that holds the bar: before <= bar < before + its sum
-    uint64_t run = k == 0 ? before[0] : before[1];
+    uint64_t run = before, left = 0;
     int found = -1;
-    uint64_t left = 0;
 #pragma unroll
     for (int i = 0; i < kMostSlices / 64; ++i) {
-      const uint64_t x = k == 0 ? s[0][i] : s[1][i];
-      if (bar >= run && bar < run + x) {
+      if (bar >= run && bar < run + s[i]) {
         found = lane * (kMostSlices / 64) + i;
         left = bar - run;
       }
-      run += x;
+      run += s[i];
     }
     const int who = __builtin_ctzll(__ballot(found >= 0));
     const int at = __shfl(found, who) * kSlice;
     left = lane_value(left, who);
-    const bool with_q = k == 0 && q != nullptr;
-    const int without = k == 0 ? skip : -1;
-    read_slice<K>(p, with_q ? q : nullptr, at, A.vocab, r);
     // sums of the chunks' waves, in the order of the tokens
-    uint64_t mine[C];
+    read_slice<K>(p, q, at, A.vocab, r);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      mine[c] = 0;
-#pragma unroll
-      for (int i = 0; i < N; ++i) mine[c] += weight<K>(r, c, i, with_q, at, without);
-      mine[c] = wave_scan(mine[c]);
-      if (lane == 63) L.part[0][c * 4 + wave] = mine[c];
+      const int e = at + (c * 256 + (int)threadIdx.x) * N;
+      double sum = q ? sum_chunk<K>(r, c, true) : sum_chunk<K>(r, c, false);
+      if (skip >= e && skip < e + N && skip < A.vocab)
+        sum -= lifted(Prob<K>::value(p[skip])) - 1536.0;
+      const uint64_t total = wave_units(sum);
+      if (lane == 0) L.part[0][c * 4 + wave] = total;
     }
     __syncthreads();
     uint64_t base = 0;
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const uint64_t x = L.part[0][c * 4 + w];
-        if (w == wave && left >= base && left < base + x) {
-          // this wave's chunk c: the lane, then the token
-          uint64_t from = base + lane_value(mine[c], lane > 0 ? lane - 1 : 0);
-          if (lane == 0) from = base;
+#pragma unroll 1
+    for (int c = 0; c < 4 * C; ++c) {
+      const uint64_t total = L.part[0][c];
+      if (left < base + total) {
+        // (chunk, wave) c has it: the lane, then the token
+        if (wave == (c & 3)) {
+          const int e = at + ((c >> 2) * 256 + (int)threadIdx.x) * N;
+          const ChunkWeights<K> x(p, q, e, A.vocab, skip);
+          uint64_t from = base + wave_scan(x.sum) - x.sum;
 #pragma unroll
           for (int i = 0; i < N; ++i) {
-            const uint64_t y = weight<K>(r, c, i, with_q, at, without);
-            if (left >= from && left < from + y)
-              L.token = at + (c * 256 + (int)threadIdx.x) * N + i;
-            from += y;
+            if (left >= from && left < from + x.w[i]) L.token = e + i;
+            from += x.w[i];
           }
         }
-        base += x;
+        break;
       }
+      base += total;
+    }
     __syncthreads();
   }
   const int token = L.token;
@@ -296,6 +362,8 @@ __global__ __launch_bounds__(256) void verify_kernel(CgVerify A, int b0, int sli
   }
 }
 
+constexpr int kAtOnce = 5 * 256;
+
 int slices_of(int vocab) { return (vocab + kSlice - 1) / kSlice; }
 
 template <Kind K>
@@ -305,8 +373,11 @@ void launch(const CgVerify& A, void* ws, hipStream_t st) {
   // (a counter a sequence: as many sequences a launch as there are counters)
   for (int b0 = 0; b0 < A.n; b0 += kKv8Counters) {
     const int n = A.n - b0 < kKv8Counters ? A.n - b0 : kKv8Counters;
-    hipLaunchKernelGGL((verify_kernel<K>), dim3((unsigned)(n * slices)), dim3(256), 0, st, A, b0,
-                       slices, parts, static_cast<uint32_t*>(ws));
+    // as many workgroups as the card holds at once, of several slices where there are more
+    const int per = (n * slices + kAtOnce - 1) / kAtOnce;
+    const int groups = (slices + per - 1) / per;
+    hipLaunchKernelGGL((verify_kernel<K>), dim3((unsigned)(n * groups)), dim3(256), 0, st, A, b0,
+                       slices, per, parts, static_cast<uint32_t*>(ws));
   }
 }
 
@@ -314,7 +385,7 @@ void launch(const CgVerify& A, void* ws, hipStream_t st) {
 
 uint64_t cg_verify_ws(int n, int vocab) {
   const int rows = n < kKv8Counters ? n : kKv8Counters;
-  return kKv8Front + (uint64_t)rows * slices_of(vocab) * 16;
+  return kKv8Front + (uint64_t)rows * slices_of(vocab) * 8;
 }
 
 hipError_t cg_launch_verify(const CgVerify& A, int dtype, void* ws, hipStream_t st) {

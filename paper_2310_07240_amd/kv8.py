@@ -163,6 +163,8 @@ class Kv8Cache:
         self._on_gpu = self.device.type == "cuda"
         self._current = torch._C._cuda_getDevice if self._on_gpu else lambda: self._index
         self._ws, self._lock = {}, threading.Lock()
+        self._ints = torch.empty(0, dtype=torch.int32, device=self.device)
+        self._reserve_bytes = {}           # (n_seq, columns) -> bytes
         self._status = _I32()
         self._status_p = ctypes.addressof(self._status)
         self._types = {torch.float16: 0, torch.bfloat16: 1}
@@ -238,6 +240,13 @@ class Kv8Cache:
 
     def _empty(self, shape, dtype, stream):
         return self._new(self.torch.empty, shape, dtype, stream)
+
+    def _int_out(self, t, name, shape, stream):
+        """(tensor, address) of an int32 output: the caller's, or a new one."""
+        if t is not None:
+            return t, self._tensor(t, name, self._i32, shape)
+        t = self._ints.new_empty(shape) if stream is None else self._empty(shape, self._i32, stream)
+        return t, t.data_ptr()
 
     def _scratch(self, stream, handle, need):
         """The stream's own scratch (address, bytes, tensor), its counters cleared once. Every call
@@ -428,13 +437,13 @@ class Kv8Cache:
         _need(parents.dim() == 1, "parents: [children] is wanted")
         m = parents.shape[0]
         if new_table is None:
-            new_table = self._empty((m, width), self._i32, stream)
+            new_table = self._int_out(None, "new_table", (m, width), stream)[0]
         to, rows, _ = self._seqs(new_table)
         _need(rows == m, f"new_table: {m} rows are wanted")
-        new_lengths = self._empty((m,), self._i32, stream)
+        new_lengths, new_p = self._int_out(None, "new_lengths", (m,), stream)
         self._launch("cg_kv8_fork", _lib().cg_kv8_fork, stream, s,
                      self._per_seq(lengths, "lengths", n), self._per_seq(parents, "parents", m),
-                     self._per_seq(ends, "ends", m), to, new_lengths.data_ptr(), self._refs(refs))
+                     self._per_seq(ends, "ends", m), to, new_p, self._refs(refs))
         return new_table, new_lengths
 
     def reserve(self, table, lengths, counts, refs, mass=None, missing=None, stream=None):
@@ -444,15 +453,17 @@ class Kv8Cache:
         are updated. Returns ``missing`` (int32 [1]): 0, or how many free pages too few there are;
         then nothing has changed, and the sequences must not be written to. ``mass``: weights that
         go with a copied page."""
-        s, n, _ = self._seqs(table)
+        s, n, width = self._seqs(table)
         _need(lengths is not None and counts is not None, "lengths and counts are wanted")
-        if missing is None:
-            missing = self._empty((1,), self._i32, stream)
+        missing, missing_p = self._int_out(missing, "missing", (1,), stream)
         L, cache = _lib(), self._with(mass)
+        need = self._reserve_bytes.get((n, width))
+        if need is None:
+            need = L.cg_kv8_reserve_workspace_bytes(self._cp, s)
+            self._reserve_bytes[n, width] = need
         self._launch("cg_kv8_reserve", L.cg_kv8_reserve, stream, s,
                      self._per_seq(lengths, "lengths", n), self._per_seq(counts, "counts", n),
-                     self._refs(refs), self._tensor(missing, "missing", self._i32, (1,)),
-                     need=L.cg_kv8_reserve_workspace_bytes(self._cp, s), cache=cache)
+                     self._refs(refs), missing_p, need=need, cache=cache)
         return missing
 
     def release(self, table, refs, keep=None, stream=None):
@@ -478,14 +489,13 @@ class Kv8Cache:
         [n_pages], -1 of a free one) for other tables, and how many are in use (int32 [1]).
         ``table`` and ``refs`` are left as they were."""
         s, n, width = self._seqs(table)
-        new_table = self._empty((n, width), self._i32, stream)
-        new_refs = self._empty((self.n_pages,), self._i32, stream)
-        moved = self._empty((self.n_pages,), self._i32, stream)
-        live = self._empty((1,), self._i32, stream)
+        new_table, table_p = self._int_out(None, "new_table", (n, width), stream)
+        new_refs, refs_p = self._int_out(None, "new_refs", (self.n_pages,), stream)
+        moved, moved_p = self._int_out(None, "moved", (self.n_pages,), stream)
+        live, live_p = self._int_out(None, "live", (1,), stream)
         L, cache = _lib(), self._with(mass)
-        self._launch("cg_kv8_compact", L.cg_kv8_compact, stream, s, self._refs(refs),
-                     new_table.data_ptr(), new_refs.data_ptr(), moved.data_ptr(), live.data_ptr(),
-                     need=L.cg_kv8_compact_workspace_bytes(self._cp), cache=cache)
+        self._launch("cg_kv8_compact", L.cg_kv8_compact, stream, s, self._refs(refs), table_p, refs_p,
+                     moved_p, live_p, need=L.cg_kv8_compact_workspace_bytes(self._cp), cache=cache)
         return new_table, new_refs, moved, live
 
     def attend_shared(self, q, shared, shared_lengths, firsts, table=None, lengths=None, scale=None,
@@ -570,17 +580,13 @@ class Kv8Cache:
         rows = self._probabilities(target, "target", target.shape, target.dtype)
         near = (0, 0, 0) if draft is None or k == 0 else self._probabilities(
             draft, "draft", (n, k, vocab), target.dtype)
-
-        def out(t, name, shape):
-            t = self._empty(shape, self._i32, stream) if t is None else t
-            return t, self._tensor(t, name, self._i32, shape)
-        tokens, tokens_p = out(tokens, "tokens", (n, k + 1))
-        accepted, accepted_p = out(accepted, "accepted", (n,))
+        tokens, tokens_p = self._int_out(tokens, "tokens", (n, k + 1), stream)
+        accepted, accepted_p = self._int_out(accepted, "accepted", (n,), stream)
         lengths_p = new_p = 0
         _need(lengths is not None or new_lengths is None, "lengths is missing")
         if lengths is not None:
             lengths_p = self._per_seq(lengths, "lengths", n)
-            new_lengths, new_p = out(new_lengths, "new_lengths", (n,))
+            new_lengths, new_p = self._int_out(new_lengths, "new_lengths", (n,), stream)
         v = _VERIFY.pack(n, k, vocab, kind, *rows, *near,
                          self._tensor(drafts, "drafts", self._i32, (n, k)),
                          self._per_seq(counts, "counts", n),

@@ -115,6 +115,11 @@ RESERVE = [
     (4096, 1, 64, [8000, 1], 2, 130, [130, 8000, 300, 1], True, True),
     (9000, 1, 64, [70, 700], 5, 120, [5000] * 10, False, True),
     (13000, 1, 64, [12000, 77], 4, 200, [1, 1, 2000, 5, 1, 1, 1, 1], True, True),
+    # more sequences than one workgroup plans for, and more pages
+    (6000, 1, 64, [70], 2100, 3, [1, 60] * 1050, False, True),
+    (6000, 1, 64, [70, 5], 1000, 5, [1, 60] * 1000, False, True),
+    (65536, 1, 64, [3000, 64], 5, 60, [700] * 10, False, False),
+    (65537, 1, 64, [3000, 64], 5, 60, [700] * 10, True, False),
 ]
 
 
@@ -146,7 +151,7 @@ def test_reserve_more_than_there_is():
     """Nothing changes where pages are missing, also where only one is; then the last one goes."""
     torch = torch_cuda()
     rng = np.random.default_rng(3)
-    for P, need in ((40, 40), (40, 41), (40, 400), (8193, 8193), (8193, 8300), (8300, 8299)):
+    for P, need in ((40, 40), (40, 41), (40, 400), (16385, 16385), (16385, 16500), (16500, 16499)):
         pool = Pool(torch, rng, P, 1, 64)
         width = need + 1
         table, refs = [[-1] * width, [-1] * width], [0] * P
@@ -203,7 +208,7 @@ def test_copy(P, H, D, mass, bounds):
 
 
 @pytest.mark.parametrize("P,H,D", [(1, 1, 64), (63, 2, 128), (4096, 1, 64), (4097, 1, 64),
-                                   (8192, 1, 64), (8193, 1, 64), (21000, 1, 64)])
+                                   (16384, 1, 64), (16385, 1, 64), (21000, 1, 64)])
 @pytest.mark.parametrize("live", [0.0, 0.1, 0.5, 0.97, 1.0])
 def test_compact(P, H, D, live):
     torch = torch_cuda()

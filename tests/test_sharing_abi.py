@@ -164,9 +164,9 @@ def test_bad_drafts(kw, code):
 def test_workspace_of_the_drafts():
     l = L()
     need = l.cg_verify_workspace_bytes(verify())
-    assert need == kv8.ZEROED + 2 * 16
+    assert need == kv8.ZEROED + 2 * 8
     assert l.cg_verify_workspace_bytes(verify(n_seq=1 << 21, vocab=1 << 20)) == (
-        kv8.ZEROED + 1024 * 256 * 16)
+        kv8.ZEROED + 1024 * 256 * 8)
     assert l.cg_verify_drafts(verify(), None, BIG, None) == -1
     assert l.cg_verify_drafts(verify(), FAKE, need - 1, None) == kv8_code("CAPACITY")
     assert l.cg_verify_drafts(verify(), ctypes.c_void_p(A + 16), BIG, None) == -1

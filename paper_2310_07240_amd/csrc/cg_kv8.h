@@ -374,10 +374,12 @@ struct KvAttnPlan {
   int32_t tiles, splits;        // 16-row tiles and splits of the pages for each (sequence, KV head)
   int32_t big;                  // prompt_kernel's row tiles; 0: attend_kernel
   bool keep_scores, many;       // for the weights (see cg_kv8_plan)
+  bool halves;                  // of a shared context: half of prompt_kernel's waves have rows
   uint64_t part_off, lse_off, score_off, total;   // workspace, in bytes
 };
 
-KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& seqs, const KvAttn& a, int D);
+KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& seqs, const KvAttn& a, int D,
+                       bool shared = false);
 
 // Which requests read a context: context p those from firsts[p] on, `most` at most, of `n_seq` with
 // `per` query tokens each.
@@ -390,6 +392,7 @@ struct KvUsers {
 // and where their partial states lie.
 struct KvSharedPlan {
   KvAttnPlan shared, own;
+  bool joins;                   // the own tokens' launch joins the contexts' states itself
   uint64_t shared_off, own_off, total;
 };
 

@@ -16,6 +16,8 @@
 // supplies for the second product, and the V operand 16 consecutive bytes of a channel.
 #include <math.h>
 
+#include <type_traits>
+
 #include "cg_kv8.h"
 
 namespace {
@@ -458,6 +460,99 @@ __device__ __forceinline__ void finish_row(const KvAttn& A, const Rows& R, int H
   if (d0 == 0) put_lse(A, R, H, h, row, lse, (top + __builtin_amdgcn_logf(l)) * kLn2);
 }
 
+// Up to 16 rows of one head from n partial states each, in the order of the states, and for each row
+// one state more (top, l: 16 threads a row, the first of them has it). state(i, x, in): where state i
+// of row x lies, and which row of it that is; scaled(f): this thread's row takes the additional state
+// times f; done(x, d, o): the other states' sum of four channels of row x. 256 threads: 16 a row find
+// the factors, then a thread takes four channels of a row, and where there are threads left they share
+// the states, whose sums meet in LDS. top and l leave as those of the row.
+template <int D, class State, class Scaled, class Done>
+__device__ __forceinline__ void join_rows(int rows, int n, float* w, float4v* sums, float& top,
+                                          float& l, State state, Scaled scaled, Done done) {
+  constexpr int kAhead = 8;
+  const int tid = threadIdx.x, row = tid >> 4, sub = tid & 15;
+  const float top0 = top;
+  if (row < rows) {
+    for (int i = sub; i < n; i += 16) {
+      int in;
+      const float* const s = state(i, row, in);
+      const float2v ml = *reinterpret_cast<const float2v*>(s + 16 * D + 2 * in);
+      w[i * 16 + row] = ml[0];
+      const float both = fmaxf(top, ml[0]), ref = both == kNegInf ? 0.0f : both;
+      l = l * __builtin_amdgcn_exp2f(top - ref) + ml[1] * __builtin_amdgcn_exp2f(ml[0] - ref);
+      top = both;
+    }
+  }
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) {
+    const float m = __shfl_xor(top, o), x = __shfl_xor(l, o);
+    const float both = fmaxf(top, m), ref = both == kNegInf ? 0.0f : both;
+    l = l * __builtin_amdgcn_exp2f(top - ref) + x * __builtin_amdgcn_exp2f(m - ref);
+    top = both;
+  }
+  const float first = __shfl(top0, (int)(threadIdx.x & 48));
+  if (row < rows) {
+    const float ref = top == kNegInf ? 0.0f : top, inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+    for (int i = sub; i < n; i += 16)
+      w[i * 16 + row] = __builtin_amdgcn_exp2f(w[i * 16 + row] - ref) * inv;
+    scaled(__builtin_amdgcn_exp2f(first - ref) * inv);
+  }
+  __syncthreads();
+  const int units = rows * (D / 4);                    // four channels of a row
+  const int shares = units < 256 ? 256 / units : 1;
+  for (int e = tid; e < units * shares; e += 256) {
+    const int share = e / units, u = e - share * units, x = u / (D / 4), d = u % (D / 4) * 4;
+    float4v o = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i0 = share; i0 < n; i0 += kAhead * shares) {
+      float4v v[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int i = i0 + k * shares;
+        int in;
+        const float* const s = state(i < n ? i : n - 1, x, in);
+        v[k] = *reinterpret_cast<const float4v*>(s + in * D + d);
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int i = i0 + k * shares;
+        const float f = i < n ? w[i * 16 + x] : 0.0f;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[c] = __builtin_fmaf(v[k][c], f, o[c]);
+      }
+    }
+    if (shares == 1) done(x, d, o);
+    else sums[e] = o;
+  }
+  if (shares > 1) {
+    __syncthreads();
+    if (tid < units) {
+      float4v o = sums[tid];
+      for (int s = 1; s < shares; ++s) o += sums[s * units + tid];
+      done(tid / (D / 4), tid % (D / 4) * 4, o);
+    }
+  }
+}
+
+// Which context request `b` reads and its place among that one's, or -1.
+__device__ __forceinline__ int context_of(const KvUsers& U, int contexts, int b, int& place) {
+  int lo = 0, hi = contexts;                           // firsts[lo - 1] <= b < firsts[hi]
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (U.firsts[mid] <= b) lo = mid + 1;
+    else hi = mid;
+  }
+  if (lo == 0) return -1;
+  const Requests q = requests_of(U, lo - 1);
+  place = b - q.first;
+  return place >= 0 && place < q.count ? lo - 1 : -1;
+}
+
+// The states of contexts that a launch before has left, for the requests' own tokens to join.
+struct ContextStates {
+  int contexts, tiles, splits;
+  const float* part;
+};
+
 // Requests that have no context see nothing: those before the first context's, between the bound of
 // a context's requests and the next one's, and behind the last. Context p's workgroup fills in the
 // ones behind p's own.
@@ -492,14 +587,18 @@ __device__ __forceinline__ void fill_without(const KvAttn& A, const KvUsers& U, 
 // Bound by the codes' bytes where there are many: 4 sequences of 8K on 32 heads, 269 MB in 51 us, 5.3
 // TB/s (a copy of 1 GiB: 5.1); one sequence of 4K on 8 heads, 8 MB, 11 us, is a chain of dependent
 // reads (length, table, codes) and the join, 6 us with a single page.
-// With SharedRows the sequences are contexts that requests share; with PARTS every split's state
-// stays in memory, for a join with those of another launch.
-template <int D, bool BF16, class Rows, bool PARTS>
+// With SharedRows the sequences are contexts that requests share. Its result is `out`, or (kParts)
+// every split's state stays in memory for a launch behind it to join, or (kJoin) the only split joins
+// what the launch before has left of the sequence's context: 32 requests of 300 tokens behind one of
+// 16K 11 us for 17 with a launch for the own tokens and one for the join.
+enum Result { kOut, kParts, kJoin };
+
+template <int D, bool BF16, class Rows, Result TO>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_kernel(KvPool pool, KvSeqs S, KvAttn A,
                                                         KvUsers U, int tiles, int splits,
                                                         int64_t items, float* part,
                                                         uint32_t* arrived, float* lse,
-                                                        float* scores, int np) {
+                                                        float* scores, int np, ContextStates C) {
   __shared__ float os[4][16][D + 4];
   __shared__ float ml[4][32];
   __shared__ uint32_t others;
@@ -511,7 +610,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_kernel(KvPool po
     const int h = (int)(unit / tiles % pool.H);
     const int vseq = (int)(unit / tiles / pool.H);
     const Rows R = rows_in<Rows>(S, A, U, vseq);
-    if constexpr (__is_same(Rows, SharedRows) && !PARTS)
+    int place = 0, context = -1;
+    if constexpr (TO == kJoin) context = context_of(U, C.contexts, R.seq, place);
+    if constexpr (__is_same(Rows, SharedRows) && TO == kOut)
       if (split == 0 && tile == 0 && h == 0) fill_without<256>(A, U, S.n, vseq, pool.H, D, lse);
     // the pages that any row of the tile sees
     const int rows = R.nq * A.group;
@@ -595,7 +696,36 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_kernel(KvPool po
         for (int c = 0; c < N; ++c) o[c] = __builtin_fmaf(os[w][row][d0 + c], f, o[c]);
       }
     }
-    if (PARTS) {
+    if constexpr (TO == kJoin) {
+      // (os has room for the factors, the sums and this row's own share; its readers come first)
+      static_assert(sizeof(os) >= (kMostSplits * 16 + 1024 + 16 * D) * sizeof(float), "room in os");
+      float* const w = &os[0][0][0];
+      float4v* const sums = reinterpret_cast<float4v*>(w + kMostSplits * 16);
+      float* const own = w + kMostSplits * 16 + 1024;
+      const int n0 = context >= 0 ? C.splits : 0, from = place * rows + tile * 16;
+      const float* const s0 = C.part + ((int64_t)(context >= 0 ? context : 0) * pool.H + h) *
+                                           C.tiles * C.splits * kPart<D>;
+      const bool first = d0 == 0 && live;
+      float t0 = first ? top : kNegInf, l0 = first ? l : 0.0f;
+      __syncthreads();
+      join_rows<D>(rows - tile * 16 < 16 ? rows - tile * 16 : 16, n0, w, sums, t0, l0,
+                   [&](int i, int x, int& in) {
+                     in = (from + x) & 15;
+                     return s0 + ((int64_t)((from + x) >> 4) * C.splits + i) * kPart<D>;
+                   },
+                   [&](float f) {
+#pragma unroll
+                     for (int c = 0; c < N; ++c) own[row * D + d0 + c] = o[c] * f;
+                   },
+                   [&](int x, int d, float4v y) {
+#pragma unroll
+                     for (int c = 0; c < 4; ++c) y[c] += own[x * D + d + c];
+                     put_out<D, BF16>(A, R, h, tile * 16 + x, d,
+                                      reinterpret_cast<const float*>(&y), 4);
+                   });
+      if (first) put_lse(A, R, pool.H, h, tile * 16 + row, lse,
+                         (t0 + __builtin_amdgcn_logf(l0)) * kLn2);
+    } else if constexpr (TO == kParts) {
       float* mine = part + it * kPart<D>;
       if (live) {
 #pragma unroll
@@ -633,16 +763,16 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_kernel(KvPool po
 
 // The splits of prompt_kernel joined: a workgroup a 16-row tile. Bound by the states' bytes: 33 MB of
 // 2000 rows of 8 heads in 4 splits, 9 us, 3.7 TB/s.
-template <int D, bool BF16, class Rows>
-__global__ __launch_bounds__(256) void join_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U,
-                                                   int tiles, int splits, int64_t items,
-                                                   const float* part, float* lse) {
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void join_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles,
+                                                   int splits, int64_t items, const float* part,
+                                                   float* lse) {
   __shared__ float w[kMostSplits * 16];
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const int tile = (int)(it % tiles);
     const int64_t r = it / tiles;
     const int h = (int)(r % pool.H);
-    const Rows R = rows_in<Rows>(S, A, U, (int)(r / pool.H));
+    const RowsOf R = rows_of(S, A, (int)(r / pool.H));
     const int rows = R.nq * A.group - tile * 16;
     join_tile<D, BF16, false, 4>(A, R, pool.H, h, tile, rows < 16 ? rows : 16,
                               part + it * splits * kPart<D>, splits, w, lse);
@@ -904,9 +1034,9 @@ constexpr int kPromptWaves = D == 256 ? 4 : 8;
 // of 8K, 64 heads, 2048 queries, 962 GFLOP in 0.92 to 1.07 ms as the clock goes, 0.90 to 1.05
 // PFLOP/s (a library product of 8192 cubed: 1.23); 500 queries of 32 heads over 4K, 33 GFLOP, 51 us.
 // `part`: where the splits' states go; null: there is one, and it is the result.
-template <int D, bool BF16, class Rows>
+template <int D, bool BF16>
 __global__ __launch_bounds__(64 * kPromptWaves<D>, kPromptWaves<D> / 4)
-void prompt_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, int tiles, int splits, int64_t it0,
+void prompt_kernel(KvPool pool, KvSeqs S, KvAttn A, int tiles, int splits, int64_t it0,
                    float* part, float* lse) {
   constexpr int NT = 64 * kPromptWaves<D>;
   __shared__ PromptLds<D> L;
@@ -918,14 +1048,9 @@ void prompt_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, int tiles, int sp
   r /= splits;
   const int tile = uniform(tiles - 1 - (int)(r % tiles));   // the tiles that see most go first
   const int seq = uniform((int)(r / tiles));
-  Rows R = rows_in<Rows>(S, A, U, seq);
+  RowsOf R = rows_of(S, A, seq);
   R.len = uniform(R.len);
   R.q_len = uniform(R.q_len);
-  if constexpr (__is_same(Rows, SharedRows)) {
-    R.first = uniform(R.first);
-    if (!part && split == 0 && tile == 0 && h == 0)
-      fill_without<NT>(A, U, S.n, seq, pool.H, D, lse);
-  }
   const int rows = R.nq * A.group, row = (tile * kPromptWaves<D> + wave) * 32 + m;
 
   half8 q[D / 16];
@@ -1409,103 +1534,444 @@ void mass_rows_kernel(KvPool pool, KvSeqs S, KvAttn A, int np, int shares, int64
   }
 }
 
-// ---- a shared context and the requests' own tokens ------------------------------------------------
-// The partial states of both, in 32 bits, joined: a workgroup a request's 16-row tile. The context's
-// states of the tile lie in rows of its own tiles, from the request's first on. Bound by the states'
-// bytes.
+// ---- a shared context of many rows ----------------------------------------------------------------
+// The rows of all requests of a context against its pages: prompt_kernel's products and weights, but
+// no row sees less than the others, so only the context's last page is masked, and the V scales are
+// taken relative to the largest of the workgroup's pages (what is 2^-60 of it counts as none: its
+// weights are summed apart, and must not move the reference that the others are rounded by).
+//
+// RW of the workgroup's waves have 32 rows each. With half of them the others take the same rows, and
+// of every page the first tile of 32 tokens goes to the first half and the second to the other (32
+// requests of four heads a group, 16K tokens: 27.9 us, 29.5 with rows for all waves); the halves'
+// states meet in LDS. A split's pages are listed in LDS first, a column a thread, with their scales: a
+// chain of lookups would be as long as a page's products. (So a split has at most a column a thread.)
+template <int D>
+struct PageList {
+  static constexpr int kColumns = 64 * kPromptWaves<D>;
+  int page[kColumns], column[kColumns];
+  float ks[kColumns], vs[kColumns];
+  int count[kPromptWaves<D>];
+  float top[kPromptWaves<D>];
+};
+
+template <int D, bool BF16, int RW>
+__global__ __launch_bounds__(64 * kPromptWaves<D>, kPromptWaves<D> / 4)
+void shared_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, int splits, int z0, float* part,
+                   float* lse) {
+  constexpr int W = kPromptWaves<D>, NT = 64 * W, TW = W / RW;
+  constexpr int kAhead = kPagesK<D> - 1;
+  static_assert(TW == 1 || (TW == 2 && kAhead == 2), "a tile of every page for each half");
+  __shared__ PromptLds<D> L;
+  __shared__ PageList<D> list;
+  const int lane = threadIdx.x & 63, m = lane & 31, half = lane >> 5;
+  const int wave = uniform(threadIdx.x >> 6), side = wave / RW;
+  const int split = blockIdx.x / pool.H, h = blockIdx.x - split * pool.H;
+  const int tile = blockIdx.y, p = z0 + blockIdx.z;
+
+  const Requests req = requests_of(U, p);
+  int len = A.lengths[p];
+  len = len < A.max_len ? len : A.max_len;
+  len = uniform(len > 0 ? len : 0);
+  const int first = uniform(req.first), count = uniform(req.count);
+  if (!part && blockIdx.x == 0 && tile == 0) fill_without<NT>(A, U, S.n, p, pool.H, D, lse);
+  const int per_user = U.per * A.group, rows = U.most * per_user, r0 = tile * (32 * RW);
+  const int columns = r0 < count * per_user ? (int)(((int64_t)len + kPage - 1) / kPage) : 0;
+  const int per = (columns + splits - 1) / splits;
+  const int j0 = split * per, j1 = j0 + per < columns ? j0 + per : columns;
+
+  // the split's pages, a column a thread
+  int n = 0;
+  float v_most = 0.0f;
+  {
+    const int j = j0 + (int)threadIdx.x;
+    const int page = j < j1 ? kv_page(S, pool.P, p, j) : -1;
+    const int64_t at = (int64_t)(page >= 0 ? page : 0) * pool.H + h;
+    const float ks = pool.ks[at], vs = pool.vs[at];
+    const uint64_t there = __ballot(page >= 0);
+    float top = page >= 0 && vs < __builtin_inff() ? vs : 0.0f;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+    if (lane == 0) {
+      list.count[wave] = __popcll(there);
+      list.top[wave] = top;
+    }
+    __syncthreads();
+    int before = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const int c = list.count[w];
+      before += w < wave ? c : 0;
+      n += c;
+      v_most = fmaxf(v_most, list.top[w]);
+    }
+    if (page >= 0) {
+      const int i = before + __popcll(there & ((1ull << lane) - 1));
+      list.page[i] = page;
+      list.column[i] = j;
+      list.ks[i] = ks;
+      list.vs[i] = vs;
+    }
+    __syncthreads();
+    n = uniform(n);
+    v_most = __builtin_bit_cast(float, uniform(__builtin_bit_cast(int, v_most)));
+  }
+
+  // this lane's row
+  const int row = r0 + (wave - side * RW) * 32 + m;
+  const int user = row / per_user, of_user = row - user * per_user;
+  const int i_row = of_user / A.group, head = h * A.group + of_user - i_row * A.group;
+  const int64_t b = first + user;
+  bool alive = user < count && len > 0;
+  if (alive && A.q_lens) alive = i_row < A.q_lens[b];
+  half8 q[D / 16];
+  const float unit = load_row32<D, BF16>(
+      A, static_cast<const uint16_t*>(A.q.p) + b * A.q.seq + (int64_t)i_row * A.q.tok +
+             (int64_t)head * A.q.head, alive, q);
+
+  float16v o[D / 32];
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[dt][e] = 0.0f;
+  float ref = -1e30f, l = 0.0f;      // O and l in units of 2^(ref - kLift), O also of v_most
+  float ref0 = -1e30f, l0 = 0.0f;    // l of the pages without V, in units of 2^ref0
+  const float v_unit = v_most > 0.0f ? 1.0f / v_most : 0.0f;
+
+  // One tile of 32 tokens: see prompt_kernel.
+  const auto tile_step = [&](float16v x, const _Float16 (*k)[D + 8], const _Float16 (*next)[D + 8],
+                             const _Float16 (*v)[kPage + 8], int pos0, float ks, float vs,
+                             auto put) -> float16v {
+    const bool cut = pos0 + 32 > len;
+    const int seen_here = len - pos0 - 16 * half;
+    const auto mask = [&](float16v& z, float to) {
+      if (cut) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) z[e] = e < seen_here ? z[e] : to;
+      }
+    };
+    const float f = unit * ks, ratio = vs * v_unit;
+    const bool with_v = !(ratio <= 0x1p-60f);
+    const float lv = with_v ? __builtin_amdgcn_logf(ratio) + (float)kLift : 0.0f;
+    const float c = with_v ? lv - ref : kNegInf;
+    const float16v y = tile_scores<D>(next, q);
+    float sum = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], f, c));
+    mask(x, 0.0f);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sum += x[e];
+    if (__builtin_expect(__any(!(sum <= kMost)) || !with_v, 0)) {
+      float g;
+      if (with_v && !__any(!(sum < __builtin_inff()))) {
+        float t = x[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) t = max2(t, x[e]);
+        const int up = __builtin_amdgcn_frexp_expf(half_max(t)) - kLift;
+        const int by = up > 0 ? up : 0;
+        g = __builtin_ldexpf(1.0f, -by);
+        ref += (float)by;
+        sum *= g;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] *= g;
+      } else {
+        x = tile_scores<D>(k, q);
+        float t = kNegInf;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) t = max2(t, !cut || e < seen_here ? x[e] : kNegInf);
+        t = half_max(t);
+        t = t == kNegInf ? t : t * f;
+        const float was = with_v ? ref : ref0;
+        const float now = fmaxf(was, with_v ? t + lv - (float)kLift : t);
+        g = __builtin_amdgcn_exp2f(was - now);
+        const float by = with_v ? lv - now : -now;
+        sum = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], f, by));
+        mask(x, 0.0f);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sum += x[e];
+        if (with_v) {
+          ref = now;
+        } else {
+          ref0 = now;
+          l0 = __builtin_fmaf(l0, g, sum);
+          g = 1.0f;
+          sum = 0.0f;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[e] = 0.0f;
+        }
+      }
+      l *= g;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[dt][e] *= g;
+    }
+    half8 a[D / 32][2];
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        a[dt][e] = *reinterpret_cast<const half8*>(&v[32 * dt + m][16 * half + 8 * e]);
+    l = sum == 0.0f ? l : __builtin_fmaf(sum, __builtin_amdgcn_rcpf(ratio), l);
+    half8 w[2];
+#pragma unroll
+    for (int e = 0; e < 16; e += 2) {
+      const half2v h2 = __builtin_convertvector((float2v{x[e], x[e + 1]}), half2v);
+      w[e >> 3][e & 7] = h2[0];
+      w[e >> 3][(e & 7) + 1] = h2[1];
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[dt][e], w[e], o[dt], 0, 0, 0);
+    put();
+    return y;
+  };
+
+  // The listed pages in turn; what a page's turn does besides its tiles is prompt_kernel's. A wave
+  // without a live row only helps with the pages.
+  const auto walk = [&](auto busy) {
+    constexpr bool kBusy = decltype(busy)::value;
+    PageRegs<D, NT> kr, vr;
+    float16v x;
+    const auto fetch_k = [&](int i) {
+      if (i < n)
+        page_fetch<D, NT>(pool.k + ((int64_t)uniform(list.page[i]) * pool.H + h) * (kPage * D), kr);
+    };
+    const auto fetch_v = [&](int i) {
+      if (i < n)
+        page_fetch<D, NT>(pool.v + ((int64_t)uniform(list.page[i]) * pool.H + h) * (kPage * D), vr);
+    };
+    const auto step = [&](const _Float16 (*k)[D + 8], const _Float16 (*next)[D + 8],
+                          const _Float16 (*v)[kPage + 8], int pos0, float ks, float vs, auto put) {
+      if constexpr (kBusy) x = tile_step(x, k, next, v, pos0, ks, vs, put);
+      else put();
+    };
+    const auto second = [&](int buf) {
+      return reinterpret_cast<const _Float16 (*)[kPage + 8]>(&L.v[buf][0][32]);
+    };
+    fetch_k(0);
+    fetch_v(0);
+    widen_k<D, NT>(kr, L.k[0]);
+    fetch_k(1);
+    widen_v<D, NT>(vr, L.v[0]);
+    fetch_v(1);
+    if (kAhead == 2) {
+      widen_k<D, NT>(kr, L.k[1]);      // (behind the last page stale codes, which nobody uses)
+      fetch_k(2);
+    }
+    __syncthreads();
+    if constexpr (kBusy) x = tile_scores<D>(L.k[0] + 32 * side, q);
+    int k0 = 0, k1 = 1;                // K buffers of this page and the next
+    for (int i = 0; i < n; ++i) {
+      const int buf = i & 1, k2 = kAhead == 2 ? 3 - k0 - k1 : k0;
+      const int pos0 = uniform(list.column[i]) * kPage;
+      const float ks = list.ks[i], vs = list.vs[i];
+      if constexpr (TW == 2) {
+        step(L.k[k0] + 32 * side, L.k[k1] + 32 * side, side ? second(buf) : L.v[buf],
+             pos0 + 32 * side, ks, vs, [&] {
+               widen_k<D, NT>(kr, L.k[k2]);
+               widen_v<D, NT>(vr, L.v[buf ^ 1]);
+             });
+        fetch_k(i + 3);
+      } else {
+        step(L.k[k0], L.k[k0] + 32, L.v[buf], pos0, ks, vs,
+             [&] { widen_k<D, NT>(kr, L.k[kAhead == 2 ? k2 : k1]); });
+        fetch_k(i + kAhead + 1);
+        if (kAhead == 1) __syncthreads();
+        step(L.k[k0] + 32, L.k[k1], second(buf), pos0 + 32, ks, vs,
+             [&] { widen_v<D, NT>(vr, L.v[buf ^ 1]); });
+      }
+      fetch_v(i + 2);
+      k0 = k1;
+      k1 = k2;
+      __syncthreads();
+    }
+  };
+  if (n > 0) {
+    if (__any(alive)) walk(std::true_type{});
+    else walk(std::false_type{});
+  }
+
+  // Both sums to one reference, and O with them; then the halves' states to one.
+  l = half_sum(l);
+  l0 = half_sum(l0);
+  const float l_ref = ref - (float)kLift;
+  const bool some = l > 0.0f || l != l, some0 = l0 > 0.0f || l0 != l0;
+  bool empty = !alive || !(some || some0);
+  float top = fmaxf(some ? l_ref : -1e30f, some0 ? ref0 : -1e30f);
+  const float to_top = some ? __builtin_amdgcn_exp2f(l_ref - top) : 0.0f;
+  float sum = l * to_top + (some0 ? l0 * __builtin_amdgcn_exp2f(ref0 - top) : 0.0f);
+  top = empty ? kNegInf : top;
+  sum = empty ? 0.0f : sum;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[dt][e] = empty ? 0.0f : o[dt][e] * to_top * v_most;
+  // a wave's own rows in LDS, a quarter of the channels at a time with halves, half of them without
+  float* const space = reinterpret_cast<float*>(&L);
+  if constexpr (TW == 2) {
+    float (*const os)[D + 4] = reinterpret_cast<float (*)[D + 4]>(space) + (wave - side * RW) * 32;
+    float2v* const ml = reinterpret_cast<float2v*>(space + 32 * RW * (D + 4)) +
+                        (wave - side * RW) * 32;
+    static_assert(sizeof(PromptLds<D>) >= 32 * RW * (D + 6) * sizeof(float), "a half's rows");
+    if (side) {
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int a = 0; a < 4; ++a)
+          *reinterpret_cast<float4v*>(&os[m][32 * dt + 8 * a + 4 * half]) =
+              float4v{o[dt][4 * a], o[dt][4 * a + 1], o[dt][4 * a + 2], o[dt][4 * a + 3]};
+      if (half == 0) ml[m] = float2v{top, sum};
+    }
+    __syncthreads();
+    if (side) return;
+    const float2v other = ml[m];
+    const float both = fmaxf(top, other[0]), base = both == kNegInf ? 0.0f : both;
+    const float f0 = __builtin_amdgcn_exp2f(top - base), f1 = __builtin_amdgcn_exp2f(other[0] - base);
+    sum = sum * f0 + other[1] * f1;
+    top = both;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const float4v w = *reinterpret_cast<const float4v*>(&os[m][32 * dt + 8 * a + 4 * half]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[dt][4 * a + e] = o[dt][4 * a + e] * f0 + w[e] * f1;
+      }
+  }
+  if (part) {
+    if (half == 0 && row < rows) {
+      const int64_t u16 = ((int64_t)p * pool.H + h) * ((rows + 15) / 16) + row / 16;
+      *reinterpret_cast<float2v*>(part + (u16 * splits + split) * kPart<D> + 16 * D +
+                                  2 * (row & 15)) = float2v{top, sum};
+    }
+  } else {
+    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[dt][e] *= inv;
+    if (lse && half == 0 && user < count)
+      lse[(b * U.per + i_row) * ((int64_t)pool.H * A.group) + head] =
+          (top + __builtin_amdgcn_logf(sum)) * kLn2;
+  }
+  // the rows leave by way of LDS, half of the channels at a time: a lane has pieces of one row, and
+  // a store should have whole ones
+  constexpr int C = D / 2, LR = C / 4, RC = 64 / LR;     // channels; lanes a row, rows a store
+  float (*const mine)[C + 4] = reinterpret_cast<float (*)[C + 4]>(space) + wave * 32;
+  static_assert(sizeof(PromptLds<D>) >= W * 32 * (C + 4) * sizeof(float), "all waves' rows");
+#pragma unroll
+  for (int part_of = 0; part_of < 2; ++part_of) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int dt = 0; dt < D / 64; ++dt)
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const float16v& from = o[part_of * (D / 64) + dt];
+        *reinterpret_cast<float4v*>(&mine[m][32 * dt + 8 * a + 4 * half]) =
+            float4v{from[4 * a], from[4 * a + 1], from[4 * a + 2], from[4 * a + 3]};
+      }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll 1
+    for (int k = 0; k < 32 / RC; ++k) {
+      const int in = k * RC + lane / LR, d = lane % LR * 4;
+      const float4v w = *reinterpret_cast<const float4v*>(&mine[in][d]);
+      const int to = r0 + (wave - side * RW) * 32 + in, d_to = part_of * C + d;
+      if (part) {
+        if (to < rows) {
+          const int64_t u16 = ((int64_t)p * pool.H + h) * ((rows + 15) / 16) + to / 16;
+          *reinterpret_cast<float4v*>(part + (u16 * splits + split) * kPart<D> + (to & 15) * D +
+                                      d_to) = w;
+        }
+      } else {
+        const int user_to = to / per_user, of = to - user_to * per_user;
+        const int i_to = of / A.group, head_to = h * A.group + of - i_to * A.group;
+        if (user_to < count) {
+          uint16_t* const dst = static_cast<uint16_t*>(A.out.p) +
+                                (int64_t)(first + user_to) * A.out.seq + (int64_t)i_to * A.out.tok +
+                                (int64_t)head_to * A.out.head + d_to;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) dst[e] = kv_narrow<BF16>(w[e]);
+        }
+      }
+    }
+  }
+}
+
+// ---- states joined ----------------------------------------------------------------------------
+struct JoinLds {
+  float w[2 * kMostSplits * 16];
+  float4v sums[256];
+};
+
+// A context's states alone: `few` rows a workgroup. Bound by the states' bytes.
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void contexts_join_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U,
+                                                            int groups, int few, int splits,
+                                                            int64_t items, const float* part,
+                                                            float* lse) {
+  __shared__ JoinLds L;
+  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const int first = (int)(it % groups) * few;
+    const int64_t ph = it / groups;
+    const int h = (int)(ph % pool.H);
+    const SharedRows R = rows_of(S, A, U, (int)(ph / pool.H));
+    const int all = R.nq * A.group, left = R.q_len * A.group - first, rows = left < few ? left : few;
+    if (rows <= 0) continue;
+    const float* const s0 = part + ph * ((all + 15) / 16) * splits * kPart<D>;
+    float top = kNegInf, l = 0.0f;
+    join_rows<D>(rows, splits, L.w, L.sums, top, l, [&](int i, int x, int& in) {
+      in = (first + x) & 15;
+      return s0 + ((int64_t)((first + x) >> 4) * splits + i) * kPart<D>;
+    }, [](float) {}, [&](int x, int d, const float4v& o) {
+      put_out<D, BF16>(A, R, h, first + x, d, reinterpret_cast<const float*>(&o), 4);
+    });
+    if ((threadIdx.x & 15) == 0 && (int)(threadIdx.x >> 4) < rows)
+      put_lse(A, R, pool.H, h, first + (threadIdx.x >> 4), lse,
+              (top + __builtin_amdgcn_logf(l)) * kLn2);
+    __syncthreads();
+  }
+  // requests without a context
+  for (int p = blockIdx.x; p < S.n; p += gridDim.x) fill_without<256>(A, U, S.n, p, pool.H, D, lse);
+}
+
+// A context's states and those of a request's own tokens: a workgroup a request's 16-row tile. The
+// context's states of the tile lie in rows of its own tiles, from the request's first on.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void shared_join_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U,
                                                           int contexts, int tiles, int shared_tiles,
                                                           int shared_splits, int splits,
                                                           int64_t items, const float* shared_part,
                                                           const float* part, float* lse) {
-  constexpr int kAhead = 8;
-  __shared__ float w[2 * kMostSplits * 16];
-  const int tid = threadIdx.x, row = tid >> 4, sub = tid & 15;
+  __shared__ JoinLds L;
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const int tile = (int)(it % tiles);
     const int64_t r = it / tiles;
     const int h = (int)(r % pool.H);
     const RowsOf R = rows_of(S, A, (int)(r / pool.H));
-    const int rows = R.nq * A.group, rows0 = rows - tile * 16 < 16 ? rows - tile * 16 : 16;
-    // the context: the last one whose requests start at this one or before
-    int lo = 0, hi = contexts;                         // firsts[lo - 1] <= seq < firsts[hi]
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (U.firsts[mid] <= R.seq) lo = mid + 1;
-      else hi = mid;
-    }
-    const int p = lo - 1;
-    int n0 = 0, from = 0;                              // the context's states; its row of row 0
-    if (p >= 0) {
-      const Requests q = requests_of(U, p);
-      if (R.seq - q.first < q.count) {
-        n0 = shared_splits;
-        from = (R.seq - q.first) * rows + tile * 16;
-      }
-    }
-    const int n = n0 + splits;
-    // state i of row x: the context's first, then the request's own
-    const float* const s0 = n0 ? shared_part + ((int64_t)p * pool.H + h) * shared_tiles *
-                                                   shared_splits * kPart<D> : nullptr;
-    const auto state = [&](int i, int x, int& in) -> const float* {
+    const int all = R.nq * A.group, rows = all - tile * 16 < 16 ? all - tile * 16 : 16;
+    int place = 0;
+    const int p = context_of(U, contexts, R.seq, place);
+    const int n0 = p >= 0 ? shared_splits : 0, from = place * all + tile * 16;
+    const float* const s0 =
+        shared_part + ((int64_t)(p >= 0 ? p : 0) * pool.H + h) * shared_tiles * shared_splits * kPart<D>;
+    float top = kNegInf, l = 0.0f;
+    join_rows<D>(rows, n0 + splits, L.w, L.sums, top, l, [&](int i, int x, int& in) {
       if (i < n0) {
         in = (from + x) & 15;
         return s0 + ((int64_t)((from + x) >> 4) * shared_splits + i) * kPart<D>;
       }
       in = x;
       return part + (it * splits + (i - n0)) * kPart<D>;
-    };
-    float top = kNegInf, l = 0.0f;
-    if (row < rows0) {
-      for (int i = sub; i < n; i += 16) {
-        int in;
-        const float* const s = state(i, row, in);
-        const float2v ml = *reinterpret_cast<const float2v*>(s + 16 * D + 2 * in);
-        w[i * 16 + row] = ml[0];
-        const float both = fmaxf(top, ml[0]), ref = both == kNegInf ? 0.0f : both;
-        l = l * __builtin_amdgcn_exp2f(top - ref) + ml[1] * __builtin_amdgcn_exp2f(ml[0] - ref);
-        top = both;
-      }
-    }
-#pragma unroll
-    for (int o = 1; o < 16; o <<= 1) {
-      const float m = __shfl_xor(top, o), x = __shfl_xor(l, o);
-      const float both = fmaxf(top, m), ref = both == kNegInf ? 0.0f : both;
-      l = l * __builtin_amdgcn_exp2f(top - ref) + x * __builtin_amdgcn_exp2f(m - ref);
-      top = both;
-    }
-    const float ref = top == kNegInf ? 0.0f : top;
-    if (row < rows0) {
-      const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-      for (int i = sub; i < n; i += 16)
-        w[i * 16 + row] = __builtin_amdgcn_exp2f(w[i * 16 + row] - ref) * inv;
-      if (sub == 0)
-        put_lse(A, R, pool.H, h, tile * 16 + row, lse, (top + __builtin_amdgcn_logf(l)) * kLn2);
-    }
-    __syncthreads();
-    for (int e = tid; e < rows0 * (D / 2); e += 256) {
-      const int x = e / (D / 2), d = e % (D / 2) * 2;
-      float o[2] = {0.0f, 0.0f};
-      for (int i0 = 0; i0 < n; i0 += kAhead) {
-        float2v v[kAhead];
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-          int in;
-          const float* const s = state(i0 + i < n ? i0 + i : n - 1, x, in);
-          v[i] = *reinterpret_cast<const float2v*>(s + in * D + d);
-        }
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-          if (i0 + i < n) {
-            const float f = w[(i0 + i) * 16 + x];
-            o[0] = __builtin_fmaf(v[i][0], f, o[0]);
-            o[1] = __builtin_fmaf(v[i][1], f, o[1]);
-          }
-        }
-      }
-      put_out<D, BF16>(A, R, h, tile * 16 + x, d, o, 2);
-    }
+    }, [](float) {}, [&](int x, int d, const float4v& o) {
+      put_out<D, BF16>(A, R, h, tile * 16 + x, d, reinterpret_cast<const float*>(&o), 4);
+    });
+    if ((threadIdx.x & 15) == 0 && (int)(threadIdx.x >> 4) < rows)
+      put_lse(A, R, pool.H, h, tile * 16 + (threadIdx.x >> 4), lse,
+              (top + __builtin_amdgcn_logf(l)) * kLn2);
     __syncthreads();
   }
 }
@@ -1520,12 +1986,12 @@ void in_launches(int64_t items, Launch launch) {
     launch(it0, (unsigned)(items - it0 < kMost ? items - it0 : kMost));
 }
 
-template <int D, bool BF16, class Rows>
-void prompt_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, const KvUsers& U,
-              const KvAttnPlan& P, float* part, float* lse, hipStream_t st) {
+template <int D, bool BF16>
+void prompt_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, const KvAttnPlan& P,
+              float* part, float* lse, hipStream_t st) {
   in_launches((int64_t)S.n * pool.H * P.big * P.splits, [&](int64_t it0, unsigned n) {
-    hipLaunchKernelGGL((prompt_kernel<D, BF16, Rows>), dim3(n), dim3(64 * kPromptWaves<D>), 0, st,
-                       pool, S, A, U, P.big, P.splits, it0, part, lse);
+    hipLaunchKernelGGL((prompt_kernel<D, BF16>), dim3(n), dim3(64 * kPromptWaves<D>), 0, st, pool,
+                       S, A, P.big, P.splits, it0, part, lse);
   });
 }
 
@@ -1566,14 +2032,15 @@ hipError_t attend_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, void* 
   const int vseqs = A.picks ? S.n * A.nq : S.n;
   const int64_t units = (int64_t)vseqs * pool.H * P.tiles;
   if (P.big)
-    prompt_d<D, BF16, RowsOf>(pool, S, A, KvUsers{}, P, P.splits > 1 ? part : nullptr, lse, st);
+    prompt_d<D, BF16>(pool, S, A, P, P.splits > 1 ? part : nullptr, lse, st);
   else
-    hipLaunchKernelGGL((attend_kernel<D, BF16, RowsOf, false>), dim3(grid_of(units * P.splits)),
+    hipLaunchKernelGGL((attend_kernel<D, BF16, RowsOf, kOut>), dim3(grid_of(units * P.splits)),
                        dim3(256), 0, st, pool, S, A, KvUsers{}, P.tiles, P.splits,
-                       units * P.splits, part, reinterpret_cast<uint32_t*>(base), lse, scores, np);
+                       units * P.splits, part, reinterpret_cast<uint32_t*>(base), lse, scores, np,
+                       ContextStates{});
   if (P.splits > 1 && P.big)
-    hipLaunchKernelGGL((join_kernel<D, BF16, RowsOf>), dim3(grid_of(units)), dim3(256), 0, st, pool,
-                       S, A, KvUsers{}, P.tiles, P.splits, units, part, lse);
+    hipLaunchKernelGGL((join_kernel<D, BF16>), dim3(grid_of(units)), dim3(256), 0, st, pool, S, A,
+                       P.tiles, P.splits, units, part, lse);
   if (A.mass_out && np) {
     const int64_t items = (int64_t)S.n * pool.H * np;
     if (P.many)
@@ -1588,6 +2055,25 @@ hipError_t attend_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, void* 
   return hipGetLastError();
 }
 
+// shared_kernel over all contexts, at most 65535 a launch. part null: the result.
+template <int D, bool BF16>
+void shared_rows_d(const KvPool& pool, const KvSeqs& C, const KvAttn& CA, const KvUsers& U,
+                   const KvAttnPlan& P, float* part, float* lse, hipStream_t st) {
+  constexpr int W = kPromptWaves<D>;
+  for (int z0 = 0; z0 < C.n; z0 += 65535) {
+    const dim3 grid((unsigned)(pool.H * P.splits), (unsigned)P.big,
+                    (unsigned)(C.n - z0 < 65535 ? C.n - z0 : 65535));
+    if constexpr (D < 256)
+      if (P.halves) {
+        hipLaunchKernelGGL((shared_kernel<D, BF16, W / 2>), grid, dim3(64 * W), 0, st, pool, C, CA, U,
+                           P.splits, z0, part, lse);
+        continue;
+      }
+    hipLaunchKernelGGL((shared_kernel<D, BF16, W>), grid, dim3(64 * W), 0, st, pool, C, CA, U,
+                       P.splits, z0, part, lse);
+  }
+}
+
 template <int D, bool BF16>
 hipError_t shared_d(const KvPool& pool, const KvSeqs& C, const KvAttn& CA, const KvUsers& U,
                     const KvSeqs& S, const KvAttn& A, void* ws, hipStream_t st) {
@@ -1599,33 +2085,41 @@ hipError_t shared_d(const KvPool& pool, const KvSeqs& C, const KvAttn& CA, const
   if (P.own.tiles == 0) {
     // the context alone
     if (P.shared.big) {
-      prompt_d<D, BF16, SharedRows>(pool, C, CA, U, P.shared, splits0 > 1 ? part0 : nullptr, A.lse,
-                                    st);
-      if (splits0 > 1)
-        hipLaunchKernelGGL((join_kernel<D, BF16, SharedRows>), dim3(grid_of(units0)), dim3(256), 0,
-                           st, pool, C, CA, U, P.shared.tiles, splits0, units0, part0, A.lse);
+      shared_rows_d<D, BF16>(pool, C, CA, U, P.shared, splits0 > 1 ? part0 : nullptr, A.lse, st);
+      if (splits0 > 1) {
+        const int few = units0 < 1024 ? 4 : 16, groups = (CA.nq * CA.group + few - 1) / few;
+        const int64_t items = (int64_t)C.n * pool.H * groups;
+        hipLaunchKernelGGL((contexts_join_kernel<D, BF16>), dim3(grid_of(items)), dim3(256), 0, st,
+                           pool, C, CA, U, groups, few, splits0, items, part0, A.lse);
+      }
     } else {
-      hipLaunchKernelGGL((attend_kernel<D, BF16, SharedRows, false>),
+      hipLaunchKernelGGL((attend_kernel<D, BF16, SharedRows, kOut>),
                          dim3(grid_of(units0 * splits0)), dim3(256), 0, st, pool, C, CA, U,
                          P.shared.tiles, splits0, units0 * splits0, part0,
-                         reinterpret_cast<uint32_t*>(base), A.lse, nullptr, 0);
+                         reinterpret_cast<uint32_t*>(base), A.lse, nullptr, 0, ContextStates{});
     }
     return hipGetLastError();
   }
   if (P.shared.big)
-    prompt_d<D, BF16, SharedRows>(pool, C, CA, U, P.shared, part0, nullptr, st);
+    shared_rows_d<D, BF16>(pool, C, CA, U, P.shared, part0, nullptr, st);
   else
-    hipLaunchKernelGGL((attend_kernel<D, BF16, SharedRows, true>), dim3(grid_of(units0 * splits0)),
+    hipLaunchKernelGGL((attend_kernel<D, BF16, SharedRows, kParts>), dim3(grid_of(units0 * splits0)),
                        dim3(256), 0, st, pool, C, CA, U, P.shared.tiles, splits0, units0 * splits0,
-                       part0, nullptr, nullptr, nullptr, 0);
+                       part0, nullptr, nullptr, nullptr, 0, ContextStates{});
   float* const part = reinterpret_cast<float*>(base + P.own_off);
   const int64_t units = (int64_t)S.n * pool.H * P.own.tiles;
+  if (P.joins) {
+    hipLaunchKernelGGL((attend_kernel<D, BF16, RowsOf, kJoin>), dim3(grid_of(units)), dim3(256), 0,
+                       st, pool, S, A, U, P.own.tiles, 1, units, nullptr, nullptr, A.lse, nullptr, 0,
+                       ContextStates{C.n, P.shared.tiles, splits0, part0});
+    return hipGetLastError();
+  }
   if (P.own.big)
-    prompt_d<D, BF16, RowsOf>(pool, S, A, KvUsers{}, P.own, part, nullptr, st);
+    prompt_d<D, BF16>(pool, S, A, P.own, part, nullptr, st);
   else
-    hipLaunchKernelGGL((attend_kernel<D, BF16, RowsOf, true>), dim3(grid_of(units * P.own.splits)),
+    hipLaunchKernelGGL((attend_kernel<D, BF16, RowsOf, kParts>), dim3(grid_of(units * P.own.splits)),
                        dim3(256), 0, st, pool, S, A, KvUsers{}, P.own.tiles, P.own.splits,
-                       units * P.own.splits, part, nullptr, nullptr, nullptr, 0);
+                       units * P.own.splits, part, nullptr, nullptr, nullptr, 0, ContextStates{});
   hipLaunchKernelGGL((shared_join_kernel<D, BF16>), dim3(grid_of(units)), dim3(256), 0, st, pool, S,
                      A, U, C.n, P.own.tiles, P.shared.tiles, splits0, P.own.splits, units, part0,
                      part, A.lse);
@@ -1637,7 +2131,7 @@ hipError_t shared_d(const KvPool& pool, const KvSeqs& C, const KvAttn& CA, const
 KvSharedPlan cg_kv8_shared_plan(const KvPool& pool, const KvSeqs& C, const KvAttn& CA,
                                 const KvSeqs& S, const KvAttn& A, int D) {
   KvSharedPlan P = {};
-  P.shared = cg_kv8_plan(pool, C, CA, D);
+  P.shared = cg_kv8_plan(pool, C, CA, D, true);
   const uint64_t state = 16ull * (D + 2) * 4;
   const bool own = S.table != nullptr;
   uint64_t at = own || P.shared.splits > 1 ? kKv8Front : 0;
@@ -1648,6 +2142,10 @@ KvSharedPlan cg_kv8_shared_plan(const KvPool& pool, const KvSeqs& C, const KvAtt
   P.own_off = at;
   if (own) {
     P.own = cg_kv8_plan(pool, S, A, D);
+    // One launch for the own tokens and the join, where a wave has four pages of them at most or
+    // there would be one split anyway.
+    P.joins = !P.own.big && (P.own.splits == 1 || ((int64_t)A.max_len + kPage - 1) / kPage <= 16);
+    if (P.joins) P.own.splits = 0;     // (no states)
     at += (uint64_t)S.n * pool.H * P.own.tiles * P.own.splits * state;
   }
   P.total = (at + 255) & ~255ull;
@@ -1664,7 +2162,7 @@ hipError_t cg_launch_kv8_shared(const KvPool& pool, const KvSeqs& C, const KvAtt
   }
 }
 
-KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& S, const KvAttn& A, int D) {
+KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& S, const KvAttn& A, int D, bool shared) {
   KvAttnPlan P;
   const int64_t rows = (int64_t)(A.picks ? 1 : A.nq) * A.group;
   P.tiles = (int)((rows + 15) / 16);
@@ -1681,9 +2179,15 @@ KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& S, const KvAttn& A, int
   const int64_t at_once = D == 64 ? 768 : D == 128 ? 512 : 256;
   const bool little = units <= at_once && units * pages <= (D == 256 ? 2048 : 8192);
   P.big = 0;
-  int64_t s, most;
-  if (P.tiles > 2 && !little && !A.picks) {
-    const int per = D == 256 ? 32 * kPromptWaves<256> : 32 * kPromptWaves<128>;
+  P.halves = false;
+  int64_t s, most, at_least = 1;
+  const bool listed = !shared || pages <= (D == 256 ? 256 : 512) * (int64_t)kMostSplits;
+  if (P.tiles > 2 && !little && !A.picks && listed) {
+    int per = D == 256 ? 32 * kPromptWaves<256> : 32 * kPromptWaves<128>;
+    P.halves = shared && D < 256 && vseqs * pool.H * ((rows + per - 1) / per) < 256;
+    if (P.halves) per /= 2;
+    // (shared_kernel lists a split's columns, one a thread)
+    at_least = shared ? (int)((pages + (D == 256 ? 256 : 512) - 1) / (D == 256 ? 256 : 512)) : 1;
     P.big = (int)((rows + per - 1) / per);
     const int64_t groups = vseqs * pool.H * P.big;
     s = (256 + groups - 1) / groups;
@@ -1707,7 +2211,7 @@ KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& S, const KvAttn& A, int
   }
   if (most > kMostSplits) most = kMostSplits;
   if (s > most) s = most;
-  if (s < 1) s = 1;
+  if (s < at_least) s = at_least;
   P.splits = (int)s;
   // Weights of few rows: their scores are kept for the second launch (8 bytes a row and token to
   // write and read again) where that is at most half of reading K again (D bytes a token), and of 8

@@ -181,6 +181,21 @@ def test_long_context_in_many_splits():
     check(1, 4, 64, "bfloat16", [7000, 64], [0, 30, 31], 31, [40] * 31, None, 3, seed=7)
 
 
+def test_long_own_tokens():
+    """Own tokens in splits of their own, of few rows and of many, behind contexts of both kinds."""
+    check(1, 2, 128, "float16", [300], [0, 2], 2, [2500, 70], seed=10)
+    check(1, 2, 64, "bfloat16", [300, 7], [0, 40, 41], 41, [1300] + [60] * 40, seed=11)
+    check(1, 1, 64, "float16", [100], [0, 1], 1, [1500], [70], 80, seed=12)
+
+
+def test_many_rows_in_tiles():
+    """More rows than a workgroup's: tiles of half and of all waves, with splits and without."""
+    check(1, 4, 64, "float16", [500], [0, 40], 40, None, seed=13)
+    check(2, 4, 128, "bfloat16", [700, 130], [0, 33, 70], 71, [9] * 71, None, 2, seed=14)
+    check(8, 1, 64, "float16", [130] * 17, list(range(18)), 17, None, None, 270, seed=15)
+    check(1, 2, 256, "float16", [900], [0, 80], 80, [3] * 80, seed=16)
+
+
 def test_logits_far_apart():
     """A context whose logits lie far above or below the own tokens' (the join's references)."""
     for scale in (8.0, -8.0):

@@ -610,8 +610,6 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_kernel(KvPool po
     const int h = (int)(unit / tiles % pool.H);
     const int vseq = (int)(unit / tiles / pool.H);
     const Rows R = rows_in<Rows>(S, A, U, vseq);
-    int place = 0, context = -1;
-    if constexpr (TO == kJoin) context = context_of(U, C.contexts, R.seq, place);
     if constexpr (__is_same(Rows, SharedRows) && TO == kOut)
       if (split == 0 && tile == 0 && h == 0) fill_without<256>(A, U, S.n, vseq, pool.H, D, lse);
     // the pages that any row of the tile sees
@@ -644,6 +642,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_kernel(KvPool po
     }
     QTile<D> Q;
     load_q<D, BF16>(A, R, h, tile, Q);
+    int place = 0, context = -1;       // (looked up beside the first page's codes)
+    if constexpr (TO == kJoin) context = uniform(context_of(U, C.contexts, R.seq, place));
     Acc<D> acc;
 #pragma unroll
     for (int dt = 0; dt < D / 16; ++dt) acc.o[dt] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
@@ -1616,6 +1616,17 @@ void shared_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, int splits, int z
     v_most = __builtin_bit_cast(float, uniform(__builtin_bit_cast(int, v_most)));
   }
 
+  // the first pages' codes are on their way while the rows are read
+  PageRegs<D, NT> kr, vr, k_first, v_first, k_second;
+  const auto fetch = [&](const int8_t* codes, int i, PageRegs<D, NT>& r) {
+    if (i < n) page_fetch<D, NT>(codes + ((int64_t)uniform(list.page[i]) * pool.H + h) * (kPage * D), r);
+  };
+  fetch(pool.k, 0, k_first);
+  fetch(pool.v, 0, v_first);
+  if (kAhead == 2) fetch(pool.k, 1, k_second);
+  fetch(pool.v, 1, vr);
+  fetch(pool.k, kAhead, kr);
+
   // this lane's row
   const int row = r0 + (wave - side * RW) * 32 + m;
   const int user = row / per_user, of_user = row - user * per_user;
@@ -1734,16 +1745,7 @@ void shared_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, int splits, int z
   // without a live row only helps with the pages.
   const auto walk = [&](auto busy) {
     constexpr bool kBusy = decltype(busy)::value;
-    PageRegs<D, NT> kr, vr;
     float16v x;
-    const auto fetch_k = [&](int i) {
-      if (i < n)
-        page_fetch<D, NT>(pool.k + ((int64_t)uniform(list.page[i]) * pool.H + h) * (kPage * D), kr);
-    };
-    const auto fetch_v = [&](int i) {
-      if (i < n)
-        page_fetch<D, NT>(pool.v + ((int64_t)uniform(list.page[i]) * pool.H + h) * (kPage * D), vr);
-    };
     const auto step = [&](const _Float16 (*k)[D + 8], const _Float16 (*next)[D + 8],
                           const _Float16 (*v)[kPage + 8], int pos0, float ks, float vs, auto put) {
       if constexpr (kBusy) x = tile_step(x, k, next, v, pos0, ks, vs, put);
@@ -1752,18 +1754,22 @@ void shared_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, int splits, int z
     const auto second = [&](int buf) {
       return reinterpret_cast<const _Float16 (*)[kPage + 8]>(&L.v[buf][0][32]);
     };
-    fetch_k(0);
-    fetch_v(0);
-    widen_k<D, NT>(kr, L.k[0]);
-    fetch_k(1);
-    widen_v<D, NT>(vr, L.v[0]);
-    fetch_v(1);
-    if (kAhead == 2) {
-      widen_k<D, NT>(kr, L.k[1]);      // (behind the last page stale codes, which nobody uses)
-      fetch_k(2);
-    }
+    // (behind the last page the registers and buffers hold anything, and nobody uses it)
+    widen_k<D, NT>(k_first, L.k[0]);
+    widen_v<D, NT>(v_first, L.v[0]);
+    if (kAhead == 2) widen_k<D, NT>(k_second, L.k[1]);
     __syncthreads();
-    if constexpr (kBusy) x = tile_scores<D>(L.k[0] + 32 * side, q);
+    if constexpr (kBusy) {
+      // the first tile's largest score is the first reference (with a V scale that counts)
+      x = tile_scores<D>(L.k[0] + 32 * side, q);
+      const float ratio = list.vs[0] * v_unit;
+      const int seen = len - uniform(list.column[0]) * kPage - 32 * side - 16 * half;
+      float t = kNegInf;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) t = max2(t, e < seen ? x[e] : kNegInf);
+      t = half_max(t) * (unit * list.ks[0]) + __builtin_amdgcn_logf(ratio);
+      if (ratio > 0x1p-60f && t > -1e30f && t < 1e30f) ref = t;
+    }
     int k0 = 0, k1 = 1;                // K buffers of this page and the next
     for (int i = 0; i < n; ++i) {
       const int buf = i & 1, k2 = kAhead == 2 ? 3 - k0 - k1 : k0;
@@ -1775,16 +1781,16 @@ void shared_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, int splits, int z
                widen_k<D, NT>(kr, L.k[k2]);
                widen_v<D, NT>(vr, L.v[buf ^ 1]);
              });
-        fetch_k(i + 3);
+        fetch(pool.k, i + 3, kr);
       } else {
         step(L.k[k0], L.k[k0] + 32, L.v[buf], pos0, ks, vs,
              [&] { widen_k<D, NT>(kr, L.k[kAhead == 2 ? k2 : k1]); });
-        fetch_k(i + kAhead + 1);
+        fetch(pool.k, i + kAhead + 1, kr);
         if (kAhead == 1) __syncthreads();
         step(L.k[k0] + 32, L.k[k1], second(buf), pos0 + 32, ks, vs,
              [&] { widen_v<D, NT>(vr, L.v[buf ^ 1]); });
       }
-      fetch_v(i + 2);
+      fetch(pool.v, i + 2, vr);
       k0 = k1;
       k1 = k2;
       __syncthreads();
@@ -1810,10 +1816,10 @@ void shared_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, int splits, int z
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[dt][e] = empty ? 0.0f : o[dt][e] * to_top * v_most;
-  // a wave's own rows in LDS, a quarter of the channels at a time with halves, half of them without
   float* const space = reinterpret_cast<float*>(&L);
+  float (*const all)[D + 4] = reinterpret_cast<float (*)[D + 4]>(space);       // halves: [32 RW]
   if constexpr (TW == 2) {
-    float (*const os)[D + 4] = reinterpret_cast<float (*)[D + 4]>(space) + (wave - side * RW) * 32;
+    float (*const os)[D + 4] = all + (wave - side * RW) * 32;
     float2v* const ml = reinterpret_cast<float2v*>(space + 32 * RW * (D + 4)) +
                         (wave - side * RW) * 32;
     static_assert(sizeof(PromptLds<D>) >= 32 * RW * (D + 6) * sizeof(float), "a half's rows");
@@ -1827,75 +1833,95 @@ void shared_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, int splits, int z
       if (half == 0) ml[m] = float2v{top, sum};
     }
     __syncthreads();
-    if (side) return;
-    const float2v other = ml[m];
-    const float both = fmaxf(top, other[0]), base = both == kNegInf ? 0.0f : both;
-    const float f0 = __builtin_amdgcn_exp2f(top - base), f1 = __builtin_amdgcn_exp2f(other[0] - base);
-    sum = sum * f0 + other[1] * f1;
-    top = both;
-#pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-      for (int a = 0; a < 4; ++a) {
-        const float4v w = *reinterpret_cast<const float4v*>(&os[m][32 * dt + 8 * a + 4 * half]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[dt][4 * a + e] = o[dt][4 * a + e] * f0 + w[e] * f1;
+    if (!side) {
+      const float2v other = ml[m];
+      const float both = fmaxf(top, other[0]), base = both == kNegInf ? 0.0f : both;
+      float f0 = __builtin_amdgcn_exp2f(top - base), f1 = __builtin_amdgcn_exp2f(other[0] - base);
+      sum = sum * f0 + other[1] * f1;
+      top = both;
+      if (!part) {
+        const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+        f0 *= inv;
+        f1 *= inv;
       }
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          float4v* const w = reinterpret_cast<float4v*>(&os[m][32 * dt + 8 * a + 4 * half]);
+          float4v y = *w;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = o[dt][4 * a + e] * f0 + y[e] * f1;
+          *w = y;
+        }
+    }
   }
-  if (part) {
+  if (TW == 2 && side) {
+    // (the first half's)
+  } else if (part) {
     if (half == 0 && row < rows) {
       const int64_t u16 = ((int64_t)p * pool.H + h) * ((rows + 15) / 16) + row / 16;
       *reinterpret_cast<float2v*>(part + (u16 * splits + split) * kPart<D> + 16 * D +
                                   2 * (row & 15)) = float2v{top, sum};
     }
   } else {
-    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+    if constexpr (TW == 1) {
+      const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
 #pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt)
+      for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) o[dt][e] *= inv;
+        for (int e = 0; e < 16; ++e) o[dt][e] *= inv;
+    }
     if (lse && half == 0 && user < count)
       lse[(b * U.per + i_row) * ((int64_t)pool.H * A.group) + head] =
           (top + __builtin_amdgcn_logf(sum)) * kLn2;
   }
-  // the rows leave by way of LDS, half of the channels at a time: a lane has pieces of one row, and
-  // a store should have whole ones
-  constexpr int C = D / 2, LR = C / 4, RC = 64 / LR;     // channels; lanes a row, rows a store
-  float (*const mine)[C + 4] = reinterpret_cast<float (*)[C + 4]>(space) + wave * 32;
-  static_assert(sizeof(PromptLds<D>) >= W * 32 * (C + 4) * sizeof(float), "all waves' rows");
+  // the rows leave by way of LDS: a lane has pieces of one row, and a store should have whole ones
+  const auto leave = [&](int to, int d, const float4v& w) {
+    if (part) {
+      if (to >= rows) return;
+      const int64_t u16 = ((int64_t)p * pool.H + h) * ((rows + 15) / 16) + to / 16;
+      *reinterpret_cast<float4v*>(part + (u16 * splits + split) * kPart<D> + (to & 15) * D + d) = w;
+    } else {
+      const int user_to = to / per_user, of = to - user_to * per_user;
+      if (user_to >= count) return;
+      const int i_to = of / A.group, head_to = h * A.group + of - i_to * A.group;
+      uint16_t* const dst = static_cast<uint16_t*>(A.out.p) +
+                            (int64_t)(first + user_to) * A.out.seq + (int64_t)i_to * A.out.tok +
+                            (int64_t)head_to * A.out.head + d;
 #pragma unroll
-  for (int part_of = 0; part_of < 2; ++part_of) {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      for (int e = 0; e < 4; ++e) dst[e] = kv_narrow<BF16>(w[e]);
+    }
+  };
+  if constexpr (TW == 2) {
+    __syncthreads();
+    constexpr int LR = D / 4;                            // threads a row
+#pragma unroll 2
+    for (int in = threadIdx.x / LR; in < 32 * RW; in += NT / LR) {
+      const int d = threadIdx.x % LR * 4;
+      leave(r0 + in, d, *reinterpret_cast<const float4v*>(&all[in][d]));
+    }
+  } else {
+    // (a wave's own rows, half of the channels at a time: there is no more room)
+    constexpr int C = D / 2, LR = C / 4, RC = 64 / LR;   // channels; lanes a row, rows a store
+    float (*const mine)[C + 4] = reinterpret_cast<float (*)[C + 4]>(space) + wave * 32;
+    static_assert(sizeof(PromptLds<D>) >= W * 32 * (C + 4) * sizeof(float), "all waves' rows");
 #pragma unroll
-    for (int dt = 0; dt < D / 64; ++dt)
+    for (int c = 0; c < 2; ++c) {
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-      for (int a = 0; a < 4; ++a) {
-        const float16v& from = o[part_of * (D / 64) + dt];
-        *reinterpret_cast<float4v*>(&mine[m][32 * dt + 8 * a + 4 * half]) =
-            float4v{from[4 * a], from[4 * a + 1], from[4 * a + 2], from[4 * a + 3]};
-      }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      for (int dt = 0; dt < D / 64; ++dt)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          const float16v& from = o[c * (D / 64) + dt];
+          *reinterpret_cast<float4v*>(&mine[m][32 * dt + 8 * a + 4 * half]) =
+              float4v{from[4 * a], from[4 * a + 1], from[4 * a + 2], from[4 * a + 3]};
+        }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll 1
-    for (int k = 0; k < 32 / RC; ++k) {
-      const int in = k * RC + lane / LR, d = lane % LR * 4;
-      const float4v w = *reinterpret_cast<const float4v*>(&mine[in][d]);
-      const int to = r0 + (wave - side * RW) * 32 + in, d_to = part_of * C + d;
-      if (part) {
-        if (to < rows) {
-          const int64_t u16 = ((int64_t)p * pool.H + h) * ((rows + 15) / 16) + to / 16;
-          *reinterpret_cast<float4v*>(part + (u16 * splits + split) * kPart<D> + (to & 15) * D +
-                                      d_to) = w;
-        }
-      } else {
-        const int user_to = to / per_user, of = to - user_to * per_user;
-        const int i_to = of / A.group, head_to = h * A.group + of - i_to * A.group;
-        if (user_to < count) {
-          uint16_t* const dst = static_cast<uint16_t*>(A.out.p) +
-                                (int64_t)(first + user_to) * A.out.seq + (int64_t)i_to * A.out.tok +
-                                (int64_t)head_to * A.out.head + d_to;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) dst[e] = kv_narrow<BF16>(w[e]);
-        }
+      for (int in = lane / LR; in < 32; in += RC) {
+        const int d = lane % LR * 4;
+        leave(r0 + wave * 32 + in, c * C + d, *reinterpret_cast<const float4v*>(&mine[in][d]));
       }
     }
   }

@@ -1537,8 +1537,9 @@ void mass_rows_kernel(KvPool pool, KvSeqs S, KvAttn A, int np, int shares, int64
 // ---- a shared context of many rows ----------------------------------------------------------------
 // The rows of all requests of a context against its pages: prompt_kernel's products and weights, but
 // no row sees less than the others, so only the context's last page is masked, and the V scales are
-// taken relative to the largest of the workgroup's pages (what is 2^-60 of it counts as none: its
-// weights are summed apart, and must not move the reference that the others are rounded by).
+// taken relative to the power of two at the largest of the workgroup's pages (what is 2^-60 of it
+// counts as none: its weights are summed apart, and must not move the reference that the others are
+// rounded by).
 //
 // RW of the workgroup's waves have 32 rows each. With half of them the others take the same rows, and
 // of every page the first tile of 32 tokens goes to the first half and the second to the other (32
@@ -1556,8 +1557,8 @@ struct PageList {
 
 template <int D, bool BF16, int RW>
 __global__ __launch_bounds__(64 * kPromptWaves<D>, kPromptWaves<D> / 4)
-void shared_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, int splits, int z0, float* part,
-                   float* lse) {
+void shared_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, int splits, int tile0, int p0,
+                   float* part, float* lse) {
   constexpr int W = kPromptWaves<D>, NT = 64 * W, TW = W / RW;
   constexpr int kAhead = kPagesK<D> - 1;
   static_assert(TW == 1 || (TW == 2 && kAhead == 2), "a tile of every page for each half");
@@ -1566,7 +1567,7 @@ void shared_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, int splits, int z
   const int lane = threadIdx.x & 63, m = lane & 31, half = lane >> 5;
   const int wave = uniform(threadIdx.x >> 6), side = wave / RW;
   const int split = blockIdx.x / pool.H, h = blockIdx.x - split * pool.H;
-  const int tile = blockIdx.y, p = z0 + blockIdx.z;
+  const int tile = tile0 + blockIdx.y, p = p0 + blockIdx.z;
 
   const Requests req = requests_of(U, p);
   int len = A.lengths[p];
@@ -1575,7 +1576,8 @@ void shared_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, int splits, int z
   const int first = uniform(req.first), count = uniform(req.count);
   if (!part && blockIdx.x == 0 && tile == 0) fill_without<NT>(A, U, S.n, p, pool.H, D, lse);
   const int per_user = U.per * A.group, rows = U.most * per_user, r0 = tile * (32 * RW);
-  const int columns = r0 < count * per_user ? (int)(((int64_t)len + kPage - 1) / kPage) : 0;
+  if (r0 >= count * per_user) return;                  // (nobody's rows)
+  const int columns = (int)(((int64_t)len + kPage - 1) / kPage);
   const int per = (columns + splits - 1) / splits;
   const int j0 = split * per, j1 = j0 + per < columns ? j0 + per : columns;
 
@@ -1644,9 +1646,9 @@ void shared_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, int splits, int z
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[dt][e] = 0.0f;
-  float ref = -1e30f, l = 0.0f;      // O and l in units of 2^(ref - kLift), O also of v_most
+  float ref = -1e30f, l = 0.0f;      // O and l in units of 2^(ref - kLift), O also of 2^v_exp
   float ref0 = -1e30f, l0 = 0.0f;    // l of the pages without V, in units of 2^ref0
-  const float v_unit = v_most > 0.0f ? 1.0f / v_most : 0.0f;
+  const int v_exp = __builtin_amdgcn_frexp_expf(v_most);         // (0 of 0)
 
   // One tile of 32 tokens: see prompt_kernel.
   const auto tile_step = [&](float16v x, const _Float16 (*k)[D + 8], const _Float16 (*next)[D + 8],
@@ -1660,7 +1662,7 @@ void shared_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, int splits, int z
         for (int e = 0; e < 16; ++e) z[e] = e < seen_here ? z[e] : to;
       }
     };
-    const float f = unit * ks, ratio = vs * v_unit;
+    const float f = unit * ks, ratio = __builtin_ldexpf(vs, -v_exp);
     const bool with_v = !(ratio <= 0x1p-60f);
     const float lv = with_v ? __builtin_amdgcn_logf(ratio) + (float)kLift : 0.0f;
     const float c = with_v ? lv - ref : kNegInf;
@@ -1762,7 +1764,7 @@ void shared_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, int splits, int z
     if constexpr (kBusy) {
       // the first tile's largest score is the first reference (with a V scale that counts)
       x = tile_scores<D>(L.k[0] + 32 * side, q);
-      const float ratio = list.vs[0] * v_unit;
+      const float ratio = __builtin_ldexpf(list.vs[0], -v_exp);
       const int seen = len - uniform(list.column[0]) * kPage - 32 * side - 16 * half;
       float t = kNegInf;
 #pragma unroll
@@ -1815,7 +1817,8 @@ void shared_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, int splits, int z
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) o[dt][e] = empty ? 0.0f : o[dt][e] * to_top * v_most;
+    for (int e = 0; e < 16; ++e)
+      o[dt][e] = empty ? 0.0f : __builtin_ldexpf(o[dt][e] * to_top, v_exp);
   float* const space = reinterpret_cast<float*>(&L);
   float (*const all)[D + 4] = reinterpret_cast<float (*)[D + 4]>(space);       // halves: [32 RW]
   if constexpr (TW == 2) {
@@ -2081,23 +2084,29 @@ hipError_t attend_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, void* 
   return hipGetLastError();
 }
 
-// shared_kernel over all contexts, at most 65535 a launch. part null: the result.
+// shared_kernel over all contexts and tiles, in launches below 2^32 threads and inside the grid's
+// limits. part null: the result.
 template <int D, bool BF16>
 void shared_rows_d(const KvPool& pool, const KvSeqs& C, const KvAttn& CA, const KvUsers& U,
                    const KvAttnPlan& P, float* part, float* lse, hipStream_t st) {
-  constexpr int W = kPromptWaves<D>;
-  for (int z0 = 0; z0 < C.n; z0 += 65535) {
-    const dim3 grid((unsigned)(pool.H * P.splits), (unsigned)P.big,
-                    (unsigned)(C.n - z0 < 65535 ? C.n - z0 : 65535));
-    if constexpr (D < 256)
-      if (P.halves) {
-        hipLaunchKernelGGL((shared_kernel<D, BF16, W / 2>), grid, dim3(64 * W), 0, st, pool, C, CA, U,
-                           P.splits, z0, part, lse);
-        continue;
-      }
-    hipLaunchKernelGGL((shared_kernel<D, BF16, W>), grid, dim3(64 * W), 0, st, pool, C, CA, U,
-                       P.splits, z0, part, lse);
-  }
+  constexpr int W = kPromptWaves<D>, kMost = 1 << 22, kSide = 65535;
+  const int x = pool.H * P.splits;
+  const auto at_most = [](int n, int most) { return n < most ? n : most < 1 ? 1 : most; };
+  const int tiles = at_most(P.big, kMost / x < kSide ? kMost / x : kSide);
+  const int contexts = at_most(C.n, kMost / x / tiles < kSide ? kMost / x / tiles : kSide);
+  for (int p0 = 0; p0 < C.n; p0 += contexts)
+    for (int tile0 = 0; tile0 < P.big; tile0 += tiles) {
+      const dim3 grid((unsigned)x, (unsigned)at_most(P.big - tile0, tiles),
+                      (unsigned)at_most(C.n - p0, contexts));
+      if constexpr (D < 256)
+        if (P.halves) {
+          hipLaunchKernelGGL((shared_kernel<D, BF16, W / 2>), grid, dim3(64 * W), 0, st, pool, C, CA,
+                             U, P.splits, tile0, p0, part, lse);
+          continue;
+        }
+      hipLaunchKernelGGL((shared_kernel<D, BF16, W>), grid, dim3(64 * W), 0, st, pool, C, CA, U,
+                         P.splits, tile0, p0, part, lse);
+    }
 }
 
 template <int D, bool BF16>
@@ -2207,13 +2216,13 @@ KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& S, const KvAttn& A, int
   P.big = 0;
   P.halves = false;
   int64_t s, most, at_least = 1;
-  const bool listed = !shared || pages <= (D == 256 ? 256 : 512) * (int64_t)kMostSplits;
-  if (P.tiles > 2 && !little && !A.picks && listed) {
+  const int64_t listed = D == 256 ? PageList<256>::kColumns : PageList<128>::kColumns;
+  if (P.tiles > 2 && !little && !A.picks && (!shared || pages <= listed * kMostSplits)) {
     int per = D == 256 ? 32 * kPromptWaves<256> : 32 * kPromptWaves<128>;
     P.halves = shared && D < 256 && vseqs * pool.H * ((rows + per - 1) / per) < 256;
     if (P.halves) per /= 2;
     // (shared_kernel lists a split's columns, one a thread)
-    at_least = shared ? (int)((pages + (D == 256 ? 256 : 512) - 1) / (D == 256 ? 256 : 512)) : 1;
+    if (shared) at_least = (pages + listed - 1) / listed;
     P.big = (int)((rows + per - 1) / per);
     const int64_t groups = vseqs * pool.H * P.big;
     s = (256 + groups - 1) / groups;
@@ -2238,6 +2247,7 @@ KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& S, const KvAttn& A, int
   if (most > kMostSplits) most = kMostSplits;
   if (s > most) s = most;
   if (s < at_least) s = at_least;
+  if (s < 1) s = 1;
   P.splits = (int)s;
   // Weights of few rows: their scores are kept for the second launch (8 bytes a row and token to
   // write and read again) where that is at most half of reading K again (D bytes a token), and of 8

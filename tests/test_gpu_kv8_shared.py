@@ -26,7 +26,7 @@ def table_of(rng, order, lengths, width=None):
 
 
 def check(H, group, D, dtype, tokens, firsts, n, own, q_lens=None, Q=1, max_users=None, seed=0,
-          scale=None, strided=False, lost=False, spoil=None):
+          scale=None, strided=False, lost=False, spoil=None, max_shared=None):
     """own: the sequences' own lengths, or None. Returns (out, lse) for further looks."""
     torch = torch_cuda()
     rng = np.random.default_rng(seed)
@@ -57,13 +57,15 @@ def check(H, group, D, dtype, tokens, firsts, n, own, q_lens=None, Q=1, max_user
                                    "lengths": ints(torch, own)}
     args = (q, torch.from_numpy(shared).cuda(), ints(torch, tokens), ints(torch, firsts))
     more.update(scale=scale, q_lens=None if q_lens is None else ints(torch, q_lens), out=out,
-                lse=lse, max_users=max_users)
+                lse=lse, max_users=max_users, max_shared=max_shared)
     cache.attend_shared(*args, **more)
     first = out.clone()
     out.fill_(9.0)
     cache.attend_shared(*args, **more)
     assert torch.equal(first, out)             # whoever ends first
     users = n if max_users is None else max_users
+    if max_shared is not None:
+        tokens = [min(x, max_shared) for x in tokens]
     want, wl, size, spread = S.attend(ref, q.float().cpu().numpy(), shared, tokens, firsts, users,
                                       table, own, [Q] * n if q_lens is None else q_lens, scale)
     off = 4 * D * 2.0 ** -24 * spread + 2.0 ** -18
@@ -174,6 +176,32 @@ def test_empty_contexts_and_no_rows():
     assert bool((lse[0] == -float("inf")).all())
     out, _ = check(1, 2, 64, "float16", [0], [0, 40], 41, None, None, 2, seed=4)
     assert bool((out == 0).all())
+
+
+@pytest.mark.parametrize("own", [True, False])
+def test_contexts_that_the_host_takes_for_empty(own):
+    """max_shared 0 with more rows than fit the card at once, and a bound inside a page."""
+    n = 300
+    lengths = [1 + i % 60 for i in range(n)] if own else None
+    for most in (0, 70):
+        check(8, 8, 64, "float16", [100, 128], [0, 200, n], n, lengths, seed=17, max_shared=most)
+
+
+@pytest.mark.parametrize("users", [3, 40])
+@pytest.mark.parametrize("own", [True, False])
+def test_v_scales_of_all_sizes(users, own):
+    """V scales that are subnormal, zero, or far apart within a context: what a token adds is relative
+    to what the others add, however small they are all."""
+    for seed, scales in enumerate(([1e-41, 3e-42], [0.0, 0.0], [1e-30, 1e-2], [2.0 ** -120, 2.0 ** -127])):
+        def spoil(cache, shared, table):
+            at = shared.ravel().tolist()
+            cache.v_scale[at[0::2]] = scales[0]
+            cache.v_scale[at[1::2]] = scales[1]
+            if table is not None:
+                cache.v_scale[sorted(set(table.ravel().tolist()) - {-1})] = scales[0]
+        out, _ = check(1, 2, 128, "bfloat16", [330], [0, users], users,
+                       [3] * users if own else None, seed=seed, spoil=spoil)
+        assert not bool(out.isnan().any())
 
 
 def test_long_context_in_many_splits():

@@ -184,7 +184,8 @@ __device__ __forceinline__ void load_q(const KvAttn& A, const Rows& R, int h, in
   const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
   const int row = tile * 16 + m;
   const int i = R.i0 + row / A.group, head = h * A.group + row % A.group;
-  const bool live = row < R.nq * A.group;
+  // (there is room for more requests of a context than it has: those have no queries to read)
+  const bool live = row < R.nq * A.group && R.exists(i);
   Q.visible = live ? R.visible(i) : 0;
   const uint16_t* src = static_cast<const uint16_t*>(A.q.p) + R.at(A.q, i) +
                         (int64_t)head * A.q.head;

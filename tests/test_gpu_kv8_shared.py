@@ -230,3 +230,11 @@ def test_logits_far_apart():
         def spoil(cache, shared, table):
             cache.k_scale[shared.ravel().tolist()] *= 20 if scale > 0 else 0.01
         check(1, 2, 64, "float16", [150], [0, 3], 3, [70, 1, 64], seed=9, scale=scale, spoil=spoil)
+
+
+def test_room_for_more_requests_than_there_are():
+    """max_users far above what a context has, with few requests and many: queries and results of
+    requests that do not exist are neither read nor written (they would lie behind the tensors)."""
+    for n, firsts, most in ((3, [0, 1, 3], 3), (400, [0, 390, 400], 400), (60, [0, 2, 60], 60)):
+        check(1, 4, 64, "float16", [130, 64], firsts, n, None, seed=18, max_users=most)
+        check(1, 4, 64, "float16", [130, 64], firsts, n, [2] * n, None, 2, seed=19, max_users=most)

@@ -3,12 +3,17 @@ into the 8-bit serving cache (``Kv8Cache``) with every layer at once, a question
 tokens attend over it, the tokens that attention passed by are evicted, and what is left goes back
 to the codec (the paper measures CacheGen on top of token dropping in Sec. 7.2).
 
-Each step is timed on the GPU (HIP events); the attention of the question is compared with the same
-attention over the decoded fp16 cache, in 32 bits. Queries and new tokens are random: no model is
-involved.
+With ``--requests``, many requests answer over each context instead (``answer``): they fork from it,
+draft tokens, attend over the pages that they share, take what the target accepts, and give their
+pages back.
+
+Each step is timed on the GPU (HIP events); the attention of the question (or of the requests' first
+step) is compared with the same attention over the decoded fp16 cache, in 32 bits. Queries, new
+tokens and probabilities are random: no model is involved.
 
 Usage: python -m paper_2310_07240_amd.serving [--workload NAME] [--heads H] [--q-heads H]
        [--question N] [--tokens N] [--keep F] [--picks N]     (one JSON line)
+       python -m paper_2310_07240_amd.serving --requests N [--drafts N] [--steps N] [--vocab N]
 """
 from __future__ import annotations
 
@@ -142,6 +147,99 @@ def run(w, kv_heads=8, q_heads=32, question=100, tokens=16, keep=0.25, picks=16,
     }
 
 
+def answer(w, kv_heads=8, q_heads=32, requests=8, drafts=4, steps=8, vocab=32000, seed=0,
+           device="cuda"):
+    """`requests` answers over every context of workload `w` at once, each `steps` times `drafts`
+    drafted tokens (one at least); returns a dict of figures."""
+    import torch
+    from paper_2310_07240_amd import workloads as W
+    from paper_2310_07240_amd.cachegen import Codec, CodecParams
+    from paper_2310_07240_amd.kv8 import PAGE, Kv8Cache
+    p = CodecParams.of(w)
+    codec = Codec(p, device)
+    times = {}
+    H, D, T = kv_heads, p.n_channels // kv_heads, p.n_tokens
+    n, R = p.n_ctx * p.n_layers, requests          # contexts: each layer of each is one
+    kv = torch.from_numpy(W.generate(w).view(np.int16)).to(device)
+    levels = torch.from_numpy(w.chunk_levels()).to(device)
+    ca, cd = codec.fit(kv)
+    words, offsets, scales = codec.encode(kv, levels, ca, cd)
+    kv = codec.decode(words, offsets, scales, levels, ca, cd)
+    x = kv.view(torch.float16).view(n, 2, T, H, D)
+
+    def ints(*shape, value=0):
+        return torch.full(shape, value, dtype=torch.int32, device=device)
+
+    # The contexts' pages. Whole ones are shared by all requests; the last, if the context ends in
+    # it, starts every request's own tokens and is copied when the request writes behind it.
+    whole, tail = T // PAGE, T % PAGE
+    q = drafts + 1                                 # the last token and the drafts behind it
+    own = -(-(tail + q * steps) // PAGE)
+    cache = Kv8Cache(n * (whole + 1) + n * R * own, H, D, device)
+    refs = ints(cache.n_pages)
+    table = ints(n, whole + own, value=-1)
+    start, held = ints(n), ints(n, value=T)
+    missing = cache.reserve(table, start, held, refs)
+    cache.store(x[:, 0], x[:, 1], table, start)
+    shared, tails = table[:, :max(1, whole)].contiguous(), table[:, whole:].contiguous()
+    shared_len, firsts = ints(n, value=whole * PAGE), torch.arange(
+        0, n * R + 1, R, dtype=torch.int32, device=device)
+    parents = torch.arange(n, dtype=torch.int32, device=device).repeat_interleave(R)
+    rows, lengths = _timed(torch, "fork", times, lambda: cache.fork(
+        tails, ints(n, value=tail), parents, refs))
+
+    g = torch.Generator(device=device).manual_seed(seed)
+
+    def random(*shape):
+        return torch.randn(shape, generator=g, device=device)
+
+    error, taken = 0.0, []
+    counts = ints(n * R, value=q)
+    for step in range(steps):
+        kn, vn, qn = random(n * R, q, H, D).half(), random(n * R, q, H, D).half(), (
+            0.5 * random(n * R, q, q_heads, D)).half()
+        logits = 2.5 * random(p.n_ctx * R, q, vocab)
+        target = torch.softmax(logits, -1)
+        draft = torch.softmax(logits[:, :drafts] + 0.6 * random(p.n_ctx * R, drafts, vocab), -1)
+        tokens = torch.multinomial(draft.view(-1, vocab), 1, generator=g).view(-1, drafts).int()
+        u = torch.rand((p.n_ctx * R, q), generator=g, device=device)
+        starts = lengths
+
+        def one():
+            cache.reserve(rows, starts, counts, refs, missing=missing)
+            cache.store(kn, vn, rows, starts)
+            return cache.attend_shared(qn, shared, shared_len, firsts, table=rows,
+                                       lengths=starts + q, max_shared=whole * PAGE,
+                                       max_len=tail + q * (step + 1), max_users=R)
+        out = _timed(torch, "step", times, one)
+        if step == 0:                              # compared on the last request
+            ref = _reference(torch, qn[-1:], torch.cat([x[-1:, 0], kn[-1:]], 1),
+                             torch.cat([x[-1:, 1], vn[-1:]], 1), T)
+            error = float((out[-1:].float() - ref).norm() / ref.norm())
+        # a request's layers go on together: verified once, cut back alike
+        _, accepted = _timed(torch, "verify", times, lambda: cache.verify(target, tokens, u,
+                                                                          draft=draft))
+        taken.append(accepted)
+        back = (drafts - accepted).view(p.n_ctx, 1, R).expand(-1, p.n_layers, -1).reshape(-1)
+        lengths = starts + q - back
+        _timed(torch, "release", times, lambda: cache.release(rows, refs, keep=lengths))
+    used = int((refs > 0).sum())
+    most = int(lengths.max())
+    # the requests end; what is left are the contexts, moved to the pool's front
+    cache.release(rows, refs)
+    table, refs, _, live = _timed(torch, "compact", times, lambda: cache.compact(table, refs))
+    k, _ = cache.load(table, start, T)
+    loaded = float((k.float() - x[:, 0].float()).norm() / x[:, 0].float().norm())
+    return {
+        "workload": w.name, "contexts": n, "requests": n * R, "tokens": T,
+        "ms": {name: round(sorted(t)[len(t) // 2], 4) for name, t in times.items()},
+        "accepted": float(torch.stack(taken).float().mean()), "missing": int(missing),
+        "pages": {"used": used, "unshared": n * R * (whole + -(-most // PAGE)),
+                  "after": int(live), "contexts": n * -(-T // PAGE)},
+        "rel_error_8bit": error, "rel_error_after": loaded,
+    }
+
+
 def main(argv=None):
     from paper_2310_07240_amd import workloads as W
     ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
@@ -152,9 +250,16 @@ def main(argv=None):
     ap.add_argument("--tokens", type=int, default=16)
     ap.add_argument("--keep", type=float, default=0.25)
     ap.add_argument("--picks", type=int, default=16)
+    ap.add_argument("--requests", type=int, default=0, help="answers over each context")
+    ap.add_argument("--drafts", type=int, default=4)
+    ap.add_argument("--steps", type=int, default=8)
+    ap.add_argument("--vocab", type=int, default=32000)
     a = ap.parse_args(argv)
     w = W.WORKLOADS[a.workload]
     for _ in range(2):                             # the first pass loads the kernels
+        if a.requests:
+            r = answer(w, a.heads, a.q_heads, a.requests, a.drafts, a.steps, a.vocab)
+            continue
         r = run(w, a.heads, a.q_heads, a.question, a.tokens, a.keep, a.picks)
     print(json.dumps(r), flush=True)
     return 0

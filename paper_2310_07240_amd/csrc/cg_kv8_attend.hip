@@ -1937,6 +1937,137 @@ struct JoinLds {
   float4v sums[256];
 };
 
+// kJoin of attend_kernel by a single wave: of a short answer three waves of four would have no page, and
+// hold their registers all the same (see one_wave).
+template <int D, bool BF16>
+__global__ __launch_bounds__(64, D == 256 ? 1 : 2) void own_join_kernel(KvPool pool, KvSeqs S, KvAttn A,
+                                                       KvUsers U, int tiles, int64_t items,
+                                                       ContextStates C, float* lse) {
+  __shared__ float os[16][D + 4];
+  __shared__ float ml[32], own_f[16], w[kMostSplits * 16];
+  const int lane = threadIdx.x, m = lane & 15, g = lane >> 4;
+  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const int tile = (int)(it % tiles);
+    const int64_t r = it / tiles;
+    const int h = (int)(r % pool.H);
+    const RowsOf R = rows_of(S, A, (int)(r / pool.H));
+    const int all = R.nq * A.group, rows = all - tile * 16 < 16 ? all - tile * 16 : 16;
+    const int most = R.most(tile * 16 / A.group, (tile * 16 + rows - 1) / A.group);
+    const int n = (most + kPage - 1) / kPage;
+    int at = 0;
+    const auto next_page = [&](int& j) -> int64_t {
+      while (j < n) {
+        at = j++;
+        const int page = kv_page(S, pool.P, R.seq, at);
+        if (page >= 0) return (int64_t)page * pool.H + h;
+      }
+      return -1;
+    };
+    int j = 0;
+    int64_t b = next_page(j);
+    KRegs<D> K;
+    VRegs<D> V;
+    if (b >= 0) {
+      load_k<D>(pool.k + b * (kPage * D), K);
+      load_v<D>(pool.v + b * (kPage * D), V);
+    }
+    QTile<D> Q;
+    load_q<D, BF16>(A, R, h, tile, Q);
+    int place = 0;
+    const int context = uniform(context_of(U, C.contexts, R.seq, place));
+    Acc<D> acc;
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) acc.o[dt] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+    acc.m = kNegInf;
+    acc.l = 0.0f;
+    while (b >= 0) {
+      const float ks = pool.ks[b], vs = pool.vs[b];
+      const int pos0 = at * kPage;
+      float x[16], keep;
+      half8 p[2];
+      const int64_t bn = next_page(j);
+      page_scores<D>(K, Q, x);
+      if (bn >= 0) load_k<D>(pool.k + bn * (kPage * D), K);
+      const float f = page_softmax<D>(x, ks, pos0, Q, acc, p, keep, nullptr);
+      page_values<D>(V, p, keep, f == 0.0f ? 0.0f : f * vs, acc);
+      if (bn >= 0) load_v<D>(pool.v + bn * (kPage * D), V);
+      b = bn;
+    }
+    acc.l = quad_sum(acc.l);
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt)
+      *reinterpret_cast<float4v*>(&os[m][16 * dt + 4 * g]) = acc.o[dt];
+    if (g == 0) {
+      ml[m] = acc.m;
+      ml[16 + m] = acc.l;
+    }
+    __syncthreads();
+    // four lanes a row find the factors of the context's states and of the own one
+    const int n0 = context >= 0 ? C.splits : 0, from = place * all + tile * 16;
+    const float* const s0 = C.part + ((int64_t)(context >= 0 ? context : 0) * pool.H + h) * C.tiles *
+                                         C.splits * kPart<D>;
+    const auto state = [&](int i, int x, int& in) -> const float* {
+      in = (from + x) & 15;
+      return s0 + ((int64_t)((from + x) >> 4) * C.splits + i) * kPart<D>;
+    };
+    const int row = lane >> 2, sub = lane & 3;
+    float top = sub == 0 ? ml[row] : kNegInf, l = sub == 0 ? ml[16 + row] : 0.0f;
+    if (row < rows) {
+      for (int i = sub; i < n0; i += 4) {
+        int in;
+        const float* const s = state(i, row, in);
+        const float2v x = *reinterpret_cast<const float2v*>(s + 16 * D + 2 * in);
+        w[i * 16 + row] = x[0];
+        const float both = fmaxf(top, x[0]), ref = both == kNegInf ? 0.0f : both;
+        l = l * __builtin_amdgcn_exp2f(top - ref) + x[1] * __builtin_amdgcn_exp2f(x[0] - ref);
+        top = both;
+      }
+    }
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) {
+      const float y = __shfl_xor(top, o), x = __shfl_xor(l, o);
+      const float both = fmaxf(top, y), ref = both == kNegInf ? 0.0f : both;
+      l = l * __builtin_amdgcn_exp2f(top - ref) + x * __builtin_amdgcn_exp2f(y - ref);
+      top = both;
+    }
+    if (row < rows) {
+      const float ref = top == kNegInf ? 0.0f : top, inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+      for (int i = sub; i < n0; i += 4)
+        w[i * 16 + row] = __builtin_amdgcn_exp2f(w[i * 16 + row] - ref) * inv;
+      if (sub == 0) {
+        own_f[row] = __builtin_amdgcn_exp2f(ml[row] - ref) * inv;
+        put_lse(A, R, pool.H, h, tile * 16 + row, lse, (top + __builtin_amdgcn_logf(l)) * kLn2);
+      }
+    }
+    __syncthreads();
+    constexpr int kAhead = 4;
+    for (int e = lane; e < rows * (D / 4); e += 64) {
+      const int x = e / (D / 4), d = e % (D / 4) * 4;
+      float4v o = *reinterpret_cast<const float4v*>(&os[x][d]);
+      const float f0 = own_f[x];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) o[c] *= f0;
+      for (int i0 = 0; i0 < n0; i0 += kAhead) {
+        float4v v[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          int in;
+          const float* const s = state(i0 + k < n0 ? i0 + k : n0 - 1, x, in);
+          v[k] = *reinterpret_cast<const float4v*>(s + in * D + d);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const float f = i0 + k < n0 ? w[(i0 + k) * 16 + x] : 0.0f;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) o[c] = __builtin_fmaf(v[k][c], f, o[c]);
+        }
+      }
+      put_out<D, BF16>(A, R, h, tile * 16 + x, d, reinterpret_cast<const float*>(&o), 4);
+    }
+    __syncthreads();
+  }
+}
+
 // A context's states alone: `few` rows a workgroup. Bound by the states' bytes.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void contexts_join_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U,
@@ -2110,6 +2241,13 @@ void shared_rows_d(const KvPool& pool, const KvSeqs& C, const KvAttn& CA, const 
     }
 }
 
+// Whether a wave alone takes a request's own tokens: few pages, or requests enough (one wave / four,
+// us, 8 heads of 128 channels, behind a context of 1000: 32 requests of a page 6.9 / 8.6, 128 8.9 / 17.7;
+// of 5 pages 64 requests 17.8 / 17.2, 128 21.4 / 30.6; of 16 pages 64 41 / 30, 128 50 / 57, 256 101 / 121;
+// 512 requests of 20 rows and a page 56 / 150. 64 channels, 4 pages: 64 10.2 / 9.8, 128 11.7 / 18.3; 256:
+// 64 23 / 27).
+bool one_wave(int64_t units, int max_len) { return max_len <= 2 * kPage || units >= 768; }
+
 template <int D, bool BF16>
 hipError_t shared_d(const KvPool& pool, const KvSeqs& C, const KvAttn& CA, const KvUsers& U,
                     const KvSeqs& S, const KvAttn& A, void* ws, hipStream_t st) {
@@ -2144,6 +2282,12 @@ hipError_t shared_d(const KvPool& pool, const KvSeqs& C, const KvAttn& CA, const
                        part0, nullptr, nullptr, nullptr, 0, ContextStates{});
   float* const part = reinterpret_cast<float*>(base + P.own_off);
   const int64_t units = (int64_t)S.n * pool.H * P.own.tiles;
+  if (P.joins && one_wave(units, A.max_len)) {
+    hipLaunchKernelGGL((own_join_kernel<D, BF16>), dim3(grid_of(units)), dim3(64), 0, st, pool, S, A,
+                       U, P.own.tiles, units, ContextStates{C.n, P.shared.tiles, splits0, part0},
+                       A.lse);
+    return hipGetLastError();
+  }
   if (P.joins) {
     hipLaunchKernelGGL((attend_kernel<D, BF16, RowsOf, kJoin>), dim3(grid_of(units)), dim3(256), 0,
                        st, pool, S, A, U, P.own.tiles, 1, units, nullptr, nullptr, A.lse, nullptr, 0,

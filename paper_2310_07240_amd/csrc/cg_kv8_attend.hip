@@ -1544,9 +1544,12 @@ void mass_rows_kernel(KvPool pool, KvSeqs S, KvAttn A, int np, int shares, int64
 //
 // RW of the workgroup's waves have 32 rows each. With half of them the others take the same rows, and
 // of every page the first tile of 32 tokens goes to the first half and the second to the other (32
-// requests of four heads a group, 16K tokens: 27.9 us, 29.5 with rows for all waves); the halves'
-// states meet in LDS. A split's pages are listed in LDS first, a column a thread, with their scales: a
-// chain of lookups would be as long as a page's products. (So a split has at most a column a thread.)
+// requests of four heads a group, 16K tokens: 29.5 -> 27.9 us); the halves' states meet in LDS. A split's
+// pages are listed in LDS first, a column a thread, with their scales: a chain of lookups would be as
+// long as a page's products. (So a split has at most a column a thread.) Those 32 requests take 25 us
+// now: 6 until the first products, 1.4 for each of a workgroup's 8 pages, where the vector instructions
+// bound (of the cycles there three in four), 3 for the halves and the states' way out. 448 queries over
+// four times 1500 tokens, 16 heads of 64 channels: 32 us, 340 TFLOP/s, bound by the exponentials.
 template <int D>
 struct PageList {
   static constexpr int kColumns = 64 * kPromptWaves<D>;
@@ -2261,7 +2264,9 @@ hipError_t shared_d(const KvPool& pool, const KvSeqs& C, const KvAttn& CA, const
     if (P.shared.big) {
       shared_rows_d<D, BF16>(pool, C, CA, U, P.shared, splits0 > 1 ? part0 : nullptr, A.lse, st);
       if (splits0 > 1) {
-        const int few = units0 < 1024 ? 4 : 16, groups = (CA.nq * CA.group + few - 1) / few;
+        // (16 rows a workgroup where that makes enough of them; 4 rows / 16, us with shared_kernel: 128
+        // rows of 8 heads in 32 splits 32.2 / 34.6, 200 of 32 heads and two contexts 52.8 / 49.0)
+        const int few = units0 < 512 ? 4 : 16, groups = (CA.nq * CA.group + few - 1) / few;
         const int64_t items = (int64_t)C.n * pool.H * groups;
         hipLaunchKernelGGL((contexts_join_kernel<D, BF16>), dim3(grid_of(items)), dim3(256), 0, st,
                            pool, C, CA, U, groups, few, splits0, items, part0, A.lse);
@@ -2322,9 +2327,12 @@ KvSharedPlan cg_kv8_shared_plan(const KvPool& pool, const KvSeqs& C, const KvAtt
   P.own_off = at;
   if (own) {
     P.own = cg_kv8_plan(pool, S, A, D);
-    // One launch for the own tokens and the join, where a wave has four pages of them at most or
-    // there would be one split anyway.
-    P.joins = !P.own.big && (P.own.splits == 1 || ((int64_t)A.max_len + kPage - 1) / kPage <= 16);
+    // One launch for the own tokens and the join, where a wave has two pages of them at most or there
+    // would be one split anyway (kernels' us with it / without, which costs another launch's 2; 8 heads
+    // of 128 channels behind a context of 1000: 8 requests of 5 pages 18.6 / 17.9, of 16 24.5 / 18.6, of
+    // 32 38.0 / 24.6; 32 requests of 5 pages behind 16K tokens 39.2 / 43.9).
+    P.joins = !P.own.big &&
+              (P.own.splits == 1 || ((int64_t)A.max_len + kPage - 1) / kPage <= 8);
     if (P.joins) P.own.splits = 0;     // (no states)
     at += (uint64_t)S.n * pool.H * P.own.tiles * P.own.splits * state;
   }
@@ -2364,13 +2372,20 @@ KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& S, const KvAttn& A, int
   const int64_t listed = D == 256 ? PageList<256>::kColumns : PageList<128>::kColumns;
   if (P.tiles > 2 && !little && !A.picks && (!shared || pages <= listed * kMostSplits)) {
     int per = D == 256 ? 32 * kPromptWaves<256> : 32 * kPromptWaves<128>;
+    // Of a shared context tiles of 128 rows by half of the waves, where those of all of them would not
+    // fill the card (128 / 256 rows, us: 448 queries over 4 x 1500 tokens, 16 heads of 64, 32.2 / 39.8 with
+    // the join that two splits need; 512 rows of 8 heads over 8K 44.2 / 47.8; 160 rows of 8 contexts and 32
+    // heads 168 / 131).
     P.halves = shared && D < 256 && vseqs * pool.H * ((rows + per - 1) / per) < 256;
     if (P.halves) per /= 2;
     // (shared_kernel lists a split's columns, one a thread)
     if (shared) at_least = (pages + listed - 1) / listed;
     P.big = (int)((rows + per - 1) / per);
     const int64_t groups = vseqs * pool.H * P.big;
-    s = (256 + groups - 1) / groups;
+    // Splits of a shared context: as many as the CUs hold at once, a workgroup each; one round more
+    // costs another prologue (rounded down / up, kernels' us: 3 contexts of 8K with 48 rows of 5 heads
+    // of 64 channels 28 / 37, 5 of 8K with 128 rows of 8 heads of 128 54 / 75, 20 of 4K 118 / 130).
+    s = shared ? 256 / groups : (256 + groups - 1) / groups;
     // a split has four pages at least (us with one, two, four and eight; 64 queries, 32 heads on 8 of
     // 128 channels: 5K tokens 41.2 40.9 38.7 36.9, twice 2.5K 32.2 32.2 33.1 34.2; of 64 channels, 5K
     // 28.5 28.5 24.9 25.4; of 256, 32 queries over 5K 55.0 54.9 47.4 48.1, 64 over 3K 44.9 44.9 43.8

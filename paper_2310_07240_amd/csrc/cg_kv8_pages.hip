@@ -153,7 +153,8 @@ struct Chunk {
 // ---- copies -----------------------------------------------------------------------------------
 // A page is copied in pieces of 16 KB of its codes, K's and then V's, a workgroup each, with four
 // 16-byte loads of a thread on their way together; the pieces share its scales, bounds and weights.
-// Bound by those bytes.
+// Bound by those bytes: 2048 pages of 8 heads of 128 channels, 554 MB read and written in 115 us, 4.8
+// TB/s (a copy of 1 GiB: 5.1).
 constexpr int kUnits = 1024;           // of 16 bytes, a piece
 
 __host__ __device__ inline int pieces_of(int H, int D) {
@@ -225,7 +226,8 @@ __device__ __forceinline__ int clamp_len(int64_t n, int width) {
   return n > 0 ? (int)n : 0;
 }
 
-// A workgroup = 256 columns of a row.
+// A workgroup = 256 columns of a row. Bound by the counts' additions (sharers of a page meet on it): 512
+// children of 66 pages 5.5 us, 8 of 16 2.9.
 __global__ __launch_bounds__(256) void fork_kernel(int P, KvSeqs S, const int32_t* lengths,
                                                    const int32_t* parents, const int32_t* ends,
                                                    int width, int per_row, int32_t* table,
@@ -360,7 +362,9 @@ __global__ __launch_bounds__(256) void list_kernel(int P, const int32_t* refs, R
 
 // All of the above in one workgroup. A thread takes a sequence's span of columns first; then the
 // spans' columns lie one after the other, a thread each, found by a search over the spans' sums in
-// LDS. Then the free pages, 16384 a step, until there are as many as wanted.
+// LDS. Then the free pages, 16384 a step, until there are as many as wanted. Bound by a chain of
+// dependent reads (lengths, table, counts) and the sums between them: 8 sequences of 256 pages 5.6 us,
+// 512 of 3500 7.0, 384 of 65536 10.9.
 constexpr int kPlanThreads = 1024, kPlanSeqs = 2048, kPlanPages = 16 * kPlanThreads;
 
 struct PlanLds {
@@ -458,7 +462,7 @@ __device__ __forceinline__ uint64_t bits_at(const uint64_t* w, int64_t at, int n
 }
 
 // Workgroup = (sequence, piece of a page): the first piece's first wave hands the pages out, all
-// pieces copy the sequence's shared page.
+// pieces copy the sequence's shared page. 512 copies of 135 KB from 32 pages 19 us, 66 MiB written.
 __global__ __launch_bounds__(256) void hand_out_kernel(KvPool pool, int D, int n, int width,
                                                        int32_t* table, const int32_t* lengths,
                                                        const int32_t* counts, int32_t* refs,
@@ -589,7 +593,8 @@ __global__ __launch_bounds__(kPlanThreads) void places_kernel(int P, const int32
   }
 }
 
-// The moves, and the table: workgroups 0 .. movers - 1 copy, the others rewrite entries.
+// The moves, and the table: workgroups 0 .. movers - 1 copy, the others rewrite entries. 1024 pages of
+// 8 heads of 128 channels, 266 MiB in 52 us, 5.3 TB/s.
 __global__ __launch_bounds__(256) void move_kernel(KvPool pool, int D, const int32_t* refs,
                                                    int64_t entries, const int32_t* table,
                                                    int32_t* new_table, int movers, int pieces,
@@ -715,6 +720,8 @@ hipError_t cg_launch_kv8_reserve(const KvPool& pool, int D, int n, int width, in
   uint64_t total;
   const Reserve R = reserve_of(ws, pool.P, n, width, &total);
   const int chunks = chunks_of(pool.P), words = words_of(width), pieces = pieces_of(pool.H, D);
+  // (65536 pages: one workgroup 10.8 us, two launches of many 17.6; a full pool costs the one 1.2 for
+  // every 16384 pages)
   if (pool.P <= 4 * kPlanPages && n <= kPlanSeqs && (int64_t)n * width <= 1 << 30) {
     hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, pool.P, n, width, table,
                        lengths, counts, refs, R, missing);
@@ -742,6 +749,8 @@ hipError_t cg_launch_kv8_compact(const KvPool& pool, const KvSeqs& S, int D, con
   uint64_t total;
   const Compact C = compact_of(ws, pool.P, &total);
   const int chunks = chunks_of(pool.P), pieces = pieces_of(pool.H, D);
+  // (as many pages as one workgroup has registers for the counts of: 4096 pages 4.9 us, 19.3 where the
+  // workgroups' counts meet in memory)
   if (pool.P <= kPlanPages) {
     hipLaunchKernelGGL(places_kernel, dim3(1), dim3(kPlanThreads), 0, st, pool.P, refs, C, moved,
                        new_refs, n_live);

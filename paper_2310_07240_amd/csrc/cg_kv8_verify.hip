@@ -10,8 +10,9 @@
 // Workgroup = (sequence, slices of 4096 probabilities of its row): each finds the row by itself (a
 // wave's lanes take a draft each), sums its slices, and the last of a sequence to arrive finds the
 // slice of the drawn token, reads it again, and the token in it. Bound by the row's bytes of p and q
-// where there are many sequences; a single one is a chain of dependent reads: count and drafts,
-// their probabilities, the row, the other slices' sums, the slice.
+// where there are many sequences: 64 of 131072 tokens, 62 MB in 20.5 us, 3.0 TB/s; a single one is a
+// chain of dependent reads: count and drafts, their probabilities, the row, the other slices' sums,
+// the slice (8.7 us of 32000 tokens).
 #include "cg_kv8.h"
 
 namespace {
@@ -362,6 +363,8 @@ __global__ __launch_bounds__(256) void verify_kernel(CgVerify A, int b0, int sli
   }
 }
 
+// Workgroups that the card holds at once, five a CU (64 sequences of 32 slices: 2048 workgroups 28 us,
+// 1024 of two slices each 20.5).
 constexpr int kAtOnce = 5 * 256;
 
 int slices_of(int vocab) { return (vocab + kSlice - 1) / kSlice; }

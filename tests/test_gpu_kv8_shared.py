@@ -216,6 +216,18 @@ def test_long_own_tokens():
     check(1, 1, 64, "float16", [100], [0, 1], 1, [1500], [70], 80, seed=12)
 
 
+def test_own_tokens_of_many_requests():
+    """A wave for a request's own tokens and its join: pages by the dozen, none, a part of one; and own
+    pages on both sides of where the waves of a workgroup take them."""
+    own = [(37 * i) % 300 for i in range(110)]
+    check(8, 2, 64, "float16", [150, 70], [0, 100, 109], 110, own, seed=20)
+    check(8, 1, 128, "bfloat16", [90], [0, 97], 97, [1 + (91 * i) % 260 for i in range(97)],
+          [(i % 4) for i in range(97)], 3, seed=21)
+    check(7, 1, 256, "float16", [66], [0, 110], 110, [(53 * i) % 200 for i in range(110)], seed=22)
+    for pages in (8, 9, 16, 17):
+        check(2, 4, 128, "float16", [200], [0, 3], 3, [64 * pages, 64 * pages - 63, 5], seed=pages)
+
+
 def test_many_rows_in_tiles():
     """More rows than a workgroup's: tiles of half and of all waves, with splits and without."""
     check(1, 4, 64, "float16", [500], [0, 40], 40, None, seed=13)

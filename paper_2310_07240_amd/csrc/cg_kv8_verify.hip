@@ -252,8 +252,10 @@ __global__ __launch_bounds__(256) void verify_kernel(CgVerify A, int b0, int sli
     const int at = i * kSlice;
     read_slice<K>(p, q, at, A.vocab, r);
     double sum = q ? sum_slice<K>(r, true) : sum_slice<K>(r, false);
-    if (threadIdx.x == 0 && skip >= at && skip < at + kSlice && skip < A.vocab)
-      sum -= lifted(Prob<K>::value(p[skip])) - 1536.0;   // (the wave's sum has it)
+    // (the thread whose sum has it: a wave's sum is never below 0)
+    if (skip >= at && skip < at + kSlice && skip < A.vocab &&
+        (skip - at) / N % 256 == (int)threadIdx.x)
+      sum -= lifted(Prob<K>::value(p[skip])) - 1536.0;
     const uint64_t part = wg_units(sum, L, i);
     if (threadIdx.x == 0) put_part(parts_of + i, part);
   }

@@ -66,6 +66,25 @@ def test_all_or_none_accepted():
     assert (accepted == 5).all()
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("vocab", [1056, 6000, 50257])
+def test_sure_drafts_that_hold_most_of_a_row(vocab, dtype):
+    """Sure drafts are the likeliest tokens: what they leave out of a row is more than what other parts
+    of it weigh, wherever in the row they lie."""
+    torch = torch_cuda()
+    target, _, _, u = case(torch, vocab, 61, 3, vocab, getattr(torch, dtype), sharp=3.0)
+    drafts = target[:, :3].argmax(-1).cpu().numpy().astype(np.int32)
+    _, accepted = check(torch, target, drafts, u)
+    assert (accepted < 3).any()
+    lone = torch.zeros_like(target)                # nearly all at the draft, a little elsewhere
+    at = torch.randint(0, vocab, (61, 4, 3), device="cuda",
+                       generator=torch.Generator(device="cuda").manual_seed(vocab))
+    lone.scatter_(2, at, 2.0 ** -9)
+    lone.scatter_(2, torch.from_numpy(drafts).cuda().long()[:, :1].expand(61, 4)[..., None], 0.75)
+    u[:, :3] = 0.9
+    check(torch, lone, np.repeat(drafts[:, :1], 3, 1), u)
+
+
 def test_values_that_are_no_probabilities():
     """NaN, infinities, negative values, values above 1, subnormals and zeros, in rows and at the
     drafts; rows without weight draw -1 or p's own."""

@@ -572,8 +572,8 @@ int cg_kv8_fork(const cg_kv8_cache* c, const cg_kv8_seqs* s, const int32_t* leng
                 const int32_t* parents, const int32_t* ends, const cg_kv8_seqs* to,
                 int32_t* new_lengths, int32_t* refs, hipStream_t stream);
 
-/* Device scratch of cg_kv8_reserve (bytes): 4 a sequence's columns and up to 4 a page. 0 if an
- * argument is invalid. */
+/* Device scratch of cg_kv8_reserve (bytes): 16 a sequence, two bits a column (in words of 64) and up
+ * to 4 a page, behind the zeroed front. 0 if an argument is invalid. */
 uint64_t cg_kv8_reserve_workspace_bytes(const cg_kv8_cache* c, const cg_kv8_seqs* s);
 
 /* Pages for tokens lengths[b] .. lengths[b] + counts[b] - 1 of every sequence (as far as its row of
@@ -602,7 +602,7 @@ int cg_kv8_release(const cg_kv8_cache* c, const cg_kv8_seqs* s, const int32_t* k
 int cg_kv8_copy(const cg_kv8_cache* c, const int32_t* src, const int32_t* dst, int32_t n,
                 hipStream_t stream);
 
-/* Device scratch of cg_kv8_compact (bytes), 8 a page. 0 if c is invalid. */
+/* Device scratch of cg_kv8_compact (bytes): 8 a page behind the zeroed front. 0 if c is invalid. */
 uint64_t cg_kv8_compact_workspace_bytes(const cg_kv8_cache* c);
 
 /* The pages in use (count above 0) move to the front of the pool: with L of them, the i-th that lies

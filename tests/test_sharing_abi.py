@@ -139,11 +139,12 @@ def test_attention_without_own_pages():
                                   BIG, None) == -1
     assert l.cg_kv8_attend_shared(cache(), contexts(lengths=None), none, attn(), FAKE, BIG, None) == -1
     assert l.cg_kv8_attend_shared(cache(), contexts(), seqs(0, 0, None), attn(), FAKE, BIG, None) == -2
-    # scratch for both is more than for the contexts alone
+    # short own tokens are joined where they are read; long ones have states, and scratch, of their own
     x = contexts(seqs=seqs(2, 100), max_len=6400)
     own = l.cg_kv8_attend_shared_workspace_bytes(cache(), x, seqs(), attn())
     alone = l.cg_kv8_attend_shared_workspace_bytes(cache(), x, none, attn(lengths=None))
-    assert own > alone > kv8.ZEROED
+    long = l.cg_kv8_attend_shared_workspace_bytes(cache(), x, seqs(2, 100), attn(max_len=6400))
+    assert long > own >= alone > kv8.ZEROED
     assert l.cg_kv8_attend_shared(cache(), x, none, attn(), FAKE, alone - 1, None) == kv8_code("CAPACITY")
     assert l.cg_kv8_attend_shared(cache(), x, none, attn(), None, BIG, None) == -1
 

@@ -10,9 +10,9 @@
 // Workgroup = (sequence, slices of 4096 probabilities of its row): each finds the row by itself (a
 // wave's lanes take a draft each), sums its slices, and the last of a sequence to arrive finds the
 // slice of the drawn token, reads it again, and the token in it. Bound by the row's bytes of p and q
-// where there are many sequences: 64 of 131072 tokens, 62 MB in 20.5 us, 3.0 TB/s; a single one is a
+// where there are many sequences: 64 of 131072 tokens, 62 MB in 20.0 us, 3.1 TB/s; a single one is a
 // chain of dependent reads: count and drafts, their probabilities, the row, the other slices' sums,
-// the slice (8.7 us of 32000 tokens).
+// the slice (8.8 us of 32000 tokens).
 #include "cg_kv8.h"
 
 namespace {
@@ -178,23 +178,19 @@ __device__ __forceinline__ double sum_slice(const SliceRegs<K>& r, bool with_q) 
   return sum;
 }
 
-// A thread's weights of one chunk, whose first probability is e: of p over q, or (q null) of p, of
-// which the token `skip` has none.
+// A thread's weights of chunk c, whose first probability is e: of p over q, or of p, of which the token
+// `skip` has none.
 template <Kind K>
 struct ChunkWeights {
-  typedef typename Prob<K>::Raw Raw;
-  static constexpr int N = 16 / sizeof(Raw);
+  static constexpr int N = SliceRegs<K>::N;
   uint64_t w[N], sum;
 
-  __device__ __forceinline__ ChunkWeights(const Raw* p, const Raw* q, int e, int vocab, int skip) {
-    Sixteen<Raw> x, y;
-    read_some(p, e, vocab, x);
-    if (q) read_some(q, e, vocab, y);
+  __device__ __forceinline__ ChunkWeights(const SliceRegs<K>& r, int c, bool with_q, int e, int skip) {
     sum = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      int64_t d = units(Prob<K>::value(x.x[i]));
-      if (q) d -= units(Prob<K>::value(y.x[i]));
+      int64_t d = units(Prob<K>::value(r.p[c].x[i]));
+      if (with_q) d -= units(Prob<K>::value(r.q[c].x[i]));
       w[i] = d > 0 && e + i != skip ? d : 0;
       sum += w[i];
     }
@@ -332,24 +328,29 @@ __global__ __launch_bounds__(256) void verify_kernel(CgVerify A, int b0, int sli
     }
     __syncthreads();
     uint64_t base = 0;
-#pragma unroll 1
-    for (int c = 0; c < 4 * C; ++c) {
-      const uint64_t total = L.part[0][c];
-      if (left < base + total) {
-        // (chunk, wave) c has it: the lane, then the token
-        if (wave == (c & 3)) {
-          const int e = at + ((c >> 2) * 256 + (int)threadIdx.x) * N;
-          const ChunkWeights<K> x(p, q, e, A.vocab, skip);
-          uint64_t from = base + wave_scan(x.sum) - x.sum;
 #pragma unroll
-          for (int i = 0; i < N; ++i) {
-            if (left >= from && left < from + x.w[i]) L.token = e + i;
-            from += x.w[i];
-          }
+    for (int c = 0; c < C; ++c) {
+      uint64_t of_wave = 0, mine = 0;              // this wave's sum, and those before it
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const uint64_t total = L.part[0][c * 4 + w];
+        if (w == wave) {
+          mine = base;
+          of_wave = total;
         }
-        break;
+        base += total;
       }
-      base += total;
+      if (left >= mine && left < mine + of_wave) {
+        // (chunk, wave) has it: the lane, then the token
+        const int e = at + (c * 256 + (int)threadIdx.x) * N;
+        const ChunkWeights<K> x(r, c, q != nullptr, e, skip);
+        uint64_t from = mine + wave_scan(x.sum) - x.sum;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          if (left >= from && left < from + x.w[i]) L.token = e + i;
+          from += x.w[i];
+        }
+      }
     }
     __syncthreads();
   }

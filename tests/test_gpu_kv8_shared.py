@@ -250,3 +250,27 @@ def test_room_for_more_requests_than_there_are():
     for n, firsts, most in ((3, [0, 1, 3], 3), (400, [0, 390, 400], 400), (60, [0, 2, 60], 60)):
         check(1, 4, 64, "float16", [130, 64], firsts, n, None, seed=18, max_users=most)
         check(1, 4, 64, "float16", [130, 64], firsts, n, [2] * n, None, 2, seed=19, max_users=most)
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("users,Q", [(3, 1), (40, 1), (9, 30)])
+@pytest.mark.parametrize("own", [True, False])
+def test_queries_that_are_no_numbers(own, users, Q, dtype):
+    """NaN or Inf in one request's queries reach no other request (rows of one tile among them)."""
+    torch = torch_cuda()
+    H, D = 2, 128
+    cache = make(torch, 10 + users, H, D)
+    q = torch.randn(users, Q, 2 * H, D, device="cuda").to(getattr(torch, dtype))
+    args = ints(torch, [list(range(9))]), ints(torch, [570]), ints(torch, [0, users])
+    more = {"table": ints(torch, [[10 + i] for i in range(users)]),
+            "lengths": ints(torch, [Q + 3] * users)} if own else {}
+    want = cache.attend_shared(q, *args, **more).float()
+    for value in (float("nan"), float("inf")):
+        bad = q.clone()
+        bad[1, Q - 1, 1, 5] = value
+        got = cache.attend_shared(bad, *args, **more).float()
+        assert bool(got[1, Q - 1, 1].isnan().any())
+        got[1, Q - 1, 1] = want[1, Q - 1, 1]
+        # both are within half a step and the weights' rounding of the same value
+        most = (4 * 2.0 ** -11 + 2 * UNIT[dtype]) * float(want.abs().max())
+        assert float((got - want).abs().max()) <= most

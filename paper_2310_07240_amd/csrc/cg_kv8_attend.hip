@@ -2368,7 +2368,14 @@ KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& S, const KvAttn& A, int
   // 11.5 / 14.0, 24 17.8 / 14.3. 4 heads, group 8, 256 channels, 2K: 32 32.7 / 34.7, 48 38.8 / 36.8.)
   // Every query token with pages of its own is a tile or more to itself.
   const int64_t at_once = D == 64 ? 768 : D == 128 ? 512 : 256;
-  const bool little = units <= at_once && units * pages <= (D == 256 ? 2048 : 8192);
+  // Of a shared context of 128 channels 64 rows or fewer leave shared_kernel a wave's work on each SIMD;
+  // where its splits of four pages fill the card, it is ahead in such calls too (both, kernels' us with
+  // the own tokens; 8 heads: 48 rows of two contexts of 4K 27.4 / 23.0, of one of 16K 37.3 / 34.7, 64
+  // rows of 8K 26.0 / 24.6, 60 of 16 heads and two of 4K 33.2 / 28.8; 80 rows of 8K 30.4 / 32.5, 128
+  // 34.3 / 41.3; of 64 channels, 64 rows of 8K 21.8 / 19.2, 48 of four of 2K 15.2 / 16.5, of 30K 30.4 /
+  // 32.3).
+  const bool fills = shared && D == 128 && rows <= 64 && vseqs * pool.H * (pages / 4) >= 256;
+  const bool little = !fills && units <= at_once && units * pages <= (D == 256 ? 2048 : 8192);
   P.big = 0;
   P.halves = false;
   int64_t s, most, at_least = 1;

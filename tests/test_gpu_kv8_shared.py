@@ -234,6 +234,8 @@ def test_many_rows_in_tiles():
     check(2, 4, 128, "bfloat16", [700, 130], [0, 33, 70], 71, [9] * 71, None, 2, seed=14)
     check(8, 1, 64, "float16", [130] * 17, list(range(18)), 17, None, None, 270, seed=15)
     check(1, 2, 256, "float16", [900], [0, 80], 80, [3] * 80, seed=16)
+    # few rows, of which two waves of a half have some, of contexts that fill the card
+    check(8, 4, 128, "float16", [500] * 15 + [449], list(range(0, 161, 10)), 160, [3] * 160, seed=23)
 
 
 def test_logits_far_apart():

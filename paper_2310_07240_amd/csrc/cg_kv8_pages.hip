@@ -10,6 +10,8 @@
 // is written and read past the XCDs' own caches (agent scope).
 #include "cg_kv8.h"
 
+#include <type_traits>
+
 namespace {
 
 constexpr int kRounds = 16, kChunk = 256 * kRounds;   // (of a workgroup of 256)
@@ -153,7 +155,7 @@ struct Chunk {
 // ---- copies -----------------------------------------------------------------------------------
 // A page is copied in pieces of 16 KB of its codes, K's and then V's, a workgroup each, with four
 // 16-byte loads of a thread on their way together; the pieces share its scales, bounds and weights.
-// Bound by those bytes: 2048 pages of 8 heads of 128 channels, 554 MB read and written in 115 us, 4.8
+// Bound by those bytes: 2048 pages of 8 heads of 128 channels, 554 MB read and written in 113 us, 4.9
 // TB/s (a copy of 1 GiB: 5.1).
 constexpr int kUnits = 1024;           // of 16 bytes, a piece
 
@@ -161,19 +163,33 @@ __host__ __device__ inline int pieces_of(int H, int D) {
   return (int)(((int64_t)8 * H * D + kUnits - 1) / kUnits);
 }
 
+// More of them than the L2s hold are read and written past the caches (without / with, whole calls, us:
+// 2048 pages 115.3 / 113.5, 1024 of a compaction 67.9 / 60.0; with few it is slower, 70 pages of 40 KB
+// 7.5 / 8.4). Copies of a shared page are only written past them: its readers then find it there (512
+// copies of 32 pages, with the calls around them, 45.2 / 35.6; read past them too 49.6).
+__device__ __forceinline__ bool past_caches(int64_t items) {
+  return items > (32 << 20) / (16 * kUnits);
+}
+
+// loads_past, stores_past: nontemporal accesses to the codes.
 __device__ __forceinline__ void copy_piece(const KvPool& pool, int D, int src, int dst, int piece,
-                                           int pieces) {
+                                           int pieces, bool loads_past, bool stores_past) {
   const int64_t half = (int64_t)4 * pool.H * D;                // 16-byte units of K (and of V)
   const uint4v* k = reinterpret_cast<const uint4v*>(pool.k);
   const uint4v* v = reinterpret_cast<const uint4v*>(pool.v);
   uint4v x[kUnits / 256];
   const int64_t u0 = (int64_t)piece * kUnits + threadIdx.x;
+  const auto read = [&](auto past) {
 #pragma unroll
-  for (int i = 0; i < kUnits / 256; ++i) {
-    const int64_t u = u0 + 256 * i;
-    if (u < half) x[i] = k[src * half + u];
-    else if (u < 2 * half) x[i] = v[src * half + u - half];
-  }
+    for (int i = 0; i < kUnits / 256; ++i) {
+      const int64_t u = u0 + 256 * i;
+      if (u >= 2 * half) continue;
+      const uint4v* const from = u < half ? k + src * half + u : v + src * half + u - half;
+      x[i] = decltype(past)::value ? __builtin_nontemporal_load(from) : *from;
+    }
+  };
+  if (loads_past) read(std::true_type{});
+  else read(std::false_type{});
   // words of the scales, the bounds and the weights
   const int H = pool.H, nb = pool.bounds ? H * (D / 2) : 0, nm = pool.mass ? H * kPage : 0;
   uint32_t* const bounds = reinterpret_cast<uint32_t*>(pool.bounds);
@@ -192,21 +208,28 @@ __device__ __forceinline__ void copy_piece(const KvPool& pool, int D, int src, i
   }
   uint4v* const k_to = reinterpret_cast<uint4v*>(pool.k);
   uint4v* const v_to = reinterpret_cast<uint4v*>(pool.v);
+  const auto write = [&](auto past) {
 #pragma unroll
-  for (int i = 0; i < kUnits / 256; ++i) {
-    const int64_t u = u0 + 256 * i;
-    if (u < half) k_to[dst * half + u] = x[i];
-    else if (u < 2 * half) v_to[dst * half + u - half] = x[i];
-  }
+    for (int i = 0; i < kUnits / 256; ++i) {
+      const int64_t u = u0 + 256 * i;
+      if (u >= 2 * half) continue;
+      uint4v* const to = u < half ? k_to + dst * half + u : v_to + dst * half + u - half;
+      if (decltype(past)::value) __builtin_nontemporal_store(x[i], to);
+      else *to = x[i];
+    }
+  };
+  if (stores_past) write(std::true_type{});
+  else write(std::false_type{});
 }
 
 __global__ __launch_bounds__(256) void copy_kernel(KvPool pool, int D, const int32_t* src,
                                                    const int32_t* dst, int pieces, int64_t items) {
+  const bool past = past_caches(items);
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const int64_t i = it / pieces;
     const int a = src[i], b = dst[i];
     if (a >= 0 && a < pool.P && b >= 0 && b < pool.P && a != b)
-      copy_piece(pool, D, a, b, (int)(it % pieces), pieces);
+      copy_piece(pool, D, a, b, (int)(it % pieces), pieces, past, past);
   }
 }
 
@@ -462,7 +485,7 @@ __device__ __forceinline__ uint64_t bits_at(const uint64_t* w, int64_t at, int n
 }
 
 // Workgroup = (sequence, piece of a page): the first piece's first wave hands the pages out, all
-// pieces copy the sequence's shared page. 512 copies of 135 KB from 32 pages 19 us, 66 MiB written.
+// pieces copy the sequence's shared page. 512 copies of 135 KB from 32 pages 17 us, 66 MiB written.
 __global__ __launch_bounds__(256) void hand_out_kernel(KvPool pool, int D, int n, int width,
                                                        int32_t* table, const int32_t* lengths,
                                                        const int32_t* counts, int32_t* refs,
@@ -473,7 +496,7 @@ __global__ __launch_bounds__(256) void hand_out_kernel(KvPool pool, int D, int n
     const int b = (int)(it / pieces), piece = (int)(it % pieces);
     const int source = R.source[b];
     int rank = R.need[b];                              // (of no use where nothing is wanted)
-    if (source >= 0) copy_piece(pool, D, source, R.list[rank], piece, pieces);
+    if (source >= 0) copy_piece(pool, D, source, R.list[rank], piece, pieces, false, true);
     if (piece != 0 || threadIdx.x >= 64) continue;
     const Span s = span_of(lengths, counts, width, b);
     for (int j0 = s.first; j0 < s.last; j0 += 64) {
@@ -594,17 +617,18 @@ __global__ __launch_bounds__(kPlanThreads) void places_kernel(int P, const int32
 }
 
 // The moves, and the table: workgroups 0 .. movers - 1 copy, the others rewrite entries. 1024 pages of
-// 8 heads of 128 channels, 266 MiB in 52 us, 5.3 TB/s.
+// 8 heads of 128 channels, 266 MiB in 51 us, 5.4 TB/s.
 __global__ __launch_bounds__(256) void move_kernel(KvPool pool, int D, const int32_t* refs,
                                                    int64_t entries, const int32_t* table,
                                                    int32_t* new_table, int movers, int pieces,
                                                    Compact C, int32_t* moved, int32_t* new_refs) {
   if ((int)blockIdx.x < movers) {
     const int64_t items = (int64_t)C.state[2] * pieces;
+    const bool past = past_caches(items);
     for (int64_t it = blockIdx.x; it < items; it += movers) {
       const int i = (int)(it / pieces), piece = (int)(it % pieces);
       const int src = C.late[i], dst = C.holes[i];
-      copy_piece(pool, D, src, dst, piece, pieces);
+      copy_piece(pool, D, src, dst, piece, pieces, past, past);
       if (piece == 0 && threadIdx.x == 0) {
         moved[src] = dst;
         new_refs[dst] = refs[src];

@@ -508,8 +508,9 @@ uint64_t cg_kv8_attend_workspace_bytes(const cg_kv8_cache* c, const cg_kv8_seqs*
  * rounded to fp16, 2^-11 of a weight, down to 2^-29 of the heaviest in its page where there are few
  * rows, and to 2^-25 of the row's heaviest (lighter ones are off by 2^-36 of it at most) where there
  * are many; there, pages whose V scale is below 2^-60 of the sequence's largest, or subnormal, may
- * add nothing to `out`. Which of the two a call takes follows its sizes and max_len. Results do not
- * depend on the order in which parts of the work end.
+ * add nothing to `out`. Where there are few rows, values are summed with weights of up to 1 before they
+ * are divided: the largest |V| times the tokens has to stay below 2^127. Which of the two a call takes
+ * follows its sizes and max_len. Results do not depend on the order in which parts of the work end.
  *   workspace   device scratch of workspace_bytes >= cg_kv8_attend_workspace_bytes, 256-byte
  *               aligned (may be NULL where that is 0), its first CG_KV8_WORKSPACE_ZEROED bytes
  *               zero.

@@ -1822,11 +1822,17 @@ void shared_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, int splits, int t
   float sum = l * to_top + (some0 ? l0 * __builtin_amdgcn_exp2f(ref0 - top) : 0.0f);
   top = empty ? kNegInf : top;
   sum = empty ? 0.0f : sum;
+  // The sum goes to [1/2, 1) by a power of two before O gets the V scales' own: then O is at most the
+  // largest |V|, and a number wherever the result is one. (The weights' unit is 2^-kLift, and there are
+  // as many as tokens: of V at 1e33 their sum would pass 32 bits.)
+  const int by = __builtin_amdgcn_frexp_expf(sum);               // (0 of 0)
+  top += (float)by;
+  sum = __builtin_ldexpf(sum, -by);
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
     for (int e = 0; e < 16; ++e)
-      o[dt][e] = empty ? 0.0f : __builtin_ldexpf(o[dt][e] * to_top, v_exp);
+      o[dt][e] = empty ? 0.0f : __builtin_ldexpf(o[dt][e] * to_top, v_exp - by);
   float* const space = reinterpret_cast<float*>(&L);
   float (*const all)[D + 4] = reinterpret_cast<float (*)[D + 4]>(space);       // halves: [32 RW]
   if constexpr (TW == 2) {
@@ -1846,9 +1852,11 @@ void shared_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, int splits, int t
     if (!side) {
       const float2v other = ml[m];
       const float both = fmaxf(top, other[0]), base = both == kNegInf ? 0.0f : both;
-      float f0 = __builtin_amdgcn_exp2f(top - base), f1 = __builtin_amdgcn_exp2f(other[0] - base);
+      // (halved, so that the sum stays below 1)
+      float f0 = 0.5f * __builtin_amdgcn_exp2f(top - base);
+      float f1 = 0.5f * __builtin_amdgcn_exp2f(other[0] - base);
       sum = sum * f0 + other[1] * f1;
-      top = both;
+      top = both + 1.0f;
       if (!part) {
         const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
         f0 *= inv;

@@ -585,11 +585,22 @@ uint64_t cg_kv8_reserve_workspace_bytes(const cg_kv8_cache* c, const cg_kv8_seqs
  * replaces goes down by one. Sequences of one call that share a page get a copy each, and pages that
  * they all leave are free behind the call, not in it.
  *   s        its table is written.
- *   missing  out [1]: 0, or how many pages more it would have taken; then nothing is changed.
+ *   missing  out [1]: 0, or how many pages more it would have taken; then nothing is changed, and
+ *            nothing may be stored: the pages may be others' too (see cg_kv8_reserve_granted).
  *   workspace as for cg_kv8_attend. */
 int cg_kv8_reserve(const cg_kv8_cache* c, const cg_kv8_seqs* s, const int32_t* lengths,
                    const int32_t* counts, int32_t* refs, int32_t* missing, void* workspace,
                    uint64_t workspace_bytes, hipStream_t stream);
+
+/* The same, and how many tokens each sequence may store behind lengths[b]:
+ *   granted  out [n_seq], or NULL: of counts[b] those that its row has room for, 0 of all sequences
+ *            where pages were missing. As the counts of the cg_kv8_store that follows, and added to
+ *            the lengths, they keep a call that found too few pages from writing to shared ones,
+ *            without the host. May be counts. */
+int cg_kv8_reserve_granted(const cg_kv8_cache* c, const cg_kv8_seqs* s, const int32_t* lengths,
+                           const int32_t* counts, int32_t* refs, int32_t* missing,
+                           int32_t* granted, void* workspace, uint64_t workspace_bytes,
+                           hipStream_t stream);
 
 /* Gives back the pages of every sequence from column ceil(keep[b] / 64) on (keep NULL: all): their
  * counts go down by one (never below 0), the entries become -1. What the pages hold stays until

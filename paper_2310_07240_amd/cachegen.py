@@ -31,7 +31,8 @@ EXPORTS = ("cg_num_chunks", "cg_num_streams", "cg_encode_bound_words",
            "cg_fit_cdf_levels", "cg_encode_with_scales", "cg_strerror",
            "cg_kv8_store", "cg_kv8_load", "cg_kv8_attend_workspace_bytes", "cg_kv8_attend",
            "cg_kv8_select_workspace_bytes", "cg_kv8_select", "cg_kv8_evict",
-           "cg_kv8_fork", "cg_kv8_reserve_workspace_bytes", "cg_kv8_reserve", "cg_kv8_release",
+           "cg_kv8_fork", "cg_kv8_reserve_workspace_bytes", "cg_kv8_reserve",
+           "cg_kv8_reserve_granted", "cg_kv8_release",
            "cg_kv8_copy", "cg_kv8_compact_workspace_bytes", "cg_kv8_compact",
            "cg_kv8_attend_shared_workspace_bytes", "cg_kv8_attend_shared",
            "cg_verify_workspace_bytes", "cg_verify_drafts")   # bound in kv8

@@ -422,7 +422,7 @@ hipError_t cg_launch_kv8_fork(const KvPool&, const KvSeqs&, const int32_t* lengt
 uint64_t cg_kv8_reserve_ws(int P, int n, int width);
 hipError_t cg_launch_kv8_reserve(const KvPool&, int D, int n, int width, int32_t* table,
                                  const int32_t* lengths, const int32_t* counts, int32_t* refs,
-                                 int32_t* missing, void* ws, hipStream_t);
+                                 int32_t* missing, int32_t* granted, void* ws, hipStream_t);
 hipError_t cg_launch_kv8_release(const KvPool&, int n, int width, int32_t* table,
                                  const int32_t* keep, int32_t* refs, hipStream_t);
 hipError_t cg_launch_kv8_copy(const KvPool&, int D, const int32_t* src, const int32_t* dst, int n,

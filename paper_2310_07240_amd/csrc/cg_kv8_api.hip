@@ -311,18 +311,27 @@ uint64_t cg_kv8_reserve_workspace_bytes(const cg_kv8_cache* c, const cg_kv8_seqs
 int cg_kv8_reserve(const cg_kv8_cache* c, const cg_kv8_seqs* s, const int32_t* lengths,
                    const int32_t* counts, int32_t* refs, int32_t* missing, void* workspace,
                    uint64_t workspace_bytes, hipStream_t stream) {
+  return cg_kv8_reserve_granted(c, s, lengths, counts, refs, missing, nullptr, workspace,
+                                workspace_bytes, stream);
+}
+
+int cg_kv8_reserve_granted(const cg_kv8_cache* c, const cg_kv8_seqs* s, const int32_t* lengths,
+                           const int32_t* counts, int32_t* refs, int32_t* missing,
+                           int32_t* granted, void* workspace, uint64_t workspace_bytes,
+                           hipStream_t stream) {
   KvPool pool;
   KvSeqs S;
   int rc = check_cache(c, &pool);
   if (rc == CG_OK) rc = check_seqs(s, pool, &S);
   if (rc != CG_OK) return rc;
-  if (bad_ints(lengths) || bad_ints(counts) || bad_ints(refs) || bad_ints(missing))
+  if (bad_ints(lengths) || bad_ints(counts) || bad_ints(refs) || bad_ints(missing) ||
+      !aligned(granted, 4))
     return CG_ERR_ARG;
   rc = check_workspace(workspace, workspace_bytes, cg_kv8_reserve_ws(pool.P, S.n, S.width));
   if (rc != CG_OK) return rc;
   return hip_rc(cg_launch_kv8_reserve(pool, c->head_dim, S.n, S.width,
                                       const_cast<int32_t*>(S.table), lengths, counts, refs, missing,
-                                      workspace, stream));
+                                      granted, workspace, stream));
 }
 
 int cg_kv8_release(const cg_kv8_cache* c, const cg_kv8_seqs* s, const int32_t* keep, int32_t* refs,

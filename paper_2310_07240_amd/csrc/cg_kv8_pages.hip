@@ -293,8 +293,8 @@ struct Reserve {
   int32_t* list;                     // [at most P] the free pages in order
 };
 
-struct Span {                        // columns that a sequence will write to
-  int first, last, start;            // (last: one behind)
+struct Span {                        // columns that a sequence will write to, and tokens
+  int first, last, start, end;       // (last, end: one behind)
 };
 
 __device__ __forceinline__ Span span_of(const int32_t* lengths, const int32_t* counts, int width,
@@ -303,6 +303,7 @@ __device__ __forceinline__ Span span_of(const int32_t* lengths, const int32_t* c
   const int64_t end = clamp_len((int64_t)start + (counts[b] > 0 ? counts[b] : 0), width);
   Span s;
   s.start = start;
+  s.end = (int)end;
   s.first = start / kPage;
   s.last = end > start ? (int)((end + kPage - 1) / kPage) : s.first;
   return s;
@@ -411,7 +412,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(int P, int n, int wi
   int cols = 0, total;
   for (int b0 = 0; b0 < n; b0 += kPlanThreads) {
     const int b = b0 + tid;
-    Span s = {0, 0, 0};
+    Span s = {0, 0, 0, 0};
     if (b < n) s = span_of(lengths, counts, width, b);
     const int at = cols + scan_wg<kPlanThreads>(s.last - s.first, L.sums, total);
     if (b < n) {
@@ -484,21 +485,27 @@ __device__ __forceinline__ uint64_t bits_at(const uint64_t* w, int64_t at, int n
   return n < 64 ? x & ((1ull << n) - 1) : x;
 }
 
-// Workgroup = (sequence, piece of a page): the first piece's first wave hands the pages out, all
-// pieces copy the sequence's shared page. 512 copies of 135 KB from 32 pages 17 us, 66 MiB written.
+// Workgroup = (sequence, piece of a page): the first piece's first wave hands the pages out and says
+// what the sequence may store, all pieces copy the sequence's shared page. 512 copies of 135 KB from 32 pages 17 us, 66 MiB written.
 __global__ __launch_bounds__(256) void hand_out_kernel(KvPool pool, int D, int n, int width,
                                                        int32_t* table, const int32_t* lengths,
                                                        const int32_t* counts, int32_t* refs,
-                                                       int pieces, int64_t items, Reserve R) {
+                                                       int32_t* granted, int pieces, int64_t items,
+                                                       Reserve R) {
   const int lane = threadIdx.x & 63, wanted = *R.state;
-  if (wanted <= 0) return;
+  if (wanted <= 0 && !granted) return;
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const int b = (int)(it / pieces), piece = (int)(it % pieces);
-    const int source = R.source[b];
-    int rank = R.need[b];                              // (of no use where nothing is wanted)
-    if (source >= 0) copy_piece(pool, D, source, R.list[rank], piece, pieces, false, true);
+    int rank = 0;
+    if (wanted > 0) {
+      const int source = R.source[b];
+      rank = R.need[b];                                // (of no use where nothing is wanted)
+      if (source >= 0) copy_piece(pool, D, source, R.list[rank], piece, pieces, false, true);
+    }
     if (piece != 0 || threadIdx.x >= 64) continue;
     const Span s = span_of(lengths, counts, width, b);
+    if (granted && lane == 0) granted[b] = wanted >= 0 ? s.end - s.start : 0;
+    if (wanted <= 0) continue;
     for (int j0 = s.first; j0 < s.last; j0 += 64) {
       const int64_t at = R.bits[b] + (j0 - s.first);
       const int left = s.last - j0;
@@ -740,7 +747,7 @@ uint64_t cg_kv8_reserve_ws(int P, int n, int width) {
 
 hipError_t cg_launch_kv8_reserve(const KvPool& pool, int D, int n, int width, int32_t* table,
                                  const int32_t* lengths, const int32_t* counts, int32_t* refs,
-                                 int32_t* missing, void* ws, hipStream_t st) {
+                                 int32_t* missing, int32_t* granted, void* ws, hipStream_t st) {
   uint64_t total;
   const Reserve R = reserve_of(ws, pool.P, n, width, &total);
   const int chunks = chunks_of(pool.P), words = words_of(width), pieces = pieces_of(pool.H, D);
@@ -757,7 +764,7 @@ hipError_t cg_launch_kv8_reserve(const KvPool& pool, int D, int n, int width, in
   }
   const int64_t items = (int64_t)n * pieces;
   hipLaunchKernelGGL(hand_out_kernel, dim3(grid_of(items)), dim3(256), 0, st, pool, D, n, width,
-                     table, lengths, counts, refs, pieces, items, R);
+                     table, lengths, counts, refs, granted, pieces, items, R);
   return hipGetLastError();
 }
 

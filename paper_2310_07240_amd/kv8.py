@@ -93,6 +93,7 @@ def _lib():
         L.cg_kv8_reserve_workspace_bytes.argtypes = [_P, _P]
         L.cg_kv8_reserve_workspace_bytes.restype = U64
         L.cg_kv8_reserve.argtypes = [_P, _P, _P, _P, _P, _P, _P, U64, _P]
+        L.cg_kv8_reserve_granted.argtypes = [_P, _P, _P, _P, _P, _P, _P, _P, U64, _P]
         L.cg_kv8_release.argtypes = [_P, _P, _P, _P, _P]
         L.cg_kv8_copy.argtypes = [_P, _P, _P, _I32, _P]
         L.cg_kv8_compact_workspace_bytes.argtypes = [_P]
@@ -105,7 +106,7 @@ def _lib():
         L.hipStreamIsCapturing.argtypes = [_P, _P]        # of the runtime that the library links
         L.hipStreamIsCapturing.restype = ctypes.c_int
         for n in ("store", "load", "attend", "select", "evict", "attend_shared", "fork", "reserve",
-                  "release", "copy", "compact"):
+                  "reserve_granted", "release", "copy", "compact"):
             getattr(L, "cg_kv8_" + n).restype = ctypes.c_int
         _LIB = L
     return _LIB
@@ -446,13 +447,19 @@ class Kv8Cache:
                      self._per_seq(ends, "ends", m), to, new_p, self._refs(refs))
         return new_table, new_lengths
 
-    def reserve(self, table, lengths, counts, refs, mass=None, missing=None, stream=None):
+    def reserve(self, table, lengths, counts, refs, mass=None, missing=None, granted=None,
+                stream=None):
         """Pages for ``counts[i]`` tokens behind the ``lengths[i]`` that sequence i holds, for a
         ``store`` that follows: free ones (lowest number first) where its row of ``table`` has none
         of its own, and a copy of a page that it shares and would write to. ``table`` and ``refs``
         are updated. Returns ``missing`` (int32 [1]): 0, or how many free pages too few there are;
-        then nothing has changed, and the sequences must not be written to. ``mass``: weights that
-        go with a copied page."""
+        then nothing has changed, and the sequences must not be written to: their pages may be
+        others' too. ``mass``: weights that go with a copied page.
+
+        granted  int32 [n_seq] to write into (may be ``counts``): the tokens of ``counts`` that may be
+                 stored, as far as the row of ``table`` goes, and none where pages were missing. A
+                 ``store`` with these counts, and lengths that grow by them, are right either way,
+                 in a captured step too."""
         s, n, width = self._seqs(table)
         _need(lengths is not None and counts is not None, "lengths and counts are wanted")
         missing, missing_p = self._int_out(missing, "missing", (1,), stream)
@@ -461,9 +468,10 @@ class Kv8Cache:
         if need is None:
             need = L.cg_kv8_reserve_workspace_bytes(self._cp, s)
             self._reserve_bytes[n, width] = need
-        self._launch("cg_kv8_reserve", L.cg_kv8_reserve, stream, s,
+        self._launch("cg_kv8_reserve", L.cg_kv8_reserve_granted, stream, s,
                      self._per_seq(lengths, "lengths", n), self._per_seq(counts, "counts", n),
-                     self._refs(refs), missing_p, need=need, cache=cache)
+                     self._refs(refs), missing_p, self._per_seq(granted, "granted", n), need=need,
+                     cache=cache)
         return missing
 
     def release(self, table, refs, keep=None, stream=None):

@@ -148,9 +148,10 @@ def run(w, kv_heads=8, q_heads=32, question=100, tokens=16, keep=0.25, picks=16,
 
 
 def answer(w, kv_heads=8, q_heads=32, requests=8, drafts=4, steps=8, vocab=32000, seed=0,
-           device="cuda"):
+           spare=None, device="cuda"):
     """`requests` answers over every context of workload `w` at once, each `steps` times `drafts`
-    drafted tokens (one at least); returns a dict of figures."""
+    drafted tokens (one at least); returns a dict of figures. `spare`: pages behind the contexts' own,
+    for the answers (default: enough); a step that finds too few changes nothing."""
     import torch
     from paper_2310_07240_amd import workloads as W
     from paper_2310_07240_amd.cachegen import Codec, CodecParams
@@ -175,11 +176,11 @@ def answer(w, kv_heads=8, q_heads=32, requests=8, drafts=4, steps=8, vocab=32000
     whole, tail = T // PAGE, T % PAGE
     q = drafts + 1                                 # the last token and the drafts behind it
     own = -(-(tail + q * steps) // PAGE)
-    cache = Kv8Cache(n * (whole + 1) + n * R * own, H, D, device)
+    cache = Kv8Cache(n * -(-T // PAGE) + (n * R * own if spare is None else spare), H, D, device)
     refs = ints(cache.n_pages)
     table = ints(n, whole + own, value=-1)
     start, held = ints(n), ints(n, value=T)
-    missing = cache.reserve(table, start, held, refs)
+    missing = cache.reserve(table, start, held, refs)      # (there are as many)
     cache.store(x[:, 0], x[:, 1], table, start)
     shared, tails = table[:, :max(1, whole)].contiguous(), table[:, whole:].contiguous()
     shared_len, firsts = ints(n, value=whole * PAGE), torch.arange(
@@ -193,8 +194,8 @@ def answer(w, kv_heads=8, q_heads=32, requests=8, drafts=4, steps=8, vocab=32000
     def random(*shape):
         return torch.randn(shape, generator=g, device=device)
 
-    error, taken = 0.0, []
-    counts = ints(n * R, value=q)
+    error, taken, short = 0.0, [], missing.clone()
+    counts, granted = ints(n * R, value=q), ints(n * R)
     for step in range(steps):
         kn, vn, qn = random(n * R, q, H, D).half(), random(n * R, q, H, D).half(), (
             0.5 * random(n * R, q, q_heads, D)).half()
@@ -206,22 +207,27 @@ def answer(w, kv_heads=8, q_heads=32, requests=8, drafts=4, steps=8, vocab=32000
         starts = lengths
 
         def one():
-            cache.reserve(rows, starts, counts, refs, missing=missing)
-            cache.store(kn, vn, rows, starts)
+            # (without pages nothing is stored, and no query is asked)
+            cache.reserve(rows, starts, counts, refs, missing=missing, granted=granted)
+            cache.store(kn, vn, rows, starts, counts=granted)
             return cache.attend_shared(qn, shared, shared_len, firsts, table=rows,
-                                       lengths=starts + q, max_shared=whole * PAGE,
-                                       max_len=tail + q * (step + 1), max_users=R)
+                                       lengths=starts + granted, q_lens=granted,
+                                       max_shared=whole * PAGE, max_len=tail + q * (step + 1),
+                                       max_users=R)
         out = _timed(torch, "step", times, one)
         if step == 0:                              # compared on the last request
             ref = _reference(torch, qn[-1:], torch.cat([x[-1:, 0], kn[-1:]], 1),
                              torch.cat([x[-1:, 1], vn[-1:]], 1), T)
             error = float((out[-1:].float() - ref).norm() / ref.norm())
-        # a request's layers go on together: verified once, cut back alike
+        short = torch.maximum(short, missing)
+        # a request's layers go on together (all get pages, or none): verified once, cut back alike
+        there = granted.view(p.n_ctx, p.n_layers, R)[:, 0].reshape(-1)
         _, accepted = _timed(torch, "verify", times, lambda: cache.verify(target, tokens, u,
-                                                                          draft=draft))
+                                                                          draft=draft,
+                                                                          counts=there - 1))
         taken.append(accepted)
-        back = (drafts - accepted).view(p.n_ctx, 1, R).expand(-1, p.n_layers, -1).reshape(-1)
-        lengths = starts + q - back
+        kept = torch.where(there > 0, accepted + 1, 0)
+        lengths = starts + kept.view(p.n_ctx, 1, R).expand(-1, p.n_layers, -1).reshape(-1)
         _timed(torch, "release", times, lambda: cache.release(rows, refs, keep=lengths))
     used = int((refs > 0).sum())
     most = int(lengths.max())
@@ -233,7 +239,7 @@ def answer(w, kv_heads=8, q_heads=32, requests=8, drafts=4, steps=8, vocab=32000
     return {
         "workload": w.name, "contexts": n, "requests": n * R, "tokens": T,
         "ms": {name: round(sorted(t)[len(t) // 2], 4) for name, t in times.items()},
-        "accepted": float(torch.stack(taken).float().mean()), "missing": int(missing),
+        "accepted": float(torch.stack(taken).float().mean()), "missing": int(short),
         "pages": {"used": used, "unshared": n * R * (whole + -(-most // PAGE)),
                   "after": int(live), "contexts": n * -(-T // PAGE)},
         "rel_error_8bit": error, "rel_error_after": loaded,

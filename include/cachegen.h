@@ -635,11 +635,14 @@ typedef struct cg_kv8_contexts {
   int32_t max_len;              /* no length is above it (longer ones are cut to it) */
   const int32_t* firsts;        /* [seqs.n_seq + 1], ascending: context p is read by sequences
                                    firsts[p] .. firsts[p + 1] - 1 of the call */
-  int32_t max_users;            /* no context is read by more of them (those behind see none) */
+  int32_t max_users;            /* no context is read by more of them (those behind see none); n_seq
+                                   where the host does not know, at little cost */
 } cg_kv8_contexts;
 
 /* Device scratch that cg_kv8_attend_shared needs (bytes); 0 if an argument is invalid or none is
- * needed. It follows max_users and the two max_len. */
+ * needed. It follows the numbers of sequences and contexts and the two max_len, whatever max_users
+ * leaves room for. CG_ERR_SHAPE: with the smaller of contexts * max_users and n_seq + contexts for the
+ * sequences, the query tokens times H are above 2^23, or their rows above 2^30. */
 uint64_t cg_kv8_attend_shared_workspace_bytes(const cg_kv8_cache* c, const cg_kv8_contexts* x,
                                               const cg_kv8_seqs* s, const cg_kv8_attn* a);
 

@@ -378,26 +378,36 @@ struct KvAttnPlan {
   uint64_t part_off, lse_off, score_off, total;   // workspace, in bytes
 };
 
-KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& seqs, const KvAttn& a, int D,
-                       bool shared = false);
-
 // Which requests read a context: context p those from firsts[p] on, `most` at most, of `n_seq` with
-// `per` query tokens each.
+// `per` query tokens and `rows` rows of a KV head each.
 struct KvUsers {
   const int32_t* firsts;
-  int32_t n_seq, most, per;
+  int32_t n_seq, most, per, rows, contexts;
+};
+
+KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& seqs, const KvAttn& a, int D,
+                       const KvUsers* shared = nullptr);
+
+// Tiles of `size` rows, a power of two, of all contexts. Where every context has room for as many requests as the
+// call's are on average (`each` > 0), context p has tiles p each .. p each + each - 1. Where it has
+// room for more, as with a bound that is the number of all requests, tiles for that room would be far
+// more than there are rows; then (each = 0) context p has those from p + firsts[p] rows / size on: as
+// a request has one context, they do not overlap, and there are `all` at most.
+struct KvTiles {
+  int32_t size, each, all;
 };
 
 // A call over contexts and the requests' own pages: the plan of each (own.tiles = 0: no own pages),
-// and where their partial states lie.
+// the contexts' tiles of 16 rows and those of shared_kernel, and where the partial states lie.
 struct KvSharedPlan {
   KvAttnPlan shared, own;
+  KvTiles small, big;
   bool joins;                   // the own tokens' launch joins the contexts' states itself
   uint64_t shared_off, own_off, total;
 };
 
 KvSharedPlan cg_kv8_shared_plan(const KvPool&, const KvSeqs& contexts, const KvAttn& over_contexts,
-                                const KvSeqs& own, const KvAttn& over_own, int D);
+                                const KvUsers&, const KvSeqs& own, const KvAttn& over_own, int D);
 hipError_t cg_launch_kv8_shared(const KvPool&, const KvSeqs& contexts, const KvAttn& over_contexts,
                                 const KvUsers&, const KvSeqs& own, const KvAttn& over_own, int D,
                                 bool bf16, void* ws, hipStream_t);

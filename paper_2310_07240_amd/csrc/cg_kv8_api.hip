@@ -121,7 +121,11 @@ int check_shared(const cg_kv8_cache* c, const cg_kv8_contexts* x, const cg_kv8_s
   U->n_seq = S->n;
   U->most = x->max_users < S->n ? x->max_users : S->n;
   U->per = A->nq;
-  const int64_t tokens = (int64_t)X->n * U->most * A->nq;
+  U->rows = A->nq * A->group;
+  U->contexts = X->n;
+  // (the work is laid out for the requests, and a request more of every context)
+  const int64_t room = (int64_t)X->n * U->most, most = (int64_t)S->n + X->n;
+  const int64_t tokens = (room < most ? room : most) * A->nq;
   if (tokens * A->group * pool->H > (1LL << 30) || tokens * pool->H > (1 << 23))
     return CG_ERR_SHAPE;
   *XA = *A;
@@ -215,7 +219,7 @@ uint64_t cg_kv8_attend_shared_workspace_bytes(const cg_kv8_cache* c, const cg_kv
   KvAttn XA, A;
   KvUsers U;
   if (check_shared(c, x, s, a, &pool, &X, &XA, &U, &S, &A) != CG_OK) return 0;
-  return cg_kv8_shared_plan(pool, X, XA, S, A, c->head_dim).total;
+  return cg_kv8_shared_plan(pool, X, XA, U, S, A, c->head_dim).total;
 }
 
 int cg_kv8_attend_shared(const cg_kv8_cache* c, const cg_kv8_contexts* x, const cg_kv8_seqs* s,
@@ -227,7 +231,7 @@ int cg_kv8_attend_shared(const cg_kv8_cache* c, const cg_kv8_contexts* x, const 
   KvUsers U;
   const int rc = check_shared(c, x, s, a, &pool, &X, &XA, &U, &S, &A);
   if (rc != CG_OK) return rc;
-  const uint64_t need = cg_kv8_shared_plan(pool, X, XA, S, A, c->head_dim).total;
+  const uint64_t need = cg_kv8_shared_plan(pool, X, XA, U, S, A, c->head_dim).total;
   if (need && (!workspace || !aligned(workspace, 256))) return CG_ERR_ARG;
   if (workspace_bytes < need) return CG_ERR_CAPACITY;
   return hip_rc(cg_launch_kv8_shared(pool, X, XA, U, S, A, c->head_dim, a->dtype == CG_KV8_BF16,

@@ -168,6 +168,38 @@ __device__ __forceinline__ SharedRows rows_of(const KvSeqs& S, const KvAttn& A, 
   return r;
 }
 
+// Where a context's tiles start (see KvTiles); `first`: its first request.
+__device__ __forceinline__ int tiles_before(const KvTiles& T, const KvUsers& U, int p, int first) {
+  // (all rows of a head are below 2^30)
+  return T.each ? p * T.each : p + ((first * U.rows) >> __builtin_ctz(T.size));
+}
+
+// The context that tile t is of, or -1, and which of its tiles (below 0 if firsts is in no order).
+// A wave looks at 64 contexts at once.
+__device__ __forceinline__ int context_at(const KvTiles& T, const KvUsers& U, int t, int& tile) {
+  int p;
+  if (T.each) {
+    p = t / T.each;
+    tile = t - p * T.each;
+    return p;
+  }
+  int lo = 0, hi = U.contexts;                         // contexts from lo on may start behind t
+  while (lo < hi) {
+    const int step = (hi - lo + 63) / 64;
+    const int64_t at = lo + (int64_t)(threadIdx.x & 63) * step;
+    bool before = false;
+    if (at < hi) before = tiles_before(T, U, (int)at, requests_of(U, (int)at).first) <= t;
+    const int c = __popcll(__ballot(before));
+    if (c == 0) break;
+    const int64_t end = lo + (int64_t)c * step;
+    lo += (c - 1) * step + 1;
+    hi = end < hi ? (int)end : hi;
+  }
+  p = uniform(lo - 1);
+  tile = p < 0 ? 0 : t - tiles_before(T, U, p, uniform(requests_of(U, p).first));
+  return p;
+}
+
 // The same of either kind.
 template <class Rows>
 __device__ __forceinline__ Rows rows_in(const KvSeqs& S, const KvAttn& A, const KvUsers& U, int i) {
@@ -534,9 +566,10 @@ __device__ __forceinline__ void join_rows(int rows, int n, float* w, float4v* su
   }
 }
 
-// Which context request `b` reads and its place among that one's, or -1.
-__device__ __forceinline__ int context_of(const KvUsers& U, int contexts, int b, int& place) {
-  int lo = 0, hi = contexts;                           // firsts[lo - 1] <= b < firsts[hi]
+// Which context request `b` reads and its place among that one's, and where its tiles start; or -1.
+__device__ __forceinline__ int context_of(const KvUsers& U, const KvTiles& T, int b, int& place,
+                                          int& tile0) {
+  int lo = 0, hi = U.contexts;                         // firsts[lo - 1] <= b < firsts[hi]
   while (lo < hi) {
     const int mid = (lo + hi) >> 1;
     if (U.firsts[mid] <= b) lo = mid + 1;
@@ -545,13 +578,24 @@ __device__ __forceinline__ int context_of(const KvUsers& U, int contexts, int b,
   if (lo == 0) return -1;
   const Requests q = requests_of(U, lo - 1);
   place = b - q.first;
+  tile0 = tiles_before(T, U, lo - 1, q.first);
   return place >= 0 && place < q.count ? lo - 1 : -1;
 }
 
-// The states of contexts that a launch before has left, for the requests' own tokens to join.
+// Contexts' tiles of 16 rows, and the states of them that a launch before has left, for the requests'
+// own tokens to join: for every tile and head those of its splits, `step` of them a tile. (Heads next to
+// each other, in the order of the requests' own workgroups: of eight heads those of one then run on one
+// XCD. 2 contexts of 75 tokens and 3 requests each 16.5 us, 17.3 with a head's tiles together.)
 struct ContextStates {
-  int contexts, tiles, splits;
+  KvTiles tiles;
+  int splits;
+  int64_t step;
   const float* part;
+
+  template <int D>
+  __device__ __forceinline__ const float* from(int h, int tile) const {
+    return part + (tile * step + h * splits) * kPart<D>;
+  }
 };
 
 // Requests that have no context see nothing: those before the first context's, between the bound of
@@ -607,11 +651,19 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_kernel(KvPool po
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const int split = (int)(it % splits);
     const int64_t unit = it / splits;
-    const int tile = (int)(unit % tiles);
-    const int h = (int)(unit / tiles % pool.H);
-    const int vseq = (int)(unit / tiles / pool.H);
+    constexpr bool kShared = __is_same(Rows, SharedRows);
+    int tile, h, vseq;
+    if constexpr (kShared) {
+      h = (int)(unit % pool.H);
+      vseq = context_at(C.tiles, U, (int)(unit / pool.H), tile);
+      if (vseq < 0 || tile < 0) continue;
+    } else {
+      tile = (int)(unit % tiles);
+      h = (int)(unit / tiles % pool.H);
+      vseq = (int)(unit / tiles / pool.H);
+    }
     const Rows R = rows_in<Rows>(S, A, U, vseq);
-    if constexpr (__is_same(Rows, SharedRows) && TO == kOut)
+    if constexpr (kShared && TO == kOut)
       if (split == 0 && tile == 0 && h == 0) fill_without<256>(A, U, S.n, vseq, pool.H, D, lse);
     // the pages that any row of the tile sees
     const int rows = R.nq * A.group;
@@ -643,8 +695,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_kernel(KvPool po
     }
     QTile<D> Q;
     load_q<D, BF16>(A, R, h, tile, Q);
-    int place = 0, context = -1;       // (looked up beside the first page's codes)
-    if constexpr (TO == kJoin) context = uniform(context_of(U, C.contexts, R.seq, place));
+    int place = 0, tile0 = 0, context = -1;      // (looked up beside the first page's codes)
+    if constexpr (TO == kJoin) context = uniform(context_of(U, C.tiles, R.seq, place, tile0));
     Acc<D> acc;
 #pragma unroll
     for (int dt = 0; dt < D / 16; ++dt) acc.o[dt] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
@@ -704,15 +756,14 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_kernel(KvPool po
       float4v* const sums = reinterpret_cast<float4v*>(w + kMostSplits * 16);
       float* const own = w + kMostSplits * 16 + 1024;
       const int n0 = context >= 0 ? C.splits : 0, from = place * rows + tile * 16;
-      const float* const s0 = C.part + ((int64_t)(context >= 0 ? context : 0) * pool.H + h) *
-                                           C.tiles * C.splits * kPart<D>;
+      const float* const s0 = C.from<D>(h, uniform(tile0));
       const bool first = d0 == 0 && live;
       float t0 = first ? top : kNegInf, l0 = first ? l : 0.0f;
       __syncthreads();
       join_rows<D>(rows - tile * 16 < 16 ? rows - tile * 16 : 16, n0, w, sums, t0, l0,
                    [&](int i, int x, int& in) {
                      in = (from + x) & 15;
-                     return s0 + ((int64_t)((from + x) >> 4) * C.splits + i) * kPart<D>;
+                     return s0 + (((from + x) >> 4) * C.step + i) * kPart<D>;
                    },
                    [&](float f) {
 #pragma unroll
@@ -1561,8 +1612,8 @@ struct PageList {
 
 template <int D, bool BF16, int RW>
 __global__ __launch_bounds__(64 * kPromptWaves<D>, kPromptWaves<D> / 4)
-void shared_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, int splits, int tile0, int p0,
-                   float* part, float* lse) {
+void shared_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, KvTiles T, KvTiles small, int splits,
+                   int tile0, int p0, float* part, float* lse) {
   constexpr int W = kPromptWaves<D>, NT = 64 * W, TW = W / RW;
   constexpr int kAhead = kPagesK<D> - 1;
   static_assert(TW == 1 || (TW == 2 && kAhead == 2), "a tile of every page for each half");
@@ -1575,7 +1626,11 @@ void shared_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, int splits, int t
   // 37.8 -> 35.0).
   const int band = (wave + side * (RW / 2)) % RW;
   const int split = blockIdx.x / pool.H, h = blockIdx.x - split * pool.H;
-  const int tile = tile0 + blockIdx.y, p = p0 + blockIdx.z;
+  int tile = tile0 + blockIdx.y, p = p0 + blockIdx.z;
+  if (T.each == 0) {
+    p = context_at(T, U, tile, tile);
+    if (p < 0) return;
+  }
 
   const Requests req = requests_of(U, p);
   int len = A.lengths[p];
@@ -1583,8 +1638,11 @@ void shared_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, int splits, int t
   len = uniform(len > 0 ? len : 0);
   const int first = uniform(req.first), count = uniform(req.count);
   if (!part && blockIdx.x == 0 && tile == 0) fill_without<NT>(A, U, S.n, p, pool.H, D, lse);
-  const int per_user = U.per * A.group, rows = U.most * per_user, r0 = tile * (32 * RW);
-  if (r0 >= count * per_user) return;                  // (nobody's rows)
+  const int per_user = U.rows, rows = count * per_user, r0 = tile * (32 * RW);
+  if (tile < 0 || r0 >= rows) return;                  // (nobody's rows)
+  // this split's state of the context's first tile, and those of the next tiles behind it
+  const int64_t step = (int64_t)pool.H * splits;
+  const int64_t u16 = tiles_before(small, U, p, first) * step + h * splits + split;
   const int columns = (int)(((int64_t)len + kPage - 1) / kPage);
   const int per = (columns + splits - 1) / splits;
   const int j0 = split * per, j1 = j0 + per < columns ? j0 + per : columns;
@@ -1878,8 +1936,7 @@ void shared_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, int splits, int t
     // (the first half's)
   } else if (part) {
     if (half == 0 && row < rows) {
-      const int64_t u16 = ((int64_t)p * pool.H + h) * ((rows + 15) / 16) + row / 16;
-      *reinterpret_cast<float2v*>(part + (u16 * splits + split) * kPart<D> + 16 * D +
+      *reinterpret_cast<float2v*>(part + (u16 + row / 16 * step) * kPart<D> + 16 * D +
                                   2 * (row & 15)) = float2v{top, sum};
     }
   } else {
@@ -1898,8 +1955,8 @@ void shared_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U, int splits, int t
   const auto leave = [&](int to, int d, const float4v& w) {
     if (part) {
       if (to >= rows) return;
-      const int64_t u16 = ((int64_t)p * pool.H + h) * ((rows + 15) / 16) + to / 16;
-      *reinterpret_cast<float4v*>(part + (u16 * splits + split) * kPart<D> + (to & 15) * D + d) = w;
+      *reinterpret_cast<float4v*>(part + (u16 + to / 16 * step) * kPart<D> + (to & 15) * D + d) =
+          w;
     } else {
       const int user_to = to / per_user, of = to - user_to * per_user;
       if (user_to >= count) return;
@@ -1987,8 +2044,8 @@ __global__ __launch_bounds__(64, D == 256 ? 1 : 2) void own_join_kernel(KvPool p
     }
     QTile<D> Q;
     load_q<D, BF16>(A, R, h, tile, Q);
-    int place = 0;
-    const int context = uniform(context_of(U, C.contexts, R.seq, place));
+    int place = 0, tile0 = 0;
+    const int context = uniform(context_of(U, C.tiles, R.seq, place, tile0));
     Acc<D> acc;
 #pragma unroll
     for (int dt = 0; dt < D / 16; ++dt) acc.o[dt] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
@@ -2018,11 +2075,10 @@ __global__ __launch_bounds__(64, D == 256 ? 1 : 2) void own_join_kernel(KvPool p
     __syncthreads();
     // four lanes a row find the factors of the context's states and of the own one
     const int n0 = context >= 0 ? C.splits : 0, from = place * all + tile * 16;
-    const float* const s0 = C.part + ((int64_t)(context >= 0 ? context : 0) * pool.H + h) * C.tiles *
-                                         C.splits * kPart<D>;
+    const float* const s0 = C.from<D>(h, uniform(tile0));
     const auto state = [&](int i, int x, int& in) -> const float* {
       in = (from + x) & 15;
-      return s0 + ((int64_t)((from + x) >> 4) * C.splits + i) * kPart<D>;
+      return s0 + (((from + x) >> 4) * C.step + i) * kPart<D>;
     };
     const int row = lane >> 2, sub = lane & 3;
     float top = sub == 0 ? ml[row] : kNegInf, l = sub == 0 ? ml[16 + row] : 0.0f;
@@ -2082,25 +2138,26 @@ __global__ __launch_bounds__(64, D == 256 ? 1 : 2) void own_join_kernel(KvPool p
   }
 }
 
-// A context's states alone: `few` rows a workgroup. Bound by the states' bytes.
+// A context's states alone: a tile of T (a few rows) a workgroup. Bound by the states' bytes.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void contexts_join_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U,
-                                                            int groups, int few, int splits,
-                                                            int64_t items, const float* part,
-                                                            float* lse) {
+                                                            KvTiles T, int64_t items,
+                                                            ContextStates C, float* lse) {
   __shared__ JoinLds L;
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
-    const int first = (int)(it % groups) * few;
-    const int64_t ph = it / groups;
-    const int h = (int)(ph % pool.H);
-    const SharedRows R = rows_of(S, A, U, (int)(ph / pool.H));
-    const int all = R.nq * A.group, left = R.q_len * A.group - first, rows = left < few ? left : few;
+    const int h = (int)(it % pool.H);
+    int tile;
+    const int p = context_at(T, U, (int)(it / pool.H), tile);
+    if (p < 0 || tile < 0) continue;
+    const SharedRows R = rows_of(S, A, U, p);
+    const int first = tile * T.size, left = R.q_len * A.group - first;
+    const int rows = left < T.size ? left : T.size;
     if (rows <= 0) continue;
-    const float* const s0 = part + ph * ((all + 15) / 16) * splits * kPart<D>;
+    const float* const s0 = C.from<D>(h, tiles_before(C.tiles, U, p, R.first));
     float top = kNegInf, l = 0.0f;
-    join_rows<D>(rows, splits, L.w, L.sums, top, l, [&](int i, int x, int& in) {
+    join_rows<D>(rows, C.splits, L.w, L.sums, top, l, [&](int i, int x, int& in) {
       in = (first + x) & 15;
-      return s0 + ((int64_t)((first + x) >> 4) * splits + i) * kPart<D>;
+      return s0 + (((first + x) >> 4) * C.step + i) * kPart<D>;
     }, [](float) {}, [&](int x, int d, const float4v& o) {
       put_out<D, BF16>(A, R, h, first + x, d, reinterpret_cast<const float*>(&o), 4);
     });
@@ -2117,10 +2174,9 @@ __global__ __launch_bounds__(256) void contexts_join_kernel(KvPool pool, KvSeqs 
 // context's states of the tile lie in rows of its own tiles, from the request's first on.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void shared_join_kernel(KvPool pool, KvSeqs S, KvAttn A, KvUsers U,
-                                                          int contexts, int tiles, int shared_tiles,
-                                                          int shared_splits, int splits,
-                                                          int64_t items, const float* shared_part,
-                                                          const float* part, float* lse) {
+                                                          int tiles, int splits, int64_t items,
+                                                          ContextStates C, const float* part,
+                                                          float* lse) {
   __shared__ JoinLds L;
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const int tile = (int)(it % tiles);
@@ -2128,16 +2184,15 @@ __global__ __launch_bounds__(256) void shared_join_kernel(KvPool pool, KvSeqs S,
     const int h = (int)(r % pool.H);
     const RowsOf R = rows_of(S, A, (int)(r / pool.H));
     const int all = R.nq * A.group, rows = all - tile * 16 < 16 ? all - tile * 16 : 16;
-    int place = 0;
-    const int p = context_of(U, contexts, R.seq, place);
-    const int n0 = p >= 0 ? shared_splits : 0, from = place * all + tile * 16;
-    const float* const s0 =
-        shared_part + ((int64_t)(p >= 0 ? p : 0) * pool.H + h) * shared_tiles * shared_splits * kPart<D>;
+    int place = 0, tile0 = 0;
+    const int p = context_of(U, C.tiles, R.seq, place, tile0);
+    const int n0 = p >= 0 ? C.splits : 0, from = place * all + tile * 16;
+    const float* const s0 = C.from<D>(h, uniform(tile0));
     float top = kNegInf, l = 0.0f;
     join_rows<D>(rows, n0 + splits, L.w, L.sums, top, l, [&](int i, int x, int& in) {
       if (i < n0) {
         in = (from + x) & 15;
-        return s0 + ((int64_t)((from + x) >> 4) * shared_splits + i) * kPart<D>;
+        return s0 + (((from + x) >> 4) * C.step + i) * kPart<D>;
       }
       in = x;
       return part + (it * splits + (i - n0)) * kPart<D>;
@@ -2234,25 +2289,34 @@ hipError_t attend_d(const KvPool& pool, const KvSeqs& S, const KvAttn& A, void* 
 // limits. part null: the result.
 template <int D, bool BF16>
 void shared_rows_d(const KvPool& pool, const KvSeqs& C, const KvAttn& CA, const KvUsers& U,
-                   const KvAttnPlan& P, float* part, float* lse, hipStream_t st) {
+                   const KvSharedPlan& P, float* part, float* lse, hipStream_t st) {
   constexpr int W = kPromptWaves<D>, kMost = 1 << 22, kSide = 65535;
-  const int x = pool.H * P.splits;
+  const int splits = P.shared.splits, x = pool.H * splits;
+  // (tiles of contexts one after the other: one dimension for them all)
+  const int all_y = P.big.each ? P.big.each : P.big.all, all_z = P.big.each ? C.n : 1;
   const auto at_most = [](int n, int most) { return n < most ? n : most < 1 ? 1 : most; };
-  const int tiles = at_most(P.big, kMost / x < kSide ? kMost / x : kSide);
-  const int contexts = at_most(C.n, kMost / x / tiles < kSide ? kMost / x / tiles : kSide);
-  for (int p0 = 0; p0 < C.n; p0 += contexts)
-    for (int tile0 = 0; tile0 < P.big; tile0 += tiles) {
-      const dim3 grid((unsigned)x, (unsigned)at_most(P.big - tile0, tiles),
-                      (unsigned)at_most(C.n - p0, contexts));
+  const int tiles = at_most(all_y, kMost / x < kSide ? kMost / x : kSide);
+  const int contexts = at_most(all_z, kMost / x / tiles < kSide ? kMost / x / tiles : kSide);
+  for (int p0 = 0; p0 < all_z; p0 += contexts)
+    for (int tile0 = 0; tile0 < all_y; tile0 += tiles) {
+      const dim3 grid((unsigned)x, (unsigned)at_most(all_y - tile0, tiles),
+                      (unsigned)at_most(all_z - p0, contexts));
       if constexpr (D < 256)
-        if (P.halves) {
+        if (P.shared.halves) {
           hipLaunchKernelGGL((shared_kernel<D, BF16, W / 2>), grid, dim3(64 * W), 0, st, pool, C, CA,
-                             U, P.splits, tile0, p0, part, lse);
+                             U, P.big, P.small, splits, tile0, p0, part, lse);
           continue;
         }
       hipLaunchKernelGGL((shared_kernel<D, BF16, W>), grid, dim3(64 * W), 0, st, pool, C, CA, U,
-                         P.splits, tile0, p0, part, lse);
+                         P.big, P.small, splits, tile0, p0, part, lse);
     }
+}
+
+// (see KvTiles)
+KvTiles tiles_of(const KvUsers& U, int size) {
+  const int64_t each = ((int64_t)U.most * U.rows + size - 1) / size, even = each * U.contexts;
+  const int64_t all = (int64_t)U.n_seq * U.rows / size + U.contexts;
+  return even <= all ? KvTiles{size, (int32_t)each, (int32_t)even} : KvTiles{size, 0, (int32_t)all};
 }
 
 // Whether a wave alone takes a request's own tokens: few pages, or requests enough (one wave / four,
@@ -2265,49 +2329,49 @@ bool one_wave(int64_t units, int max_len) { return max_len <= 2 * kPage || units
 template <int D, bool BF16>
 hipError_t shared_d(const KvPool& pool, const KvSeqs& C, const KvAttn& CA, const KvUsers& U,
                     const KvSeqs& S, const KvAttn& A, void* ws, hipStream_t st) {
-  const KvSharedPlan P = cg_kv8_shared_plan(pool, C, CA, S, A, D);
+  const KvSharedPlan P = cg_kv8_shared_plan(pool, C, CA, U, S, A, D);
   char* base = static_cast<char*>(ws);
   float* const part0 = reinterpret_cast<float*>(base + P.shared_off);
-  const int64_t units0 = (int64_t)C.n * pool.H * P.shared.tiles;
+  const int64_t units0 = (int64_t)pool.H * P.small.all;
   const int splits0 = P.shared.splits;
+  const ContextStates states = {P.small, splits0, (int64_t)pool.H * splits0, part0};
   if (P.own.tiles == 0) {
     // the context alone
     if (P.shared.big) {
-      shared_rows_d<D, BF16>(pool, C, CA, U, P.shared, splits0 > 1 ? part0 : nullptr, A.lse, st);
+      shared_rows_d<D, BF16>(pool, C, CA, U, P, splits0 > 1 ? part0 : nullptr, A.lse, st);
       if (splits0 > 1) {
         // (16 rows a workgroup where that makes enough of them; 4 rows / 16, us with shared_kernel: 128
         // rows of 8 heads in 32 splits 32.2 / 34.6, 200 of 32 heads and two contexts 52.8 / 49.0)
-        const int few = units0 < 512 ? 4 : 16, groups = (CA.nq * CA.group + few - 1) / few;
-        const int64_t items = (int64_t)C.n * pool.H * groups;
+        const KvTiles few = tiles_of(U, units0 < 512 ? 4 : 16);
+        const int64_t items = (int64_t)pool.H * few.all;
         hipLaunchKernelGGL((contexts_join_kernel<D, BF16>), dim3(grid_of(items)), dim3(256), 0, st,
-                           pool, C, CA, U, groups, few, splits0, items, part0, A.lse);
+                           pool, C, CA, U, few, items, states, A.lse);
       }
     } else {
       hipLaunchKernelGGL((attend_kernel<D, BF16, SharedRows, kOut>),
                          dim3(grid_of(units0 * splits0)), dim3(256), 0, st, pool, C, CA, U,
-                         P.shared.tiles, splits0, units0 * splits0, part0,
-                         reinterpret_cast<uint32_t*>(base), A.lse, nullptr, 0, ContextStates{});
+                         0, splits0, units0 * splits0, part0, reinterpret_cast<uint32_t*>(base),
+                         A.lse, nullptr, 0, states);
     }
     return hipGetLastError();
   }
   if (P.shared.big)
-    shared_rows_d<D, BF16>(pool, C, CA, U, P.shared, part0, nullptr, st);
+    shared_rows_d<D, BF16>(pool, C, CA, U, P, part0, nullptr, st);
   else
     hipLaunchKernelGGL((attend_kernel<D, BF16, SharedRows, kParts>), dim3(grid_of(units0 * splits0)),
-                       dim3(256), 0, st, pool, C, CA, U, P.shared.tiles, splits0, units0 * splits0,
-                       part0, nullptr, nullptr, nullptr, 0, ContextStates{});
+                       dim3(256), 0, st, pool, C, CA, U, 0, splits0, units0 * splits0, part0, nullptr,
+                       nullptr, nullptr, 0, states);
   float* const part = reinterpret_cast<float*>(base + P.own_off);
   const int64_t units = (int64_t)S.n * pool.H * P.own.tiles;
   if (P.joins && one_wave(units, A.max_len)) {
     hipLaunchKernelGGL((own_join_kernel<D, BF16>), dim3(grid_of(units)), dim3(64), 0, st, pool, S, A,
-                       U, P.own.tiles, units, ContextStates{C.n, P.shared.tiles, splits0, part0},
-                       A.lse);
+                       U, P.own.tiles, units, states, A.lse);
     return hipGetLastError();
   }
   if (P.joins) {
     hipLaunchKernelGGL((attend_kernel<D, BF16, RowsOf, kJoin>), dim3(grid_of(units)), dim3(256), 0,
                        st, pool, S, A, U, P.own.tiles, 1, units, nullptr, nullptr, A.lse, nullptr, 0,
-                       ContextStates{C.n, P.shared.tiles, splits0, part0});
+                       states);
     return hipGetLastError();
   }
   if (P.own.big)
@@ -2317,23 +2381,25 @@ hipError_t shared_d(const KvPool& pool, const KvSeqs& C, const KvAttn& CA, const
                        dim3(256), 0, st, pool, S, A, KvUsers{}, P.own.tiles, P.own.splits,
                        units * P.own.splits, part, nullptr, nullptr, nullptr, 0, ContextStates{});
   hipLaunchKernelGGL((shared_join_kernel<D, BF16>), dim3(grid_of(units)), dim3(256), 0, st, pool, S,
-                     A, U, C.n, P.own.tiles, P.shared.tiles, splits0, P.own.splits, units, part0,
-                     part, A.lse);
+                     A, U, P.own.tiles, P.own.splits, units, states, part, A.lse);
   return hipGetLastError();
 }
 
 }  // namespace
 
 KvSharedPlan cg_kv8_shared_plan(const KvPool& pool, const KvSeqs& C, const KvAttn& CA,
-                                const KvSeqs& S, const KvAttn& A, int D) {
+                                const KvUsers& U, const KvSeqs& S, const KvAttn& A, int D) {
   KvSharedPlan P = {};
-  P.shared = cg_kv8_plan(pool, C, CA, D, true);
+  P.shared = cg_kv8_plan(pool, C, CA, D, &U);
+  P.small = tiles_of(U, 16);
+  P.big = tiles_of(U, 32 * (D == 256 ? kPromptWaves<256> : kPromptWaves<128>) /
+                          (P.shared.halves ? 2 : 1));
   const uint64_t state = 16ull * (D + 2) * 4;
   const bool own = S.table != nullptr;
   uint64_t at = own || P.shared.splits > 1 ? kKv8Front : 0;
   P.shared_off = at;
   if (own || P.shared.splits > 1)
-    at += (uint64_t)C.n * pool.H * P.shared.tiles * P.shared.splits * state;
+    at += (uint64_t)pool.H * P.small.all * P.shared.splits * state;
   at = (at + 255) & ~255ull;
   P.own_off = at;
   if (own) {
@@ -2361,12 +2427,23 @@ hipError_t cg_launch_kv8_shared(const KvPool& pool, const KvSeqs& C, const KvAtt
   }
 }
 
-KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& S, const KvAttn& A, int D, bool shared) {
+KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& S, const KvAttn& A, int D,
+                       const KvUsers* shared) {
   KvAttnPlan P;
-  const int64_t rows = (int64_t)(A.picks ? 1 : A.nq) * A.group;
+  int64_t rows = (int64_t)(A.picks ? 1 : A.nq) * A.group;
+  if (shared) {
+    // the rows of a context as if all requests had one, alike: the bound of a context's requests may be
+    // as many as there are, and only the device knows who reads what
+    const int64_t users = ((int64_t)shared->n_seq + shared->contexts - 1) / shared->contexts;
+    rows = (users < shared->most ? users : shared->most) * shared->rows;
+  }
   P.tiles = (int)((rows + 15) / 16);
   const int64_t vseqs = A.picks ? (int64_t)S.n * A.nq : S.n;
-  const int64_t units = vseqs * pool.H * P.tiles;
+  // tiles of all contexts, or of all sequences
+  const auto all_tiles = [&](int size) -> int64_t {
+    return shared ? tiles_of(*shared, size).all : vseqs * ((rows + size - 1) / size);
+  };
+  const int64_t units = pool.H * all_tiles(16);
   const int64_t pages = A.picks ? A.n_picks : ((int64_t)A.max_len + kPage - 1) / kPage;
   // From three 16-row tiles on, the rows share the pages through LDS (prompt_kernel), but not where
   // there is little to do: a call that attend_kernel's workgroups hold at once, of at most 8192
@@ -2384,22 +2461,29 @@ KvAttnPlan cg_kv8_plan(const KvPool& pool, const KvSeqs& S, const KvAttn& A, int
   // 32.3).
   const bool fills = shared && D == 128 && rows <= 64 && vseqs * pool.H * (pages / 4) >= 256;
   const bool little = !fills && units <= at_once && units * pages <= (D == 256 ? 2048 : 8192);
+  // Of contexts that leave room for unequal numbers of requests (see KvTiles) some have more rows than the
+  // average, and attend_kernel's tiles without rows take places of others: there two tiles are enough
+  // (three / two, us of calls that bound the requests of a context by all; 8 heads, group 4, 128
+  // channels: 4 contexts of 8K and 8 requests each 44.9 / 28.8, 32 of 2K 66.2 / 47.0, 40 requests of one of
+  // 4K and 9 of nine more 46.8 / 46.1, 256 channels, 4 of 4K and 4 each 55.9 / 37.2; 64 channels 21.3 /
+  // 22.9 and 25.1 / 36.5).
+  const bool uneven = shared && D > 64 && tiles_of(*shared, 16).each == 0;
   P.big = 0;
   P.halves = false;
   int64_t s, most, at_least = 1;
   const int64_t listed = D == 256 ? PageList<256>::kColumns : PageList<128>::kColumns;
-  if (P.tiles > 2 && !little && !A.picks && (!shared || pages <= listed * kMostSplits)) {
+  if (P.tiles > (uneven ? 1 : 2) && !little && !A.picks && (!shared || pages <= listed * kMostSplits)) {
     int per = D == 256 ? 32 * kPromptWaves<256> : 32 * kPromptWaves<128>;
     // Of a shared context tiles of 128 rows by half of the waves, where those of all of them would not
     // fill the card (128 / 256 rows, us: 448 queries over 4 x 1500 tokens, 16 heads of 64, 32.2 / 39.8 with
     // the join that two splits need; 512 rows of 8 heads over 8K 44.2 / 47.8; 160 rows of 8 contexts and 32
     // heads 168 / 131).
-    P.halves = shared && D < 256 && vseqs * pool.H * ((rows + per - 1) / per) < 256;
+    P.halves = shared && D < 256 && pool.H * all_tiles(per) < 256;
     if (P.halves) per /= 2;
     // (shared_kernel lists a split's columns, one a thread)
     if (shared) at_least = (pages + listed - 1) / listed;
     P.big = (int)((rows + per - 1) / per);
-    const int64_t groups = vseqs * pool.H * P.big;
+    const int64_t groups = pool.H * all_tiles(per);
     // Splits of a shared context: as many as the CUs hold at once, a workgroup each; one round more
     // costs another prologue (rounded down / up, kernels' us: 3 contexts of 8K with 48 rows of 5 heads
     // of 64 channels 28 / 37, 5 of 8K with 128 rows of 8 heads of 128 54 / 75, 20 of 4K 118 / 130).

@@ -520,7 +520,7 @@ class Kv8Cache:
                        as over an encoder's states.
         max_shared, max_len, max_users  bounds that the host knows of shared_lengths, of lengths and
                        of the sequences that share a context (default: the tables' widths, n_seq);
-                       the work is laid out for them.
+                       the work is laid out for them, but for no more rows than the sequences have.
         scale, q_lens, lse  as in ``attend``."""
         x, contexts, x_width = self._seqs(shared)
         _need(q.dim() == 4, "q: [n_seq, n_q, n_q_heads, head_dim] is wanted")

@@ -124,3 +124,37 @@ def test_contexts_of_a_request_each(C, Q, H, group, tokens):
     off = (a.float() - b.float()).abs().max()
     assert float(off) <= 4 * 2.0 ** -11 * 127 * float(cache.v_scale.max())
     assert bool((a != 0).any())
+
+
+@pytest.mark.parametrize("H,group,D,tokens,users,Q", [
+    (1, 2, 64, 64, [1], 1), (3, 2, 128, 1200, [2, 1], 2), (8, 16, 64, 1000, [60], 1),
+    (32, 8, 64, 256, [30, 200], 1), (2, 8, 256, 700, [70], 1),
+])
+def test_many_requests_without_a_context(H, group, D, tokens, users, Q):
+    """In front of the first context's, behind the bound of each, and behind the last: zeros and -inf, and
+    the others are what they are without them."""
+    torch = torch_cuda()
+    pages = -(-tokens // 64)
+    cache = make(torch, len(users) * pages, H, D)
+    firsts = [40] + [40 + 50 * (i + 1) + sum(users[:i + 1]) for i in range(len(users))]
+    n, most = firsts[-1] + 333, max(users)
+    q = torch.randn(n, Q, H * group, D, device="cuda").half()
+    out, lse = torch.full_like(q, 7.0), torch.full((n, Q, H * group), 7.0, device="cuda")
+    shared = torch.arange(len(users) * pages, dtype=torch.int32, device="cuda").view(len(users), pages)
+    args = shared, ints(torch, [tokens] * len(users))
+    cache.attend_shared(q, *args, ints(torch, firsts), out=out, lse=lse, max_users=most)
+    has = torch.zeros(n, dtype=torch.bool, device="cuda")
+    for a, b in zip(firsts, firsts[1:]):
+        has[a:min(b, a + most)] = True
+    assert bool((out[~has] == 0).all()) and bool((lse[~has] == -float("inf")).all())
+    inner = [0]
+    for a, b in zip(firsts, firsts[1:]):
+        inner.append(inner[-1] + min(b - a, most))
+    same = torch.empty_like(q[has])
+    other = torch.empty_like(lse[has])
+    cache.attend_shared(q[has].contiguous(), *args, ints(torch, inner), out=same, lse=other,
+                        max_users=most)
+    # (both off by 2^-11 of a weight and half a step of the output, as above)
+    off = (out[has].float() - same.float()).abs().max()
+    assert float(off) <= 4 * 2.0 ** -11 * 127 * float(cache.v_scale.max())
+    assert bool(lse[has].isfinite().all())

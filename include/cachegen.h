@@ -664,8 +664,9 @@ int cg_kv8_attend_shared(const cg_kv8_cache* c, const cg_kv8_contexts* x, const 
  * p_j is row j of its target probabilities (n_drafts + 1 rows: the last is behind all drafts), q_j
  * row j of the draft's. x_j is accepted while u_j q_j(x_j) < p_j(x_j) (so with probability
  * min(1, p / q)); the first that is not ends the drafts, and one more token is drawn, from the
- * weights max(p_j - q_j, 0) there, or from p of the row behind the last accepted draft: the tokens
- * are distributed as the target's. */
+ * weights max(p_j - q_j, 0) there, or from p of the row behind the last accepted draft. With exact u
+ * the tokens would be distributed as the target's; the last one is drawn with 24 bits of its u (see
+ * cg_verify_drafts), so that its probability is off by up to 2^-24. */
 #define CG_VERIFY_MAX_VOCAB (1 << 20)
 #define CG_VERIFY_MAX_DRAFTS 1024
 enum { CG_KV8_F32 = 2 };        /* a type of probabilities, beside CG_KV8_F16 and CG_KV8_BF16 */

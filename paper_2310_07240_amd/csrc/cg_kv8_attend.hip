@@ -1600,10 +1600,17 @@ void mass_rows_kernel(KvPool pool, KvSeqs S, KvAttn A, int np, int shares, int64
 // of every page the first tile of 32 tokens goes to the first half and the second to the other (32
 // requests of four heads a group, 16K tokens: 29.5 -> 27.9 us); the halves' states meet in LDS. A split's
 // pages are listed in LDS first, a column a thread, with their scales: a chain of lookups would be as
-// long as a page's products. (So a split has at most a column a thread.) Those 32 requests take 25 us
-// now: 6 until the first products, 1.4 for each of a workgroup's 8 pages, where the vector instructions
-// bound (of the cycles there three in four), 3 for the halves and the states' way out. 448 queries over
-// four times 1500 tokens, 16 heads of 64 channels: 32 us, 340 TFLOP/s, bound by the exponentials.
+// long as a page's products. (So a split has at most a column a thread.)
+//
+// Weights go to V's product as fp16, 2^-11 of a weight, and bf16 rows to K's under a power of two each:
+// the codes have 8 bits, and products of 32-bit operands a sixteenth of the rate. Sums are 32-bit.
+//
+// Those 32 requests take 25 us now: 6 until the first products, 1.4 for each of a workgroup's 8 pages, 3
+// for the halves and the states' way out. Of a page's 3360 cycles the two waves of a SIMD take half to
+// issue their vector instructions (142 each, 4 cycles, and 16 exponentials, 16 cycles); the rest is the
+// order of its steps: products, weights, products, a barrier. 448 queries over four times 1500 tokens, 16
+// heads of 64 channels: 29 us, 380 TFLOP/s; a page of shorter products takes 0.75 us, 1800 cycles, of
+// which those instructions (140 and 16) are 1630, a third of them the exponentials; 10 us are its ends.
 template <int D>
 struct PageList {
   static constexpr int kColumns = 64 * kPromptWaves<D>;

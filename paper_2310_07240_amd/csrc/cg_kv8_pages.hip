@@ -156,7 +156,7 @@ struct Chunk {
 // A page is copied in pieces of 16 KB of its codes, K's and then V's, a workgroup each, with four
 // 16-byte loads of a thread on their way together; the pieces share its scales, bounds and weights.
 // Bound by those bytes: 2048 pages of 8 heads of 128 channels, 554 MB read and written in 113 us, 4.9
-// TB/s (a copy of 1 GiB: 5.1).
+// TB/s (a copy of 1 GiB: 5.1); 96 us where the Infinity Cache has a part of them from the call before.
 constexpr int kUnits = 1024;           // of 16 bytes, a piece
 
 __host__ __device__ inline int pieces_of(int H, int D) {
@@ -165,8 +165,10 @@ __host__ __device__ inline int pieces_of(int H, int D) {
 
 // More of them than the L2s hold are read and written past the caches (without / with, whole calls, us:
 // 2048 pages 115.3 / 113.5, 1024 of a compaction 67.9 / 60.0; with few it is slower, 70 pages of 40 KB
-// 7.5 / 8.4). Copies of a shared page are only written past them: its readers then find it there (512
-// copies of 32 pages, with the calls around them, 45.2 / 35.6; read past them too 49.6).
+// 7.5 / 8.4). Copies of a shared page are only written past them, however few: its readers then find it
+// there (512 copies of 32 pages, with the calls around them, 45.2 / 35.6; read past them too 49.6). With the
+// store and the attention that come next both are alike: 8 requests 38.1 / 38.9, 64 50.1 / 49.4, 512
+// 155.8 / 157.0.
 __device__ __forceinline__ bool past_caches(int64_t items) {
   return items > (32 << 20) / (16 * kUnits);
 }
@@ -752,7 +754,9 @@ hipError_t cg_launch_kv8_reserve(const KvPool& pool, int D, int n, int width, in
   const Reserve R = reserve_of(ws, pool.P, n, width, &total);
   const int chunks = chunks_of(pool.P), words = words_of(width), pieces = pieces_of(pool.H, D);
   // (65536 pages: one workgroup 10.8 us, two launches of many 17.6; a full pool costs the one 1.2 for
-  // every 16384 pages)
+  // every 16384 pages. Many columns are dear to it: whole calls that want 1024 of them 13.5 / 18.4 us,
+  // 4096 18.6 / 19.8, 16384 41 / 20, 65536 145 / 22. But only the device knows how many a call touches,
+  // and a step of answers touches one or two a sequence.)
   if (pool.P <= 4 * kPlanPages && n <= kPlanSeqs && (int64_t)n * width <= 1 << 30) {
     hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, pool.P, n, width, table,
                        lengths, counts, refs, R, missing);
@@ -781,7 +785,8 @@ hipError_t cg_launch_kv8_compact(const KvPool& pool, const KvSeqs& S, int D, con
   const Compact C = compact_of(ws, pool.P, &total);
   const int chunks = chunks_of(pool.P), pieces = pieces_of(pool.H, D);
   // (as many pages as one workgroup has registers for the counts of: 4096 pages 4.9 us, 19.3 where the
-  // workgroups' counts meet in memory)
+  // workgroups' counts meet in memory; whole calls with nothing to move, 16384 pages 10.9 us, 16385 19.3,
+  // 65536 20.1)
   if (pool.P <= kPlanPages) {
     hipLaunchKernelGGL(places_kernel, dim3(1), dim3(kPlanThreads), 0, st, pool.P, refs, C, moved,
                        new_refs, n_live);
